@@ -485,6 +485,139 @@ sync_status sync_simulate_noalloc(const sync_programs *h, sync_thr_mode mode, co
  * that may still use the handle's memory. */
 void sync_free_programs(sync_programs *h);
 
+/* ---------------------------------------------------------------------------
+ * Operators of an attention block, between its projections: the norm of every
+ * query and key head with the position rotation, and causal attention with
+ * grouped heads over packed sequences of different lengths.  They are the
+ * work whose tile walk (head, query tile, key tile; trip counts that follow
+ * from the lengths) the programs above describe.
+ *
+ * Tensors are caller-owned device memory of one type, described by their
+ * strides in elements; the entries of one head are contiguous.  Calls run
+ * asynchronously on `stream`; arguments are checked on the host before
+ * anything is launched.  Results are deterministic: every sum has a fixed
+ * order, no result depends on which block ran first. */
+
+typedef enum { SYNC_BF16 = 0, SYNC_FP16 = 1, SYNC_FP32 = 2 } sync_dtype;
+
+/* Entry d of head h of row r is data[r * row_stride + h * head_stride + d]. */
+typedef struct {
+  void *data;
+  int64_t rows;
+  int64_t row_stride, head_stride;
+} sync_rows;
+
+/* Norm and rotation of `heads` query heads and `kv_heads` key heads of every
+ * token in one pass.  With x a head's `dim` entries, w its weights and
+ * (c, s) = (cos, sin)[position of the token]:
+ *   z = x / sqrt(mean(x^2) + eps) * w,
+ *   y = z with pair j < rotated/2 turned: (a, b) -> (a c_j - b s_j, b c_j + a s_j),
+ * where pair j is entries (j, j + rotated/2), or (2j, 2j + 1) when interleaved,
+ * and entries from `rotated` on are not turned.  Computed in 32 bits, rounded
+ * once.  Every field is checked: dim even and in 2..256, rotated even and in
+ * 0..dim, eps > 0 and finite, heads and kv_heads >= 1, the tensors' rows equal. */
+typedef struct {
+  int32_t dtype;              /* sync_dtype of q, k, weights and outputs       */
+  int32_t heads, kv_heads, dim;
+  int32_t rotated;            /* entries of a head that are rotated            */
+  int32_t interleaved;        /* 0: pairs (j, j + rotated/2); 1: (2j, 2j + 1)  */
+  float eps;
+  sync_rows q, k;             /* inputs                                        */
+  const void *q_weight, *k_weight;  /* [dim] each, or NULL for weights of 1    */
+  const float *cos, *sin;     /* [n_positions][rotated/2]                      */
+  int64_t n_positions;
+  const int32_t *positions;   /* [rows], or NULL: the row's index.  A position
+                                 outside 0..n_positions-1 makes its token's
+                                 outputs NaN                                   */
+} sync_norm_rope;
+
+/* Writes the outputs y of q and k (rows, strides as given; either may be its
+ * own input: every entry is read before it is written). */
+sync_status sync_qk_norm_rope(const sync_norm_rope *p, const sync_rows *q_out, const sync_rows *k_out,
+                              void *stream);
+
+/* Bytes of device workspace that sync_qk_norm_rope_backward needs for these
+ * sizes on the current device (16-byte aligned, contents irrelevant). */
+sync_status sync_qk_norm_rope_workspace(const sync_norm_rope *p, int64_t *bytes);
+
+/* Gradient of the above: from the inputs and the outputs' gradients dq_out,
+ * dk_out to the inputs' gradients dq, dk (rows as the inputs; either may be
+ * its dq_out or dk_out) and the weights' dq_weight, dk_weight ([dim], of
+ * dtype; NULL where the weight is).  The weights' sums over tokens and heads
+ * are held in 32 bits, per block first and then over the blocks in order. */
+sync_status sync_qk_norm_rope_backward(const sync_norm_rope *p, const sync_rows *dq_out,
+                                       const sync_rows *dk_out, const sync_rows *dq, const sync_rows *dk,
+                                       void *dq_weight, void *dk_weight, void *workspace,
+                                       int64_t workspace_bytes, void *stream);
+
+/* A packed batch of sequences (host pointers, borrowed for the call).
+ * Sequence i has q_len[i] queries in rows q_start[i].. of the query tensors
+ * and k_len[i] keys in rows k_start[i].. of the key and value tensors, all
+ * lengths >= 0; NULL starts: packed without gaps in order.  Its query j sees
+ * keys 0 .. j + k_len - q_len: the last query sees every key, and where there
+ * are fewer keys than queries the first ones see none.  Query ranges must not
+ * overlap; key ranges may (a shared beginning), unless train is set. */
+typedef struct {
+  int32_t n_seqs;
+  const int32_t *q_len, *k_len;
+  const int64_t *q_start, *k_start;
+  int32_t heads, kv_heads;    /* heads is a multiple of kv_heads; query head h
+                                 reads key head h / (heads / kv_heads)         */
+  int32_t head_dim;           /* a multiple of 8 in 8..128                     */
+  int32_t dtype;              /* SYNC_BF16 or SYNC_FP16                        */
+  int32_t train;              /* 1: sync_attn_backward will be called          */
+} sync_attn_desc;
+
+typedef struct {
+  int64_t q_rows, k_rows;     /* rows that the tensors must have at least      */
+  int64_t n_queries, n_keys;  /* rows that belong to sequences                 */
+  int64_t pairs;              /* visible (query, key) pairs of one head        */
+  int64_t device_bytes;       /* device memory held by the plan                */
+  int32_t n_items;            /* work items of a forward call                  */
+  int32_t n_splits;           /* of them, pieces of a key range that is split  */
+} sync_attn_sizes;
+
+typedef struct sync_attn sync_attn;   /* opaque; owns device memory */
+
+/* Lays out the work of a packed batch on `device`: which block takes which
+ * tiles, and the workspace.  Waits until the plan is on the device.  A plan
+ * serves any number of calls on tensors of its sizes; calls on one plan share
+ * its workspace and must not overlap on the GPU.  SYNC_ERR_ARG for a field
+ * outside its range, SYNC_ERR_MALFORMED for ranges that overlap,
+ * SYNC_ERR_OVERFLOW for rows past INT32_MAX. */
+sync_status sync_attn_plan(const sync_attn_desc *desc, int device, sync_attn **out);
+
+sync_status sync_attn_query(const sync_attn *plan, sync_attn_sizes *out);
+
+/* o = softmax(scale * q k^T over the visible keys) v, for every query row of
+ * every sequence; rows outside the sequences are not written, and a query
+ * that sees no key gets zeros.  q, o: [q_rows][heads][head_dim]; k, v:
+ * [k_rows][kv_heads][head_dim]; data 16-byte aligned, strides multiples of 8
+ * elements; scale > 0.  lse: NULL, or [heads][q.rows] float, the logarithm of
+ * each row's sum of exponentials (-inf for a query that sees no key).
+ * Products are summed in 32 bits, the softmax's maximum and sum are held in
+ * 32 bits, and its unnormalised weights are rounded to dtype for the second
+ * product.  Keys and values of other sequences never reach a row, whatever
+ * they hold; within a sequence, a NaN or an infinity in the value of a key
+ * may reach earlier queries too. */
+sync_status sync_attn_forward(const sync_attn *plan, const sync_rows *q, const sync_rows *k,
+                              const sync_rows *v, float scale, const sync_rows *o, float *lse,
+                              void *stream);
+
+/* Gradients of sync_attn_forward for a plan with train set, from its inputs,
+ * its outputs o and lse, and o's gradient d_o.  dq is written for every query
+ * row, dk and dv (summed over the query heads of their key head) for every
+ * key row of the sequences.  The weights and their gradients are rounded to
+ * dtype for the products, sums are held in 32 bits. */
+sync_status sync_attn_backward(const sync_attn *plan, const sync_rows *q, const sync_rows *k,
+                               const sync_rows *v, const sync_rows *o, const float *lse,
+                               const sync_rows *d_o, float scale, const sync_rows *dq,
+                               const sync_rows *dk, const sync_rows *dv, void *stream);
+
+/* Releases a plan (NULL is ignored).  Waits for the device, as
+ * sync_free_programs does. */
+void sync_attn_free(sync_attn *plan);
+
 /* Message for the last non-OK status returned on this thread ("" if none). */
 const char *sync_last_error(void);
 

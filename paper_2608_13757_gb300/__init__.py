@@ -10,6 +10,14 @@ is missing -- there is no CPU fallback.
     thr = sg.sync_eval_thresholds(h, sg.THR_PERLOOP)  # int32 [n_pairs_padded]
     counts, first_bad = sg.sync_check_minimal(h, sg.THR_PERLOOP, thr)
     res = sg.sync_simulate(h, sg.THR_PERLOOP, thr, sg.SimParams(), sg.SIM_BARRIER_FREE)
+
+The operators of an attention block, whose tile walk such programs describe,
+are in ``attention`` and re-exported here:
+
+    q, k = sg.sync_qk_norm_rope(q, k, wq, wk, cos, sin)
+    plan = sg.sync_attn_plan(lengths, lengths, heads, kv_heads, head_dim, q.dtype, train=True)
+    o, lse = sg.sync_attn_forward(plan, q, k, v, lse=True)
+    dq, dk, dv = sg.sync_attn_backward(plan, q, k, v, o, lse, do)
 """
 from __future__ import annotations
 
@@ -30,7 +38,9 @@ PROG_OK, PROG_OVERFLOW, PROG_DEADLOCK, PROG_ROUND_GUARD, PROG_TIMEOUT = 0, 4, 7,
 # every symbol include/sync.h declares
 EXPORTS = ("sync_load_programs", "sync_query", "sync_pair_offsets", "sync_eval_thresholds",
            "sync_check_minimal", "sync_simulate", "sync_simulate_fused", "sync_simulate_noalloc",
-           "sync_free_programs", "sync_last_error", "sync_kernel_launches", "sync_validate_programs")
+           "sync_free_programs", "sync_last_error", "sync_kernel_launches", "sync_validate_programs",
+           "sync_qk_norm_rope", "sync_qk_norm_rope_workspace", "sync_qk_norm_rope_backward",
+           "sync_attn_plan", "sync_attn_query", "sync_attn_forward", "sync_attn_backward", "sync_attn_free")
 NOALLOC_SCRATCH_BYTES = 64 << 20
 CODE_BYTES_PER_INSTR = 16
 
@@ -101,8 +111,9 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.sync_last_error.restype = ctypes.c_char_p
     lib.sync_kernel_launches.argtypes = []
     lib.sync_kernel_launches.restype = ctypes.c_int64
+    attention.declare(lib)
     for f in EXPORTS:
-        if f not in ("sync_free_programs", "sync_last_error", "sync_kernel_launches"):
+        if f not in ("sync_free_programs", "sync_attn_free", "sync_last_error", "sync_kernel_launches"):
             getattr(lib, f).restype = ctypes.c_int
     return lib
 
@@ -346,3 +357,8 @@ def sync_simulate_noalloc(h: Programs, mode, thr, params: SimParams | None = Non
 
 def sync_free_programs(h: Programs):
     h.close()
+
+
+from . import attention  # noqa: E402  (uses the binding above)
+from .attention import (AttnPlan, sync_attn_backward, sync_attn_forward, sync_attn_plan,  # noqa: E402,F401
+                        sync_qk_norm_rope, sync_qk_norm_rope_backward)
