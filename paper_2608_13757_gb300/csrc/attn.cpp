@@ -3,9 +3,10 @@
 #include <algorithm>
 #include <cmath>
 #include <cstring>
+#include <functional>
 #include <memory>
 #include <new>
-#include <numeric>
+#include <queue>
 #include <string>
 #include <utility>
 #include <vector>
@@ -185,12 +186,160 @@ AttnTensor attn_tensor(const sync_rows* t, int64_t rows, const char* what) {
   need(t->data || rows == 0, what);
   need(reinterpret_cast<uintptr_t>(t->data) % 16 == 0 && t->row_stride % 8 == 0 && t->head_stride % 8 == 0,
        "attention tensors must be 16-byte aligned with strides that are multiples of 8 entries");
+  need(t->rows == 0 || (t->row_stride > 0 && t->head_stride > 0 && t->row_stride < (1ll << 38) && t->head_stride < (1ll << 38)),
+       "strides must be positive and below 2^38 entries");
   AttnTensor r;
   r.data = t->data;
   r.rows = t->rows;
   r.row = t->row_stride;
   r.head = t->head_stride;
   return r;
+}
+
+using EncodeTiled = decltype(&cuTensorMapEncodeTiled);
+
+EncodeTiled encode_tiled() {
+  static const EncodeTiled f = [] {
+    void* p = nullptr;
+    cudaDriverEntryPointQueryResult r;
+    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &r) != cudaSuccess ||
+        r != cudaDriverEntryPointSuccess)
+      p = nullptr;
+    return reinterpret_cast<EncodeTiled>(p);
+  }();
+  if (!f) fail(SYNC_ERR_CUDA, "the driver has no cuTensorMapEncodeTiled");
+  return f;
+}
+
+// Boxes of 64 entries, box_heads heads and box_rows rows; entries past the
+// head's end and rows past the tensor's read as zero.
+CUtensorMap tile_map(const AttnTensor& t, bool bf16, int heads, int dim, int box_heads, int box_rows) {
+  CUtensorMap m;
+  const cuuint64_t size[3] = {(cuuint64_t)dim, (cuuint64_t)heads, (cuuint64_t)t.rows};
+  const cuuint64_t stride[2] = {2ull * (cuuint64_t)t.head, 2ull * (cuuint64_t)t.row};
+  const cuuint32_t box[3] = {64, (cuuint32_t)box_heads, (cuuint32_t)box_rows}, one[3] = {1, 1, 1};
+  const CUresult e = encode_tiled()(&m, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, t.data,
+                                    size, stride, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                                    CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  if (e != CUDA_SUCCESS) fail(SYNC_ERR_ARG, "a tensor's strides or address have no tile map (error " + std::to_string(e) + ")");
+  return m;
+}
+
+// A sequence whose heads fill query tiles badly packs the heads of a group
+// into one tile (128 / group queries each) where that takes fewer tiles.
+bool packs(const AttnSeq& s, int group) {
+  if (group == 1 || group > kTile) return false;
+  const int64_t per = kTile / group;
+  return (s.lq + per - 1) / per < (int64_t)group * ((s.lq + kTile - 1) / kTile);
+}
+
+struct ForwardWork {
+  std::vector<AttnItem> item;
+  std::vector<int32_t> block_first;
+  std::vector<AttnSplit> split;
+  int32_t slots = 0;
+};
+
+// Items of a forward call and which block takes which.  An item's cost is the
+// key tiles that its query tiles meet and kItemCost for what it does besides.
+// One that costs more than its share of a block is split along its keys
+// into pieces of at least kMinPiece tiles.  The blocks take items from the
+// most expensive on, always the block that has least.
+constexpr int64_t kItemCost = 2, kMinPiece = 2;
+
+ForwardWork forward_work(const sync_attn_desc* d, const std::vector<AttnSeq>& seq, int num_sms) {
+  const int group = d->heads / d->kv_heads;
+  struct Draft {
+    AttnItem it;
+    int64_t cost;
+  };
+  std::vector<Draft> draft;
+  int64_t total = 0;
+  for (int32_t i = 0; i < d->n_seqs; ++i) {
+    const AttnSeq& s = seq[(size_t)i];
+    const bool packed = packs(s, group);
+    const int64_t per = packed ? kTile / group : kTile;
+    for (int32_t h = 0; h < d->heads; h += packed ? group : 1)
+      for (int64_t q0 = 0; q0 < s.lq; q0 += 2 * per) {
+        auto tiles = [&](int64_t first) -> int64_t {
+          if (first >= s.lq) return 0;
+          const int64_t seen = std::min<int64_t>(first + per, s.lq) + s.lk - s.lq;
+          return seen > 0 ? (seen + kTile - 1) / kTile : 0;
+        };
+        const int64_t n0 = tiles(q0), n1 = tiles(q0 + per);
+        draft.push_back({{i, h, (int32_t)q0, packed, 0, (int32_t)std::max(n0, n1), -1, 0}, n0 + n1 + kItemCost});
+        total += draft.back().cost;
+      }
+  }
+  ForwardWork w;
+  std::vector<Draft> all;
+  const int64_t share = std::max<int64_t>(1, total / num_sms);
+  for (const Draft& x : draft) {
+    const int64_t n = x.it.kt1, pieces = std::min(n / kMinPiece, 2 * x.cost / share);
+    if (x.cost <= share * 3 / 4 || pieces < 2) {
+      all.push_back(x);
+      continue;
+    }
+    AttnItem it = x.it;
+    it.group = (int32_t)w.split.size();
+    w.split.push_back({w.slots, (int32_t)pieces});
+    w.slots += (int32_t)pieces;
+    for (int64_t p = 0; p < pieces; ++p) {
+      it.kt0 = (int32_t)(n * p / pieces);
+      it.kt1 = (int32_t)(n * (p + 1) / pieces);
+      it.piece = (int32_t)p;
+      all.push_back({it, (x.cost - kItemCost) * (it.kt1 - it.kt0) / n + kItemCost});
+    }
+  }
+  std::stable_sort(all.begin(), all.end(), [](const Draft& x, const Draft& y) { return x.cost > y.cost; });
+  const int blocks = (int)std::min<int64_t>(num_sms, (int64_t)all.size());
+  std::vector<std::vector<int32_t>> of((size_t)blocks);
+  using Load = std::pair<int64_t, int32_t>;
+  std::priority_queue<Load, std::vector<Load>, std::greater<Load>> least;
+  for (int32_t b = 0; b < blocks; ++b) least.push({0, b});
+  for (size_t i = 0; i < all.size(); ++i) {
+    Load l = least.top();
+    least.pop();
+    of[(size_t)l.second].push_back((int32_t)i);
+    l.first += all[i].cost;
+    least.push(l);
+  }
+  w.block_first.push_back(0);
+  for (const auto& b : of) {
+    for (int32_t i : b) w.item.push_back(all[(size_t)i].it);
+    w.block_first.push_back((int32_t)w.item.size());
+  }
+  return w;
+}
+
+// Device memory of a plan, laid out first, then allocated and filled at once.
+class Arena {
+ public:
+  template <class T>
+  size_t add(const std::vector<T>& v) {
+    const size_t at = reserve(v.size() * sizeof(T));
+    if (!v.empty()) {
+      host_.resize(at + v.size() * sizeof(T));
+      std::memcpy(host_.data() + at, v.data(), v.size() * sizeof(T));
+    }
+    return at;
+  }
+  size_t reserve(size_t bytes) {      // after every add(): not filled
+    const size_t at = (size_ + 255) / 256 * 256;
+    size_ = at + bytes;
+    return at;
+  }
+  size_t size() const { return size_; }
+  const std::vector<uint8_t>& host() const { return host_; }
+
+ private:
+  size_t size_ = 0;
+  std::vector<uint8_t> host_;
+};
+
+void check_gave_up(const sync_attn* plan) {
+  if (*static_cast<volatile int*>(plan->error))
+    fail(SYNC_ERR_CUDA, "an earlier call on this plan gave up waiting inside a kernel: its results are not valid");
 }
 
 }  // namespace
@@ -245,13 +394,14 @@ sync_status sync_attn_plan(const sync_attn_desc* desc, int device, sync_attn** o
     check_attn(desc);
     sync_attn_sizes sz{};
     const std::vector<AttnSeq> seq = sequences(desc, sz);
-    std::vector<AttnItem> qi, ki;
-    for (int32_t i = 0; i < desc->n_seqs; ++i) {
-      for (int32_t h = 0; h < desc->heads; ++h)
-        for (int32_t t = 0; t * kTile < seq[(size_t)i].lq; ++t) qi.push_back({i, h, t, 0});
-      for (int32_t h = 0; h < desc->kv_heads; ++h)
-        for (int32_t t = 0; t * kTile < seq[(size_t)i].lk; ++t) ki.push_back({i, h, t, 0});
-    }
+    std::vector<AttnTile> qt, kt;
+    if (desc->train)
+      for (int32_t i = 0; i < desc->n_seqs; ++i) {
+        for (int32_t h = 0; h < desc->heads; ++h)
+          for (int32_t t = 0; (int64_t)t * kTile < seq[(size_t)i].lq; ++t) qt.push_back({i, h, t, 0});
+        for (int32_t h = 0; h < desc->kv_heads; ++h)
+          for (int32_t t = 0; (int64_t)t * kTile < seq[(size_t)i].lk; ++t) kt.push_back({i, h, t, 0});
+      }
     DeviceScope scope(device);
     std::unique_ptr<sync_attn, void (*)(sync_attn*)> P(new sync_attn, sync_attn_free);
     P->device = device;
@@ -263,31 +413,37 @@ sync_status sync_attn_plan(const sync_attn_desc* desc, int device, sync_attn** o
     a.kv_heads = desc->kv_heads;
     a.dim = desc->head_dim;
     a.num_sms = P->num_sms;
-    auto put = [&](const auto& v) {
-      using T = typename std::decay_t<decltype(v)>::value_type;
-      void* d = nullptr;
-      if (v.empty()) return static_cast<const T*>(nullptr);
-      cuda(cudaMalloc(&d, v.size() * sizeof(T)), "sync_attn_plan");
-      P->blocks.push_back(d);
-      sz.device_bytes += (int64_t)(v.size() * sizeof(T));
-      cuda(cudaMemcpy(d, v.data(), v.size() * sizeof(T), cudaMemcpyHostToDevice), "sync_attn_plan");
-      return static_cast<const T*>(d);
-    };
-    a.seq = put(seq);
-    a.q_item = put(qi);
-    a.n_q_items = (int)qi.size();
-    a.k_item = put(ki);
-    a.n_k_items = (int)ki.size();
-    if (P->train && sz.q_rows) {
-      void* d = nullptr;
-      const size_t bytes = (size_t)sz.q_rows * (size_t)a.heads * sizeof(float);
-      cuda(cudaMalloc(&d, bytes), "sync_attn_plan");
-      P->blocks.push_back(d);
-      sz.device_bytes += (int64_t)bytes;
-      a.delta = static_cast<float*>(d);
-      a.delta_rows = sz.q_rows;
-    }
-    sz.n_items = a.n_q_items;
+    const ForwardWork w = forward_work(desc, seq, P->num_sms);
+    a.n_blocks = (int)w.block_first.size() - 1;
+    a.n_q_tiles = (int)qt.size();
+    a.n_k_tiles = (int)kt.size();
+    a.delta_rows = sz.q_rows;
+    Arena m;
+    const size_t at_seq = m.add(seq), at_item = m.add(w.item), at_first = m.add(w.block_first), at_split = m.add(w.split),
+                 at_count = m.add(std::vector<int32_t>(2 * w.split.size(), 0)), at_qt = m.add(qt), at_kt = m.add(kt);
+    const size_t padded = a.dim <= 64 ? 64 : 128;
+    const size_t at_part = m.reserve((size_t)w.slots * 2 * kTile * padded * sizeof(float)),
+                 at_part_lse = m.reserve((size_t)w.slots * 2 * kTile * sizeof(float)),
+                 at_delta = m.reserve(P->train ? (size_t)sz.q_rows * (size_t)a.heads * sizeof(float) : 0);
+    cuda(cudaMallocHost(reinterpret_cast<void**>(&P->error), sizeof(int)), "sync_attn_plan");
+    *P->error = 0;
+    a.error = P->error;
+    cuda(cudaMalloc(&P->block, std::max<size_t>(m.size(), 1)), "sync_attn_plan");
+    cuda(cudaMemcpy(P->block, m.host().data(), m.host().size(), cudaMemcpyHostToDevice), "sync_attn_plan");
+    uint8_t* base = static_cast<uint8_t*>(P->block);
+    a.seq = reinterpret_cast<const AttnSeq*>(base + at_seq);
+    a.item = reinterpret_cast<const AttnItem*>(base + at_item);
+    a.block_first = reinterpret_cast<const int32_t*>(base + at_first);
+    a.split = reinterpret_cast<const AttnSplit*>(base + at_split);
+    a.split_count = reinterpret_cast<int32_t*>(base + at_count);
+    a.q_tile = reinterpret_cast<const AttnTile*>(base + at_qt);
+    a.k_tile = reinterpret_cast<const AttnTile*>(base + at_kt);
+    a.part_o = reinterpret_cast<float*>(base + at_part);
+    a.part_lse = reinterpret_cast<float*>(base + at_part_lse);
+    a.delta = reinterpret_cast<float*>(base + at_delta);
+    sz.device_bytes = (int64_t)m.size();
+    sz.n_items = (int32_t)w.item.size();
+    sz.n_splits = w.slots;
     P->sz = sz;
     *out = P.release();
   });
@@ -312,9 +468,18 @@ sync_status sync_attn_forward(const sync_attn* plan, const sync_rows* q, const s
     a.v = attn_tensor(v, plan->sz.k_rows, "v must not be NULL");
     a.o = attn_tensor(o, plan->sz.q_rows, "o must not be NULL");
     a.lse = lse;
-    if (!a.n_q_items) return;
+    if (!a.n_blocks) return;
+    check_gave_up(plan);
     DeviceScope scope(plan->device);
-    cuda(launch_attn_forward(a, static_cast<cudaStream_t>(stream)), "sync_attn_forward");
+    const int group = a.heads / a.kv_heads;
+    AttnMaps m{};
+    m.q = tile_map(a.q, a.bf16, a.heads, a.dim, 1, kTile);
+    m.q_group = group > kTile ? m.q : tile_map(a.q, a.bf16, a.heads, a.dim, group, kTile / group);
+    if (a.k.rows) {
+      m.k = tile_map(a.k, a.bf16, a.kv_heads, a.dim, 1, kTile);
+      m.v = tile_map(a.v, a.bf16, a.kv_heads, a.dim, 1, kTile);
+    }
+    cuda(launch_attn_forward(a, m, static_cast<cudaStream_t>(stream)), "sync_attn_forward");
   });
 }
 
@@ -337,7 +502,8 @@ sync_status sync_attn_backward(const sync_attn* plan, const sync_rows* q, const 
     a.dk = attn_tensor(dk, plan->sz.k_rows, "dk must not be NULL");
     a.dv = attn_tensor(dv, plan->sz.k_rows, "dv must not be NULL");
     a.lse = const_cast<float*>(lse);
-    if (!a.n_q_items && !a.n_k_items) return;
+    if (!a.n_q_tiles && !a.n_k_tiles) return;
+    check_gave_up(plan);
     DeviceScope scope(plan->device);
     cuda(launch_attn_backward(a, static_cast<cudaStream_t>(stream)), "sync_attn_backward");
   });
@@ -349,7 +515,8 @@ void sync_attn_free(sync_attn* plan) {
   const bool have = cudaGetDevice(&was) == cudaSuccess;
   cudaSetDevice(plan->device);
   cudaDeviceSynchronize();
-  for (void* b : plan->blocks) cudaFree(b);
+  if (plan->block) cudaFree(plan->block);
+  if (plan->error) cudaFreeHost(plan->error);
   if (have && was != plan->device) cudaSetDevice(was);
   delete plan;
 }

@@ -42,7 +42,7 @@ __device__ __forceinline__ float dot(const float* x, const float* y) {
 
 template <class T>
 __global__ void __launch_bounds__(256) k_attn_dq(const __grid_constant__ AttnArgs a) {
-  const AttnItem it = a.q_item[blockIdx.x];
+  const AttnTile it = a.q_tile[blockIdx.x];
   const AttnSeq s = a.seq[it.seq];
   const int lane = threadIdx.x % 32, kh = it.head / (a.heads / a.kv_heads);
   for (int r = it.tile * kTile + threadIdx.x / 32; r < min(s.lq, (it.tile + 1) * kTile); r += 8) {
@@ -67,7 +67,7 @@ __global__ void __launch_bounds__(256) k_attn_dq(const __grid_constant__ AttnArg
 
 template <class T>
 __global__ void __launch_bounds__(256) k_attn_dkv(const __grid_constant__ AttnArgs a) {
-  const AttnItem it = a.k_item[blockIdx.x];
+  const AttnTile it = a.k_tile[blockIdx.x];
   const AttnSeq s = a.seq[it.seq];
   const int lane = threadIdx.x % 32, group = a.heads / a.kv_heads;
   for (int j = it.tile * kTile + threadIdx.x / 32; j < min(s.lk, (it.tile + 1) * kTile); j += 8) {
@@ -95,13 +95,13 @@ __global__ void __launch_bounds__(256) k_attn_dkv(const __grid_constant__ AttnAr
 
 template <class T>
 cudaError_t launch(const AttnArgs& a, cudaStream_t st) {
-  if (a.n_q_items) {
-    k_attn_dq<T><<<a.n_q_items, 256, 0, st>>>(a);
+  if (a.n_q_tiles) {
+    k_attn_dq<T><<<a.n_q_tiles, 256, 0, st>>>(a);
     if (cudaError_t e = cudaGetLastError()) return e;
     count_launch();
   }
-  if (a.n_k_items) {
-    k_attn_dkv<T><<<a.n_k_items, 256, 0, st>>>(a);
+  if (a.n_k_tiles) {
+    k_attn_dkv<T><<<a.n_k_tiles, 256, 0, st>>>(a);
     if (cudaError_t e = cudaGetLastError()) return e;
     count_launch();
   }

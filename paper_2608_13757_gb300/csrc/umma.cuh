@@ -1,0 +1,206 @@
+// sm_103a building blocks of the attention kernels: mbarriers whose waits
+// give up, TMA tile loads, tcgen05 products with operands in shared memory
+// or tensor memory, and tensor memory transfers.
+//
+// Tiles in shared memory are 128 rows of 64 16-bit entries (128 bytes a row)
+// in the 128-byte swizzle that the TMA load writes, 16 KB each; wider rows
+// take one such block per 64 entries.
+#pragma once
+
+#include <cuda.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+namespace syncgb {
+namespace umma {
+
+constexpr int kBlockBytes = 128 * 128;   // 128 rows of 64 entries
+
+__device__ __forceinline__ uint32_t smem_addr(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+
+__device__ __forceinline__ bool elect_one() {
+  uint32_t one;
+  asm volatile("{\n.reg .pred p;\nelect.sync _|p, 0xffffffff;\nselp.b32 %0, 1, 0, p;\n}" : "=r"(one));
+  return one;
+}
+
+// ---- mbarriers ----
+__device__ __forceinline__ void bar_init(uint32_t bar, uint32_t count) {
+  asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
+}
+__device__ __forceinline__ void bar_init_visible() {
+  asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+}
+__device__ __forceinline__ void bar_expect(uint32_t bar, uint32_t bytes) {
+  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void bar_arrive(uint32_t bar) {
+  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n.reg .pred p;\nmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\nselp.b32 %0, 1, 0, p;\n}"
+      : "=r"(ok)
+      : "r"(bar), "r"(parity)
+      : "memory");
+  return ok;
+}
+__device__ __forceinline__ uint64_t now_ns() {
+  uint64_t t;
+  asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t));
+  return t;
+}
+
+// What a wait that never ends would mean is a defect; it then gives up after
+// kGiveUpNs, says so in *error (host-visible) and lets the block's other
+// waits give up too, so the kernel always ends.
+constexpr uint64_t kGiveUpNs = 1000000000ull;
+struct Waits {
+  volatile int* dead;     // shared by the block
+  int* error;             // host-visible
+};
+__device__ __forceinline__ bool bar_wait_slow(uint32_t bar, uint32_t parity, Waits w) {
+  const uint64_t t0 = now_ns();
+  for (uint32_t i = 1;; ++i) {
+    if (bar_try(bar, parity)) return true;
+    if (i % 16 == 0) {
+      if (*w.dead) return false;
+      if (now_ns() - t0 > kGiveUpNs) {
+        *w.dead = 1;
+        *reinterpret_cast<volatile int*>(w.error) = 1;
+        return false;
+      }
+    }
+  }
+}
+__device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, Waits w) {
+  return bar_try(bar, parity) || bar_wait_slow(bar, parity, w);
+}
+// The same for a whole warp, with one answer for all lanes.
+__device__ __forceinline__ bool bar_wait_warp(uint32_t bar, uint32_t parity, Waits w) {
+  return __all_sync(~0u, bar_wait(bar, parity, w));
+}
+
+// ---- TMA ----
+// A box of a [rows][heads][entries] tensor at (entry, head, row).
+__device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap* map, uint32_t bar, int entry, int head,
+                                         int row) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
+      ::"r"(dst), "l"(map), "r"(bar), "r"(entry), "r"(head), "r"(row)
+      : "memory");
+}
+// Orders this thread's shared memory writes before later products' reads.
+__device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+
+// ---- tcgen05 ----
+template <int COLS>
+__device__ __forceinline__ void tmem_alloc(uint32_t where) {
+  asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(where), "n"(COLS) : "memory");
+  asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+}
+template <int COLS>
+__device__ __forceinline__ void tmem_free(uint32_t addr) {
+  asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(addr), "n"(COLS));
+}
+__device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+// Arrives on `bar` when every product issued so far by this thread is done.
+__device__ __forceinline__ void commit(uint32_t bar) {
+  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+
+// Instruction descriptor: f32 accumulators, 128 x n, 16-bit operands; B with
+// its contracted dimension contiguous, or (b_rows) with its n dimension
+// contiguous.
+__host__ __device__ __forceinline__ uint32_t instr(bool bf16, int n, bool b_rows) {
+  const uint32_t t = bf16 ? 1 : 0;
+  return 1u << 4 | t << 7 | t << 10 | (b_rows ? 1u << 16 : 0u) | (uint32_t)(n / 8) << 17 | (128u / 16) << 24;
+}
+// Shared memory descriptor of a swizzled tile.  Contracted dimension
+// contiguous: 8-row groups are 1024 bytes apart.  Otherwise (b_rows) the same
+// 1024 bytes separate groups of 8 contracted rows, and blocks of 64 columns
+// are kBlockBytes apart.
+__device__ __forceinline__ uint64_t tile_desc(uint32_t addr) {
+  return (uint64_t)(addr >> 4 & 0x3fff) | (uint64_t)(kBlockBytes >> 4) << 16 | (uint64_t)(1024 >> 4) << 32 | 1ull << 46 |
+         2ull << 61;
+}
+// The contracted dimension moves by 16 entries: 32 bytes within a row and a
+// block further every 64 entries, or 16 rows.
+__device__ __forceinline__ uint64_t step_along(int k) { return (uint64_t)((k / 4 * kBlockBytes + k % 4 * 32) >> 4); }
+__device__ __forceinline__ uint64_t step_rows(int k) { return (uint64_t)(k * 16 * 128 >> 4); }
+
+__device__ __forceinline__ void mma(uint32_t d, uint64_t a, uint64_t b, uint32_t i, bool add) {
+  asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\ntcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}" ::"r"(d),
+               "l"(a), "l"(b), "r"(i), "r"((uint32_t)add)
+               : "memory");
+}
+// A from tensor memory: 16-bit pairs, 8 columns per 16 contracted entries.
+__device__ __forceinline__ void mma_tmem(uint32_t d, uint32_t a, uint64_t b, uint32_t i, bool add) {
+  asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\ntcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}" ::"r"(d),
+               "r"(a), "l"(b), "r"(i), "r"((uint32_t)add)
+               : "memory");
+}
+
+// Columns of this warp's 32 lanes, one lane per thread.
+__device__ __forceinline__ void tmem_ld16(uint32_t addr, float* x) {
+  uint32_t* r = reinterpret_cast<uint32_t*>(x);
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+               : "r"(addr));
+}
+__device__ __forceinline__ void tmem_ld32(uint32_t addr, float* x) {
+  uint32_t* r = reinterpret_cast<uint32_t*>(x);
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+               : "r"(addr));
+}
+__device__ __forceinline__ void tmem_st16(uint32_t addr, const uint32_t* r) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15};" ::"r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(addr)
+               : "memory");
+}
+__device__ __forceinline__ void tmem_st32(uint32_t addr, const uint32_t* r) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31};" ::"r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]), "r"(addr)
+               : "memory");
+}
+
+// A warpgroup's registers per thread, given up or taken from what the block
+// was launched with.
+template <int N>
+__device__ __forceinline__ void regs_down() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
+template <int N>
+__device__ __forceinline__ void regs_up() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
+
+// ---- arithmetic ----
+__device__ __forceinline__ float exp2_fast(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+// Two values rounded to 16 bits, the first in the low half.
+template <bool BF16>
+__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
+  uint32_t r;
+  if (BF16)
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  else
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+template <bool BF16>
+__device__ __forceinline__ float2 unpack2(uint32_t r) {
+  float2 f;
+  if (BF16) {
+    f.x = __uint_as_float(r << 16);
+    f.y = __uint_as_float(r & 0xffff0000u);
+  } else {
+    asm("{\n.reg .f16 a, b;\nmov.b32 {a, b}, %2;\ncvt.f32.f16 %0, a;\ncvt.f32.f16 %1, b;\n}" : "=f"(f.x), "=f"(f.y) : "r"(r));
+  }
+  return f;
+}
+
+}  // namespace umma
+}  // namespace syncgb
