@@ -247,13 +247,39 @@ struct ForwardWork {
 // most expensive on, always the block that has least.
 constexpr int64_t kItemCost = 2, kMinPiece = 2;
 
+template <class T>
+struct Draft {
+  T it;
+  int64_t cost;
+};
+
+// The drafts in the order of the blocks that take them: from the most
+// expensive on, always to the block that has least.
+template <class T>
+void assign(std::vector<Draft<T>>& all, int num_sms, std::vector<T>& item, std::vector<int32_t>& first) {
+  std::stable_sort(all.begin(), all.end(), [](const Draft<T>& x, const Draft<T>& y) { return x.cost > y.cost; });
+  const int blocks = (int)std::min<int64_t>(num_sms, (int64_t)all.size());
+  std::vector<std::vector<int32_t>> of((size_t)blocks);
+  using Load = std::pair<int64_t, int32_t>;
+  std::priority_queue<Load, std::vector<Load>, std::greater<Load>> least;
+  for (int32_t b = 0; b < blocks; ++b) least.push({0, b});
+  for (size_t i = 0; i < all.size(); ++i) {
+    Load l = least.top();
+    least.pop();
+    of[(size_t)l.second].push_back((int32_t)i);
+    l.first += all[i].cost;
+    least.push(l);
+  }
+  first.push_back(0);
+  for (const auto& b : of) {
+    for (int32_t i : b) item.push_back(all[(size_t)i].it);
+    first.push_back((int32_t)item.size());
+  }
+}
+
 ForwardWork forward_work(const sync_attn_desc* d, const std::vector<AttnSeq>& seq, int num_sms) {
   const int group = d->heads / d->kv_heads;
-  struct Draft {
-    AttnItem it;
-    int64_t cost;
-  };
-  std::vector<Draft> draft;
+  std::vector<Draft<AttnItem>> draft;
   int64_t total = 0;
   for (int32_t i = 0; i < d->n_seqs; ++i) {
     const AttnSeq& s = seq[(size_t)i];
@@ -272,9 +298,9 @@ ForwardWork forward_work(const sync_attn_desc* d, const std::vector<AttnSeq>& se
       }
   }
   ForwardWork w;
-  std::vector<Draft> all;
+  std::vector<Draft<AttnItem>> all;
   const int64_t share = std::max<int64_t>(1, total / num_sms);
-  for (const Draft& x : draft) {
+  for (const Draft<AttnItem>& x : draft) {
     const int64_t n = x.it.kt1, pieces = std::min(n / kMinPiece, 2 * x.cost / share);
     if (x.cost <= share * 3 / 4 || pieces < 2) {
       all.push_back(x);
@@ -291,25 +317,29 @@ ForwardWork forward_work(const sync_attn_desc* d, const std::vector<AttnSeq>& se
       all.push_back({it, (x.cost - kItemCost) * (it.kt1 - it.kt0) / n + kItemCost});
     }
   }
-  std::stable_sort(all.begin(), all.end(), [](const Draft& x, const Draft& y) { return x.cost > y.cost; });
-  const int blocks = (int)std::min<int64_t>(num_sms, (int64_t)all.size());
-  std::vector<std::vector<int32_t>> of((size_t)blocks);
-  using Load = std::pair<int64_t, int32_t>;
-  std::priority_queue<Load, std::vector<Load>, std::greater<Load>> least;
-  for (int32_t b = 0; b < blocks; ++b) least.push({0, b});
-  for (size_t i = 0; i < all.size(); ++i) {
-    Load l = least.top();
-    least.pop();
-    of[(size_t)l.second].push_back((int32_t)i);
-    l.first += all[i].cost;
-    least.push(l);
-  }
-  w.block_first.push_back(0);
-  for (const auto& b : of) {
-    for (int32_t i : b) w.item.push_back(all[(size_t)i].it);
-    w.block_first.push_back((int32_t)w.item.size());
-  }
+  assign(all, num_sms, w.item, w.block_first);
   return w;
+}
+
+// Tiles of the gradients' two walks: key tiles with the query tiles that see
+// them, over all heads of their group, and query tiles with the keys they see.
+void gradient_work(const sync_attn_desc* d, const std::vector<AttnSeq>& seq, std::vector<Draft<AttnTile>>& q,
+                   std::vector<Draft<AttnTile>>& k) {
+  const int64_t group = d->heads / d->kv_heads;
+  for (int32_t i = 0; i < d->n_seqs; ++i) {
+    const AttnSeq& s = seq[(size_t)i];
+    const int64_t tiles = (s.lq + kTile - 1) / kTile, offset = (int64_t)s.lk - s.lq;
+    for (int32_t h = 0; h < d->heads; ++h)
+      for (int32_t t = 0; t < tiles; ++t) {
+        const int64_t seen = std::min<int64_t>((t + 1ll) * kTile, s.lq) + offset;
+        q.push_back({{i, h, t, 0}, std::max<int64_t>(0, (seen + kTile - 1) / kTile) + kItemCost});
+      }
+    for (int32_t h = 0; h < d->kv_heads; ++h)
+      for (int32_t t = 0; (int64_t)t * kTile < s.lk; ++t) {
+        const int64_t first = std::max<int64_t>(0, t * (int64_t)kTile - offset) / kTile;
+        k.push_back({{i, h, t, 0}, std::max<int64_t>(0, tiles - first) * group + kItemCost});
+      }
+  }
 }
 
 // Device memory of a plan, laid out first, then allocated and filled at once.
@@ -394,14 +424,6 @@ sync_status sync_attn_plan(const sync_attn_desc* desc, int device, sync_attn** o
     check_attn(desc);
     sync_attn_sizes sz{};
     const std::vector<AttnSeq> seq = sequences(desc, sz);
-    std::vector<AttnTile> qt, kt;
-    if (desc->train)
-      for (int32_t i = 0; i < desc->n_seqs; ++i) {
-        for (int32_t h = 0; h < desc->heads; ++h)
-          for (int32_t t = 0; (int64_t)t * kTile < seq[(size_t)i].lq; ++t) qt.push_back({i, h, t, 0});
-        for (int32_t h = 0; h < desc->kv_heads; ++h)
-          for (int32_t t = 0; (int64_t)t * kTile < seq[(size_t)i].lk; ++t) kt.push_back({i, h, t, 0});
-      }
     DeviceScope scope(device);
     std::unique_ptr<sync_attn, void (*)(sync_attn*)> P(new sync_attn, sync_attn_free);
     P->device = device;
@@ -415,12 +437,20 @@ sync_status sync_attn_plan(const sync_attn_desc* desc, int device, sync_attn** o
     a.num_sms = P->num_sms;
     const ForwardWork w = forward_work(desc, seq, P->num_sms);
     a.n_blocks = (int)w.block_first.size() - 1;
-    a.n_q_tiles = (int)qt.size();
-    a.n_k_tiles = (int)kt.size();
+    std::vector<AttnTile> qt, kt;
+    std::vector<int32_t> q_first, k_first;
+    if (P->train) {
+      std::vector<Draft<AttnTile>> q, k;
+      gradient_work(desc, seq, q, k);
+      assign(q, P->num_sms, qt, q_first);
+      assign(k, P->num_sms, kt, k_first);
+      a.n_q_blocks = (int)q_first.size() - 1;
+      a.n_k_blocks = (int)k_first.size() - 1;
+    }
     a.delta_rows = sz.q_rows;
     Arena m;
     const size_t at_seq = m.add(seq), at_item = m.add(w.item), at_first = m.add(w.block_first), at_split = m.add(w.split),
-                 at_count = m.add(std::vector<int32_t>(2 * w.split.size(), 0)), at_qt = m.add(qt), at_kt = m.add(kt);
+                 at_count = m.add(std::vector<int32_t>(2 * w.split.size(), 0)), at_qt = m.add(qt), at_kt = m.add(kt), at_qf = m.add(q_first), at_kf = m.add(k_first);
     const size_t padded = a.dim <= 64 ? 64 : 128;
     const size_t at_part = m.reserve((size_t)w.slots * 2 * kTile * padded * sizeof(float)),
                  at_part_lse = m.reserve((size_t)w.slots * 2 * kTile * sizeof(float)),
@@ -438,6 +468,8 @@ sync_status sync_attn_plan(const sync_attn_desc* desc, int device, sync_attn** o
     a.split_count = reinterpret_cast<int32_t*>(base + at_count);
     a.q_tile = reinterpret_cast<const AttnTile*>(base + at_qt);
     a.k_tile = reinterpret_cast<const AttnTile*>(base + at_kt);
+    a.q_first = reinterpret_cast<const int32_t*>(base + at_qf);
+    a.k_first = reinterpret_cast<const int32_t*>(base + at_kf);
     a.part_o = reinterpret_cast<float*>(base + at_part);
     a.part_lse = reinterpret_cast<float*>(base + at_part_lse);
     a.delta = reinterpret_cast<float*>(base + at_delta);
@@ -502,10 +534,19 @@ sync_status sync_attn_backward(const sync_attn* plan, const sync_rows* q, const 
     a.dk = attn_tensor(dk, plan->sz.k_rows, "dk must not be NULL");
     a.dv = attn_tensor(dv, plan->sz.k_rows, "dv must not be NULL");
     a.lse = const_cast<float*>(lse);
-    if (!a.n_q_tiles && !a.n_k_tiles) return;
+    if (!a.n_q_blocks && !a.n_k_blocks) return;
     check_gave_up(plan);
     DeviceScope scope(plan->device);
-    cuda(launch_attn_backward(a, static_cast<cudaStream_t>(stream)), "sync_attn_backward");
+    AttnMaps m{};
+    if (a.q.rows) {
+      m.q = tile_map(a.q, a.bf16, a.heads, a.dim, 1, kTile);
+      m.d_o = tile_map(a.d_o, a.bf16, a.heads, a.dim, 1, kTile);
+    }
+    if (a.k.rows) {
+      m.k = tile_map(a.k, a.bf16, a.kv_heads, a.dim, 1, kTile);
+      m.v = tile_map(a.v, a.bf16, a.kv_heads, a.dim, 1, kTile);
+    }
+    cuda(launch_attn_backward(a, m, static_cast<cudaStream_t>(stream)), "sync_attn_backward");
   });
 }
 

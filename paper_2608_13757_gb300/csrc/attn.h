@@ -61,8 +61,10 @@ struct AttnArgs {
   const AttnSplit* split = nullptr;
   int32_t* split_count = nullptr;  // [splits][2]: pieces that are done
   float *part_o = nullptr, *part_lse = nullptr;   // [slots][2][kTile](dim padded), [slots][2][kTile]
+  // gradients: tiles of block b are tile[first[b] .. first[b + 1])
   const AttnTile *q_tile = nullptr, *k_tile = nullptr;
-  int n_q_tiles = 0, n_k_tiles = 0;
+  const int32_t *q_first = nullptr, *k_first = nullptr;
+  int n_q_blocks = 0, n_k_blocks = 0;
   int* error = nullptr;            // host-visible: a kernel gave up waiting
   int num_sms = 0;
 };
@@ -74,7 +76,7 @@ struct AttnMaps {
 };
 
 cudaError_t launch_attn_forward(const AttnArgs& a, const AttnMaps& m, cudaStream_t st);
-cudaError_t launch_attn_backward(const AttnArgs& a, cudaStream_t st);
+cudaError_t launch_attn_backward(const AttnArgs& a, const AttnMaps& m, cudaStream_t st);
 
 }  // namespace syncgb
 

@@ -55,7 +55,8 @@ def head(q, k, v, scale, do=None):
     delta = (do * o).sum(1, keepdim=True)
     delta_err = ((o_err + u * o.abs()) * do.abs()).sum(1, keepdim=True) + 2.0 ** -18 * (do.abs() @ v.abs().T).amax(1, keepdim=True) if m else delta
     ds = w * (dp - delta)
-    ds_err = (u + 2 * small) * ds.abs() + w * delta_err + tiny + small * w * (do.abs() @ v.abs().T)
+    # a weight below 2^-126 is zero
+    ds_err = (u + 2 * small) * ds.abs() + w * delta_err + tiny + 2.0 ** -126 * (dp - delta).abs() + small * w * (do.abs() @ v.abs().T)
     dv, dq, dk = w.T @ do, ds @ k * scale, ds.T @ q * scale
     r["dv"], r["dv_tol"] = dv, (u + 2 * small) * (w.T @ do.abs()) + tiny * do.abs().sum(0) + u * dv.abs() + tiny
     r["dq"], r["dq_tol"] = dq, (ds_err @ k.abs()) * scale + u * dq.abs() + tiny
