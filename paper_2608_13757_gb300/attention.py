@@ -75,73 +75,76 @@ def _need(ok, what):
         raise _sg.SyncError(_sg.ERR_ARG, what)
 
 
-class _On:
-    """The device of a call made current and its stream, for allocations too."""
+class _current:
+    """The device of a call that has no handle, made current where it is not."""
 
-    def __init__(self, device, stream):
+    def __init__(self, device):
         import torch
-        self.device = torch.cuda.device(device)
-        if stream is not None and not isinstance(stream, torch.cuda.Stream):
-            stream = torch.cuda.ExternalStream(int(stream), device=device)
-        self.given = stream
-        self.scope = torch.cuda.stream(stream) if stream is not None else None
+        self.scope = torch.cuda.device(device) if torch.cuda.current_device() != device else None
 
     def __enter__(self):
-        import torch
-        self.device.__enter__()
         if self.scope is not None:
             self.scope.__enter__()
-        return ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
 
     def __exit__(self, *a):
         if self.scope is not None:
             self.scope.__exit__(*a)
-        self.device.__exit__(*a)
 
 
-def _rows(t, name, like=None, heads=None, dim=None) -> Rows:
-    """A [rows, heads, dim] tensor's description; `like`: a tensor whose device
-    and type it must have."""
-    _need(t.dim() == 3, f"{name} must be [rows, heads, dim]")
+class _On:
+    """The stream of a call that names one, current for allocations too.  (A
+    call that names none takes the current stream of its device directly.)"""
+
+    def __init__(self, device, stream):
+        import torch
+        if not isinstance(stream, torch.cuda.Stream):
+            stream = torch.cuda.ExternalStream(int(stream), device=device)
+        self.stream, self.scope = stream, torch.cuda.stream(stream)
+
+    def __enter__(self):
+        self.scope.__enter__()
+        return self.stream.cuda_stream
+
+    def __exit__(self, *a):
+        self.scope.__exit__(*a)
+
+
+def _rows(t, name, dtype, device, heads, dim) -> Rows:
+    """A [rows, heads, dim] tensor's description, checked against the call's."""
+    if t.dim() != 3 or t.dtype is not dtype or t.get_device() != device:
+        _need(t.dim() == 3, f"{name} must be [rows, heads, dim]")
+        _need(t.dtype is dtype and t.get_device() == device, f"{name} must be {dtype} on GPU {device}")
     n, h, d = t.shape
-    _need(t.is_cuda and (like is None or t.device == like.device), f"{name} must be on the call's GPU")
-    _need(like is None or t.dtype == like.dtype, f"{name} must have the type of q")
-    _need(heads is None or h == heads, f"{name} must have {heads} heads")
-    _need(dim is None or d == dim, f"{name} must have heads of {dim} entries")
     rs, hs, ds = t.stride()
-    _need(ds == 1 or d == 1 or n == 0, f"{name}: the entries of a head must be contiguous")
+    if h != heads or d != dim or ds != 1:
+        _need(h == heads and d == dim, f"{name} must have {heads} heads of {dim} entries")
+        _need(n == 0, f"{name}: the entries of a head must be contiguous")
     # the stride of a dimension of size 1 is never used: pass a plain one
-    if h == 1:
-        hs = d
-    if n <= 1:
-        rs = h * d
-    return Rows(t.data_ptr(), n, rs, hs)
+    return Rows(t.data_ptr(), n, rs if n > 1 else h * d, hs if h > 1 else d)
 
 
-def _vector(t, name, like, n, dtype):
+def _vector(t, name, device, n, dtype):
     if t is None:
         return None
-    _need(t.device == like.device and t.dtype == dtype, f"{name} must be {dtype} on the call's GPU")
-    _need(t.numel() == n and t.is_contiguous(), f"{name} must be contiguous with {n} entries")
+    if t.dtype is not dtype or t.get_device() != device or t.numel() != n or not t.is_contiguous():
+        _need(False, f"{name} must be contiguous {dtype} with {n} entries on GPU {device}")
     return t.data_ptr()
 
 
 def _norm_rope(q, k, q_weight, k_weight, cos, sin, positions, eps, interleaved):
     import torch
-    _need(q.dim() == 3 and k.dim() == 3, "q and k must be [rows, heads, dim]")
+    if q.dim() != 3 or k.dim() != 3 or cos.dim() != 2 or cos.shape != sin.shape or not q.is_cuda:
+        _need(q.dim() == 3 and k.dim() == 3, "q and k must be [rows, heads, dim]")
+        _need(q.is_cuda, "q must be on a GPU")
+        _need(False, "cos and sin must be [positions, rotated / 2]")
     n, heads, dim = q.shape
-    p = NormRope()
-    p.dtype, p.heads, p.kv_heads, p.dim = _code(q.dtype), heads, k.shape[1], dim
-    p.q, p.k = _rows(q, "q"), _rows(k, "k", q, None, dim)
-    p.eps, p.interleaved = eps, int(interleaved)
-    p.q_weight = _vector(q_weight, "q_weight", q, dim, q.dtype)
-    p.k_weight = _vector(k_weight, "k_weight", q, dim, q.dtype)
-    _need(cos.dim() == 2 and cos.shape == sin.shape, "cos and sin must be [positions, rotated / 2]")
-    p.rotated, p.n_positions = 2 * cos.shape[1], cos.shape[0]
-    p.cos = _vector(cos, "cos", q, cos.numel(), torch.float32)
-    p.sin = _vector(sin, "sin", q, sin.numel(), torch.float32)
-    p.positions = _vector(positions, "positions", q, n, torch.int32)
-    return p
+    dtype, device, kv_heads, (n_pos, half) = q.dtype, q.get_device(), k.shape[1], cos.shape
+    return NormRope(_code(dtype), heads, kv_heads, dim, 2 * half, bool(interleaved), eps,
+                    _rows(q, "q", dtype, device, heads, dim), _rows(k, "k", dtype, device, kv_heads, dim),
+                    _vector(q_weight, "q_weight", device, dim, dtype), _vector(k_weight, "k_weight", device, dim, dtype),
+                    _vector(cos, "cos", device, n_pos * half, torch.float32),
+                    _vector(sin, "sin", device, n_pos * half, torch.float32), n_pos,
+                    _vector(positions, "positions", device, n, torch.int32))
 
 
 def sync_qk_norm_rope(q, k, q_weight, k_weight, cos, sin, positions=None, eps: float = 1e-6,
@@ -152,13 +155,17 @@ def sync_qk_norm_rope(q, k, q_weight, k_weight, cos, sin, positions=None, eps: f
     the table gives NaN.  Returns the pair of outputs; out=(q, k) works in place."""
     import torch
     p = _norm_rope(q, k, q_weight, k_weight, cos, sin, positions, eps, interleaved)
-    with _On(q.device, stream) as st:
-        if out is None:
-            out = (torch.empty(q.shape, dtype=q.dtype, device=q.device),
-                   torch.empty(k.shape, dtype=q.dtype, device=q.device))
-        _sg._check(_sg.lib().sync_qk_norm_rope(
-            ctypes.byref(p), ctypes.byref(_rows(out[0], "out[0]", q, p.heads, p.dim)),
-            ctypes.byref(_rows(out[1], "out[1]", q, p.kv_heads, p.dim)), st))
+    if stream is not None:
+        with _On(q.device, stream):
+            return sync_qk_norm_rope(q, k, q_weight, k_weight, cos, sin, positions, eps, interleaved, out)
+    if out is None:
+        out = (torch.empty(q.shape, dtype=q.dtype, device=q.device),
+               torch.empty(k.shape, dtype=q.dtype, device=q.device))
+    device = q.get_device()
+    a = [_rows(t, name, q.dtype, device, h, p.dim) for t, name, h in ((out[0], "out[0]", p.heads),
+                                                                     (out[1], "out[1]", p.kv_heads))]
+    with _current(device):
+        _sg._check(_sg.lib().sync_qk_norm_rope(p, a[0], a[1], torch.cuda.current_stream(device).cuda_stream))
     return out
 
 
@@ -169,20 +176,24 @@ def sync_qk_norm_rope_backward(q, k, dq_out, dk_out, q_weight, k_weight, cos, si
     be the outputs' gradients themselves."""
     import torch
     p = _norm_rope(q, k, q_weight, k_weight, cos, sin, positions, eps, interleaved)
-    with _On(q.device, stream) as st:
-        if out is None:
-            out = (torch.empty(q.shape, dtype=q.dtype, device=q.device),
-                   torch.empty(k.shape, dtype=q.dtype, device=q.device))
-        dw = [torch.empty(p.dim, dtype=q.dtype, device=q.device) if w is not None else None for w in (q_weight, k_weight)]
-        need = ctypes.c_int64()
-        _sg._check(_sg.lib().sync_qk_norm_rope_workspace(ctypes.byref(p), ctypes.byref(need)))
+    if stream is not None:
+        with _On(q.device, stream):
+            return sync_qk_norm_rope_backward(q, k, dq_out, dk_out, q_weight, k_weight, cos, sin, positions, eps,
+                                              interleaved, out)
+    if out is None:
+        out = (torch.empty(q.shape, dtype=q.dtype, device=q.device),
+               torch.empty(k.shape, dtype=q.dtype, device=q.device))
+    dw = [torch.empty(p.dim, dtype=q.dtype, device=q.device) if w is not None else None for w in (q_weight, k_weight)]
+    device = q.get_device()
+    a = [_rows(t, name, q.dtype, device, h, p.dim)
+         for t, name, h in ((dq_out, "dq_out", p.heads), (dk_out, "dk_out", p.kv_heads), (out[0], "out[0]", p.heads),
+                            (out[1], "out[1]", p.kv_heads))]
+    need = ctypes.c_int64()
+    with _current(device):
+        _sg._check(_sg.lib().sync_qk_norm_rope_workspace(p, need))
         work = torch.empty(need.value, dtype=torch.uint8, device=q.device)
-        _sg._check(_sg.lib().sync_qk_norm_rope_backward(
-            ctypes.byref(p), ctypes.byref(_rows(dq_out, "dq_out", q, p.heads, p.dim)),
-            ctypes.byref(_rows(dk_out, "dk_out", q, p.kv_heads, p.dim)),
-            ctypes.byref(_rows(out[0], "out[0]", q, p.heads, p.dim)),
-            ctypes.byref(_rows(out[1], "out[1]", q, p.kv_heads, p.dim)),
-            _sg._ptr(dw[0]), _sg._ptr(dw[1]), _sg._ptr(work), need.value, st))
+        _sg._check(_sg.lib().sync_qk_norm_rope_backward(p, *a, _sg._ptr(dw[0]), _sg._ptr(dw[1]), _sg._ptr(work),
+                                                        need.value, torch.cuda.current_stream(device).cuda_stream))
     return out[0], out[1], dw[0], dw[1]
 
 
@@ -193,8 +204,9 @@ class AttnPlan:
     def __init__(self, handle, device, heads, kv_heads, head_dim, dtype):
         self._h = handle
         self.device, self.heads, self.kv_heads, self.head_dim, self.dtype = device, heads, kv_heads, head_dim, dtype
-        self.sizes = AttnSizes()
+        self.index, self.sizes = device.index, AttnSizes()
         _sg._check(_sg.lib().sync_attn_query(handle, ctypes.byref(self.sizes)))
+        self.n_queries, self.n_keys = self.sizes.n_queries, self.sizes.n_keys
 
     @property
     def handle(self):
@@ -220,8 +232,7 @@ def sync_attn_plan(q_lens, k_lens, heads: int, kv_heads: int, head_dim: int, dty
     k_lens[i] tokens whose keys it attends to, causally.  Starts are rows of the
     query and key tensors (None: packed without gaps)."""
     import torch
-    device = torch.cuda.current_device() if device is None else torch.device("cuda", device).index \
-        if isinstance(device, int) else torch.device(device).index
+    index = torch.cuda.current_device() if device is None else device if isinstance(device, int) else torch.device(device).index
     arrays = []
     for v, kind, name in ((q_lens, np.int32, "q_lens"), (k_lens, np.int32, "k_lens"), (q_starts, np.int64, "q_starts"),
                           (k_starts, np.int64, "k_starts")):
@@ -240,61 +251,58 @@ def sync_attn_plan(q_lens, k_lens, heads: int, kv_heads: int, head_dim: int, dty
         if a is not None:
             setattr(d, field, a.ctypes.data_as(ctypes.POINTER(kind)))
     h = ctypes.c_void_p()
-    _sg._check(_sg.lib().sync_attn_plan(ctypes.byref(d), int(device), ctypes.byref(h)))
-    return AttnPlan(h, torch.device("cuda", device), heads, kv_heads, head_dim, dtype)
+    _sg._check(_sg.lib().sync_attn_plan(ctypes.byref(d), index, ctypes.byref(h)))
+    return AttnPlan(h, torch.device("cuda", index), heads, kv_heads, head_dim, dtype)
 
 
-def _attn_rows(plan, tensors):
-    got = []
-    for t, name, heads in tensors:
-        _need(t.device == plan.device and t.dtype == plan.dtype, f"{name} must be {plan.dtype} on {plan.device}")
-        got.append(_rows(t, name, None, heads, plan.head_dim))
-    return [ctypes.byref(r) for r in got]
-
-
-def _new(like_rows, heads, plan, covered):
+def _new(rows, heads, plan, covered):
     """An output: rows that no sequence has are zero."""
     import torch
-    make = torch.empty if covered == like_rows else torch.zeros
-    return make((like_rows, heads, plan.head_dim), dtype=plan.dtype, device=plan.device)
+    make = torch.empty if covered == rows else torch.zeros
+    return make((rows, heads, plan.head_dim), dtype=plan.dtype, device=plan.device)
 
 
 def sync_attn_forward(plan: AttnPlan, q, k, v, scale: float | None = None, out=None, lse=False, stream=None):
     """Causal attention of a planned batch.  With lse=True (or a float32 tensor
     [heads, rows of q] to write) returns (o, lse), as the gradient needs."""
     import torch
-    scale = plan.head_dim ** -0.5 if scale is None else float(scale)
-    with _On(plan.device, stream) as st:
-        if out is None:
-            out = _new(q.shape[0], plan.heads, plan, plan.sizes.n_queries)
-        if lse is True:
-            lse = torch.full((plan.heads, q.shape[0]), -float("inf"), dtype=torch.float32, device=plan.device) \
-                if plan.sizes.n_queries != q.shape[0] else \
-                torch.empty((plan.heads, q.shape[0]), dtype=torch.float32, device=plan.device)
-        elif lse is False:
-            lse = None
-        if lse is not None:
-            _vector(lse, "lse", q, plan.heads * q.shape[0], torch.float32)
-        a = _attn_rows(plan, ((q, "q", plan.heads), (k, "k", plan.kv_heads), (v, "v", plan.kv_heads),
-                              (out, "out", plan.heads)))
-        _need(out.shape[0] == q.shape[0], "out must have the rows of q")
-        _sg._check(_sg.lib().sync_attn_forward(plan.handle, a[0], a[1], a[2], scale, a[3], _sg._ptr(lse), st))
-    return out if lse is None else (out, lse)
+    if stream is not None:
+        with _On(plan.device, stream):
+            return sync_attn_forward(plan, q, k, v, scale, out, lse)
+    dtype, device, heads, kv, dim = plan.dtype, plan.index, plan.heads, plan.kv_heads, plan.head_dim
+    a = (_rows(q, "q", dtype, device, heads, dim), _rows(k, "k", dtype, device, kv, dim),
+         _rows(v, "v", dtype, device, kv, dim))
+    n = q.shape[0]
+    if out is None:
+        out = _new(n, heads, plan, plan.n_queries)
+    o = _rows(out, "out", dtype, device, heads, dim)
+    if o.rows != n:
+        _need(False, "out must have the rows of q")
+    if lse is True:
+        lse = torch.empty((heads, n), dtype=torch.float32, device=plan.device)
+        if plan.n_queries != n:
+            lse.fill_(-float("inf"))
+    at = None if lse is False or lse is None else _vector(lse, "lse", device, heads * n, torch.float32)
+    _sg._check(_sg.lib().sync_attn_forward(plan.handle, *a, dim ** -0.5 if scale is None else scale, o, at,
+                                           torch.cuda.current_stream(device).cuda_stream))
+    return out if at is None and not isinstance(lse, torch.Tensor) else (out, lse)
 
 
 def sync_attn_backward(plan: AttnPlan, q, k, v, o, lse, do, scale: float | None = None, out=None, stream=None):
     """(dq, dk, dv) of sync_attn_forward, for a plan made with train=True."""
     import torch
-    scale = plan.head_dim ** -0.5 if scale is None else float(scale)
-    with _On(plan.device, stream) as st:
-        _vector(lse, "lse", q, plan.heads * q.shape[0], torch.float32)
-        if out is None:
-            out = (_new(q.shape[0], plan.heads, plan, plan.sizes.n_queries),
-                   _new(k.shape[0], plan.kv_heads, plan, plan.sizes.n_keys),
-                   _new(k.shape[0], plan.kv_heads, plan, plan.sizes.n_keys))
-        a = _attn_rows(plan, ((q, "q", plan.heads), (k, "k", plan.kv_heads), (v, "v", plan.kv_heads),
-                              (o, "o", plan.heads), (do, "do", plan.heads), (out[0], "dq", plan.heads),
-                              (out[1], "dk", plan.kv_heads), (out[2], "dv", plan.kv_heads)))
-        _sg._check(_sg.lib().sync_attn_backward(plan.handle, a[0], a[1], a[2], a[3], _sg._ptr(lse), a[4], scale, a[5],
-                                                a[6], a[7], st))
+    if stream is not None:
+        with _On(plan.device, stream):
+            return sync_attn_backward(plan, q, k, v, o, lse, do, scale, out)
+    dtype, device, heads, kv, dim = plan.dtype, plan.index, plan.heads, plan.kv_heads, plan.head_dim
+    a = [_rows(t, name, dtype, device, h, dim) for t, name, h in ((q, "q", heads), (k, "k", kv), (v, "v", kv),
+                                                                 (o, "o", heads), (do, "do", heads))]
+    n, m = q.shape[0], k.shape[0]
+    at = _vector(lse, "lse", device, heads * n, torch.float32)
+    if out is None:
+        out = (_new(n, heads, plan, plan.n_queries), _new(m, kv, plan, plan.n_keys), _new(m, kv, plan, plan.n_keys))
+    d = [_rows(t, name, dtype, device, h, dim) for t, name, h in ((out[0], "dq", heads), (out[1], "dk", kv),
+                                                                 (out[2], "dv", kv))]
+    _sg._check(_sg.lib().sync_attn_backward(plan.handle, *a[:4], at, a[4], dim ** -0.5 if scale is None else scale, *d,
+                                            torch.cuda.current_stream(device).cuda_stream))
     return tuple(out)

@@ -26,7 +26,7 @@ ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 CU = ["k_tiles.cu", "k_load.cu", "k_thresholds.cu", "k_simulate.cu", "k_sweep.cu", "k_sweep_maps.cu", "k_bar.cu", "k_piece.cu", "k_noalloc.cu",
       "k_qk_norm.cu", "k_attn_fwd.cu", "k_attn_bwd.cu"]
 CPP = ["capi.cpp", "attn.cpp"]
-HEADERS = [os.path.join(CSRC, "enc.h"), os.path.join(CSRC, "progbuild.cuh"), os.path.join(CSRC, "cost.cuh"), os.path.join(CSRC, "sweep.cuh"), os.path.join(CSRC, "bar.cuh"), os.path.join(CSRC, "trip.cuh"), os.path.join(CSRC, "handle.h"), os.path.join(CSRC, "waitval.cuh"), os.path.join(CSRC, "attn.h"), os.path.join(CSRC, "umma.cuh"), os.path.join(CSRC, "norm.h"), os.path.join(ROOT, "include", "sync.h")]
+HEADERS = [os.path.join(CSRC, "enc.h"), os.path.join(CSRC, "progbuild.cuh"), os.path.join(CSRC, "cost.cuh"), os.path.join(CSRC, "sweep.cuh"), os.path.join(CSRC, "bar.cuh"), os.path.join(CSRC, "trip.cuh"), os.path.join(CSRC, "handle.h"), os.path.join(CSRC, "waitval.cuh"), os.path.join(CSRC, "attn.h"), os.path.join(CSRC, "umma.cuh"), os.path.join(CSRC, "launch.cuh"), os.path.join(CSRC, "norm.h"), os.path.join(ROOT, "include", "sync.h")]
 
 
 def _sources():

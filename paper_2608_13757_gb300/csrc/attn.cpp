@@ -143,6 +143,11 @@ void check_attn(const sync_attn_desc* d) {
   need(d->dtype == SYNC_BF16 || d->dtype == SYNC_FP16, "dtype must be SYNC_BF16 or SYNC_FP16");
 }
 
+struct AttnSeq {
+  int64_t q0, k0;                  // first rows in the query and key tensors
+  int32_t lq, lk;
+};
+
 std::vector<AttnSeq> sequences(const sync_attn_desc* d, sync_attn_sizes& sz) {
   std::vector<AttnSeq> seq((size_t)d->n_seqs);
   int64_t q = 0, k = 0;
@@ -237,7 +242,7 @@ struct ForwardWork {
   std::vector<AttnItem> item;
   std::vector<int32_t> block_first;
   std::vector<AttnSplit> split;
-  int32_t slots = 0;
+  int32_t slots = 0, merge_rows = 0;
 };
 
 // Items of a forward call and which block takes which.  An item's cost is the
@@ -281,19 +286,25 @@ ForwardWork forward_work(const sync_attn_desc* d, const std::vector<AttnSeq>& se
   const int group = d->heads / d->kv_heads;
   std::vector<Draft<AttnItem>> draft;
   int64_t total = 0;
-  for (int32_t i = 0; i < d->n_seqs; ++i) {
-    const AttnSeq& s = seq[(size_t)i];
+  for (const AttnSeq& s : seq) {
     const bool packed = packs(s, group);
-    const int64_t per = packed ? kTile / group : kTile;
+    const int32_t per = packed ? kTile / group : kTile;
     for (int32_t h = 0; h < d->heads; h += packed ? group : 1)
       for (int64_t q0 = 0; q0 < s.lq; q0 += 2 * per) {
-        auto tiles = [&](int64_t first) -> int64_t {
-          if (first >= s.lq) return 0;
-          const int64_t seen = std::min<int64_t>(first + per, s.lq) + s.lk - s.lq;
-          return seen > 0 ? (seen + kTile - 1) / kTile : 0;
-        };
-        const int64_t n0 = tiles(q0), n1 = tiles(q0 + per);
-        draft.push_back({{i, h, (int32_t)q0, packed, 0, (int32_t)std::max(n0, n1), -1, 0}, n0 + n1 + kItemCost});
+        AttnItem it{};
+        it.q_row = s.q0 + q0;
+        it.k_row = s.k0;
+        it.head = h;
+        it.packed = packed;
+        it.seen = (int32_t)(q0 + s.lk - s.lq + 1);
+        it.keys = s.lk;
+        it.slot = -1;
+        for (int t = 0; t < 2; ++t) {
+          it.rows[t] = (int32_t)std::max<int64_t>(0, std::min<int64_t>(per, s.lq - q0 - t * per));
+          const int64_t most = (int64_t)it.seen + t * per + it.rows[t] - 1;      // keys that the last query sees
+          it.n[t] = it.rows[t] && most > 0 ? (int32_t)((most + kTile - 1) / kTile) : 0;
+        }
+        draft.push_back({it, it.n[0] + it.n[1] + kItemCost});
         total += draft.back().cost;
       }
   }
@@ -301,20 +312,23 @@ ForwardWork forward_work(const sync_attn_desc* d, const std::vector<AttnSeq>& se
   std::vector<Draft<AttnItem>> all;
   const int64_t share = std::max<int64_t>(1, total / num_sms);
   for (const Draft<AttnItem>& x : draft) {
-    const int64_t n = x.it.kt1, pieces = std::min(n / kMinPiece, 2 * x.cost / share);
+    const int64_t n = std::max(x.it.n[0], x.it.n[1]), pieces = std::min(n / kMinPiece, 2 * x.cost / share);
     if (x.cost <= share * 3 / 4 || pieces < 2) {
       all.push_back(x);
       continue;
     }
-    AttnItem it = x.it;
-    it.group = (int32_t)w.split.size();
-    w.split.push_back({w.slots, (int32_t)pieces});
-    w.slots += (int32_t)pieces;
+    const int heads = x.it.packed ? group : 1;
+    w.split.push_back({x.it.q_row, x.it.head, x.it.packed, {x.it.rows[0], x.it.rows[1]}, w.slots, (int32_t)pieces});
+    w.merge_rows = std::max(w.merge_rows, (x.it.rows[0] + x.it.rows[1]) * heads);
     for (int64_t p = 0; p < pieces; ++p) {
-      it.kt0 = (int32_t)(n * p / pieces);
-      it.kt1 = (int32_t)(n * (p + 1) / pieces);
-      it.piece = (int32_t)p;
-      all.push_back({it, (x.cost - kItemCost) * (it.kt1 - it.kt0) / n + kItemCost});
+      const int32_t first = (int32_t)(n * p / pieces), last = (int32_t)(n * (p + 1) / pieces);
+      AttnItem it = x.it;
+      it.k_row += (int64_t)first * kTile;
+      it.seen -= first * kTile;
+      it.keys -= first * kTile;
+      for (int t = 0; t < 2; ++t) it.n[t] = std::max(0, std::min(x.it.n[t], last) - first);
+      it.slot = w.slots++;
+      all.push_back({it, it.n[0] + it.n[1] + kItemCost});
     }
   }
   assign(all, num_sms, w.item, w.block_first);
@@ -326,18 +340,32 @@ ForwardWork forward_work(const sync_attn_desc* d, const std::vector<AttnSeq>& se
 void gradient_work(const sync_attn_desc* d, const std::vector<AttnSeq>& seq, std::vector<Draft<AttnTile>>& q,
                    std::vector<Draft<AttnTile>>& k) {
   const int64_t group = d->heads / d->kv_heads;
-  for (int32_t i = 0; i < d->n_seqs; ++i) {
-    const AttnSeq& s = seq[(size_t)i];
+  for (const AttnSeq& s : seq) {
     const int64_t tiles = (s.lq + kTile - 1) / kTile, offset = (int64_t)s.lk - s.lq;
+    AttnTile it{};
     for (int32_t h = 0; h < d->heads; ++h)
-      for (int32_t t = 0; t < tiles; ++t) {
-        const int64_t seen = std::min<int64_t>((t + 1ll) * kTile, s.lq) + offset;
-        q.push_back({{i, h, t, 0}, std::max<int64_t>(0, (seen + kTile - 1) / kTile) + kItemCost});
+      for (int64_t q0 = 0; q0 < s.lq; q0 += kTile) {
+        const int64_t most = std::min<int64_t>(q0 + kTile, s.lq) + offset;       // keys that the last query sees
+        it.q_row = s.q0 + q0;
+        it.k_row = s.k0;
+        it.head = h;
+        it.n = (int32_t)(most > 0 ? (most + kTile - 1) / kTile : 0);
+        it.rows = (int32_t)(s.lq - q0);
+        it.keys = s.lk;
+        it.seen = (int32_t)(q0 + offset + 1);
+        q.push_back({it, it.n + kItemCost});
       }
     for (int32_t h = 0; h < d->kv_heads; ++h)
-      for (int32_t t = 0; (int64_t)t * kTile < s.lk; ++t) {
-        const int64_t first = std::max<int64_t>(0, t * (int64_t)kTile - offset) / kTile;
-        k.push_back({{i, h, t, 0}, std::max<int64_t>(0, tiles - first) * group + kItemCost});
+      for (int64_t k0 = 0; k0 < s.lk; k0 += kTile) {
+        const int64_t first = std::min(tiles, std::max<int64_t>(0, k0 - offset) / kTile);   // the first tile that sees key k0
+        it.q_row = s.q0 + first * kTile;
+        it.k_row = s.k0 + k0;
+        it.head = h;
+        it.n = (int32_t)(tiles - first);
+        it.rows = (int32_t)(s.lq - first * kTile);
+        it.keys = (int32_t)(s.lk - k0);
+        it.seen = (int32_t)(first * kTile + offset + 1 - k0);
+        k.push_back({it, it.n * group + kItemCost});
       }
   }
 }
@@ -449,8 +477,8 @@ sync_status sync_attn_plan(const sync_attn_desc* desc, int device, sync_attn** o
     }
     a.delta_rows = sz.q_rows;
     Arena m;
-    const size_t at_seq = m.add(seq), at_item = m.add(w.item), at_first = m.add(w.block_first), at_split = m.add(w.split),
-                 at_count = m.add(std::vector<int32_t>(2 * w.split.size(), 0)), at_qt = m.add(qt), at_kt = m.add(kt), at_qf = m.add(q_first), at_kf = m.add(k_first);
+    const size_t at_item = m.add(w.item), at_first = m.add(w.block_first), at_split = m.add(w.split),
+                 at_qt = m.add(qt), at_kt = m.add(kt), at_qf = m.add(q_first), at_kf = m.add(k_first);
     const size_t padded = a.dim <= 64 ? 64 : 128;
     const size_t at_part = m.reserve((size_t)w.slots * 2 * kTile * padded * sizeof(float)),
                  at_part_lse = m.reserve((size_t)w.slots * 2 * kTile * sizeof(float)),
@@ -461,11 +489,11 @@ sync_status sync_attn_plan(const sync_attn_desc* desc, int device, sync_attn** o
     cuda(cudaMalloc(&P->block, std::max<size_t>(m.size(), 1)), "sync_attn_plan");
     cuda(cudaMemcpy(P->block, m.host().data(), m.host().size(), cudaMemcpyHostToDevice), "sync_attn_plan");
     uint8_t* base = static_cast<uint8_t*>(P->block);
-    a.seq = reinterpret_cast<const AttnSeq*>(base + at_seq);
     a.item = reinterpret_cast<const AttnItem*>(base + at_item);
     a.block_first = reinterpret_cast<const int32_t*>(base + at_first);
     a.split = reinterpret_cast<const AttnSplit*>(base + at_split);
-    a.split_count = reinterpret_cast<int32_t*>(base + at_count);
+    a.n_splits = (int)w.split.size();
+    a.merge_rows = w.merge_rows;
     a.q_tile = reinterpret_cast<const AttnTile*>(base + at_qt);
     a.k_tile = reinterpret_cast<const AttnTile*>(base + at_kt);
     a.q_first = reinterpret_cast<const int32_t*>(base + at_qf);

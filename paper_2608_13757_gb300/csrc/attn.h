@@ -16,28 +16,34 @@ void count_launch();
 
 constexpr int kTile = 128;         // rows of a query tile and of a key tile
 
-struct AttnSeq {
-  int64_t q0, k0;                  // first rows in the query and key tensors
-  int32_t lq, lk;
-};
-
-// A forward item: two consecutive query tiles of a sequence against the key
-// tiles [kt0, kt1).  A tile's rows are 128 queries of one head, or (packed)
-// the queries' heads of a group, 128 / group queries.
-struct AttnItem {
-  int32_t seq, head, q0, packed;   // head: the first one of a packed tile
-  int32_t kt0, kt1;
-  int32_t group, piece;            // a split key range: which, and its piece; group -1: whole
+// A forward item: two consecutive query tiles of a sequence against a range of
+// key tiles.  A tile's rows are 128 queries of one head, or (packed) the
+// queries' heads of a group, 128 / group queries.  Everything a block needs to
+// know is in these 64 bytes, so that an item costs one access.
+struct alignas(64) AttnItem {
+  int64_t q_row, k_row;            // rows of the tensors: first query, first key of the range
+  int32_t head, packed;            // head: the first one of a packed tile
+  int32_t rows[2];                 // queries of each tile
+  int32_t n[2];                    // key tiles that each meets
+  int32_t seen;                    // keys of the range that the first query sees (may be negative); the next sees one more
+  int32_t keys;                    // keys of the sequence from k_row on
+  int32_t slot;                    // where a piece of a split range leaves its result; -1: the range is whole
 };
 
 // A split key range: its pieces' results are at slot, slot + 1, ...
 struct AttnSplit {
-  int32_t slot, pieces;
+  int64_t q_row;
+  int32_t head, packed, rows[2], slot, pieces;
 };
 
-// A query tile of one head, or a key tile of one key head (gradients).
-struct AttnTile {
-  int32_t seq, head, tile, pad;
+// A gradient item.  Key walk: a key tile of a key head against n query tiles
+// of each head of its group, from q_row on.  Query walk: a query tile of a
+// head against n key tiles from k_row on.
+struct alignas(64) AttnTile {
+  int64_t q_row, k_row;
+  int32_t head, n;
+  int32_t rows, keys;              // queries from q_row on and keys from k_row on that are the sequence's
+  int32_t seen;                    // keys from k_row on that the query at q_row sees (may be negative)
 };
 
 struct AttnTensor {
@@ -49,7 +55,6 @@ struct AttnArgs {
   bool bf16 = true;
   int heads = 0, kv_heads = 0, dim = 0;
   float scale = 0.f;
-  const AttnSeq* seq = nullptr;
   AttnTensor q, k, v, o, d_o, dq, dk, dv;
   float* lse = nullptr;            // [heads][q.rows]
   float* delta = nullptr;          // [heads][delta_rows], the plan's
@@ -59,7 +64,7 @@ struct AttnArgs {
   const int32_t* block_first = nullptr;
   int n_blocks = 0;
   const AttnSplit* split = nullptr;
-  int32_t* split_count = nullptr;  // [splits][2]: pieces that are done
+  int n_splits = 0, merge_rows = 0;               // most rows of a split range
   float *part_o = nullptr, *part_lse = nullptr;   // [slots][2][kTile](dim padded), [slots][2][kTile]
   // gradients: tiles of block b are tile[first[b] .. first[b + 1])
   const AttnTile *q_tile = nullptr, *k_tile = nullptr;

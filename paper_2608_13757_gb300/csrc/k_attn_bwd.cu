@@ -20,6 +20,7 @@
 #include <algorithm>
 
 #include "attn.h"
+#include "launch.cuh"
 #include "umma.cuh"
 
 namespace syncgb {
@@ -166,18 +167,6 @@ struct Loader {
   }
 };
 
-// The walk of a key tile: query tiles [first, tiles) of every head of its group.
-struct KeyWalk {
-  int first, tiles, steps;
-};
-__device__ __forceinline__ KeyWalk key_walk(const AttnTile& it, const AttnSeq& s, int group) {
-  KeyWalk k;
-  k.tiles = (s.lq + kTile - 1) / kTile;
-  k.first = min(k.tiles, max(0, it.tile * kTile - (s.lk - s.lq)) / kTile);   // the first query that sees the first key
-  k.steps = (k.tiles - k.first) * group;
-  return k;
-}
-
 template <int DP, bool BF16>
 __global__ void __launch_bounds__(kThreads, 1) k_attn_dkv(const __grid_constant__ AttnArgs a,
                                                           const __grid_constant__ CUtensorMap q_map,
@@ -212,13 +201,11 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dkv(const __grid_constant_
       bool ok = true;
       for (int i = i0; ok && i < i1; ++i) {
         const AttnTile it = a.k_tile[i];
-        const AttnSeq s = a.seq[it.seq];
-        const KeyWalk k = key_walk(it, s, group);
-        if (!k.steps) continue;
-        ok = load.stay(&k_map, &v_map, it.head, (int)s.k0 + it.tile * kTile);
+        if (!it.n) continue;
+        ok = load.stay(&k_map, &v_map, it.head, (int)it.k_row);
         for (int h = it.head * group; ok && h < (it.head + 1) * group; ++h)
-          for (int t = k.first; ok && t < k.tiles; ++t)
-            ok = load.next(&q_map, h, (int)s.q0 + t * kTile) && load.next(&do_map, h, (int)s.q0 + t * kTile);
+          for (int t = 0; ok && t < it.n; ++t)
+            ok = load.next(&q_map, h, (int)it.q_row + t * kTile) && load.next(&do_map, h, (int)it.q_row + t * kTile);
       }
       load.finish();
     } else if (warp == 9 && elect_one()) {                  // ---- products
@@ -272,9 +259,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dkv(const __grid_constant_
         return true;
       };
       for (int i = i0; i < i1; ++i) {
-        const AttnTile it = a.k_tile[i];
-        const KeyWalk k = key_walk(it, a.seq[it.seq], group);
-        if (k.steps && !run(k.steps)) break;
+        const int steps = a.k_tile[i].n * group;
+        if (steps && !run(steps)) break;
       }
       commit(b.done);
       bar_wait(b.done, 0, w);
@@ -282,19 +268,19 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dkv(const __grid_constant_
       const int lane = threadIdx.x % 32;
       uint32_t n = 0;
       bool ok = true;
+      after_previous();                                      // delta is there
+      let_next_start();
       for (int i = i0; ok && i < i1; ++i) {
         const AttnTile it = a.k_tile[i];
-        const AttnSeq s = a.seq[it.seq];
-        const KeyWalk k = key_walk(it, s, group);
-        for (int h = it.head * group; ok && k.steps && h < (it.head + 1) * group; ++h)
-          for (int t = k.first; t < k.tiles; ++t, ++n) {
+        for (int h = it.head * group; ok && h < (it.head + 1) * group; ++h)
+          for (int t = 0; t < it.n; ++t, ++n) {
             const uint32_t st = n % L::kStatStages;
             float lse[4], delta[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
               const int q = t * kTile + lane + 32 * e;
-              lse[e] = q < s.lq ? __ldg(a.lse + h * a.q.rows + s.q0 + q) * kLog2e : -INFINITY;
-              delta[e] = q < s.lq ? a.delta[h * a.delta_rows + s.q0 + q] : 0.f;
+              lse[e] = q < it.rows ? __ldg(a.lse + h * a.q.rows + it.q_row + q) * kLog2e : -INFINITY;
+              delta[e] = q < it.rows ? a.delta[h * a.delta_rows + it.q_row + q] : 0.f;
               if (lse[e] == -INFINITY) lse[e] = INFINITY;    // no weight for a row that sees nothing
             }
             if (n >= L::kStatStages && !(ok = bar_wait_warp(b.stat_free + 8 * st, (n / L::kStatStages - 1) & 1, w))) break;
@@ -317,20 +303,18 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dkv(const __grid_constant_
     uint32_t n = 0, pos = 0, items = 0;
     for (int i = i0; i < i1; ++i) {
       const AttnTile it = a.k_tile[i];
-      const AttnSeq s = a.seq[it.seq];
-      const KeyWalk k = key_walk(it, s, group);
-      const int key = it.tile * kTile + r, offset = s.lk - s.lq;
+      if (i + 1 < i1) asm volatile("prefetch.global.L1 [%0];" ::"l"(a.k_tile + i + 1));
+      const int steps = it.n * group;
       bool ok = true;
-      int t = k.first;
-      for (int j = 0; j < k.steps; ++j, ++n, pos += 2) {
+      int t = 0;
+      for (int j = 0; j < steps; ++j, ++n, pos += 2) {
         const uint32_t st = n % L::kStatStages;
         const float* stat = reinterpret_cast<const float*>(sm + L::kStats + st * L::kStatBytes) + c0;
         // queries [from, to) of this half see the key
-        const int q0 = t * kTile + c0, from = key - offset - q0, to = s.lq - q0;
-        const bool masked = t * kTile < it.tile * kTile + kTile - 1 - offset || (t + 1) * kTile > s.lq;
-        const bool tail = (t + 1) * kTile > s.lq;
-        const int rows = s.lq - t * kTile;
-        t = t + 1 < k.tiles ? t + 1 : k.first;
+        const int q0 = t * kTile, rows = it.rows - q0;
+        const int from = r + 1 - it.seen - q0 - c0, to = rows - c0;
+        const bool tail = rows < kTile, masked = it.seen + q0 < kTile || tail;
+        t = t + 1 < it.n ? t + 1 : 0;
         float p[64];
         if (!(ok = bar_wait_warp(b.stat_full + 8 * st, n / L::kStatStages & 1, w) && bar_wait_warp(b.s_full, n & 1, w))) break;
         fence_after();
@@ -395,24 +379,19 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dkv(const __grid_constant_
         }
       }
       if (!ok) break;
-      if (k.steps) {
+      if (steps) {
         if (!bar_wait_warp(b.out_full, items++ & 1, w)) break;
         fence_after();
       }
       const AttnTensor& out = half ? a.dk : a.dv;
-      uint8_t* row = static_cast<uint8_t*>(out.data) + 2 * ((s.k0 + key) * out.row + it.head * out.head);
-      write_row<BF16>(tmem + lanes + (half ? kDk : kDv), row, 0, DP, a.dim, half ? a.scale : 1.f, k.steps > 0, key < s.lk);
+      uint8_t* row = static_cast<uint8_t*>(out.data) + 2 * ((it.k_row + r) * out.row + it.head * out.head);
+      write_row<BF16>(tmem + lanes + (half ? kDk : kDv), row, 0, DP, a.dim, half ? a.scale : 1.f, steps > 0, r < it.keys);
     }
   }
   __syncwarp();
   fence_before();
   __syncthreads();
   if (warp == 9) tmem_free<512>(tmem);
-}
-
-// Key tiles that a query tile's last row sees.
-__device__ __forceinline__ int query_walk(const AttnTile& it, const AttnSeq& s) {
-  return max(0, min((it.tile + 1) * kTile, s.lq) + s.lk - s.lq + kTile - 1) / kTile;
 }
 
 template <int DP, bool BF16>
@@ -449,13 +428,11 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dq(const __grid_constant__
       bool ok = true;
       for (int i = i0; ok && i < i1; ++i) {
         const AttnTile it = a.q_tile[i];
-        const AttnSeq s = a.seq[it.seq];
-        const int n = query_walk(it, s);
-        if (!n) continue;
-        ok = load.stay(&q_map, &do_map, it.head, (int)s.q0 + it.tile * kTile);
-        for (int j = 0; ok && j < n; ++j)
-          ok = load.next(&k_map, it.head / group, (int)s.k0 + j * kTile) &&
-               load.next(&v_map, it.head / group, (int)s.k0 + j * kTile);
+        if (!it.n) continue;
+        ok = load.stay(&q_map, &do_map, it.head, (int)it.q_row);
+        for (int j = 0; ok && j < it.n; ++j)
+          ok = load.next(&k_map, it.head / group, (int)it.k_row + j * kTile) &&
+               load.next(&v_map, it.head / group, (int)it.k_row + j * kTile);
       }
       load.finish();
     } else if (warp == 9 && elect_one()) {                  // ---- products
@@ -512,8 +489,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dq(const __grid_constant__
         return true;
       };
       for (int i = i0; i < i1; ++i) {
-        const AttnTile it = a.q_tile[i];
-        const int steps = query_walk(it, a.seq[it.seq]);
+        const int steps = a.q_tile[i].n;
         if (steps && !run(steps)) break;
       }
       commit(b.done);
@@ -527,20 +503,21 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dq(const __grid_constant__
     uint32_t n = 0, pos = 0, items = 0;
     for (int i = i0; i < i1; ++i) {
       const AttnTile it = a.q_tile[i];
-      const AttnSeq s = a.seq[it.seq];
-      const int steps = query_walk(it, s), query = it.tile * kTile + r, offset = s.lk - s.lq;
-      const bool valid = query < s.lq;
+      if (i + 1 < i1) asm volatile("prefetch.global.L1 [%0];" ::"l"(a.q_tile + i + 1));
+      const int steps = it.n;
+      const int64_t query = it.q_row + r;
+      const bool valid = r < it.rows;
       float lse = INFINITY, delta = 0.f;
       if (valid) {
-        lse = __ldg(a.lse + it.head * a.q.rows + s.q0 + query) * kLog2e;
-        delta = a.delta[it.head * a.delta_rows + s.q0 + query];
+        lse = __ldg(a.lse + it.head * a.q.rows + query) * kLog2e;
+        delta = a.delta[it.head * a.delta_rows + query];
         if (lse == -INFINITY) lse = INFINITY;                // no weight for a row that sees nothing
       }
       bool ok = true;
       for (int j = 0; j < steps; ++j, ++n, pos += 2) {
         const uint32_t S = tmem + lanes + kS + n % 2 * 128 + c0;
-        const int seen = query + offset - j * kTile - c0 + 1;            // keys of this half that the row sees
-        const bool masked = j * kTile + kTile - 1 > it.tile * kTile + offset;
+        const int seen = it.seen + r - j * kTile - c0;                   // keys of this half that the row sees
+        const bool masked = (j + 1) * kTile > it.seen;
         float p[64];
         if (!(ok = bar_wait_warp(b.s_full + 8 * (n % 2), n / 2 & 1, w))) break;
         fence_after();
@@ -566,7 +543,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dq(const __grid_constant__
           for (int e = 0; e < 32; ++e) y[e] = pack2<BF16>(d[2 * e], d[2 * e + 1]);
           tmem_st32(Dp, y);
         }
-        if ((j + 1) * kTile > s.lk) clear_rows<DP>(sm + L::kRing + pos % L::kStages * L::kTileBytes, s.lk - j * kTile);
+        if ((j + 1) * kTile > it.keys) clear_rows<DP>(sm + L::kRing + pos % L::kStages * L::kTileBytes, it.keys - j * kTile);
         wait_st();
         fence_before();
         arrive_warp(b.ds_ready);
@@ -576,7 +553,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dq(const __grid_constant__
         if (!bar_wait_warp(b.out_full, items++ & 1, w)) break;
         fence_after();
       }
-      uint8_t* row = static_cast<uint8_t*>(a.dq.data) + 2 * ((s.q0 + query) * a.dq.row + it.head * a.dq.head);
+      uint8_t* row = static_cast<uint8_t*>(a.dq.data) + 2 * (query * a.dq.row + it.head * a.dq.head);
       write_row<BF16>(tmem + lanes + kDq, row, half * DP / 2, (half + 1) * DP / 2, a.dim, a.scale, steps > 0, valid);
     }
   }
@@ -584,11 +561,13 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dq(const __grid_constant__
   fence_before();
   __syncthreads();
   if (warp == 9) tmem_free<512>(tmem);
+  after_previous();                                          // no later kernel overtakes the key walk
 }
 
 // delta of every row and head, eight entries per lane; LANES lanes a head.
 template <int LANES, bool BF16>
 __global__ void __launch_bounds__(256) k_attn_delta(const __grid_constant__ AttnArgs a) {
+  let_next_start();
   const int64_t unit = (blockIdx.x * 256ll + threadIdx.x) / LANES;
   const int e = threadIdx.x % LANES * 8;
   const int64_t row = unit / a.heads;
@@ -610,12 +589,15 @@ __global__ void __launch_bounds__(256) k_attn_delta(const __grid_constant__ Attn
   if (row < a.delta_rows && threadIdx.x % LANES == 0) a.delta[head * a.delta_rows + row] = sum;
 }
 
+// The walks start early: the key walk's loads and products run before delta is
+// there, and the query walk, which needs nothing of the key walk, takes the
+// SMs that its last blocks leave.  (The key walk's blocks let it start only
+// once delta is there.)
 template <class K>
-cudaError_t walk(K kernel, int blocks, int bytes, const AttnArgs& a, const AttnMaps& m, cudaStream_t st) {
-  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+cudaError_t walk(K kernel, int blocks, int bytes, std::atomic<uint64_t>& allowed, const AttnArgs& a, const AttnMaps& m, cudaStream_t st) {
+  cudaError_t e = allow_smem(kernel, bytes, allowed);
   if (e != cudaSuccess) return e;
-  kernel<<<blocks, kThreads, bytes, st>>>(a, m.q, m.k, m.v, m.d_o);
-  e = cudaGetLastError();
+  e = launch_early(kernel, blocks, kThreads, bytes, st, a, m.q, m.k, m.v, m.d_o);
   if (e == cudaSuccess) count_launch();
   return e;
 }
@@ -624,6 +606,7 @@ template <int DP, bool BF16>
 cudaError_t launch(const AttnArgs& a, const AttnMaps& m, cudaStream_t st) {
   using L = Layout<DP>;
   static_assert(L::kBytes <= 227 * 1024, "shared memory");
+  static std::atomic<uint64_t> dkv_allowed{0}, dq_allowed{0};
   cudaError_t e = cudaSuccess;
   if (a.delta_rows) {
     const int64_t blocks = (a.delta_rows * a.heads * (DP / 8) + 255) / 256;
@@ -631,8 +614,8 @@ cudaError_t launch(const AttnArgs& a, const AttnMaps& m, cudaStream_t st) {
     if ((e = cudaGetLastError()) != cudaSuccess) return e;
     count_launch();
   }
-  if (a.n_k_blocks && (e = walk(k_attn_dkv<DP, BF16>, a.n_k_blocks, L::kBytes, a, m, st)) != cudaSuccess) return e;
-  if (a.n_q_blocks && (e = walk(k_attn_dq<DP, BF16>, a.n_q_blocks, L::kBytes, a, m, st)) != cudaSuccess) return e;
+  if (a.n_k_blocks && (e = walk(k_attn_dkv<DP, BF16>, a.n_k_blocks, L::kBytes, dkv_allowed, a, m, st)) != cudaSuccess) return e;
+  if (a.n_q_blocks && (e = walk(k_attn_dq<DP, BF16>, a.n_q_blocks, L::kBytes, dq_allowed, a, m, st)) != cudaSuccess) return e;
   return cudaSuccess;
 }
 

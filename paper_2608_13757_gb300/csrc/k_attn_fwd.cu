@@ -12,11 +12,11 @@
 // Rows of a tile are consecutive queries of one head, or, where a sequence
 // has few queries, the queries of all heads of a group (row = query * group +
 // head): their keys are then read once for the group.  A key range that would
-// leave SMs idle is split into pieces whose results are merged by whichever
-// block finishes last, in the order of the pieces.
+// leave SMs idle is split into pieces, whose results a second kernel merges.
 #include <algorithm>
 
 #include "attn.h"
+#include "launch.cuh"
 #include "umma.cuh"
 
 namespace syncgb {
@@ -40,24 +40,9 @@ struct Layout {
   static constexpr int kStages = DP == 128 ? 5 : 10;        // key and value tiles in flight
   static constexpr int kRing = 2 * kTileBytes;              // after the two query tiles
   static constexpr int kBars = kRing + kStages * kTileBytes;
-  static constexpr int kInts = kBars + 104 + 16 * kStages;  // after the barriers: dead, tensor memory, last[2]
-  static constexpr int kBytes = kInts + 16 + 1024;          // alignment
+  static constexpr int kInts = kBars + 88 + 16 * kStages;   // after the barriers: dead, tensor memory
+  static constexpr int kBytes = kInts + 8 + 1024;           // alignment
 };
-
-// What an item asks of query tile t: key tiles, and its rows.
-struct Part {
-  int n;          // key tiles
-  int first;      // first query
-  int rows;       // queries
-};
-__device__ __forceinline__ Part part_of(const AttnItem& it, const AttnSeq& s, int per, int t) {
-  Part p;
-  p.first = it.q0 + t * per;
-  p.rows = max(0, min(per, s.lq - p.first));
-  const int seen = max(0, p.first + p.rows + s.lk - s.lq);          // keys that the last row sees
-  p.n = p.rows ? max(0, min(it.kt1, (seen + kTile - 1) / kTile) - it.kt0) : 0;
-  return p;
-}
 
 template <bool BF16>
 __device__ __forceinline__ void store8(void* p, const float* x) {
@@ -80,10 +65,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_fwd(const __grid_constant_
   uint8_t* sm = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~(uintptr_t)1023);
   const uint32_t base = smem_addr(sm), bars = base + L::kBars;
   const uint32_t q_full = bars, q_free = bars + 16, s_full = bars + 32, p_full = bars + 48, o_full = bars + 64,
-                 merge = bars + 80, done = bars + 96, full = bars + 104, free_ = full + 8 * L::kStages;
+                 done = bars + 80, full = bars + 88, free_ = full + 8 * L::kStages;
   int* const shared_int = reinterpret_cast<int*>(sm + L::kInts);
   const Waits w{shared_int, a.error};
-  int* const last_one = shared_int + 2;
   const int warp = threadIdx.x / 32;
 
   if (threadIdx.x == 0) {
@@ -93,7 +77,6 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_fwd(const __grid_constant_
       bar_init(s_full + 8 * t, 1);
       bar_init(p_full + 8 * t, 4);
       bar_init(o_full + 8 * t, 1);
-      bar_init(merge + 8 * t, 128);
     }
     bar_init(done, 1);
     for (int i = 0; i < L::kStages; ++i) {
@@ -110,6 +93,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_fwd(const __grid_constant_
   const uint32_t tmem = (uint32_t)shared_int[1];
 
   const int group = a.heads / a.kv_heads, packed_rows = kTile / group;
+  if (threadIdx.x == 0) let_next_start();
   const int i0 = a.block_first[blockIdx.x], i1 = a.block_first[blockIdx.x + 1];
 
   if (warp >= 8) {
@@ -129,23 +113,19 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_fwd(const __grid_constant_
       };
       for (int i = i0; ok && i < i1; ++i) {
         const AttnItem it = a.item[i];
-        const AttnSeq s = a.seq[it.seq];
-        const int per = it.packed ? packed_rows : kTile;
-        const int kh = it.head / group;
-        const Part p[2] = {part_of(it, s, per, 0), part_of(it, s, per, 1)};
-        const int n = max(p[0].n, p[1].n);
+        const int per = it.packed ? packed_rows : kTile, kh = it.head / group, n = max(it.n[0], it.n[1]);
         for (int t = 0; ok && t < 2; ++t) {
-          if (!p[t].n) continue;
+          if (!it.n[t]) continue;
           if (qn[t] && !bar_wait(q_free + 8 * t, (qn[t] - 1) & 1, w)) { ok = false; break; }
           bar_expect(q_full + 8 * t, DP / 64 * (it.packed ? packed_rows * group : kTile) * 128);
 #pragma unroll
           for (int c = 0; c < DP / 64; ++c)
             tma_load(base + t * L::kTileBytes + c * kBlockBytes, it.packed ? &qg_map : &q_map, q_full + 8 * t, 64 * c,
-                     it.head, (int)s.q0 + p[t].first);
+                     it.head, (int)it.q_row + t * per);
           ++qn[t];
         }
         for (int j = 0; ok && j < n; ++j) {
-          const int row = (int)s.k0 + (it.kt0 + j) * kTile;
+          const int row = (int)it.k_row + j * kTile;
           ok = load(&k_map, kh, row) && load(&v_map, kh, row);
         }
       }
@@ -165,33 +145,33 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_fwd(const __grid_constant_
         for (int e = 0; e < ksteps; ++e) mma(tmem + s_col(t), q + step_along(e), k + step_along(e), i_s, e > 0);
         commit(s_full + 8 * t);
       };
-      auto run = [&](const Part* p) {
-        const int n = max(p[0].n, p[1].n);
+      auto run = [&](const int* tiles) {
+        const int n = max(tiles[0], tiles[1]);
         if (!n) return true;
         if (!arrived(pos)) return false;
         for (int t = 0; t < 2; ++t) {
-          if (!p[t].n) continue;
+          if (!tiles[t]) continue;
           if (!bar_wait(q_full + 8 * t, qn[t]++ & 1, w)) return false;
           fence_after();
           scores(t, pos);
-          if (p[t].n == 1) commit(q_free + 8 * t);
+          if (tiles[t] == 1) commit(q_free + 8 * t);
         }
         commit(free_ + 8 * (pos % L::kStages));
         for (int j = 0; j < n; ++j, pos += 2) {
           if (!arrived(pos + 1) || (j + 1 < n && !arrived(pos + 2))) return false;
           for (int t = 0; t < 2; ++t) {
-            if (j < p[t].n) {
+            if (j < tiles[t]) {
               if (!bar_wait(p_full + 8 * t, pn[t]++ & 1, w)) return false;
               fence_after();
               const uint64_t v = tile(pos + 1);
 #pragma unroll
               for (int e = 0; e < kTile / 16; ++e)
                 mma_tmem(tmem + o_col(t), tmem + s_col(t) + 8 * e, v + step_rows(e), i_o, j > 0 || e > 0);
-              if (j + 1 == p[t].n) commit(o_full + 8 * t);
+              if (j + 1 == tiles[t]) commit(o_full + 8 * t);
             }
-            if (j + 1 < p[t].n) {
+            if (j + 1 < tiles[t]) {
               scores(t, pos + 2);
-              if (j + 2 == p[t].n) commit(q_free + 8 * t);
+              if (j + 2 == tiles[t]) commit(q_free + 8 * t);
             }
           }
           commit(free_ + 8 * ((pos + 1) % L::kStages));
@@ -200,11 +180,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_fwd(const __grid_constant_
         return true;
       };
       for (int i = i0; i < i1; ++i) {
-        const AttnItem it = a.item[i];
-        const AttnSeq s = a.seq[it.seq];
-        const int per = it.packed ? packed_rows : kTile;
-        const Part p[2] = {part_of(it, s, per, 0), part_of(it, s, per, 1)};
-        if (!run(p)) break;
+        const int tiles[2] = {a.item[i].n[0], a.item[i].n[1]};
+        if (!run(tiles)) break;
       }
       commit(done);
       bar_wait(done, 0, w);
@@ -215,29 +192,29 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_fwd(const __grid_constant_
     const uint32_t lanes = (uint32_t)(warp % 4 * 32) << 16, S = tmem + s_col(t) + lanes, O = tmem + o_col(t) + lanes;
     const float c2 = a.scale * 1.4426950408889634f;          // weights are powers of two
     const float slack = 8.f / c2;                            // see below
-    uint32_t pos = 0, sn = 0, on = 0, mn = 0;
+    uint32_t pos = 0, sn = 0, on = 0;
     for (int i = i0; i < i1; ++i) {
       const AttnItem it = a.item[i];
-      const AttnSeq s = a.seq[it.seq];
+      if (i + 1 < i1) asm volatile("prefetch.global.L1 [%0];" ::"l"(a.item + i + 1));
       const int per = it.packed ? packed_rows : kTile;
-      const Part p[2] = {part_of(it, s, per, 0), part_of(it, s, per, 1)};
-      const int n = p[t].n, rq = it.packed ? r / group : r;
+      const int n = it.n[t], rows = it.rows[t], rq = it.packed ? r / group : r;
       const int head = it.packed ? it.head + r % group : it.head;
-      const int query = p[t].first + rq, offset = s.lk - s.lq;
-      const bool valid = rq < p[t].rows;
-      const int last_key = min(query, s.lq - 1) + offset;    // the last one that this row sees
+      const int64_t query = it.q_row + t * per + rq;
+      const bool valid = rq < rows;
+      const int least = it.seen + t * per;                   // keys that the tile's first query sees
+      const int seen_all = min(least + rq, it.keys);         // and this row
       float m = -INFINITY, l = 0.f;
       bool ok = true;
       for (int j = 0; j < n; ++j) {
-        const int k0 = (it.kt0 + j) * kTile;
+        const int k0 = j * kTile;
         if (!(ok = bar_wait_warp(s_full + 8 * t, sn++ & 1, w))) break;
         fence_after();
         float x[kTile];
 #pragma unroll
         for (int c = 0; c < kTile; c += 32) tmem_ld32(S + c, x + c);
         wait_ld();
-        if (k0 + kTile - 1 > p[t].first + offset) {           // some row does not see the whole tile
-          const int seen = last_key - k0 + 1;
+        if (k0 + kTile > least) {                             // some row does not see the whole tile
+          const int seen = seen_all - k0;
 #pragma unroll
           for (int c = 0; c < kTile; ++c) x[c] = c < seen ? x[c] : -INFINITY;
         }
@@ -284,14 +261,14 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_fwd(const __grid_constant_
           tmem_st16(S + c / 2, y);
         }
         l += (l4[0] + l4[1]) + (l4[2] + l4[3]);
-        if (k0 + kTile > s.lk) {
+        if (k0 + kTile > it.keys) {
           // The tile ends past the sequence: its values there belong to others
           // and may be anything, so they are cleared (both groups write the
           // same zeros).
           const uint32_t at = pos + 2 * j + 1, st = at % L::kStages;
           if (!(ok = bar_wait_warp(full + 8 * st, at / L::kStages & 1, w))) break;
           uint8_t* v = sm + L::kRing + st * L::kTileBytes;
-          for (int b = (s.lk - k0) * 8 + r; b < kTile * 8; b += 128)
+          for (int b = (it.keys - k0) * 8 + r; b < kTile * 8; b += 128)
 #pragma unroll
             for (int c = 0; c < DP / 64; ++c) *reinterpret_cast<uint4*>(v + c * kBlockBytes + b * 16) = make_uint4(0, 0, 0, 0);
           fence_async();
@@ -301,7 +278,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_fwd(const __grid_constant_
         __syncwarp();
         if (threadIdx.x % 32 == 0) bar_arrive(p_full + 8 * t);
       }
-      pos += 2 * max(p[0].n, p[1].n);
+      pos += 2 * max(it.n[0], it.n[1]);
       if (!ok) break;
       if (n) {
         if (!bar_wait_warp(o_full + 8 * t, on++ & 1, w)) break;
@@ -309,8 +286,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_fwd(const __grid_constant_
       }
       const float by = l == 0.f ? 0.f : 1.f / l;
       const float lse2 = l == 0.f ? -INFINITY : fmaf(m, c2, log2f(l));
-      if (it.group < 0) {
-        uint8_t* out = static_cast<uint8_t*>(a.o.data) + 2 * ((s.q0 + query) * a.o.row + head * a.o.head);
+      if (it.slot < 0) {
+        uint8_t* out = static_cast<uint8_t*>(a.o.data) + 2 * (query * a.o.row + head * a.o.head);
 #pragma unroll 1
         for (int c = 0; c < DP; c += 32) {
           float o[32];
@@ -325,15 +302,12 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_fwd(const __grid_constant_
             for (int e = 0; e < 32; e += 8)
               if (c + e < a.dim) store8<BF16>(out + 2 * (c + e), o + e);
         }
-        if (valid && a.lse) a.lse[head * a.q.rows + s.q0 + query] = lse2 * 0.6931471805599453f;
+        if (valid && a.lse) a.lse[head * a.q.rows + query] = lse2 * 0.6931471805599453f;
         continue;
       }
-      // A piece of a split key range: its rows, scaled by its own sum, and
-      // their logarithms, for the piece that finishes last.
-      const AttnSplit g = a.split[it.group];
-      float* part = a.part_o + ((int64_t)(g.slot + it.piece) * 2 + t) * kTile * DP;
-      float* part_lse = a.part_lse + ((int64_t)(g.slot + it.piece) * 2 + t) * kTile;
-      if (p[t].rows == 0) continue;                           // no piece of this tile has rows
+      // A piece of a split key range leaves its rows, scaled by its own sum,
+      // and their logarithms.
+      float* part = a.part_o + ((int64_t)it.slot * 2 + t) * kTile * DP;
 #pragma unroll 1
       for (int c = 0; c < DP; c += 32) {
         float o[32];
@@ -349,48 +323,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_fwd(const __grid_constant_
             *reinterpret_cast<float4*>(part + r * DP + c + e) = f;
           }
       }
-      if (valid) part_lse[r] = lse2;
-      __threadfence();
-      bar_arrive(merge + 8 * t);
-      if (!bar_wait_warp(merge + 8 * t, mn++ & 1, w)) break;
-      if (r == 0) {
-        const int before = atomicAdd(a.split_count + 2 * it.group + t, 1);
-        last_one[t] = before == g.pieces - 1;
-        if (before == g.pieces - 1) a.split_count[2 * it.group + t] = 0;
-      }
-      bar_arrive(merge + 8 * t);
-      if (!bar_wait_warp(merge + 8 * t, mn++ & 1, w)) break;
-      if (!last_one[t]) continue;
-      __threadfence();
-      const int lane = threadIdx.x % 32;
-      const float* lse0 = a.part_lse + ((int64_t)g.slot * 2 + t) * kTile;
-      const float* o0 = a.part_o + ((int64_t)g.slot * 2 + t) * kTile * DP;
-      for (int row = warp % 4; row < p[t].rows * (it.packed ? group : 1); row += 4) {
-        float top = -INFINITY;
-        for (int k = lane; k < g.pieces; k += 32) top = fmaxf(top, __ldcg(lse0 + (int64_t)k * 2 * kTile + row));
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, o));
-        const float from = top == -INFINITY ? 0.f : top;
-        float acc[DP / 32], sum = 0.f;
-#pragma unroll
-        for (int e = 0; e < DP / 32; ++e) acc[e] = 0.f;
-#pragma unroll 4
-        for (int k = 0; k < g.pieces; ++k) {
-          const float f = exp2_fast(__ldcg(lse0 + (int64_t)k * 2 * kTile + row) - from);
-          sum += f;
-#pragma unroll
-          for (int e = 0; e < DP / 32; ++e) acc[e] += f * __ldcg(o0 + ((int64_t)k * 2 * kTile + row) * DP + lane * (DP / 32) + e);
-        }
-        const float inv = sum == 0.f ? 0.f : 1.f / sum;
-        const int rq1 = it.packed ? row / group : row, h1 = it.packed ? it.head + row % group : it.head;
-        const int64_t at = s.q0 + p[t].first + rq1;
-        if (lane * (DP / 32) < a.dim) {
-          uint8_t* out = static_cast<uint8_t*>(a.o.data) + 2 * (at * a.o.row + h1 * a.o.head + lane * (DP / 32));
-#pragma unroll
-          for (int e = 0; e < DP / 32; e += 2) *reinterpret_cast<uint32_t*>(out + 2 * e) = pack2<BF16>(acc[e] * inv, acc[e + 1] * inv);
-        }
-        if (a.lse && lane == 0) a.lse[h1 * a.q.rows + at] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * 0.6931471805599453f;
-      }
+      if (valid) a.part_lse[((int64_t)it.slot * 2 + t) * kTile + r] = lse2;
     }
   }
   __syncwarp();
@@ -399,15 +332,55 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_fwd(const __grid_constant_
   if (warp == 9) tmem_free<kCols>(tmem);
 }
 
+// Rows of split key ranges from their pieces, in the order of the pieces: a
+// warp per row, DP / 32 entries per lane.
+template <int DP, bool BF16>
+__global__ void __launch_bounds__(256) k_attn_merge(const __grid_constant__ AttnArgs a) {
+  after_previous();
+  const AttnSplit s = a.split[blockIdx.x];
+  const int group = a.heads / a.kv_heads, heads = s.packed ? group : 1, lane = threadIdx.x % 32;
+  int row = blockIdx.y * 8 + threadIdx.x / 32;
+  const int n0 = s.rows[0] * heads, t = row >= n0;
+  if (t) row -= n0;
+  if (row >= s.rows[t] * heads) return;
+  const float* lse = a.part_lse + ((int64_t)s.slot * 2 + t) * kTile + row;
+  const float* part = a.part_o + (((int64_t)s.slot * 2 + t) * kTile + row) * DP + lane * (DP / 32);
+  float top = -INFINITY;
+  for (int k = lane; k < s.pieces; k += 32) top = fmaxf(top, lse[(int64_t)k * 2 * kTile]);
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, o));
+  const float from = top == -INFINITY ? 0.f : top;
+  float acc[DP / 32] = {}, sum = 0.f;
+#pragma unroll 8
+  for (int k = 0; k < s.pieces; ++k) {
+    const float f = exp2_fast(lse[(int64_t)k * 2 * kTile] - from);
+    sum += f;
+#pragma unroll
+    for (int e = 0; e < DP / 32; ++e) acc[e] = fmaf(f, part[(int64_t)k * 2 * kTile * DP + e], acc[e]);
+  }
+  const float by = sum == 0.f ? 0.f : 1.f / sum;
+  const int head = s.packed ? s.head + row % group : s.head;
+  const int64_t query = s.q_row + t * (s.packed ? kTile / group : kTile) + (s.packed ? row / group : row);
+  if (lane * (DP / 32) < a.dim) {
+    uint8_t* out = static_cast<uint8_t*>(a.o.data) + 2 * (query * a.o.row + head * a.o.head + lane * (DP / 32));
+#pragma unroll
+    for (int e = 0; e < DP / 32; e += 2) *reinterpret_cast<uint32_t*>(out + 2 * e) = pack2<BF16>(acc[e] * by, acc[e + 1] * by);
+  }
+  if (a.lse && lane == 0) a.lse[head * a.q.rows + query] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * 0.6931471805599453f;
+}
+
 template <int DP, bool BF16>
 cudaError_t launch(const AttnArgs& a, const AttnMaps& m, cudaStream_t st) {
   using L = Layout<DP>;
-  // set on every call: a device keeps its own value, and the call costs a microsecond at most
-  cudaError_t e = cudaFuncSetAttribute(k_attn_fwd<DP, BF16>, cudaFuncAttributeMaxDynamicSharedMemorySize, L::kBytes);
+  static std::atomic<uint64_t> allowed{0};
+  cudaError_t e = allow_smem(k_attn_fwd<DP, BF16>, L::kBytes, allowed);
   if (e != cudaSuccess) return e;
   k_attn_fwd<DP, BF16><<<a.n_blocks, kThreads, L::kBytes, st>>>(a, m.q, m.q_group, m.k, m.v);
-  e = cudaGetLastError();
-  if (e == cudaSuccess) count_launch();
+  if ((e = cudaGetLastError()) != cudaSuccess) return e;
+  count_launch();
+  if (!a.n_splits) return cudaSuccess;
+  const dim3 grid((unsigned)a.n_splits, (unsigned)(a.merge_rows + 7) / 8);
+  if ((e = launch_early(k_attn_merge<DP, BF16>, grid, 256, 0, st, a)) == cudaSuccess) count_launch();
   return e;
 }
 
