@@ -94,6 +94,7 @@ __device__ __forceinline__ void write_row(uint32_t acc, void* row, int c0, int c
 #pragma unroll 1
   for (int c = c0; c < c1; c += 32) {
     float x[32];
+    __syncwarp();
     if (any) {
       tmem_ld32(acc + c, x);
       wait_ld();
@@ -119,26 +120,14 @@ __device__ __forceinline__ void clear_rows(uint8_t* tile, int rows) {
   fence_async();
 }
 
-__device__ __forceinline__ void arrive_warp(uint32_t bar) {
-  __syncwarp();
-  if (threadIdx.x % 32 == 0) bar_arrive(bar);
-}
-
-// The swizzle goes by address bits: tiles start at multiples of 1024 bytes, as
-// the start of a block's shared memory does.
-__device__ __forceinline__ bool swizzle_aligned(uint32_t base, Waits w) {
-  if (base % 1024 == 0) return true;
-  if (threadIdx.x == 0) *reinterpret_cast<volatile int*>(w.error) = 1;
-  return false;
-}
-
-// Loads of one block: a ring of tiles, two tiles that stay for an item.
+// Loads of one block, by one warp: a ring of tiles, two tiles that stay for an item.
 template <int DP>
 struct Loader {
   using L = Layout<DP>;
   uint32_t base;
   const Bars<DP>& b;
   Waits w;
+  bool leader;
   uint32_t pos = 0, fixed = 0;
   __device__ __forceinline__ void tile(uint32_t dst, const CUtensorMap* map, uint32_t bar, int head, int row) {
 #pragma unroll
@@ -146,17 +135,21 @@ struct Loader {
   }
   __device__ __forceinline__ bool stay(const CUtensorMap* m0, const CUtensorMap* m1, int head, int row) {
     if (fixed && !bar_wait(b.fixed_free, (fixed - 1) & 1, w)) return false;
-    bar_expect(b.fixed_full, 2 * L::kTileBytes);
-    tile(base, m0, b.fixed_full, head, row);
-    tile(base + L::kTileBytes, m1, b.fixed_full, head, row);
+    if (leader) {
+      bar_expect(b.fixed_full, 2 * L::kTileBytes);
+      tile(base, m0, b.fixed_full, head, row);
+      tile(base + L::kTileBytes, m1, b.fixed_full, head, row);
+    }
     ++fixed;
     return true;
   }
   __device__ __forceinline__ bool next(const CUtensorMap* map, int head, int row) {
     const uint32_t st = pos % L::kStages;
     if (pos >= L::kStages && !bar_wait(b.free_ + 8 * st, (pos / L::kStages - 1) & 1, w)) return false;
-    bar_expect(b.full + 8 * st, L::kTileBytes);
-    tile(base + L::kRing + st * L::kTileBytes, map, b.full + 8 * st, head, row);
+    if (leader) {
+      bar_expect(b.full + 8 * st, L::kTileBytes);
+      tile(base + L::kRing + st * L::kTileBytes, map, b.full + 8 * st, head, row);
+    }
     ++pos;
     return true;
   }
@@ -180,7 +173,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dkv(const __grid_constant_
   const Bars<DP> b(base + L::kBars);
   int* const shared_int = reinterpret_cast<int*>(sm + L::kInts);
   const Waits w{shared_int, a.error};
-  const int warp = threadIdx.x / 32;
+  const int warp = uniform(threadIdx.x / 32);
   if (!swizzle_aligned(base, w)) return;
   if (threadIdx.x == 0) {
     b.init();
@@ -192,48 +185,57 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dkv(const __grid_constant_
   fence_after();
   const uint32_t tmem = (uint32_t)shared_int[1];
   const int group = a.heads / a.kv_heads;
-  const int i0 = a.k_first[blockIdx.x], i1 = a.k_first[blockIdx.x + 1];
+  const int i0 = uniform(a.k_first[blockIdx.x]), i1 = uniform(a.k_first[blockIdx.x + 1]);
 
   if (warp >= 8) {
     regs_down<kRegsFew>();
-    if (warp == 8 && elect_one()) {                         // ---- loads
-      Loader<DP> load{base, b, w};
+    const bool leader = elect_one();
+    if (warp == 8) {                                        // ---- loads
+      Loader<DP> load{base, b, w, leader};
       bool ok = true;
       for (int i = i0; ok && i < i1; ++i) {
         const AttnTile it = a.k_tile[i];
-        if (!it.n) continue;
-        ok = load.stay(&k_map, &v_map, it.head, (int)it.k_row);
-        for (int h = it.head * group; ok && h < (it.head + 1) * group; ++h)
-          for (int t = 0; ok && t < it.n; ++t)
+        const int n = uniform(it.n), head = uniform(it.head);
+        if (!n) continue;
+        ok = load.stay(&k_map, &v_map, head, (int)it.k_row);
+        for (int h = head * group; ok && h < (head + 1) * group; ++h)
+          for (int t = 0; ok && t < n; ++t)
             ok = load.next(&q_map, h, (int)it.q_row + t * kTile) && load.next(&do_map, h, (int)it.q_row + t * kTile);
       }
       load.finish();
-    } else if (warp == 9 && elect_one()) {                  // ---- products
+    } else if (warp == 9) {                                 // ---- products
       const int ksteps = (a.dim + 15) / 16;
       const uint32_t i_s = instr(BF16, kTile, false), i_o = instr(BF16, ksteps * 16, true);
       uint32_t pos = 0, fixed = 0, n = 0;                    // n: steps so far
       auto tile = [&](uint32_t at) { return tile_desc(base + L::kRing + at % L::kStages * L::kTileBytes); };
       auto arrived = [&](uint32_t at) { return bar_wait(b.full + 8 * (at % L::kStages), at / L::kStages & 1, w); };
-      auto release = [&](uint32_t at) { commit(b.free_ + 8 * (at % L::kStages)); };
-      auto across = [&](uint32_t d, uint64_t x, uint32_t at) {       // keys by queries
-        const uint64_t y = tile(at);
-        for (int e = 0; e < ksteps; ++e) mma(tmem + d, x + step_along(e), y + step_along(e), i_s, e > 0);
+      auto done_with = [&](uint32_t bar) {
+        if (leader) commit(bar);
+      };
+      auto release = [&](uint32_t at) { done_with(b.free_ + 8 * (at % L::kStages)); };
+      auto across = [&](uint32_t d, uint32_t x, uint32_t at) {       // keys by queries
+        const uint32_t y = tile(at);
+        if (leader)
+#pragma unroll
+          for (int e = 0; e < DP / 16; ++e)
+            if (e < ksteps) mma(tmem + d, x + step_along(e), y + step_along(e), i_s, e > 0);
       };
       auto gradient = [&](uint32_t d, uint32_t x, uint32_t at, bool add) {
-        const uint64_t y = tile(at);
+        const uint32_t y = tile(at);
+        if (leader)
 #pragma unroll
-        for (int e = 0; e < kTile / 16; ++e) mma_tmem(tmem + d, tmem + x + e / 4 * 64 + e % 4 * 8, y + step_rows(e), i_o, add || e > 0);
+          for (int e = 0; e < kTile / 16; ++e) mma_tmem(tmem + d, tmem + x + e / 4 * 64 + e % 4 * 8, y + step_rows(e), i_o, add || e > 0);
       };
-      const uint64_t K = tile_desc(base), V = tile_desc(base + L::kTileBytes);
+      const uint32_t K = tile_desc(base), V = tile_desc(base + L::kTileBytes);
       auto run = [&](int steps) {
         if (!bar_wait(b.fixed_full, fixed++ & 1, w) || !arrived(pos)) return false;
         fence_after();
         across(kS, K, pos);
-        commit(b.s_full);
+        done_with(b.s_full);
         if (!arrived(pos + 1)) return false;
         across(kDp, V, pos + 1);
-        commit(b.dp_full);
-        if (steps == 1) commit(b.fixed_free);
+        done_with(b.dp_full);
+        if (steps == 1) done_with(b.fixed_free);
         for (int j = 0; j < steps; ++j, pos += 2, ++n) {
           if (!bar_wait(b.p_ready, n & 1, w)) return false;
           fence_after();
@@ -242,7 +244,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dkv(const __grid_constant_
           if (j + 1 < steps) {
             if (!arrived(pos + 2)) return false;
             across(kS, K, pos + 2);
-            commit(b.s_full);
+            done_with(b.s_full);
           }
           if (!bar_wait(b.ds_ready, n & 1, w)) return false;
           fence_after();
@@ -251,18 +253,18 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dkv(const __grid_constant_
           if (j + 1 < steps) {
             if (!arrived(pos + 3)) return false;
             across(kDp, V, pos + 3);
-            commit(b.dp_full);
-            if (j + 2 == steps) commit(b.fixed_free);
+            done_with(b.dp_full);
+            if (j + 2 == steps) done_with(b.fixed_free);
           }
         }
-        commit(b.out_full);
+        done_with(b.out_full);
         return true;
       };
       for (int i = i0; i < i1; ++i) {
-        const int steps = a.k_tile[i].n * group;
+        const int steps = uniform(a.k_tile[i].n) * group;
         if (steps && !run(steps)) break;
       }
-      commit(b.done);
+      done_with(b.done);
       bar_wait(b.done, 0, w);
     } else if (warp == 10) {                                // ---- lse and delta of the query tiles
       const int lane = threadIdx.x % 32;
@@ -272,8 +274,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dkv(const __grid_constant_
       let_next_start();
       for (int i = i0; ok && i < i1; ++i) {
         const AttnTile it = a.k_tile[i];
-        for (int h = it.head * group; ok && h < (it.head + 1) * group; ++h)
-          for (int t = 0; t < it.n; ++t, ++n) {
+        const int tiles = uniform(it.n), head = uniform(it.head);
+        for (int h = head * group; ok && h < (head + 1) * group; ++h)
+          for (int t = 0; t < tiles; ++t, ++n) {
             const uint32_t st = n % L::kStatStages;
             float lse[4], delta[4];
 #pragma unroll
@@ -283,19 +286,20 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dkv(const __grid_constant_
               delta[e] = q < it.rows ? a.delta[h * a.delta_rows + it.q_row + q] : 0.f;
               if (lse[e] == -INFINITY) lse[e] = INFINITY;    // no weight for a row that sees nothing
             }
-            if (n >= L::kStatStages && !(ok = bar_wait_warp(b.stat_free + 8 * st, (n / L::kStatStages - 1) & 1, w))) break;
+            if (n >= L::kStatStages && !(ok = bar_wait(b.stat_free + 8 * st, (n / L::kStatStages - 1) & 1, w))) break;
             float* at = reinterpret_cast<float*>(sm + L::kStats + st * L::kStatBytes);
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
               at[lane + 32 * e] = lse[e];
               at[kTile + lane + 32 * e] = delta[e];
             }
-            arrive_warp(b.stat_full + 8 * st);
+            bar_arrive_warp(b.stat_full + 8 * st, leader);
           }
       }
     }
   } else {                                                  // ---- arithmetic: a key per lane, 64 queries
     regs_up<kRegsMany>();
+    const bool leader = elect_one();
     const int half = warp / 4, r = threadIdx.x % 128, c0 = 64 * half;
     const uint32_t lanes = (uint32_t)(warp % 4 * 32) << 16;
     const uint32_t S = tmem + lanes + kS + c0, Dp = tmem + lanes + kDp + c0;
@@ -304,19 +308,19 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dkv(const __grid_constant_
     for (int i = i0; i < i1; ++i) {
       const AttnTile it = a.k_tile[i];
       if (i + 1 < i1) asm volatile("prefetch.global.L1 [%0];" ::"l"(a.k_tile + i + 1));
-      const int steps = it.n * group;
+      const int tiles = uniform(it.n), steps = tiles * group, queries = uniform(it.rows), first_seen = uniform(it.seen);
       bool ok = true;
       int t = 0;
       for (int j = 0; j < steps; ++j, ++n, pos += 2) {
         const uint32_t st = n % L::kStatStages;
         const float* stat = reinterpret_cast<const float*>(sm + L::kStats + st * L::kStatBytes) + c0;
         // queries [from, to) of this half see the key
-        const int q0 = t * kTile, rows = it.rows - q0;
-        const int from = r + 1 - it.seen - q0 - c0, to = rows - c0;
-        const bool tail = rows < kTile, masked = it.seen + q0 < kTile || tail;
-        t = t + 1 < it.n ? t + 1 : 0;
+        const int q0 = t * kTile, rows = queries - q0;
+        const int from = r + 1 - first_seen - q0 - c0, to = rows - c0;
+        const bool tail = rows < kTile, masked = first_seen + q0 < kTile || tail;
+        t = t + 1 < tiles ? t + 1 : 0;
         float p[64];
-        if (!(ok = bar_wait_warp(b.stat_full + 8 * st, n / L::kStatStages & 1, w) && bar_wait_warp(b.s_full, n & 1, w))) break;
+        if (!(ok = bar_wait(b.stat_full + 8 * st, n / L::kStatStages & 1, w) && bar_wait(b.s_full, n & 1, w))) break;
         fence_after();
         tmem_ld32(S, p);
         tmem_ld32(S + 32, p + 32);
@@ -340,13 +344,13 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dkv(const __grid_constant_
         }
         if (tail) {
           const uint32_t at = pos + 1, sg = at % L::kStages;
-          if (!(ok = bar_wait_warp(b.full + 8 * sg, at / L::kStages & 1, w))) break;
+          if (!(ok = bar_wait(b.full + 8 * sg, at / L::kStages & 1, w))) break;
           clear_rows<DP>(sm + L::kRing + sg * L::kTileBytes, rows);
         }
         wait_st();
         fence_before();
-        arrive_warp(b.p_ready);
-        if (!(ok = bar_wait_warp(b.dp_full, n & 1, w))) break;
+        bar_arrive_warp(b.p_ready, leader);
+        if (!(ok = bar_wait(b.dp_full, n & 1, w))) break;
         fence_after();
         float d[64];
         tmem_ld32(Dp, d);
@@ -372,15 +376,12 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dkv(const __grid_constant_
         if (tail) clear_rows<DP>(sm + L::kRing + pos % L::kStages * L::kTileBytes, rows);   // there since S is
         wait_st();
         fence_before();
-        __syncwarp();
-        if (threadIdx.x % 32 == 0) {
-          bar_arrive(b.ds_ready);
-          bar_arrive(b.stat_free + 8 * st);
-        }
+        bar_arrive_warp(b.ds_ready, leader);
+        bar_arrive_warp(b.stat_free + 8 * st, leader);
       }
       if (!ok) break;
       if (steps) {
-        if (!bar_wait_warp(b.out_full, items++ & 1, w)) break;
+        if (!bar_wait(b.out_full, items++ & 1, w)) break;
         fence_after();
       }
       const AttnTensor& out = half ? a.dk : a.dv;
@@ -407,7 +408,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dq(const __grid_constant__
   const Bars<DP> b(base + L::kBars);
   int* const shared_int = reinterpret_cast<int*>(sm + L::kInts);
   const Waits w{shared_int, a.error};
-  const int warp = threadIdx.x / 32;
+  const int warp = uniform(threadIdx.x / 32);
   if (!swizzle_aligned(base, w)) return;
   if (threadIdx.x == 0) {
     b.init();
@@ -419,37 +420,45 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dq(const __grid_constant__
   fence_after();
   const uint32_t tmem = (uint32_t)shared_int[1];
   const int group = a.heads / a.kv_heads;
-  const int i0 = a.q_first[blockIdx.x], i1 = a.q_first[blockIdx.x + 1];
+  const int i0 = uniform(a.q_first[blockIdx.x]), i1 = uniform(a.q_first[blockIdx.x + 1]);
 
   if (warp >= 8) {
     regs_down<kRegsFew>();
-    if (warp == 8 && elect_one()) {                         // ---- loads
-      Loader<DP> load{base, b, w};
+    const bool leader = elect_one();
+    if (warp == 8) {                                        // ---- loads
+      Loader<DP> load{base, b, w, leader};
       bool ok = true;
       for (int i = i0; ok && i < i1; ++i) {
         const AttnTile it = a.q_tile[i];
-        if (!it.n) continue;
+        const int n = uniform(it.n);
+        if (!n) continue;
         ok = load.stay(&q_map, &do_map, it.head, (int)it.q_row);
-        for (int j = 0; ok && j < it.n; ++j)
+        for (int j = 0; ok && j < n; ++j)
           ok = load.next(&k_map, it.head / group, (int)it.k_row + j * kTile) &&
                load.next(&v_map, it.head / group, (int)it.k_row + j * kTile);
       }
       load.finish();
-    } else if (warp == 9 && elect_one()) {                  // ---- products
+    } else if (warp == 9) {                                 // ---- products
       const int ksteps = (a.dim + 15) / 16;
       const uint32_t i_s = instr(BF16, kTile, false), i_o = instr(BF16, ksteps * 16, true);
       uint32_t pos = 0, fixed = 0, n = 0;
       auto tile = [&](uint32_t at) { return tile_desc(base + L::kRing + at % L::kStages * L::kTileBytes); };
       auto arrived = [&](uint32_t at) { return bar_wait(b.full + 8 * (at % L::kStages), at / L::kStages & 1, w); };
-      auto release = [&](uint32_t at) { commit(b.free_ + 8 * (at % L::kStages)); };
-      const uint64_t Q = tile_desc(base), dO = tile_desc(base + L::kTileBytes);
-      auto across = [&](uint32_t d, uint64_t x, uint32_t at) {       // queries by keys
-        const uint64_t y = tile(at);
-        for (int e = 0; e < ksteps; ++e) mma(tmem + d, x + step_along(e), y + step_along(e), i_s, e > 0);
+      auto done_with = [&](uint32_t bar) {
+        if (leader) commit(bar);
+      };
+      auto release = [&](uint32_t at) { done_with(b.free_ + 8 * (at % L::kStages)); };
+      const uint32_t Q = tile_desc(base), dO = tile_desc(base + L::kTileBytes);
+      auto across = [&](uint32_t d, uint32_t x, uint32_t at) {       // queries by keys
+        const uint32_t y = tile(at);
+        if (leader)
+#pragma unroll
+          for (int e = 0; e < DP / 16; ++e)
+            if (e < ksteps) mma(tmem + d, x + step_along(e), y + step_along(e), i_s, e > 0);
       };
       auto scores = [&](uint32_t step, uint32_t at) {
         across(kS + step % 2 * 128, Q, at);
-        commit(b.s_full + 8 * (step % 2));
+        done_with(b.s_full + 8 * (step % 2));
       };
       auto run = [&](int steps) {
         if (!bar_wait(b.fixed_full, fixed++ & 1, w) || !arrived(pos)) return false;
@@ -457,46 +466,48 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dq(const __grid_constant__
         scores(n, pos);
         if (!arrived(pos + 1)) return false;
         across(kDp, dO, pos + 1);
-        commit(b.dp_full);
+        done_with(b.dp_full);
         release(pos + 1);
         if (steps > 1) {
           if (!arrived(pos + 2)) return false;
           scores(n + 1, pos + 2);
         } else {
-          commit(b.fixed_free);
+          done_with(b.fixed_free);
         }
         for (int j = 0; j < steps; ++j, pos += 2, ++n) {
           if (!bar_wait(b.ds_ready, n & 1, w)) return false;
           fence_after();
-          const uint64_t k = tile(pos);
+          const uint32_t k = tile(pos);
+          if (leader)
 #pragma unroll
-          for (int e = 0; e < kTile / 16; ++e)
-            mma_tmem(tmem + kDq, tmem + kDp + e / 4 * 64 + e % 4 * 8, k + step_rows(e), i_o, j > 0 || e > 0);
+            for (int e = 0; e < kTile / 16; ++e)
+              mma_tmem(tmem + kDq, tmem + kDp + e / 4 * 64 + e % 4 * 8, k + step_rows(e), i_o, j > 0 || e > 0);
           release(pos);
           if (j + 1 < steps) {
             if (!arrived(pos + 3)) return false;
             across(kDp, dO, pos + 3);
-            commit(b.dp_full);
+            done_with(b.dp_full);
             release(pos + 3);
           }
           if (j + 2 < steps) {
             if (!arrived(pos + 4)) return false;
             scores(n + 2, pos + 4);
           }
-          if (j + 2 == steps) commit(b.fixed_free);
+          if (j + 2 == steps) done_with(b.fixed_free);
         }
-        commit(b.out_full);
+        done_with(b.out_full);
         return true;
       };
       for (int i = i0; i < i1; ++i) {
-        const int steps = a.q_tile[i].n;
+        const int steps = uniform(a.q_tile[i].n);
         if (steps && !run(steps)) break;
       }
-      commit(b.done);
+      done_with(b.done);
       bar_wait(b.done, 0, w);
     }
   } else {                                                  // ---- arithmetic: a query per lane, 64 keys
     regs_up<kRegsMany>();
+    const bool leader = elect_one();
     const int half = warp / 4, r = threadIdx.x % 128, c0 = 64 * half;
     const uint32_t lanes = (uint32_t)(warp % 4 * 32) << 16, Dp = tmem + lanes + kDp + c0;
     const float c2 = a.scale * kLog2e;
@@ -504,7 +515,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dq(const __grid_constant__
     for (int i = i0; i < i1; ++i) {
       const AttnTile it = a.q_tile[i];
       if (i + 1 < i1) asm volatile("prefetch.global.L1 [%0];" ::"l"(a.q_tile + i + 1));
-      const int steps = it.n;
+      const int steps = uniform(it.n), first_seen = uniform(it.seen), keys = uniform(it.keys);
       const int64_t query = it.q_row + r;
       const bool valid = r < it.rows;
       float lse = INFINITY, delta = 0.f;
@@ -516,17 +527,17 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dq(const __grid_constant__
       bool ok = true;
       for (int j = 0; j < steps; ++j, ++n, pos += 2) {
         const uint32_t S = tmem + lanes + kS + n % 2 * 128 + c0;
-        const int seen = it.seen + r - j * kTile - c0;                   // keys of this half that the row sees
-        const bool masked = (j + 1) * kTile > it.seen;
+        const int seen = first_seen + r - j * kTile - c0;                   // keys of this half that the row sees
+        const bool masked = (j + 1) * kTile > first_seen;
         float p[64];
-        if (!(ok = bar_wait_warp(b.s_full + 8 * (n % 2), n / 2 & 1, w))) break;
+        if (!(ok = bar_wait(b.s_full + 8 * (n % 2), n / 2 & 1, w))) break;
         fence_after();
         tmem_ld32(S, p);
         tmem_ld32(S + 32, p + 32);
         wait_ld();
 #pragma unroll
         for (int e = 0; e < 64; ++e) p[e] = exp2_fast(fmaf(p[e], c2, -lse));
-        if (!(ok = bar_wait_warp(b.dp_full, n & 1, w))) break;
+        if (!(ok = bar_wait(b.dp_full, n & 1, w))) break;
         fence_after();
         float d[64];
         tmem_ld32(Dp, d);
@@ -543,14 +554,14 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dq(const __grid_constant__
           for (int e = 0; e < 32; ++e) y[e] = pack2<BF16>(d[2 * e], d[2 * e + 1]);
           tmem_st32(Dp, y);
         }
-        if ((j + 1) * kTile > it.keys) clear_rows<DP>(sm + L::kRing + pos % L::kStages * L::kTileBytes, it.keys - j * kTile);
+        if ((j + 1) * kTile > keys) clear_rows<DP>(sm + L::kRing + pos % L::kStages * L::kTileBytes, keys - j * kTile);
         wait_st();
         fence_before();
-        arrive_warp(b.ds_ready);
+        bar_arrive_warp(b.ds_ready, leader);
       }
       if (!ok) break;
       if (steps) {
-        if (!bar_wait_warp(b.out_full, items++ & 1, w)) break;
+        if (!bar_wait(b.out_full, items++ & 1, w)) break;
         fence_after();
       }
       uint8_t* row = static_cast<uint8_t*>(a.dq.data) + 2 * (query * a.dq.row + it.head * a.dq.head);

@@ -2,12 +2,19 @@
 //
 // One block per SM takes work items in turn: two query tiles of 128 rows
 // against a range of 128-key tiles, S = Q K^T and O += P V on the tensor
-// cores with accumulators in tensor memory.  Warps by role: four for each
-// query tile (a thread has a row: running maximum and sum of the softmax
-// with no exchange between lanes), one loads tiles, one issues products.
-// The two query tiles take turns on the tensor cores: while one's softmax
-// runs, the other's products do.  P replaces S in tensor memory as the first
-// operand of the second product and never passes through shared memory.
+// cores with accumulators in tensor memory.  Warps by role: eight for the
+// softmax of each query tile, one that loads keys and values, one that loads
+// queries, and one that issues the products of each query tile.  The two
+// query tiles share the loads and go at their own pace: while one's softmax
+// runs, the other's products do, also from one item to the next.  P replaces
+// S in tensor memory as the first operand of the second product and never
+// passes through shared memory.
+//
+// A softmax thread has half a row, 64 scores in registers; the two threads of
+// a row exchange their maximum through shared memory once per tile.  With
+// whole rows (one group of four warps per query tile) a tile's softmax took
+// 2100 cycles, its 128 dependent steps bound by latency, and 128-row tiles of
+// one item took turns in 3230 cycles where their products take 2048.
 //
 // Rows of a tile are consecutive queries of one head, or, where a sequence
 // has few queries, the queries of all heads of a group (row = query * group +
@@ -24,10 +31,10 @@ namespace {
 
 using namespace umma;
 
-constexpr int kThreads = 384;          // two softmax groups of 4 warps; one warp loads, one multiplies, two are idle
+constexpr int kThreads = 384;          // two softmax groups of 4 warps, and 4 warps with a role each
 // Registers per thread: 168 at launch (3 warpgroups of 168 = 504), of which
 // the softmax groups take most, so that a row of scores stays in registers.
-constexpr int kRegsMany = 224, kRegsFew = 56;
+constexpr int kRegsMany = 216, kRegsFew = 72;
 static_assert(2 * kRegsMany + kRegsFew <= 3 * 168, "register split");
 constexpr int kCols = 512;
 // columns of query tile t's scores and outputs
@@ -40,8 +47,8 @@ struct Layout {
   static constexpr int kStages = DP == 128 ? 5 : 10;        // key and value tiles in flight
   static constexpr int kRing = 2 * kTileBytes;              // after the two query tiles
   static constexpr int kBars = kRing + kStages * kTileBytes;
-  static constexpr int kInts = kBars + 88 + 16 * kStages;   // after the barriers: dead, tensor memory
-  static constexpr int kBytes = kInts + 8 + 1024;           // alignment
+  static constexpr int kInts = kBars + 104 + 16 * kStages;  // after the barriers: dead, tensor memory
+  static constexpr int kBytes = kInts + 8;
 };
 
 template <bool BF16>
@@ -61,32 +68,32 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_fwd(const __grid_constant_
                                                           const __grid_constant__ CUtensorMap k_map,
                                                           const __grid_constant__ CUtensorMap v_map) {
   using L = Layout<DP>;
-  extern __shared__ uint8_t raw[];
-  uint8_t* sm = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~(uintptr_t)1023);
+  extern __shared__ __align__(1024) uint8_t sm[];
   const uint32_t base = smem_addr(sm), bars = base + L::kBars;
   const uint32_t q_full = bars, q_free = bars + 16, s_full = bars + 32, p_full = bars + 48, o_full = bars + 64,
-                 done = bars + 80, full = bars + 88, free_ = full + 8 * L::kStages;
+                 p_half = bars + 80, done = bars + 96, full = bars + 104, free_ = full + 8 * L::kStages;
   int* const shared_int = reinterpret_cast<int*>(sm + L::kInts);
   const Waits w{shared_int, a.error};
-  const int warp = threadIdx.x / 32;
-
+  const int warp = uniform(threadIdx.x / 32);
+  if (!swizzle_aligned(base, w)) return;
   if (threadIdx.x == 0) {
     for (int t = 0; t < 2; ++t) {
       bar_init(q_full + 8 * t, 1);
       bar_init(q_free + 8 * t, 1);
       bar_init(s_full + 8 * t, 1);
+      bar_init(p_half + 8 * t, 4);
       bar_init(p_full + 8 * t, 4);
       bar_init(o_full + 8 * t, 1);
     }
-    bar_init(done, 1);
+    bar_init(done, 2);
     for (int i = 0; i < L::kStages; ++i) {
       bar_init(full + 8 * i, 1);
-      bar_init(free_ + 8 * i, 1);
+      bar_init(free_ + 8 * i, 2);
     }
     bar_init_visible();
     shared_int[0] = 0;
   }
-  if (warp == 9) tmem_alloc<kCols>(smem_addr(shared_int + 1));
+  if (warp == 8) tmem_alloc<kCols>(smem_addr(shared_int + 1));
   fence_before();
   __syncthreads();
   fence_after();
@@ -94,120 +101,149 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_fwd(const __grid_constant_
 
   const int group = a.heads / a.kv_heads, packed_rows = kTile / group;
   if (threadIdx.x == 0) let_next_start();
-  const int i0 = a.block_first[blockIdx.x], i1 = a.block_first[blockIdx.x + 1];
+  const int i0 = uniform(a.block_first[blockIdx.x]), i1 = uniform(a.block_first[blockIdx.x + 1]);
 
   if (warp >= 8) {
     regs_down<kRegsFew>();
-    if (warp == 8 && elect_one()) {                         // ---- loads
-      uint32_t pos = 0, qn[2] = {0, 0};
+    const bool leader = elect_one();
+    if (warp == 8) {                                        // ---- loads of key and value tiles
+      uint32_t pos = 0;
       bool ok = true;
       auto load = [&](const CUtensorMap* map, int head, int row) {
         const uint32_t st = pos % L::kStages, bar = full + 8 * st;
         if (pos >= L::kStages && !bar_wait(free_ + 8 * st, (pos / L::kStages - 1) & 1, w)) return false;
-        bar_expect(bar, L::kTileBytes);
+        if (leader) {
+          bar_expect(bar, L::kTileBytes);
 #pragma unroll
-        for (int c = 0; c < DP / 64; ++c)
-          tma_load(base + L::kRing + st * L::kTileBytes + c * kBlockBytes, map, bar, 64 * c, head, row);
+          for (int c = 0; c < DP / 64; ++c)
+            tma_load(base + L::kRing + st * L::kTileBytes + c * kBlockBytes, map, bar, 64 * c, head, row);
+        }
         ++pos;
         return true;
       };
       for (int i = i0; ok && i < i1; ++i) {
         const AttnItem it = a.item[i];
-        const int per = it.packed ? packed_rows : kTile, kh = it.head / group, n = max(it.n[0], it.n[1]);
-        for (int t = 0; ok && t < 2; ++t) {
-          if (!it.n[t]) continue;
-          if (qn[t] && !bar_wait(q_free + 8 * t, (qn[t] - 1) & 1, w)) { ok = false; break; }
-          bar_expect(q_full + 8 * t, DP / 64 * (it.packed ? packed_rows * group : kTile) * 128);
-#pragma unroll
-          for (int c = 0; c < DP / 64; ++c)
-            tma_load(base + t * L::kTileBytes + c * kBlockBytes, it.packed ? &qg_map : &q_map, q_full + 8 * t, 64 * c,
-                     it.head, (int)it.q_row + t * per);
-          ++qn[t];
-        }
-        for (int j = 0; ok && j < n; ++j) {
-          const int row = (int)it.k_row + j * kTile;
-          ok = load(&k_map, kh, row) && load(&v_map, kh, row);
-        }
+        const int n = uniform(max(it.n[0], it.n[1])), row = (int)it.k_row, head = it.head / group;
+        for (int j = 0; ok && j < n; ++j) ok = load(&k_map, head, row + j * kTile) && load(&v_map, head, row + j * kTile);
       }
       // nothing is in flight when the block ends
       for (uint32_t i = pos > L::kStages ? pos - L::kStages : 0; i < pos; ++i)
         bar_wait(full + 8 * (i % L::kStages), i / L::kStages & 1, w);
-      for (int t = 0; t < 2; ++t)
-        if (qn[t]) bar_wait(q_full + 8 * t, (qn[t] - 1) & 1, w);
-    } else if (warp == 9 && elect_one()) {                  // ---- products
-      const int ksteps = (a.dim + 15) / 16, n_out = ksteps * 16;
-      const uint32_t i_s = instr(BF16, kTile, false), i_o = instr(BF16, n_out, true);
-      uint32_t pos = 0, qn[2] = {0, 0}, pn[2] = {0, 0};
-      auto tile = [&](uint32_t at) { return tile_desc(base + L::kRing + at % L::kStages * L::kTileBytes); };
-      auto arrived = [&](uint32_t at) { return bar_wait(full + 8 * (at % L::kStages), at / L::kStages & 1, w); };
-      auto scores = [&](int t, uint32_t at) {
-        const uint64_t q = tile_desc(base + t * L::kTileBytes), k = tile(at);
-        for (int e = 0; e < ksteps; ++e) mma(tmem + s_col(t), q + step_along(e), k + step_along(e), i_s, e > 0);
-        commit(s_full + 8 * t);
-      };
-      auto run = [&](const int* tiles) {
-        const int n = max(tiles[0], tiles[1]);
-        if (!n) return true;
-        if (!arrived(pos)) return false;
-        for (int t = 0; t < 2; ++t) {
-          if (!tiles[t]) continue;
-          if (!bar_wait(q_full + 8 * t, qn[t]++ & 1, w)) return false;
-          fence_after();
-          scores(t, pos);
-          if (tiles[t] == 1) commit(q_free + 8 * t);
-        }
-        commit(free_ + 8 * (pos % L::kStages));
-        for (int j = 0; j < n; ++j, pos += 2) {
-          if (!arrived(pos + 1) || (j + 1 < n && !arrived(pos + 2))) return false;
-          for (int t = 0; t < 2; ++t) {
-            if (j < tiles[t]) {
-              if (!bar_wait(p_full + 8 * t, pn[t]++ & 1, w)) return false;
-              fence_after();
-              const uint64_t v = tile(pos + 1);
+    } else if (warp == 9) {                                 // ---- loads of query tiles
+      uint32_t n[2] = {0, 0};
+      bool ok = true;
+      for (int i = i0; ok && i < i1; ++i) {
+        const AttnItem it = a.item[i];
+        const int packed = uniform(it.packed), row = (int)it.q_row;
 #pragma unroll
-              for (int e = 0; e < kTile / 16; ++e)
-                mma_tmem(tmem + o_col(t), tmem + s_col(t) + 8 * e, v + step_rows(e), i_o, j > 0 || e > 0);
-              if (j + 1 == tiles[t]) commit(o_full + 8 * t);
-            }
-            if (j + 1 < tiles[t]) {
-              scores(t, pos + 2);
-              if (j + 2 == tiles[t]) commit(q_free + 8 * t);
-            }
+        for (int t = 0; t < 2; ++t) {
+          if (!ok || !uniform(it.n[t])) continue;
+          if (n[t] && !(ok = bar_wait(q_free + 8 * t, (n[t] - 1) & 1, w))) continue;
+          if (leader) {
+            bar_expect(q_full + 8 * t, DP / 64 * (packed ? packed_rows * group : kTile) * 128);
+#pragma unroll
+            for (int c = 0; c < DP / 64; ++c)
+              tma_load(base + t * L::kTileBytes + c * kBlockBytes, packed ? &qg_map : &q_map, q_full + 8 * t, 64 * c,
+                       it.head, row + t * (packed ? packed_rows : kTile));
           }
-          commit(free_ + 8 * ((pos + 1) % L::kStages));
-          if (j + 1 < n) commit(free_ + 8 * ((pos + 2) % L::kStages));
+          ++n[t];
+        }
+      }
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+        if (n[t]) bar_wait(q_full + 8 * t, (n[t] - 1) & 1, w);
+    } else {                                                // ---- products of query tile t
+      const int t = warp - 10, ksteps = (a.dim + 15) / 16;
+      const uint32_t i_s = instr(BF16, kTile, false), i_o = instr(BF16, ksteps * 16, true);
+      const uint32_t S = tmem + s_col(t), O = tmem + o_col(t);
+      const uint32_t Q = tile_desc(base + t * L::kTileBytes), ring = tile_desc(base + L::kRing);
+      uint32_t pos = 0, items = 0, steps = 0;
+      auto tile = [&](uint32_t at) { return ring + at % L::kStages * (L::kTileBytes >> 4); };
+      auto arrived = [&](uint32_t at) { return bar_wait(full + 8 * (at % L::kStages), at / L::kStages & 1, w); };
+      auto scores = [&](uint32_t at, bool last) {
+        const uint32_t k = tile(at);
+        if (leader) {
+#pragma unroll
+          for (int e = 0; e < DP / 16; ++e)
+            if (e < ksteps) mma(S, Q + step_along(e), k + step_along(e), i_s, e > 0);
+          commit(s_full + 8 * t);
+          commit(free_ + 8 * (at % L::kStages));
+          if (last) commit(q_free + 8 * t);
+        }
+      };
+      auto run = [&](int n, int all) {                      // n of the item's key tiles are this query tile's
+        if (n) {
+          if (!arrived(pos) || !bar_wait(q_full + 8 * t, items++ & 1, w)) return false;
+          fence_after();
+          scores(pos, n == 1);
+          for (int j = 0; j < n; ++j, pos += 2) {
+            const uint32_t v = tile(pos + 1);
+            if (!arrived(pos + 1) || !bar_wait(p_half + 8 * t, steps & 1, w)) return false;
+            fence_after();
+            if (leader)
+#pragma unroll
+              for (int e = 0; e < kTile / 32; ++e) mma_tmem(O, S + 8 * e, v + step_rows(e), i_o, j > 0 || e > 0);
+            if (j + 1 < n && !arrived(pos + 2)) return false;
+            if (!bar_wait(p_full + 8 * t, steps++ & 1, w)) return false;
+            fence_after();
+            if (leader) {
+#pragma unroll
+              for (int e = kTile / 32; e < kTile / 16; ++e) mma_tmem(O, S + 8 * e, v + step_rows(e), i_o, true);
+              commit(free_ + 8 * ((pos + 1) % L::kStages));
+              if (j + 1 == n) commit(o_full + 8 * t);
+            }
+            if (j + 1 < n) scores(pos + 2, j + 2 == n);
+          }
+        }
+        for (int j = 2 * n; j < 2 * all; ++j, ++pos) {       // the other's: let go as they come
+          if (!arrived(pos)) return false;
+          bar_arrive_warp(free_ + 8 * (pos % L::kStages), leader);
         }
         return true;
       };
-      for (int i = i0; i < i1; ++i) {
-        const int tiles[2] = {a.item[i].n[0], a.item[i].n[1]};
-        if (!run(tiles)) break;
-      }
-      commit(done);
+      for (int i = i0; i < i1; ++i)
+        if (!run(uniform(a.item[i].n[t]), uniform(max(a.item[i].n[0], a.item[i].n[1])))) break;
+      if (leader) commit(done);
       bar_wait(done, 0, w);
     }
-  } else {                                                  // ---- softmax of query tile t
+  } else {                                                  // ---- softmax: a row of query tile t per thread
     regs_up<kRegsMany>();
     const int t = warp / 4, r = threadIdx.x % 128;
+    const bool leader = elect_one();
     const uint32_t lanes = (uint32_t)(warp % 4 * 32) << 16, S = tmem + s_col(t) + lanes, O = tmem + o_col(t) + lanes;
     const float c2 = a.scale * 1.4426950408889634f;          // weights are powers of two
     const float slack = 8.f / c2;                            // see below
     uint32_t pos = 0, sn = 0, on = 0;
     for (int i = i0; i < i1; ++i) {
-      const AttnItem it = a.item[i];
-      if (i + 1 < i1) asm volatile("prefetch.global.L1 [%0];" ::"l"(a.item + i + 1));
-      const int per = it.packed ? packed_rows : kTile;
-      const int n = it.n[t], rows = it.rows[t], rq = it.packed ? r / group : r;
-      const int head = it.packed ? it.head + r % group : it.head;
-      const int64_t query = it.q_row + t * per + rq;
-      const bool valid = rq < rows;
-      const int least = it.seen + t * per;                   // keys that the tile's first query sees
-      const int seen_all = min(least + rq, it.keys);         // and this row
+      const AttnItem* const at_item = a.item + i;
+      if (i + 1 < i1) asm volatile("prefetch.global.L1 [%0];" ::"l"(at_item + 1));
+      const int packed = uniform(at_item->packed), n = uniform(at_item->n[t]), keys = uniform(at_item->keys);
+      const int per = packed ? packed_rows : kTile, rq = packed ? r / group : r;
+      const int least = uniform(at_item->seen) + t * per;    // keys that the tile's first query sees
+      const int seen_all = min(least + rq, keys);            // and this row
+      const bool valid = rq < at_item->rows[t], busy = __any_sync(~0u, valid);
       float m = -INFINITY, l = 0.f;
       bool ok = true;
       for (int j = 0; j < n; ++j) {
         const int k0 = j * kTile;
-        if (!(ok = bar_wait_warp(s_full + 8 * t, sn++ & 1, w))) break;
+        if (!(ok = bar_wait(s_full + 8 * t, sn++ & 1, w))) break;
+        if (k0 + kTile > keys) {
+          // Values past the sequence's end belong to other sequences and may
+          // be anything; a zero weight does not hide a NaN, so they are
+          // cleared (both query tiles write the same zeros).
+          const uint32_t at = pos + 2 * j + 1, st = at % L::kStages;
+          if (!(ok = bar_wait(full + 8 * st, at / L::kStages & 1, w))) break;
+          uint8_t* v = sm + L::kRing + st * L::kTileBytes;
+          for (int b = (keys - k0) * 8 + r; b < kTile * 8; b += 128)
+#pragma unroll
+            for (int c = 0; c < DP / 64; ++c) *reinterpret_cast<uint4*>(v + c * kBlockBytes + b * 16) = make_uint4(0, 0, 0, 0);
+          fence_async();
+        }
+        if (!busy) {                                         // rows that nobody asked for
+          bar_arrive_warp(p_half + 8 * t, leader);
+          bar_arrive_warp(p_full + 8 * t, leader);
+          continue;
+        }
         fence_after();
         float x[kTile];
 #pragma unroll
@@ -247,89 +283,88 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_fwd(const __grid_constant_
           }
         }
         const float shift = m == -INFINITY ? 0.f : m * c2;
-        float l4[4] = {0.f, 0.f, 0.f, 0.f};
+        const uint64_t c22 = pair_bits(c2, c2), shift2 = pair_bits(-shift, -shift);
+        uint64_t l2[2] = {0, 0};
 #pragma unroll
         for (int c = 0; c < kTile; c += 32) {
           uint32_t y[16];
 #pragma unroll
           for (int e = 0; e < 32; e += 2) {
-            const float u = exp2_fast(fmaf(x[c + e], c2, -shift)), v = exp2_fast(fmaf(x[c + e + 1], c2, -shift));
-            l4[e / 2 % 2] += u;
-            l4[2 + e / 2 % 2] += v;
+            float u, v;
+            pair_split(fma2(pair_bits(x[c + e], x[c + e + 1]), c22, shift2), u, v);
+            u = exp2_fast(u);
+            v = exp2_fast(v);
+            l2[e / 2 % 2] = add2(l2[e / 2 % 2], pair_bits(u, v));
             y[e / 2] = pack2<BF16>(u, v);
           }
           tmem_st16(S + c / 2, y);
-        }
-        l += (l4[0] + l4[1]) + (l4[2] + l4[3]);
-        if (k0 + kTile > it.keys) {
-          // The tile ends past the sequence: its values there belong to others
-          // and may be anything, so they are cleared (both groups write the
-          // same zeros).
-          const uint32_t at = pos + 2 * j + 1, st = at % L::kStages;
-          if (!(ok = bar_wait_warp(full + 8 * st, at / L::kStages & 1, w))) break;
-          uint8_t* v = sm + L::kRing + st * L::kTileBytes;
-          for (int b = (it.keys - k0) * 8 + r; b < kTile * 8; b += 128)
-#pragma unroll
-            for (int c = 0; c < DP / 64; ++c) *reinterpret_cast<uint4*>(v + c * kBlockBytes + b * 16) = make_uint4(0, 0, 0, 0);
-          fence_async();
+          if (c == 32) {                                      // the first half may be multiplied
+            wait_st();
+            fence_before();
+            bar_arrive_warp(p_half + 8 * t, leader);
+          }
         }
         wait_st();
         fence_before();
-        __syncwarp();
-        if (threadIdx.x % 32 == 0) bar_arrive(p_full + 8 * t);
+        bar_arrive_warp(p_full + 8 * t, leader);
+        float l4[4];
+        pair_split(l2[0], l4[0], l4[1]);
+        pair_split(l2[1], l4[2], l4[3]);
+        l += (l4[0] + l4[1]) + (l4[2] + l4[3]);
       }
-      pos += 2 * max(it.n[0], it.n[1]);
       if (!ok) break;
+      pos += 2 * uniform(max(at_item->n[0], at_item->n[1]));
       if (n) {
-        if (!bar_wait_warp(o_full + 8 * t, on++ & 1, w)) break;
+        if (!bar_wait(o_full + 8 * t, on++ & 1, w)) break;
         fence_after();
       }
-      const float by = l == 0.f ? 0.f : 1.f / l;
-      const float lse2 = l == 0.f ? -INFINITY : fmaf(m, c2, log2f(l));
-      if (it.slot < 0) {
-        uint8_t* out = static_cast<uint8_t*>(a.o.data) + 2 * (query * a.o.row + head * a.o.head);
-#pragma unroll 1
-        for (int c = 0; c < DP; c += 32) {
-          float o[32];
-          if (n) {
-            tmem_ld32(O + c, o);
-            wait_ld();
-          }
-#pragma unroll
-          for (int e = 0; e < 32; ++e) o[e] = n && l != 0.f ? o[e] * by : 0.f;
-          if (valid)
-#pragma unroll
-            for (int e = 0; e < 32; e += 8)
-              if (c + e < a.dim) store8<BF16>(out + 2 * (c + e), o + e);
-        }
-        if (valid && a.lse) a.lse[head * a.q.rows + query] = lse2 * 0.6931471805599453f;
-        continue;
+      if (!busy) continue;
+      const bool some = n && l != 0.f;
+      const float by = some ? 1.f / l : 0.f;
+      const int slot = uniform(at_item->slot);
+      const int head = at_item->head + (packed ? r % group : 0);
+      const int64_t query = at_item->q_row + t * per + rq;
+      const int64_t place = ((int64_t)slot * 2 + t) * kTile + r;
+      if (valid) {
+        const float lse2 = l == 0.f ? -INFINITY : fmaf(m, c2, log2f(l));
+        if (slot >= 0)
+          a.part_lse[place] = lse2;
+        else if (a.lse)
+          a.lse[head * a.q.rows + query] = lse2 * 0.6931471805599453f;
       }
-      // A piece of a split key range leaves its rows, scaled by its own sum,
-      // and their logarithms.
-      float* part = a.part_o + ((int64_t)it.slot * 2 + t) * kTile * DP;
+      // A piece of a split key range leaves its rows in 32 bits, scaled by its
+      // own sum; whole ranges are done.
+      uint8_t* out = slot >= 0 ? reinterpret_cast<uint8_t*>(a.part_o + place * DP)
+                               : static_cast<uint8_t*>(a.o.data) + 2 * (query * a.o.row + head * a.o.head);
 #pragma unroll 1
       for (int c = 0; c < DP; c += 32) {
         float o[32];
+        __syncwarp();
         if (n) {
           tmem_ld32(O + c, o);
           wait_ld();
         }
-        if (valid)
 #pragma unroll
-          for (int e = 0; e < 32; e += 4) {
-            float4 f = make_float4(o[e] * by, o[e + 1] * by, o[e + 2] * by, o[e + 3] * by);
-            if (!n || l == 0.f) f = make_float4(0.f, 0.f, 0.f, 0.f);
-            *reinterpret_cast<float4*>(part + r * DP + c + e) = f;
-          }
+        for (int e = 0; e < 32; ++e) o[e] = some ? o[e] * by : 0.f;
+        if (slot >= 0) {
+          if (valid)
+#pragma unroll
+            for (int e = 0; e < 32; e += 4) *reinterpret_cast<float4*>(out + 4 * e) = make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
+          out += 128;
+        } else {
+          if (valid)
+#pragma unroll
+            for (int e = 0; e < 32; e += 8)
+              if (c + e < a.dim) store8<BF16>(out + 2 * e, o + e);
+          out += 64;
+        }
       }
-      if (valid) a.part_lse[((int64_t)it.slot * 2 + t) * kTile + r] = lse2;
     }
   }
   __syncwarp();
   fence_before();
   __syncthreads();
-  if (warp == 9) tmem_free<kCols>(tmem);
+  if (warp == 8) tmem_free<kCols>(tmem);
 }
 
 // Rows of split key ranges from their pieces, in the order of the pieces: a

@@ -89,12 +89,29 @@ __device__ __forceinline__ bool bar_wait_slow(uint32_t bar, uint32_t parity, Wai
     }
   }
 }
+// By a whole warp, with one answer for all lanes.  (What a warp decides, it
+// decides by votes and by values of its first lane, which the compiler knows
+// to be the same for all lanes: a branch that may diverge costs the kernels
+// here some 50 cycles, ten times a tile.)
 __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, Waits w) {
-  return bar_try(bar, parity) || bar_wait_slow(bar, parity, w);
+  if (__all_sync(~0u, bar_try(bar, parity))) return true;
+  return __all_sync(~0u, bar_wait_slow(bar, parity, w));
 }
-// The same for a whole warp, with one answer for all lanes.
-__device__ __forceinline__ bool bar_wait_warp(uint32_t bar, uint32_t parity, Waits w) {
-  return __all_sync(~0u, bar_wait(bar, parity, w));
+__device__ __forceinline__ int uniform(int x) { return __shfl_sync(~0u, x, 0); }
+// One lane of the warp arrives, for all.
+__device__ __forceinline__ void bar_arrive_warp(uint32_t bar, bool leader) {
+  __syncwarp();
+  asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %1, 0;\n@p mbarrier.arrive.shared::cta.b64 _, [%0];\n}" ::"r"(bar),
+               "r"((uint32_t)leader)
+               : "memory");
+}
+
+// The swizzle goes by address bits: tiles start at multiples of 1024 bytes, as
+// the start of a block's shared memory does.
+__device__ __forceinline__ bool swizzle_aligned(uint32_t base, Waits w) {
+  if (base % 1024 == 0) return true;
+  if (threadIdx.x == 0) *reinterpret_cast<volatile int*>(w.error) = 1;
+  return false;
 }
 
 // ---- TMA ----
@@ -138,26 +155,31 @@ __host__ __device__ __forceinline__ uint32_t instr(bool bf16, int n, bool b_rows
 // Shared memory descriptor of a swizzled tile.  Contracted dimension
 // contiguous: 8-row groups are 1024 bytes apart.  Otherwise (b_rows) the same
 // 1024 bytes separate groups of 8 contracted rows, and blocks of 64 columns
-// are kBlockBytes apart.
-__device__ __forceinline__ uint64_t tile_desc(uint32_t addr) {
-  return (uint64_t)(addr >> 4 & 0x3fff) | (uint64_t)(kBlockBytes >> 4) << 16 | (uint64_t)(1024 >> 4) << 32 | 1ull << 46 |
-         2ull << 61;
+// are kBlockBytes apart.  The address is in the low word; the high one is the
+// same for every tile.
+constexpr uint32_t kDescHigh = 1024 >> 4 | 1u << 14 | 2u << 29;
+__device__ __forceinline__ uint32_t tile_desc(uint32_t addr) {
+  return (addr >> 4 & 0x3fff) | (uint32_t)(kBlockBytes >> 4) << 16;
 }
 // The contracted dimension moves by 16 entries: 32 bytes within a row and a
 // block further every 64 entries, or 16 rows.
-__device__ __forceinline__ uint64_t step_along(int k) { return (uint64_t)((k / 4 * kBlockBytes + k % 4 * 32) >> 4); }
-__device__ __forceinline__ uint64_t step_rows(int k) { return (uint64_t)(k * 16 * 128 >> 4); }
+__device__ __forceinline__ constexpr uint32_t step_along(int k) { return (k / 4 * kBlockBytes + k % 4 * 32) >> 4; }
+__device__ __forceinline__ constexpr uint32_t step_rows(int k) { return k * 16 * 128 >> 4; }
 
-__device__ __forceinline__ void mma(uint32_t d, uint64_t a, uint64_t b, uint32_t i, bool add) {
-  asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\ntcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}" ::"r"(d),
-               "l"(a), "l"(b), "r"(i), "r"((uint32_t)add)
-               : "memory");
+__device__ __forceinline__ void mma(uint32_t d, uint32_t a, uint32_t b, uint32_t i, bool add) {
+  asm volatile(
+      "{\n.reg .pred p;\n.reg .b64 x, y;\nsetp.ne.b32 p, %4, 0;\nmov.b64 x, {%1, %5};\nmov.b64 y, {%2, %5};\n"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], x, y, %3, p;\n}" ::"r"(d),
+      "r"(a), "r"(b), "r"(i), "r"((uint32_t)add), "r"(kDescHigh)
+      : "memory");
 }
 // A from tensor memory: 16-bit pairs, 8 columns per 16 contracted entries.
-__device__ __forceinline__ void mma_tmem(uint32_t d, uint32_t a, uint64_t b, uint32_t i, bool add) {
-  asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\ntcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}" ::"r"(d),
-               "r"(a), "l"(b), "r"(i), "r"((uint32_t)add)
-               : "memory");
+__device__ __forceinline__ void mma_tmem(uint32_t d, uint32_t a, uint32_t b, uint32_t i, bool add) {
+  asm volatile(
+      "{\n.reg .pred p;\n.reg .b64 y;\nsetp.ne.b32 p, %4, 0;\nmov.b64 y, {%2, %5};\n"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], y, %3, p;\n}" ::"r"(d),
+      "r"(a), "r"(b), "r"(i), "r"((uint32_t)add), "r"(kDescHigh)
+      : "memory");
 }
 
 // Columns of this warp's 32 lanes, one lane per thread.
@@ -194,6 +216,30 @@ __device__ __forceinline__ float exp2_fast(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
+}
+// Two 32-bit operations in one instruction.
+__device__ __forceinline__ uint64_t pair_bits(float lo, float hi) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+  return r;
+}
+__device__ __forceinline__ void pair_split(uint64_t r, float& lo, float& hi) {
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(r));
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
 }
 // Two values rounded to 16 bits, the first in the low half.
 template <bool BF16>
