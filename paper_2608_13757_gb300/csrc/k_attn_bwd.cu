@@ -77,20 +77,11 @@ struct Bars {
   }
 };
 
-template <bool BF16>
-__device__ __forceinline__ void store8(void* p, const float* x, float by) {
-  uint4 v;
-  v.x = pack2<BF16>(x[0] * by, x[1] * by);
-  v.y = pack2<BF16>(x[2] * by, x[3] * by);
-  v.z = pack2<BF16>(x[4] * by, x[5] * by);
-  v.w = pack2<BF16>(x[6] * by, x[7] * by);
-  *static_cast<uint4*>(p) = v;
-}
-
 // Columns [c0, c1) of this thread's lane of an accumulator, to a row of an
 // output; zeros where nothing was accumulated.
 template <bool BF16>
 __device__ __forceinline__ void write_row(uint32_t acc, void* row, int c0, int c1, int dim, float by, bool any, bool valid) {
+  const RowWriter out(row, valid);
 #pragma unroll 1
   for (int c = c0; c < c1; c += 32) {
     float x[32];
@@ -98,14 +89,10 @@ __device__ __forceinline__ void write_row(uint32_t acc, void* row, int c0, int c
     if (any) {
       tmem_ld32(acc + c, x);
       wait_ld();
-    } else {
-#pragma unroll
-      for (int e = 0; e < 32; ++e) x[e] = 0.f;
     }
-    if (valid)
 #pragma unroll
-      for (int e = 0; e < 32; e += 8)
-        if (c + e < dim) store8<BF16>(static_cast<uint8_t*>(row) + 2 * (c + e), x + e, by);
+    for (int e = 0; e < 32; ++e) x[e] = any ? x[e] * by : 0.f;
+    out.write<BF16>(x, c, dim);
   }
 }
 
@@ -126,7 +113,7 @@ struct Loader {
   using L = Layout<DP>;
   uint32_t base;
   const Bars<DP>& b;
-  Waits w;
+  int* error;
   bool leader;
   uint32_t pos = 0, fixed = 0;
   __device__ __forceinline__ void tile(uint32_t dst, const CUtensorMap* map, uint32_t bar, int head, int row) {
@@ -134,7 +121,7 @@ struct Loader {
     for (int c = 0; c < DP / 64; ++c) tma_load(dst + c * kBlockBytes, map, bar, 64 * c, head, row);
   }
   __device__ __forceinline__ bool stay(const CUtensorMap* m0, const CUtensorMap* m1, int head, int row) {
-    if (fixed && !bar_wait(b.fixed_free, (fixed - 1) & 1, w)) return false;
+    if (fixed && !bar_wait(b.fixed_free, (fixed - 1) & 1, error)) return false;
     if (leader) {
       bar_expect(b.fixed_full, 2 * L::kTileBytes);
       tile(base, m0, b.fixed_full, head, row);
@@ -145,7 +132,7 @@ struct Loader {
   }
   __device__ __forceinline__ bool next(const CUtensorMap* map, int head, int row) {
     const uint32_t st = pos % L::kStages;
-    if (pos >= L::kStages && !bar_wait(b.free_ + 8 * st, (pos / L::kStages - 1) & 1, w)) return false;
+    if (pos >= L::kStages && !bar_wait(b.free_ + 8 * st, (pos / L::kStages - 1) & 1, error)) return false;
     if (leader) {
       bar_expect(b.full + 8 * st, L::kTileBytes);
       tile(base + L::kRing + st * L::kTileBytes, map, b.full + 8 * st, head, row);
@@ -154,9 +141,10 @@ struct Loader {
     return true;
   }
   __device__ __forceinline__ void finish() {                // nothing is in flight when the block ends
+#pragma unroll 1
     for (uint32_t i = pos > L::kStages ? pos - L::kStages : 0; i < pos; ++i)
-      bar_wait(b.full + 8 * (i % L::kStages), i / L::kStages & 1, w);
-    if (fixed) bar_wait(b.fixed_full, (fixed - 1) & 1, w);
+      bar_wait(b.full + 8 * (i % L::kStages), i / L::kStages & 1, error);
+    if (fixed) bar_wait(b.fixed_full, (fixed - 1) & 1, error);
   }
 };
 
@@ -172,18 +160,16 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dkv(const __grid_constant_
   const uint32_t base = smem_addr(sm);
   const Bars<DP> b(base + L::kBars);
   int* const shared_int = reinterpret_cast<int*>(sm + L::kInts);
-  const Waits w{shared_int, a.error};
   const int warp = uniform(threadIdx.x / 32);
-  if (!swizzle_aligned(base, w)) return;
+  if (!swizzle_aligned(base, a.error)) return;
   if (threadIdx.x == 0) {
     b.init();
-    shared_int[0] = 0;
   }
-  if (warp == 9) tmem_alloc<512>(smem_addr(shared_int + 1));
+  if (warp == 9) tmem_alloc<512>(smem_addr(shared_int));
   fence_before();
   __syncthreads();
   fence_after();
-  const uint32_t tmem = (uint32_t)shared_int[1];
+  const uint32_t tmem = (uint32_t)shared_int[0];
   const int group = a.heads / a.kv_heads;
   const int i0 = uniform(a.k_first[blockIdx.x]), i1 = uniform(a.k_first[blockIdx.x + 1]);
 
@@ -191,14 +177,17 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dkv(const __grid_constant_
     regs_down<kRegsFew>();
     const bool leader = elect_one();
     if (warp == 8) {                                        // ---- loads
-      Loader<DP> load{base, b, w, leader};
+      Loader<DP> load{base, b, a.error, leader};
       bool ok = true;
+#pragma unroll 1
       for (int i = i0; ok && i < i1; ++i) {
         const AttnTile it = a.k_tile[i];
         const int n = uniform(it.n), head = uniform(it.head);
         if (!n) continue;
         ok = load.stay(&k_map, &v_map, head, (int)it.k_row);
+#pragma unroll 1
         for (int h = head * group; ok && h < (head + 1) * group; ++h)
+#pragma unroll 1
           for (int t = 0; ok && t < n; ++t)
             ok = load.next(&q_map, h, (int)it.q_row + t * kTile) && load.next(&do_map, h, (int)it.q_row + t * kTile);
       }
@@ -208,27 +197,25 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dkv(const __grid_constant_
       const uint32_t i_s = instr(BF16, kTile, false), i_o = instr(BF16, ksteps * 16, true);
       uint32_t pos = 0, fixed = 0, n = 0;                    // n: steps so far
       auto tile = [&](uint32_t at) { return tile_desc(base + L::kRing + at % L::kStages * L::kTileBytes); };
-      auto arrived = [&](uint32_t at) { return bar_wait(b.full + 8 * (at % L::kStages), at / L::kStages & 1, w); };
+      auto arrived = [&](uint32_t at) { return bar_wait(b.full + 8 * (at % L::kStages), at / L::kStages & 1, a.error); };
       auto done_with = [&](uint32_t bar) {
         if (leader) commit(bar);
       };
       auto release = [&](uint32_t at) { done_with(b.free_ + 8 * (at % L::kStages)); };
       auto across = [&](uint32_t d, uint32_t x, uint32_t at) {       // keys by queries
         const uint32_t y = tile(at);
-        if (leader)
-#pragma unroll
-          for (int e = 0; e < DP / 16; ++e)
-            if (e < ksteps) mma(tmem + d, x + step_along(e), y + step_along(e), i_s, e > 0);
+        if (leader) mma_along(tmem + d, x, y, i_s, ksteps);
       };
       auto gradient = [&](uint32_t d, uint32_t x, uint32_t at, bool add) {
         const uint32_t y = tile(at);
-        if (leader)
-#pragma unroll
-          for (int e = 0; e < kTile / 16; ++e) mma_tmem(tmem + d, tmem + x + e / 4 * 64 + e % 4 * 8, y + step_rows(e), i_o, add || e > 0);
+        if (leader) {
+          mma_rows(tmem + d, tmem + x, y, i_o, add);
+          mma_rows(tmem + d, tmem + x + 64, y + step_rows(4), i_o, true);
+        }
       };
       const uint32_t K = tile_desc(base), V = tile_desc(base + L::kTileBytes);
       auto run = [&](int steps) {
-        if (!bar_wait(b.fixed_full, fixed++ & 1, w) || !arrived(pos)) return false;
+        if (!bar_wait(b.fixed_full, fixed++ & 1, a.error) || !arrived(pos)) return false;
         fence_after();
         across(kS, K, pos);
         done_with(b.s_full);
@@ -236,8 +223,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dkv(const __grid_constant_
         across(kDp, V, pos + 1);
         done_with(b.dp_full);
         if (steps == 1) done_with(b.fixed_free);
+#pragma unroll 1
         for (int j = 0; j < steps; ++j, pos += 2, ++n) {
-          if (!bar_wait(b.p_ready, n & 1, w)) return false;
+          if (!bar_wait(b.p_ready, n & 1, a.error)) return false;
           fence_after();
           gradient(kDv, kS, pos + 1, j > 0);
           release(pos + 1);
@@ -246,7 +234,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dkv(const __grid_constant_
             across(kS, K, pos + 2);
             done_with(b.s_full);
           }
-          if (!bar_wait(b.ds_ready, n & 1, w)) return false;
+          if (!bar_wait(b.ds_ready, n & 1, a.error)) return false;
           fence_after();
           gradient(kDk, kDp, pos, j > 0);
           release(pos);
@@ -260,22 +248,26 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dkv(const __grid_constant_
         done_with(b.out_full);
         return true;
       };
+#pragma unroll 1
       for (int i = i0; i < i1; ++i) {
         const int steps = uniform(a.k_tile[i].n) * group;
         if (steps && !run(steps)) break;
       }
       done_with(b.done);
-      bar_wait(b.done, 0, w);
+      bar_wait(b.done, 0, a.error);
     } else if (warp == 10) {                                // ---- lse and delta of the query tiles
       const int lane = threadIdx.x % 32;
       uint32_t n = 0;
       bool ok = true;
       after_previous();                                      // delta is there
       let_next_start();
+#pragma unroll 1
       for (int i = i0; ok && i < i1; ++i) {
         const AttnTile it = a.k_tile[i];
         const int tiles = uniform(it.n), head = uniform(it.head);
+#pragma unroll 1
         for (int h = head * group; ok && h < (head + 1) * group; ++h)
+#pragma unroll 1
           for (int t = 0; t < tiles; ++t, ++n) {
             const uint32_t st = n % L::kStatStages;
             float lse[4], delta[4];
@@ -286,7 +278,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dkv(const __grid_constant_
               delta[e] = q < it.rows ? a.delta[h * a.delta_rows + it.q_row + q] : 0.f;
               if (lse[e] == -INFINITY) lse[e] = INFINITY;    // no weight for a row that sees nothing
             }
-            if (n >= L::kStatStages && !(ok = bar_wait(b.stat_free + 8 * st, (n / L::kStatStages - 1) & 1, w))) break;
+            if (n >= L::kStatStages && !(ok = bar_wait(b.stat_free + 8 * st, (n / L::kStatStages - 1) & 1, a.error))) break;
             float* at = reinterpret_cast<float*>(sm + L::kStats + st * L::kStatBytes);
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
@@ -305,12 +297,14 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dkv(const __grid_constant_
     const uint32_t S = tmem + lanes + kS + c0, Dp = tmem + lanes + kDp + c0;
     const float c2 = a.scale * kLog2e;
     uint32_t n = 0, pos = 0, items = 0;
+#pragma unroll 1
     for (int i = i0; i < i1; ++i) {
       const AttnTile it = a.k_tile[i];
       if (i + 1 < i1) asm volatile("prefetch.global.L1 [%0];" ::"l"(a.k_tile + i + 1));
       const int tiles = uniform(it.n), steps = tiles * group, queries = uniform(it.rows), first_seen = uniform(it.seen);
       bool ok = true;
       int t = 0;
+#pragma unroll 1
       for (int j = 0; j < steps; ++j, ++n, pos += 2) {
         const uint32_t st = n % L::kStatStages;
         const float* stat = reinterpret_cast<const float*>(sm + L::kStats + st * L::kStatBytes) + c0;
@@ -320,7 +314,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dkv(const __grid_constant_
         const bool tail = rows < kTile, masked = first_seen + q0 < kTile || tail;
         t = t + 1 < tiles ? t + 1 : 0;
         float p[64];
-        if (!(ok = bar_wait(b.stat_full + 8 * st, n / L::kStatStages & 1, w) && bar_wait(b.s_full, n & 1, w))) break;
+        if (!(ok = bar_wait(b.stat_full + 8 * st, n / L::kStatStages & 1, a.error) && bar_wait(b.s_full, n & 1, a.error))) break;
         fence_after();
         tmem_ld32(S, p);
         tmem_ld32(S + 32, p + 32);
@@ -344,13 +338,13 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dkv(const __grid_constant_
         }
         if (tail) {
           const uint32_t at = pos + 1, sg = at % L::kStages;
-          if (!(ok = bar_wait(b.full + 8 * sg, at / L::kStages & 1, w))) break;
+          if (!(ok = bar_wait(b.full + 8 * sg, at / L::kStages & 1, a.error))) break;
           clear_rows<DP>(sm + L::kRing + sg * L::kTileBytes, rows);
         }
         wait_st();
         fence_before();
         bar_arrive_warp(b.p_ready, leader);
-        if (!(ok = bar_wait(b.dp_full, n & 1, w))) break;
+        if (!(ok = bar_wait(b.dp_full, n & 1, a.error))) break;
         fence_after();
         float d[64];
         tmem_ld32(Dp, d);
@@ -381,7 +375,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dkv(const __grid_constant_
       }
       if (!ok) break;
       if (steps) {
-        if (!bar_wait(b.out_full, items++ & 1, w)) break;
+        if (!bar_wait(b.out_full, items++ & 1, a.error)) break;
         fence_after();
       }
       const AttnTensor& out = half ? a.dk : a.dv;
@@ -407,18 +401,16 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dq(const __grid_constant__
   const uint32_t base = smem_addr(sm);
   const Bars<DP> b(base + L::kBars);
   int* const shared_int = reinterpret_cast<int*>(sm + L::kInts);
-  const Waits w{shared_int, a.error};
   const int warp = uniform(threadIdx.x / 32);
-  if (!swizzle_aligned(base, w)) return;
+  if (!swizzle_aligned(base, a.error)) return;
   if (threadIdx.x == 0) {
     b.init();
-    shared_int[0] = 0;
   }
-  if (warp == 9) tmem_alloc<512>(smem_addr(shared_int + 1));
+  if (warp == 9) tmem_alloc<512>(smem_addr(shared_int));
   fence_before();
   __syncthreads();
   fence_after();
-  const uint32_t tmem = (uint32_t)shared_int[1];
+  const uint32_t tmem = (uint32_t)shared_int[0];
   const int group = a.heads / a.kv_heads;
   const int i0 = uniform(a.q_first[blockIdx.x]), i1 = uniform(a.q_first[blockIdx.x + 1]);
 
@@ -426,13 +418,15 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dq(const __grid_constant__
     regs_down<kRegsFew>();
     const bool leader = elect_one();
     if (warp == 8) {                                        // ---- loads
-      Loader<DP> load{base, b, w, leader};
+      Loader<DP> load{base, b, a.error, leader};
       bool ok = true;
+#pragma unroll 1
       for (int i = i0; ok && i < i1; ++i) {
         const AttnTile it = a.q_tile[i];
         const int n = uniform(it.n);
         if (!n) continue;
         ok = load.stay(&q_map, &do_map, it.head, (int)it.q_row);
+#pragma unroll 1
         for (int j = 0; ok && j < n; ++j)
           ok = load.next(&k_map, it.head / group, (int)it.k_row + j * kTile) &&
                load.next(&v_map, it.head / group, (int)it.k_row + j * kTile);
@@ -443,7 +437,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dq(const __grid_constant__
       const uint32_t i_s = instr(BF16, kTile, false), i_o = instr(BF16, ksteps * 16, true);
       uint32_t pos = 0, fixed = 0, n = 0;
       auto tile = [&](uint32_t at) { return tile_desc(base + L::kRing + at % L::kStages * L::kTileBytes); };
-      auto arrived = [&](uint32_t at) { return bar_wait(b.full + 8 * (at % L::kStages), at / L::kStages & 1, w); };
+      auto arrived = [&](uint32_t at) { return bar_wait(b.full + 8 * (at % L::kStages), at / L::kStages & 1, a.error); };
       auto done_with = [&](uint32_t bar) {
         if (leader) commit(bar);
       };
@@ -451,17 +445,14 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dq(const __grid_constant__
       const uint32_t Q = tile_desc(base), dO = tile_desc(base + L::kTileBytes);
       auto across = [&](uint32_t d, uint32_t x, uint32_t at) {       // queries by keys
         const uint32_t y = tile(at);
-        if (leader)
-#pragma unroll
-          for (int e = 0; e < DP / 16; ++e)
-            if (e < ksteps) mma(tmem + d, x + step_along(e), y + step_along(e), i_s, e > 0);
+        if (leader) mma_along(tmem + d, x, y, i_s, ksteps);
       };
       auto scores = [&](uint32_t step, uint32_t at) {
         across(kS + step % 2 * 128, Q, at);
         done_with(b.s_full + 8 * (step % 2));
       };
       auto run = [&](int steps) {
-        if (!bar_wait(b.fixed_full, fixed++ & 1, w) || !arrived(pos)) return false;
+        if (!bar_wait(b.fixed_full, fixed++ & 1, a.error) || !arrived(pos)) return false;
         fence_after();
         scores(n, pos);
         if (!arrived(pos + 1)) return false;
@@ -474,14 +465,15 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dq(const __grid_constant__
         } else {
           done_with(b.fixed_free);
         }
+#pragma unroll 1
         for (int j = 0; j < steps; ++j, pos += 2, ++n) {
-          if (!bar_wait(b.ds_ready, n & 1, w)) return false;
+          if (!bar_wait(b.ds_ready, n & 1, a.error)) return false;
           fence_after();
           const uint32_t k = tile(pos);
-          if (leader)
-#pragma unroll
-            for (int e = 0; e < kTile / 16; ++e)
-              mma_tmem(tmem + kDq, tmem + kDp + e / 4 * 64 + e % 4 * 8, k + step_rows(e), i_o, j > 0 || e > 0);
+          if (leader) {
+            mma_rows(tmem + kDq, tmem + kDp, k, i_o, j > 0);
+            mma_rows(tmem + kDq, tmem + kDp + 64, k + step_rows(4), i_o, true);
+          }
           release(pos);
           if (j + 1 < steps) {
             if (!arrived(pos + 3)) return false;
@@ -498,12 +490,13 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dq(const __grid_constant__
         done_with(b.out_full);
         return true;
       };
+#pragma unroll 1
       for (int i = i0; i < i1; ++i) {
         const int steps = uniform(a.q_tile[i].n);
         if (steps && !run(steps)) break;
       }
       done_with(b.done);
-      bar_wait(b.done, 0, w);
+      bar_wait(b.done, 0, a.error);
     }
   } else {                                                  // ---- arithmetic: a query per lane, 64 keys
     regs_up<kRegsMany>();
@@ -512,6 +505,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dq(const __grid_constant__
     const uint32_t lanes = (uint32_t)(warp % 4 * 32) << 16, Dp = tmem + lanes + kDp + c0;
     const float c2 = a.scale * kLog2e;
     uint32_t n = 0, pos = 0, items = 0;
+#pragma unroll 1
     for (int i = i0; i < i1; ++i) {
       const AttnTile it = a.q_tile[i];
       if (i + 1 < i1) asm volatile("prefetch.global.L1 [%0];" ::"l"(a.q_tile + i + 1));
@@ -525,19 +519,20 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dq(const __grid_constant__
         if (lse == -INFINITY) lse = INFINITY;                // no weight for a row that sees nothing
       }
       bool ok = true;
+#pragma unroll 1
       for (int j = 0; j < steps; ++j, ++n, pos += 2) {
         const uint32_t S = tmem + lanes + kS + n % 2 * 128 + c0;
         const int seen = first_seen + r - j * kTile - c0;                   // keys of this half that the row sees
         const bool masked = (j + 1) * kTile > first_seen;
         float p[64];
-        if (!(ok = bar_wait(b.s_full + 8 * (n % 2), n / 2 & 1, w))) break;
+        if (!(ok = bar_wait(b.s_full + 8 * (n % 2), n / 2 & 1, a.error))) break;
         fence_after();
         tmem_ld32(S, p);
         tmem_ld32(S + 32, p + 32);
         wait_ld();
 #pragma unroll
         for (int e = 0; e < 64; ++e) p[e] = exp2_fast(fmaf(p[e], c2, -lse));
-        if (!(ok = bar_wait(b.dp_full, n & 1, w))) break;
+        if (!(ok = bar_wait(b.dp_full, n & 1, a.error))) break;
         fence_after();
         float d[64];
         tmem_ld32(Dp, d);
@@ -561,7 +556,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dq(const __grid_constant__
       }
       if (!ok) break;
       if (steps) {
-        if (!bar_wait(b.out_full, items++ & 1, w)) break;
+        if (!bar_wait(b.out_full, items++ & 1, a.error)) break;
         fence_after();
       }
       uint8_t* row = static_cast<uint8_t*>(a.dq.data) + 2 * (query * a.dq.row + it.head * a.dq.head);

@@ -34,12 +34,24 @@ using namespace umma;
 constexpr int kThreads = 384;          // two softmax groups of 4 warps, and 4 warps with a role each
 // Registers per thread: 168 at launch (3 warpgroups of 168 = 504), of which
 // the softmax groups take most, so that a row of scores stays in registers.
-constexpr int kRegsMany = 216, kRegsFew = 72;
+constexpr int kRegsMany = 224, kRegsFew = 56;
 static_assert(2 * kRegsMany + kRegsFew <= 3 * 168, "register split");
 constexpr int kCols = 512;
 // columns of query tile t's scores and outputs
 __device__ __forceinline__ constexpr uint32_t s_col(int t) { return 128 * t; }
 __device__ __forceinline__ constexpr uint32_t o_col(int t) { return 256 + 128 * t; }
+
+// A place in the ring of tiles and the parity of its use there.
+template <int STAGES>
+struct Place {
+  uint32_t stage = 0, parity = 0;
+  __device__ __forceinline__ void next() {
+    if (++stage == STAGES) {
+      stage = 0;
+      parity ^= 1;
+    }
+  }
+};
 
 template <int DP>
 struct Layout {
@@ -51,14 +63,14 @@ struct Layout {
   static constexpr int kBytes = kInts + 8;
 };
 
-template <bool BF16>
-__device__ __forceinline__ void store8(void* p, const float* x) {
-  uint4 v;
-  v.x = pack2<BF16>(x[0], x[1]);
-  v.y = pack2<BF16>(x[2], x[3]);
-  v.z = pack2<BF16>(x[4], x[5]);
-  v.w = pack2<BF16>(x[6], x[7]);
-  *static_cast<uint4*>(p) = v;
+// Of 16 scores of a row, those from `seen` on become -inf.
+__device__ __forceinline__ void hide16(uint32_t addr, int seen) {
+  float x[16];
+  tmem_ld16(addr, x);
+  wait_ld();
+#pragma unroll
+  for (int c = 0; c < 16; ++c) x[c] = c < seen ? x[c] : -INFINITY;
+  tmem_st16(addr, reinterpret_cast<uint32_t*>(x));
 }
 
 template <int DP, bool BF16>
@@ -73,10 +85,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_fwd(const __grid_constant_
   const uint32_t q_full = bars, q_free = bars + 16, s_full = bars + 32, p_full = bars + 48, o_full = bars + 64,
                  p_half = bars + 80, done = bars + 96, full = bars + 104, free_ = full + 8 * L::kStages;
   int* const shared_int = reinterpret_cast<int*>(sm + L::kInts);
-  const Waits w{shared_int, a.error};
   const int warp = uniform(threadIdx.x / 32);
-  if (!swizzle_aligned(base, w)) return;
+  if (!swizzle_aligned(base, a.error)) return;
   if (threadIdx.x == 0) {
+#pragma unroll 1
     for (int t = 0; t < 2; ++t) {
       bar_init(q_full + 8 * t, 1);
       bar_init(q_free + 8 * t, 1);
@@ -86,18 +98,18 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_fwd(const __grid_constant_
       bar_init(o_full + 8 * t, 1);
     }
     bar_init(done, 2);
+#pragma unroll 1
     for (int i = 0; i < L::kStages; ++i) {
       bar_init(full + 8 * i, 1);
       bar_init(free_ + 8 * i, 2);
     }
     bar_init_visible();
-    shared_int[0] = 0;
   }
-  if (warp == 8) tmem_alloc<kCols>(smem_addr(shared_int + 1));
+  if (warp == 8) tmem_alloc<kCols>(smem_addr(shared_int));
   fence_before();
   __syncthreads();
   fence_after();
-  const uint32_t tmem = (uint32_t)shared_int[1];
+  const uint32_t tmem = (uint32_t)shared_int[0];
 
   const int group = a.heads / a.kv_heads, packed_rows = kTile / group;
   if (threadIdx.x == 0) let_next_start();
@@ -107,38 +119,48 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_fwd(const __grid_constant_
     regs_down<kRegsFew>();
     const bool leader = elect_one();
     if (warp == 8) {                                        // ---- loads of key and value tiles
-      uint32_t pos = 0;
-      bool ok = true;
+      Place<L::kStages> at;
+      bool ok = true, first = true;                         // first: of the ring, whose places are free
       auto load = [&](const CUtensorMap* map, int head, int row) {
-        const uint32_t st = pos % L::kStages, bar = full + 8 * st;
-        if (pos >= L::kStages && !bar_wait(free_ + 8 * st, (pos / L::kStages - 1) & 1, w)) return false;
+        const uint32_t bar = full + 8 * at.stage;
+        if (!first && !bar_wait(free_ + 8 * at.stage, at.parity ^ 1, a.error)) return false;
         if (leader) {
           bar_expect(bar, L::kTileBytes);
 #pragma unroll
           for (int c = 0; c < DP / 64; ++c)
-            tma_load(base + L::kRing + st * L::kTileBytes + c * kBlockBytes, map, bar, 64 * c, head, row);
+            tma_load(base + L::kRing + at.stage * L::kTileBytes + c * kBlockBytes, map, bar, 64 * c, head, row);
         }
-        ++pos;
+        at.next();
+        first = first && at.stage;
         return true;
       };
+#pragma unroll 1
       for (int i = i0; ok && i < i1; ++i) {
         const AttnItem it = a.item[i];
-        const int n = uniform(max(it.n[0], it.n[1])), row = (int)it.k_row, head = it.head / group;
-        for (int j = 0; ok && j < n; ++j) ok = load(&k_map, head, row + j * kTile) && load(&v_map, head, row + j * kTile);
+        const int n = 2 * uniform(max(it.n[0], it.n[1])), head = it.head / group;
+        int row = (int)it.k_row;
+#pragma unroll 1
+        for (int j = 0; ok && j < n; ++j) {                  // a key tile, then its value tile
+          ok = load(j % 2 ? &v_map : &k_map, head, row);
+          row += j % 2 * kTile;
+        }
       }
       // nothing is in flight when the block ends
-      for (uint32_t i = pos > L::kStages ? pos - L::kStages : 0; i < pos; ++i)
-        bar_wait(full + 8 * (i % L::kStages), i / L::kStages & 1, w);
+#pragma unroll 1
+      for (int i = 0; i < L::kStages; ++i) {
+        if (!first || (uint32_t)i < at.stage) bar_wait(full + 8 * i, at.parity ^ ((uint32_t)i >= at.stage), a.error);
+      }
     } else if (warp == 9) {                                 // ---- loads of query tiles
       uint32_t n[2] = {0, 0};
       bool ok = true;
+#pragma unroll 1
       for (int i = i0; ok && i < i1; ++i) {
         const AttnItem it = a.item[i];
         const int packed = uniform(it.packed), row = (int)it.q_row;
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
           if (!ok || !uniform(it.n[t])) continue;
-          if (n[t] && !(ok = bar_wait(q_free + 8 * t, (n[t] - 1) & 1, w))) continue;
+          if (n[t] && !(ok = bar_wait(q_free + 8 * t, (n[t] - 1) & 1, a.error))) continue;
           if (leader) {
             bar_expect(q_full + 8 * t, DP / 64 * (packed ? packed_rows * group : kTile) * 128);
 #pragma unroll
@@ -151,89 +173,91 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_fwd(const __grid_constant_
       }
 #pragma unroll
       for (int t = 0; t < 2; ++t)
-        if (n[t]) bar_wait(q_full + 8 * t, (n[t] - 1) & 1, w);
+        if (n[t]) bar_wait(q_full + 8 * t, (n[t] - 1) & 1, a.error);
     } else {                                                // ---- products of query tile t
       const int t = warp - 10, ksteps = (a.dim + 15) / 16;
       const uint32_t i_s = instr(BF16, kTile, false), i_o = instr(BF16, ksteps * 16, true);
       const uint32_t S = tmem + s_col(t), O = tmem + o_col(t);
       const uint32_t Q = tile_desc(base + t * L::kTileBytes), ring = tile_desc(base + L::kRing);
-      uint32_t pos = 0, items = 0, steps = 0;
-      auto tile = [&](uint32_t at) { return ring + at % L::kStages * (L::kTileBytes >> 4); };
-      auto arrived = [&](uint32_t at) { return bar_wait(full + 8 * (at % L::kStages), at / L::kStages & 1, w); };
-      auto scores = [&](uint32_t at, bool last) {
-        const uint32_t k = tile(at);
+      Place<L::kStages> at;                                  // of the next tile
+      uint32_t items = 0, steps = 0;
+      auto arrived = [&] { return bar_wait(full + 8 * at.stage, at.parity, a.error); };
+      auto tile = [&] { return ring + at.stage * (L::kTileBytes >> 4); };
+      auto scores = [&](bool first, bool last) {
+        if (!arrived() || (first && !bar_wait(q_full + 8 * t, items++ & 1, a.error))) return false;
+        fence_after();
         if (leader) {
-#pragma unroll
-          for (int e = 0; e < DP / 16; ++e)
-            if (e < ksteps) mma(S, Q + step_along(e), k + step_along(e), i_s, e > 0);
+          mma_along(S, Q, tile(), i_s, ksteps);
           commit(s_full + 8 * t);
-          commit(free_ + 8 * (at % L::kStages));
+          commit(free_ + 8 * at.stage);
           if (last) commit(q_free + 8 * t);
         }
+        at.next();
+        return true;
       };
       auto run = [&](int n, int all) {                      // n of the item's key tiles are this query tile's
-        if (n) {
-          if (!arrived(pos) || !bar_wait(q_full + 8 * t, items++ & 1, w)) return false;
+#pragma unroll 1
+        for (int j = 0; j < n; ++j) {
+          if (j == 0 && !scores(true, n == 1)) return false;
+          const uint32_t v = tile(), v_free = free_ + 8 * at.stage;
+          if (!arrived() || !bar_wait(p_half + 8 * t, steps & 1, a.error)) return false;
           fence_after();
-          scores(pos, n == 1);
-          for (int j = 0; j < n; ++j, pos += 2) {
-            const uint32_t v = tile(pos + 1);
-            if (!arrived(pos + 1) || !bar_wait(p_half + 8 * t, steps & 1, w)) return false;
-            fence_after();
-            if (leader)
-#pragma unroll
-              for (int e = 0; e < kTile / 32; ++e) mma_tmem(O, S + 8 * e, v + step_rows(e), i_o, j > 0 || e > 0);
-            if (j + 1 < n && !arrived(pos + 2)) return false;
-            if (!bar_wait(p_full + 8 * t, steps++ & 1, w)) return false;
-            fence_after();
-            if (leader) {
-#pragma unroll
-              for (int e = kTile / 32; e < kTile / 16; ++e) mma_tmem(O, S + 8 * e, v + step_rows(e), i_o, true);
-              commit(free_ + 8 * ((pos + 1) % L::kStages));
-              if (j + 1 == n) commit(o_full + 8 * t);
-            }
-            if (j + 1 < n) scores(pos + 2, j + 2 == n);
+          if (leader) mma_rows(O, S, v, i_o, j > 0);
+          at.next();
+          if (!bar_wait(p_full + 8 * t, steps++ & 1, a.error)) return false;
+          fence_after();
+          if (leader) {
+            mma_rows(O, S + 32, v + step_rows(4), i_o, true);
+            commit(v_free);
+            if (j + 1 == n) commit(o_full + 8 * t);
           }
+          if (j + 1 < n && !scores(false, j + 2 == n)) return false;
         }
-        for (int j = 2 * n; j < 2 * all; ++j, ++pos) {       // the other's: let go as they come
-          if (!arrived(pos)) return false;
-          bar_arrive_warp(free_ + 8 * (pos % L::kStages), leader);
+#pragma unroll 1
+        for (int j = 2 * n; j < 2 * all; ++j, at.next()) {   // the other's: let go as they come
+          if (!arrived()) return false;
+          bar_arrive_warp(free_ + 8 * at.stage, leader);
         }
         return true;
       };
+#pragma unroll 1
       for (int i = i0; i < i1; ++i)
         if (!run(uniform(a.item[i].n[t]), uniform(max(a.item[i].n[0], a.item[i].n[1])))) break;
       if (leader) commit(done);
-      bar_wait(done, 0, w);
+      bar_wait(done, 0, a.error);
     }
   } else {                                                  // ---- softmax: a row of query tile t per thread
     regs_up<kRegsMany>();
     const int t = warp / 4, r = threadIdx.x % 128;
     const bool leader = elect_one();
+    const int packed_q = r / group, packed_h = r % group;    // query and head of a packed tile's row
     const uint32_t lanes = (uint32_t)(warp % 4 * 32) << 16, S = tmem + s_col(t) + lanes, O = tmem + o_col(t) + lanes;
     const float c2 = a.scale * 1.4426950408889634f;          // weights are powers of two
     const float slack = 8.f / c2;                            // see below
     uint32_t pos = 0, sn = 0, on = 0;
+#pragma unroll 1
     for (int i = i0; i < i1; ++i) {
       const AttnItem* const at_item = a.item + i;
       if (i + 1 < i1) asm volatile("prefetch.global.L1 [%0];" ::"l"(at_item + 1));
       const int packed = uniform(at_item->packed), n = uniform(at_item->n[t]), keys = uniform(at_item->keys);
-      const int per = packed ? packed_rows : kTile, rq = packed ? r / group : r;
+      const int per = packed ? packed_rows : kTile, rq = packed ? packed_q : r;
       const int least = uniform(at_item->seen) + t * per;    // keys that the tile's first query sees
       const int seen_all = min(least + rq, keys);            // and this row
       const bool valid = rq < at_item->rows[t], busy = __any_sync(~0u, valid);
       float m = -INFINITY, l = 0.f;
       bool ok = true;
+#pragma unroll 1
       for (int j = 0; j < n; ++j) {
         const int k0 = j * kTile;
-        if (!(ok = bar_wait(s_full + 8 * t, sn++ & 1, w))) break;
+        if (!(ok = bar_wait(s_full + 8 * t, sn++ & 1, a.error))) break;
         if (k0 + kTile > keys) {
           // Values past the sequence's end belong to other sequences and may
           // be anything; a zero weight does not hide a NaN, so they are
           // cleared (both query tiles write the same zeros).
           const uint32_t at = pos + 2 * j + 1, st = at % L::kStages;
-          if (!(ok = bar_wait(full + 8 * st, at / L::kStages & 1, w))) break;
+          if (!(ok = bar_wait(full + 8 * st, at / L::kStages & 1, a.error))) break;
           uint8_t* v = sm + L::kRing + st * L::kTileBytes;
+#pragma unroll 1
           for (int b = (keys - k0) * 8 + r; b < kTile * 8; b += 128)
 #pragma unroll
             for (int c = 0; c < DP / 64; ++c) *reinterpret_cast<uint4*>(v + c * kBlockBytes + b * 16) = make_uint4(0, 0, 0, 0);
@@ -245,15 +269,37 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_fwd(const __grid_constant_
           continue;
         }
         fence_after();
+        if (k0 + kTile > least) {                             // some row does not see the whole tile
+          const int seen = seen_all - k0;
+#pragma unroll 1
+          for (int c = max(0, uniform(seen)) & ~15; c < kTile; c += 16) hide16(S + c, seen - c);
+          wait_st();
+        }
         float x[kTile];
 #pragma unroll
         for (int c = 0; c < kTile; c += 32) tmem_ld32(S + c, x + c);
         wait_ld();
-        if (k0 + kTile > least) {                             // some row does not see the whole tile
-          const int seen = seen_all - k0;
+        // The weights of the first half with the maximum known so far, while
+        // the tile's own is found (the one keeps the special function unit
+        // busy, the other the integer unit).
+        const uint64_t c22 = pair_bits(c2, c2);
+        uint64_t l2[2];
+        uint32_t y[kTile / 4];
+        auto weights = [&](const float* s, uint32_t* p) {
+          const float shift = m == -INFINITY ? 0.f : m * c2;
+          const uint64_t shift2 = pair_bits(-shift, -shift);
 #pragma unroll
-          for (int c = 0; c < kTile; ++c) x[c] = c < seen ? x[c] : -INFINITY;
-        }
+          for (int e = 0; e < kTile / 2; e += 2) {
+            float u, v;
+            pair_split(fma2(pair_bits(s[e], s[e + 1]), c22, shift2), u, v);
+            u = exp2_fast(u);
+            v = exp2_fast(v);
+            l2[e / 2 % 2] = add2(l2[e / 2 % 2], pair_bits(u, v));
+            p[e / 2] = pack2<BF16>(u, v);
+          }
+        };
+        l2[0] = l2[1] = 0;
+        weights(x, y);
         float m4[4] = {x[0], x[1], x[2], x[3]};
 #pragma unroll
         for (int c = 4; c < kTile; c += 8)
@@ -266,44 +312,30 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_fwd(const __grid_constant_
         // decides for itself, so that no other row of its tile changes its
         // rounding.  All products up to the last tile's are done when this
         // tile's scores are.
-        const bool rises = j > 0 && top > m + slack;
-        if (j == 0) m = top;
+        const bool rises = j == 0 || top > m + slack;
         if (__any_sync(~0u, rises)) {
-          const float by = rises ? exp2_fast((m - top) * c2) : 1.f;
+          const float by = rises && j > 0 ? exp2_fast((m - top) * c2) : 1.f;
           m = rises ? top : m;
           l *= by;
+          if (j > 0)
 #pragma unroll 1
-          for (int c = 0; c < DP; c += 16) {
-            float o[16];
-            tmem_ld16(O + c, o);
-            wait_ld();
+            for (int c = 0; c < DP; c += 16) {
+              float o[16];
+              tmem_ld16(O + c, o);
+              wait_ld();
 #pragma unroll
-            for (int e = 0; e < 16; ++e) o[e] *= by;
-            tmem_st16(O + c, reinterpret_cast<uint32_t*>(o));
-          }
+              for (int e = 0; e < 16; ++e) o[e] *= by;
+              tmem_st16(O + c, reinterpret_cast<uint32_t*>(o));
+            }
+          l2[0] = l2[1] = 0;
+          weights(x, y);
         }
-        const float shift = m == -INFINITY ? 0.f : m * c2;
-        const uint64_t c22 = pair_bits(c2, c2), shift2 = pair_bits(-shift, -shift);
-        uint64_t l2[2] = {0, 0};
-#pragma unroll
-        for (int c = 0; c < kTile; c += 32) {
-          uint32_t y[16];
-#pragma unroll
-          for (int e = 0; e < 32; e += 2) {
-            float u, v;
-            pair_split(fma2(pair_bits(x[c + e], x[c + e + 1]), c22, shift2), u, v);
-            u = exp2_fast(u);
-            v = exp2_fast(v);
-            l2[e / 2 % 2] = add2(l2[e / 2 % 2], pair_bits(u, v));
-            y[e / 2] = pack2<BF16>(u, v);
-          }
-          tmem_st16(S + c / 2, y);
-          if (c == 32) {                                      // the first half may be multiplied
-            wait_st();
-            fence_before();
-            bar_arrive_warp(p_half + 8 * t, leader);
-          }
-        }
+        tmem_st32(S, y);
+        wait_st();                                            // the first half may be multiplied
+        fence_before();
+        bar_arrive_warp(p_half + 8 * t, leader);
+        weights(x + kTile / 2, y);
+        tmem_st32(S + 32, y);
         wait_st();
         fence_before();
         bar_arrive_warp(p_full + 8 * t, leader);
@@ -315,49 +347,51 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_fwd(const __grid_constant_
       if (!ok) break;
       pos += 2 * uniform(max(at_item->n[0], at_item->n[1]));
       if (n) {
-        if (!bar_wait(o_full + 8 * t, on++ & 1, w)) break;
+        if (!bar_wait(o_full + 8 * t, on++ & 1, a.error)) break;
         fence_after();
       }
       if (!busy) continue;
       const bool some = n && l != 0.f;
-      const float by = some ? 1.f / l : 0.f;
+      const float by = __fdividef(1.f, l);
       const int slot = uniform(at_item->slot);
-      const int head = at_item->head + (packed ? r % group : 0);
+      const int head = at_item->head + (packed ? packed_h : 0);
       const int64_t query = at_item->q_row + t * per + rq;
-      const int64_t place = ((int64_t)slot * 2 + t) * kTile + r;
       if (valid) {
-        const float lse2 = l == 0.f ? -INFINITY : fmaf(m, c2, log2f(l));
+        const float lse2 = l == 0.f ? -INFINITY : fmaf(m, c2, __log2f(l));
         if (slot >= 0)
-          a.part_lse[place] = lse2;
+          a.part_lse[((int64_t)slot * 2 + t) * kTile + r] = lse2;
         else if (a.lse)
           a.lse[head * a.q.rows + query] = lse2 * 0.6931471805599453f;
       }
-      // A piece of a split key range leaves its rows in 32 bits, scaled by its
-      // own sum; whole ranges are done.
-      uint8_t* out = slot >= 0 ? reinterpret_cast<uint8_t*>(a.part_o + place * DP)
-                               : static_cast<uint8_t*>(a.o.data) + 2 * (query * a.o.row + head * a.o.head);
+      if (slot >= 0) {
+        // A piece of a split key range leaves its rows in 32 bits, scaled by
+        // its own sum: four columns of all rows side by side.
+        float* part = a.part_o + ((int64_t)slot * 2 + t) * kTile * DP + 4 * r;
+#pragma unroll 1
+        for (int c = 0; c < DP; c += 16) {
+          float o[16];
+          __syncwarp();
+          tmem_ld16(O + c, o);
+          wait_ld();
+#pragma unroll
+          for (int e = 0; e < 16; ++e) o[e] = some ? o[e] * by : 0.f;
+          if (valid)
+#pragma unroll
+            for (int e = 0; e < 16; e += 4)
+              *reinterpret_cast<float4*>(part + (c + e) * kTile) = make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
+        }
+        continue;
+      }
+      RowWriter out(static_cast<uint8_t*>(a.o.data) + 2 * (query * a.o.row + head * a.o.head), valid);
 #pragma unroll 1
       for (int c = 0; c < DP; c += 32) {
         float o[32];
         __syncwarp();
-        if (n) {
-          tmem_ld32(O + c, o);
-          wait_ld();
-        }
+        tmem_ld32(O + c, o);
+        wait_ld();
 #pragma unroll
         for (int e = 0; e < 32; ++e) o[e] = some ? o[e] * by : 0.f;
-        if (slot >= 0) {
-          if (valid)
-#pragma unroll
-            for (int e = 0; e < 32; e += 4) *reinterpret_cast<float4*>(out + 4 * e) = make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
-          out += 128;
-        } else {
-          if (valid)
-#pragma unroll
-            for (int e = 0; e < 32; e += 8)
-              if (c + e < a.dim) store8<BF16>(out + 2 * e, o + e);
-          out += 64;
-        }
+        out.write<BF16>(o, c, a.dim);
       }
     }
   }
@@ -368,7 +402,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_fwd(const __grid_constant_
 }
 
 // Rows of split key ranges from their pieces, in the order of the pieces: a
-// warp per row, DP / 32 entries per lane.
+// warp per row, four columns per lane (of the first DP / 4 lanes).
 template <int DP, bool BF16>
 __global__ void __launch_bounds__(256) k_attn_merge(const __grid_constant__ AttnArgs a) {
   after_previous();
@@ -379,27 +413,32 @@ __global__ void __launch_bounds__(256) k_attn_merge(const __grid_constant__ Attn
   if (t) row -= n0;
   if (row >= s.rows[t] * heads) return;
   const float* lse = a.part_lse + ((int64_t)s.slot * 2 + t) * kTile + row;
-  const float* part = a.part_o + (((int64_t)s.slot * 2 + t) * kTile + row) * DP + lane * (DP / 32);
+  const float* part = a.part_o + ((int64_t)s.slot * 2 + t) * kTile * DP + lane % (DP / 4) * 4 * kTile + row * 4;
   float top = -INFINITY;
   for (int k = lane; k < s.pieces; k += 32) top = fmaxf(top, lse[(int64_t)k * 2 * kTile]);
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, o));
   const float from = top == -INFINITY ? 0.f : top;
-  float acc[DP / 32] = {}, sum = 0.f;
+  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+  float sum = 0.f;
 #pragma unroll 8
   for (int k = 0; k < s.pieces; ++k) {
     const float f = exp2_fast(lse[(int64_t)k * 2 * kTile] - from);
+    const float4 x = *reinterpret_cast<const float4*>(part + (int64_t)k * 2 * kTile * DP);
     sum += f;
-#pragma unroll
-    for (int e = 0; e < DP / 32; ++e) acc[e] = fmaf(f, part[(int64_t)k * 2 * kTile * DP + e], acc[e]);
+    acc.x = fmaf(f, x.x, acc.x);
+    acc.y = fmaf(f, x.y, acc.y);
+    acc.z = fmaf(f, x.z, acc.z);
+    acc.w = fmaf(f, x.w, acc.w);
   }
   const float by = sum == 0.f ? 0.f : 1.f / sum;
   const int head = s.packed ? s.head + row % group : s.head;
   const int64_t query = s.q_row + t * (s.packed ? kTile / group : kTile) + (s.packed ? row / group : row);
-  if (lane * (DP / 32) < a.dim) {
-    uint8_t* out = static_cast<uint8_t*>(a.o.data) + 2 * (query * a.o.row + head * a.o.head + lane * (DP / 32));
-#pragma unroll
-    for (int e = 0; e < DP / 32; e += 2) *reinterpret_cast<uint32_t*>(out + 2 * e) = pack2<BF16>(acc[e] * by, acc[e + 1] * by);
+  if (lane < DP / 4 && lane * 4 < a.dim) {
+    uint2 v;
+    v.x = pack2<BF16>(acc.x * by, acc.y * by);
+    v.y = pack2<BF16>(acc.z * by, acc.w * by);
+    *reinterpret_cast<uint2*>(static_cast<uint8_t*>(a.o.data) + 2 * (query * a.o.row + head * a.o.head + lane * 4)) = v;
   }
   if (a.lse && lane == 0) a.lse[head * a.q.rows + query] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * 0.6931471805599453f;
 }

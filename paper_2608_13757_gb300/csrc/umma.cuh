@@ -61,42 +61,27 @@ __device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity) {
       : "memory");
   return ok;
 }
-__device__ __forceinline__ uint64_t now_ns() {
-  uint64_t t;
-  asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t));
-  return t;
+// A wait by a whole warp, with one answer for all lanes.  One that never ends
+// would be a defect: it gives up after kTries, about a second (the hardware
+// suspends a try for 4 us), and says so in *error (host-visible).  A warp that
+// gave up does nothing more, so the waits that depend on it give up too, and
+// the kernel always ends.
+//
+// The kernels' code has to stay small: at 44 KB a change that added 8 KB
+// outside all loops made the attention of a long prompt 15% slower, for the
+// instruction cache.  So this is a short loop, and what is rare is a loop
+// rather than unrolled.
+constexpr int kTries = 1 << 18;
+__device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, int* error) {
+#pragma unroll 1
+  for (int i = 0; i < kTries; ++i)
+    if (__all_sync(~0u, bar_try(bar, parity))) return true;
+  *reinterpret_cast<volatile int*>(error) = 1;
+  return false;
 }
-
-// What a wait that never ends would mean is a defect; it then gives up after
-// kGiveUpNs, says so in *error (host-visible) and lets the block's other
-// waits give up too, so the kernel always ends.
-constexpr uint64_t kGiveUpNs = 1000000000ull;
-struct Waits {
-  volatile int* dead;     // shared by the block
-  int* error;             // host-visible
-};
-__device__ __forceinline__ bool bar_wait_slow(uint32_t bar, uint32_t parity, Waits w) {
-  const uint64_t t0 = now_ns();
-  for (uint32_t i = 1;; ++i) {
-    if (bar_try(bar, parity)) return true;
-    if (i % 16 == 0) {
-      if (*w.dead) return false;
-      if (now_ns() - t0 > kGiveUpNs) {
-        *w.dead = 1;
-        *reinterpret_cast<volatile int*>(w.error) = 1;
-        return false;
-      }
-    }
-  }
-}
-// By a whole warp, with one answer for all lanes.  (What a warp decides, it
-// decides by votes and by values of its first lane, which the compiler knows
-// to be the same for all lanes: a branch that may diverge costs the kernels
-// here some 50 cycles, ten times a tile.)
-__device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, Waits w) {
-  if (__all_sync(~0u, bar_try(bar, parity))) return true;
-  return __all_sync(~0u, bar_wait_slow(bar, parity, w));
-}
+// (What a warp decides, it decides by votes and by values of its first lane,
+// which the compiler knows to be the same for all lanes: branches that may
+// diverge cost more.)
 __device__ __forceinline__ int uniform(int x) { return __shfl_sync(~0u, x, 0); }
 // One lane of the warp arrives, for all.
 __device__ __forceinline__ void bar_arrive_warp(uint32_t bar, bool leader) {
@@ -108,9 +93,9 @@ __device__ __forceinline__ void bar_arrive_warp(uint32_t bar, bool leader) {
 
 // The swizzle goes by address bits: tiles start at multiples of 1024 bytes, as
 // the start of a block's shared memory does.
-__device__ __forceinline__ bool swizzle_aligned(uint32_t base, Waits w) {
+__device__ __forceinline__ bool swizzle_aligned(uint32_t base, int* error) {
   if (base % 1024 == 0) return true;
-  if (threadIdx.x == 0) *reinterpret_cast<volatile int*>(w.error) = 1;
+  if (threadIdx.x == 0) *reinterpret_cast<volatile int*>(error) = 1;
   return false;
 }
 
@@ -180,6 +165,21 @@ __device__ __forceinline__ void mma_tmem(uint32_t d, uint32_t a, uint32_t b, uin
       "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], y, %3, p;\n}" ::"r"(d),
       "r"(a), "r"(b), "r"(i), "r"((uint32_t)add), "r"(kDescHigh)
       : "memory");
+}
+
+// d = a b^T over `ksteps` steps of 16 contracted entries of two tiles with the
+// contracted dimension contiguous.
+__device__ __forceinline__ void mma_along(uint32_t d, uint32_t a, uint32_t b, uint32_t i, int ksteps) {
+#pragma unroll 1
+  for (int e = 0; e < ksteps; e += 4, a += kBlockBytes >> 4, b += kBlockBytes >> 4)
+#pragma unroll
+    for (int f = 0; f < 4; ++f)
+      if (e + f < ksteps) mma(d, a + step_along(f), b + step_along(f), i, e + f > 0);
+}
+// d (+)= a b over 64 contracted rows of a tile, a in tensor memory.
+__device__ __forceinline__ void mma_rows(uint32_t d, uint32_t a, uint32_t b, uint32_t i, bool add) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) mma_tmem(d, a + 8 * e, b + step_rows(e), i, add || e > 0);
 }
 
 // Columns of this warp's 32 lanes, one lane per thread.
@@ -262,6 +262,47 @@ __device__ __forceinline__ float2 unpack2(uint32_t r) {
   }
   return f;
 }
+
+// Writes 128-row tiles whose rows lie one per lane, 32 columns at a time: four
+// lanes exchange their 16-byte pieces so that a store takes 64 bytes of 8 rows
+// instead of 16 bytes of 32.  (Those took some 5000 cycles per tile of 128
+// columns; these take 1000.)
+struct RowWriter {
+  uint8_t* row[4];     // this lane's piece of the four rows of its group of lanes
+  bool on[4];
+  __device__ __forceinline__ RowWriter(void* mine, bool valid) {
+    const int lane = threadIdx.x % 32;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int from = lane / 4 * 4 + e;
+      row[e] = reinterpret_cast<uint8_t*>(__shfl_sync(~0u, reinterpret_cast<uint64_t>(mine), from)) + lane % 4 * 16;
+      on[e] = __shfl_sync(~0u, (int)valid, from);
+    }
+  }
+  template <bool BF16>
+  __device__ __forceinline__ void write(const float* x, int c, int dim) const {
+    const int lane = threadIdx.x % 32;
+    uint32_t v[4][4];                                        // piece, word
+#pragma unroll
+    for (int e = 0; e < 16; ++e) v[e / 4][e % 4] = pack2<BF16>(x[2 * e], x[2 * e + 1]);
+#pragma unroll
+    for (int bit = 2; bit; bit >>= 1)                        // lane i, piece j  <->  lane j, piece i
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        if (j & bit) continue;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const bool up = lane & bit;
+          const uint32_t got = __shfl_xor_sync(~0u, up ? v[j][k] : v[j + bit][k], bit);
+          v[j][k] = up ? got : v[j][k];
+          v[j + bit][k] = up ? v[j + bit][k] : got;
+        }
+      }
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (on[e] && c + lane % 4 * 8 < dim) *reinterpret_cast<uint4*>(row[e] + 2 * c) = make_uint4(v[e][0], v[e][1], v[e][2], v[e][3]);
+  }
+};
 
 }  // namespace umma
 }  // namespace syncgb
