@@ -246,11 +246,9 @@ struct ForwardWork {
 };
 
 // Items of a forward call and which block takes which.  An item's cost is the
-// key tiles that its query tiles meet and kItemCost for what it does besides.
-// One that costs more than its share of a block is split along its keys
-// into pieces of at least kMinPiece tiles.  The blocks take items from the
-// most expensive on, always the block that has least.
-constexpr int64_t kItemCost = 2, kMinPiece = 2;
+// key tiles that its query tiles meet and kItemCost for what it does besides
+// (a tile of one query tile takes about 0.8 us, an item's start and end 1.5).
+constexpr int64_t kItemCost = 2, kMinPiece = 1;
 
 template <class T>
 struct Draft {
@@ -259,20 +257,23 @@ struct Draft {
 };
 
 // The drafts in the order of the blocks that take them: from the most
-// expensive on, always to the block that has least.
+// expensive on, always to the block that has least.  Returns the most that a
+// block has.
 template <class T>
-void assign(std::vector<Draft<T>>& all, int num_sms, std::vector<T>& item, std::vector<int32_t>& first) {
+int64_t assign(std::vector<Draft<T>>& all, int num_sms, std::vector<T>& item, std::vector<int32_t>& first) {
   std::stable_sort(all.begin(), all.end(), [](const Draft<T>& x, const Draft<T>& y) { return x.cost > y.cost; });
   const int blocks = (int)std::min<int64_t>(num_sms, (int64_t)all.size());
   std::vector<std::vector<int32_t>> of((size_t)blocks);
   using Load = std::pair<int64_t, int32_t>;
   std::priority_queue<Load, std::vector<Load>, std::greater<Load>> least;
   for (int32_t b = 0; b < blocks; ++b) least.push({0, b});
+  int64_t most = 0;
   for (size_t i = 0; i < all.size(); ++i) {
     Load l = least.top();
     least.pop();
     of[(size_t)l.second].push_back((int32_t)i);
     l.first += all[i].cost;
+    most = std::max(most, l.first);
     least.push(l);
   }
   first.push_back(0);
@@ -280,6 +281,7 @@ void assign(std::vector<Draft<T>>& all, int num_sms, std::vector<T>& item, std::
     for (int32_t i : b) item.push_back(all[(size_t)i].it);
     first.push_back((int32_t)item.size());
   }
+  return most;
 }
 
 ForwardWork forward_work(const sync_attn_desc* d, const std::vector<AttnSeq>& seq, int num_sms) {
@@ -309,29 +311,66 @@ ForwardWork forward_work(const sync_attn_desc* d, const std::vector<AttnSeq>& se
       }
   }
   ForwardWork w;
-  std::vector<Draft<AttnItem>> all;
-  const int64_t share = std::max<int64_t>(1, total / num_sms);
+  std::vector<Draft<AttnItem>> whole = draft;
+  const int64_t most = assign(whole, num_sms, w.item, w.block_first);
+  const int64_t share = std::max((total + kItemCost * num_sms) / num_sms + 1, kMinPiece + kItemCost);
+  // Whole items balance well where there are many.  Where the fullest block
+  // has 1/16 more than its share, the items are laid end to end and cut into
+  // equal shares: an item that crosses a cut is split along its keys, and its
+  // pieces' results are merged.  (At most one cut per block: split results
+  // cost a write and a read in 32 bits.)
+  if (most <= share + share / 16) return w;
+  w = ForwardWork{};
+  w.block_first.push_back(0);
+  int64_t room = share;
+  auto next_block = [&] {
+    if ((int)w.block_first.size() == num_sms) return false;    // the last block takes what is left
+    w.block_first.push_back((int32_t)w.item.size());
+    room = share;
+    return true;
+  };
   for (const Draft<AttnItem>& x : draft) {
-    const int64_t n = std::max(x.it.n[0], x.it.n[1]), pieces = std::min(n / kMinPiece, 2 * x.cost / share);
-    if (x.cost <= share * 3 / 4 || pieces < 2) {
-      all.push_back(x);
-      continue;
-    }
-    const int heads = x.it.packed ? group : 1;
-    w.split.push_back({x.it.q_row, x.it.head, x.it.packed, {x.it.rows[0], x.it.rows[1]}, w.slots, (int32_t)pieces});
-    w.merge_rows = std::max(w.merge_rows, (x.it.rows[0] + x.it.rows[1]) * heads);
-    for (int64_t p = 0; p < pieces; ++p) {
-      const int32_t first = (int32_t)(n * p / pieces), last = (int32_t)(n * (p + 1) / pieces);
+    const int32_t n = std::max(x.it.n[0], x.it.n[1]);
+    auto cost = [&](int32_t a, int32_t b) {                    // of key tiles [a, b)
+      int64_t c = kItemCost;
+      for (int t = 0; t < 2; ++t) c += std::max(0, std::min(x.it.n[t], b) - std::min(x.it.n[t], a));
+      return c;
+    };
+    int32_t from = 0, pieces = 0;
+    const int32_t slot0 = w.slots;
+    while (true) {
+      int32_t to = n;
+      bool full = false;
+      if (cost(from, n) > room + 1) {
+        to = from;
+        while (to < n && cost(from, to + 1) <= room) ++to;
+        full = true;
+        if (to - from < kMinPiece || n - to < kMinPiece) {     // not worth a piece here, or nothing left for the next
+          if (room < share && to - from < kMinPiece && next_block()) continue;
+          to = n - to < kMinPiece ? n : from + kMinPiece;
+        }
+        if ((int)w.block_first.size() == num_sms) to = n;
+      }
       AttnItem it = x.it;
-      it.k_row += (int64_t)first * kTile;
-      it.seen -= first * kTile;
-      it.keys -= first * kTile;
-      for (int t = 0; t < 2; ++t) it.n[t] = std::max(0, std::min(x.it.n[t], last) - first);
-      it.slot = w.slots++;
-      all.push_back({it, it.n[0] + it.n[1] + kItemCost});
+      it.k_row += (int64_t)from * kTile;
+      it.seen -= from * kTile;
+      it.keys -= from * kTile;
+      for (int t = 0; t < 2; ++t) it.n[t] = std::max(0, std::min(x.it.n[t], to) - from);
+      const bool split = from > 0 || to < n;
+      if (split) it.slot = w.slots++;
+      pieces += split;
+      room -= cost(from, to);
+      w.item.push_back(it);
+      if (full || room <= 0) next_block();
+      from = to;
+      if (to == n) break;
     }
+    if (!pieces) continue;
+    w.split.push_back({x.it.q_row, x.it.head, x.it.packed, {x.it.rows[0], x.it.rows[1]}, slot0, pieces});
+    w.merge_rows = std::max(w.merge_rows, (x.it.rows[0] + x.it.rows[1]) * (x.it.packed ? group : 1));
   }
-  assign(all, num_sms, w.item, w.block_first);
+  w.block_first.push_back((int32_t)w.item.size());
+  while (w.block_first.size() > 2 && w.block_first[w.block_first.size() - 2] == w.block_first.back()) w.block_first.pop_back();
   return w;
 }
 

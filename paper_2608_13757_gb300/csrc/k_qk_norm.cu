@@ -13,6 +13,7 @@
 
 #include <algorithm>
 
+#include "launch.cuh"
 #include "norm.h"
 #include "sync.h"
 
@@ -141,127 +142,150 @@ __device__ __forceinline__ float sum_lanes(float v) {
   return v;
 }
 
-// Head h of the query heads followed by the key heads, at token t.
-template <class T>
-__device__ __forceinline__ T* head_of(const NormTensor& q, const NormTensor& k, int heads, int64_t t, int h) {
-  return h < heads ? static_cast<T*>(q.data) + t * q.row + h * q.head
-                   : static_cast<T*>(k.data) + t * k.row + (h - heads) * k.head;
+// Heads that a group of LANES lanes holds at a time: their loads are issued
+// together, before anything is stored (outputs may be inputs, so the compiler
+// cannot move a load over a store).
+constexpr int kAhead = 2;
+
+// Heads [h0, h1) of one token and one tensor, G at a time by the warp's groups.
+template <class T, class S>
+__device__ __forceinline__ void forward_heads(const NormArgs& a, const S& l, const NormTensor& in, const NormTensor& out,
+                                              const void* weight, int64_t t, int h0, int h1, const float* c,
+                                              const float* s) {
+  constexpr int VEC = S::VEC, G = 32 / S::LANES;
+  const int group = (threadIdx.x % 32) / S::LANES;
+  const T* x = static_cast<const T*>(in.data) + t * in.row;
+  T* y = static_cast<T*>(out.data) + t * out.row;
+  float w[2 * VEC];
+  l.weights(weight, w);
+#pragma unroll 1
+  for (int hb = h0; hb < h1; hb += kAhead * G) {   // the same trips for every lane: the sums take whole warps
+    float v[kAhead][2 * VEC];
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
+#pragma unroll
+      for (int i = 0; i < 2 * VEC; ++i) v[k][i] = 0.f;
+      const int h = hb + k * G + group;
+      if (l.on() && h < h1) l.read(x + h * in.head, v[k]);
+    }
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
+      float ss = 0.f;
+#pragma unroll
+      for (int i = 0; i < 2 * VEC; ++i) ss += v[k][i] * v[k][i];
+      const float r = rsqrtf(sum_lanes<S::LANES>(ss) * a.inv_dim + a.eps);
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) {
+        const float p = v[k][i] * r * w[i], q = v[k][VEC + i] * r * w[VEC + i];
+        v[k][i] = p * c[i] - q * s[i];
+        v[k][VEC + i] = q * c[i] + p * s[i];
+      }
+      const int h = hb + k * G + group;
+      if (l.on() && h < h1) l.write(y + h * out.head, v[k]);
+    }
+  }
 }
 
-// a.split warps share a token, a.per heads each.
+// a.split warps share a token, a.per heads each (the query heads, then the key heads).
 template <class T, class S>
 __global__ void __launch_bounds__(kThreads) k_norm_rope(const __grid_constant__ NormArgs a) {
-  constexpr int VEC = S::VEC, G = 32 / S::LANES;   // G heads of a warp at a time
   const int64_t warp = blockIdx.x * (int64_t)kWarps + threadIdx.x / 32;
   const int64_t t = warp / a.split;
   if (t >= a.rows) return;
   const int h0 = (int)(warp - t * a.split) * a.per, h1 = min(a.heads + a.kv_heads, h0 + a.per);
   const S l(a);
-  float c[VEC], s[VEC], wq[2 * VEC], wk[2 * VEC];
+  float c[S::VEC], s[S::VEC];
   l.angles(a, t, c, s);
-  l.weights(a.q_weight, wq);
-  l.weights(a.k_weight, wk);
-  const int group = (threadIdx.x % 32) / S::LANES;
-#pragma unroll 2
-  for (int hb = h0; hb < h1; hb += G) {   // the same trips for every lane: the sums take whole warps
-    const int h = hb + group;
-    const bool on = l.on() && h < h1;
-    float x[2 * VEC];
-#pragma unroll
-    for (int i = 0; i < 2 * VEC; ++i) x[i] = 0.f;
-    if (on) l.read(head_of<const T>(a.q, a.k, a.heads, t, h), x);
-    float ss = 0.f;
-#pragma unroll
-    for (int i = 0; i < 2 * VEC; ++i) ss += x[i] * x[i];
-    const float r = rsqrtf(sum_lanes<S::LANES>(ss) * a.inv_dim + a.eps);
-    if (!on) continue;
-#pragma unroll
-    for (int i = 0; i < VEC; ++i) {
-      const float u = x[i] * r * (h < a.heads ? wq[i] : wk[i]);
-      const float v = x[VEC + i] * r * (h < a.heads ? wq[VEC + i] : wk[VEC + i]);
-      x[i] = u * c[i] - v * s[i];
-      x[VEC + i] = v * c[i] + u * s[i];
-    }
-    l.write(head_of<T>(a.q_out, a.k_out, a.heads, t, h), x);
-  }
+  forward_heads<T>(a, l, a.q, a.q_out, a.q_weight, t, h0, min(h1, a.heads), c, s);
+  forward_heads<T>(a, l, a.k, a.k_out, a.k_weight, t, max(h0 - a.heads, 0), h1 - a.heads, c, s);
 }
 
 // Gradient, with xh = r x the normed head: dx = r (w dz - xh mean(w dz xh)),
-// dw = sum of dz xh, dz the output's gradient turned back.  Warps take
-// (token, part of its heads) in turn; the weights' sums stay in registers
-// until the end, go through shared memory in warp order and leave as one row
-// per block, so their order does not depend on the run.
+// dw = sum of dz xh, dz the output's gradient turned back.  Warps take tokens
+// in turn, once for the queries and once for the keys; the weights' sums stay
+// in registers until the end, go through shared memory in warp order and
+// leave as one row per block, so their order does not depend on the run.
 template <class T, class S>
-__global__ void __launch_bounds__(kThreads, 2) k_norm_rope_grad(const __grid_constant__ NormArgs a) {
+__device__ __forceinline__ void gradient_heads(const NormArgs& a, const S& l, const NormTensor& in, const NormTensor& grad,
+                                               const NormTensor& out, int heads, const void* weight, float* row) {
   constexpr int VEC = S::VEC, G = 32 / S::LANES;
-  extern __shared__ float part[];         // [kWarps][q, k][dim]
-  const S l(a);
   const int group = (threadIdx.x % 32) / S::LANES;
-  float wq[2 * VEC], wk[2 * VEC], gq[2 * VEC], gk[2 * VEC];
-  l.weights(a.q_weight, wq);
-  l.weights(a.k_weight, wk);
+  // with few tokens several warps share one, a whole number of rounds of G heads each
+  const int rounds = (heads + G - 1) / G, split = max(1, min(rounds, a.split)), per = (rounds + split - 1) / split * G;
+  const int64_t all = a.rows * split;
+  float w[2 * VEC], g[2 * VEC];
+  l.weights(weight, w);
 #pragma unroll
-  for (int i = 0; i < 2 * VEC; ++i) gq[i] = gk[i] = 0.f;
-  const int64_t all = a.rows * a.split;
+  for (int i = 0; i < 2 * VEC; ++i) g[i] = 0.f;
+#pragma unroll 1
   for (int64_t warp = blockIdx.x * (int64_t)kWarps + threadIdx.x / 32; warp < all; warp += gridDim.x * (int64_t)kWarps) {
-    const int64_t t = warp / a.split;
-    const int h0 = (int)(warp - t * a.split) * a.per, h1 = min(a.heads + a.kv_heads, h0 + a.per);
+    const int64_t t = warp / split;
+    const int h0 = (int)(warp - t * split) * per, h1 = min(heads, h0 + per);
+    const T* x = static_cast<const T*>(in.data) + t * in.row;
+    const T* dy = static_cast<const T*>(grad.data) + t * grad.row;
+    T* dx = static_cast<T*>(out.data) + t * out.row;
     float c[VEC], s[VEC];
     l.angles(a, t, c, s);
-#pragma unroll 2
-    for (int hb = h0; hb < h1; hb += G) {
-      const int h = hb + group;
-      const bool on = l.on() && h < h1, isq = h < a.heads;
-      float x[2 * VEC], d[2 * VEC];
+#pragma unroll 1
+    for (int hb = h0; hb < h1; hb += kAhead * G) {
+      float v[kAhead][2 * VEC], d[kAhead][2 * VEC];
 #pragma unroll
-      for (int i = 0; i < 2 * VEC; ++i) x[i] = d[i] = 0.f;
-      if (on) {
-        l.read(head_of<const T>(a.q, a.k, a.heads, t, h), x);
-        l.read(head_of<const T>(a.q_out, a.k_out, a.heads, t, h), d);
-      }
-      float ss = 0.f, xd = 0.f;
+      for (int k = 0; k < kAhead; ++k) {
 #pragma unroll
-      for (int i = 0; i < VEC; ++i) {     // back through the rotation
-        const float u = d[i], v = d[VEC + i];
-        d[i] = u * c[i] + v * s[i];
-        d[VEC + i] = v * c[i] - u * s[i];
+        for (int i = 0; i < 2 * VEC; ++i) v[k][i] = d[k][i] = 0.f;
+        const int h = hb + k * G + group;
+        if (l.on() && h < h1) {
+          l.read(x + h * in.head, v[k]);
+          l.read(dy + h * grad.head, d[k]);
+        }
       }
 #pragma unroll
-      for (int i = 0; i < 2 * VEC; ++i) {
-        ss += x[i] * x[i];
-        xd += x[i] * d[i] * (isq ? wq[i] : wk[i]);
-      }
-      const float r = rsqrtf(sum_lanes<S::LANES>(ss) * a.inv_dim + a.eps);
-      const float m = sum_lanes<S::LANES>(xd) * a.inv_dim * r * r;
-      if (!on) continue;
+      for (int k = 0; k < kAhead; ++k) {
+        float ss = 0.f, xd = 0.f;
 #pragma unroll
-      for (int i = 0; i < 2 * VEC; ++i) {
-        const float g = d[i] * x[i] * r;
-        gq[i] += isq ? g : 0.f;
-        gk[i] += isq ? 0.f : g;
-        d[i] = r * (d[i] * (isq ? wq[i] : wk[i]) - x[i] * m);
+        for (int i = 0; i < VEC; ++i) {     // back through the rotation
+          const float p = d[k][i], q = d[k][VEC + i];
+          d[k][i] = p * c[i] + q * s[i];
+          d[k][VEC + i] = q * c[i] - p * s[i];
+        }
+#pragma unroll
+        for (int i = 0; i < 2 * VEC; ++i) {
+          ss += v[k][i] * v[k][i];
+          xd += v[k][i] * d[k][i] * w[i];
+        }
+        const float r = rsqrtf(sum_lanes<S::LANES>(ss) * a.inv_dim + a.eps);
+        const float m = sum_lanes<S::LANES>(xd) * a.inv_dim * r * r;
+        const int h = hb + k * G + group;
+        if (!(l.on() && h < h1)) continue;
+#pragma unroll
+        for (int i = 0; i < 2 * VEC; ++i) {
+          g[i] += d[k][i] * v[k][i] * r;
+          d[k][i] = r * (d[k][i] * w[i] - v[k][i] * m);
+        }
+        l.write(dx + h * out.head, d[k]);
       }
-      l.write(head_of<T>(a.dq, a.dk, a.heads, t, h), d);
     }
   }
 #pragma unroll
   for (int i = 0; i < 2 * VEC; ++i)
 #pragma unroll
-    for (int o = S::LANES; o < 32; o <<= 1) {
-      gq[i] += __shfl_xor_sync(~0u, gq[i], o);
-      gk[i] += __shfl_xor_sync(~0u, gk[i], o);
-    }
-  if (group == 0) {
-    float* row = part + threadIdx.x / 32 * 2 * a.dim;
+    for (int o = S::LANES; o < 32; o <<= 1) g[i] += __shfl_xor_sync(~0u, g[i], o);
+  if (group == 0)
 #pragma unroll
     for (int i = 0; i < VEC; ++i)
       if (l.has(i)) {
-        row[l.lo(i)] = gq[i];
-        row[l.hi(i)] = gq[VEC + i];
-        row[a.dim + l.lo(i)] = gk[i];
-        row[a.dim + l.hi(i)] = gk[VEC + i];
+        row[l.lo(i)] = g[i];
+        row[l.hi(i)] = g[VEC + i];
       }
-  }
+}
+
+template <class T, class S>
+__global__ void __launch_bounds__(kThreads, 2) k_norm_rope_grad(const __grid_constant__ NormArgs a) {
+  extern __shared__ float part[];         // [kWarps][q, k][dim]
+  const S l(a);
+  float* const row = part + threadIdx.x / 32 * 2 * a.dim;
+  gradient_heads<T>(a, l, a.q, a.q_out, a.dq, a.heads, a.q_weight, row);
+  gradient_heads<T>(a, l, a.k, a.k_out, a.dk, a.kv_heads, a.k_weight, row + a.dim);
   __syncthreads();
   for (int e = threadIdx.x; e < 2 * a.dim; e += kThreads) {
     float v = 0.f;
@@ -269,6 +293,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_norm_rope_grad(const __grid_con
     for (int w = 0; w < kWarps; ++w) v += part[w * 2 * a.dim + e];
     a.partial[(int64_t)blockIdx.x * 2 * a.dim + e] = v;
   }
+  let_next_start();
 }
 
 // The blocks' rows summed in a fixed order: a block takes 32 columns, its
@@ -276,6 +301,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_norm_rope_grad(const __grid_con
 template <class T>
 __global__ void __launch_bounds__(1024) k_norm_weights(const __grid_constant__ NormArgs a, int blocks) {
   __shared__ float part[32][33];
+  after_previous();
   const int lane = threadIdx.x % 32, w = threadIdx.x / 32, e = blockIdx.x * 32 + lane;
   float v = 0.f;
   if (e < 2 * a.dim)
@@ -296,26 +322,26 @@ cudaError_t launch(NormArgs a, cudaStream_t st) {
   // per SM are resident, about), in whole rounds of G heads.
   constexpr int G = 32 / S::LANES;
   const int rounds = (a.heads + a.kv_heads + G - 1) / G;
-  const int64_t want = (int64_t)a.num_sms * 32;
-  const int split = (int)std::min<int64_t>(rounds, std::max<int64_t>(1, want / std::max<int64_t>(1, a.rows)));
-  a.per = (rounds + split - 1) / split * G;
-  a.split = (a.heads + a.kv_heads + a.per - 1) / a.per;
-  const int64_t blocks = (a.rows * a.split + kWarps - 1) / kWarps;
+  const int64_t want = (int64_t)a.num_sms * 32 / std::max<int64_t>(1, a.rows);
   if (!a.grad) {
-    if (blocks == 0) return cudaSuccess;
-    k_norm_rope<T, S><<<(unsigned)blocks, kThreads, 0, st>>>(a);
+    if (a.rows == 0) return cudaSuccess;
+    const int split = (int)std::min<int64_t>(rounds, std::max<int64_t>(1, want));
+    a.per = (rounds + split - 1) / split * G;
+    a.split = (a.heads + a.kv_heads + a.per - 1) / a.per;
+    k_norm_rope<T, S><<<(unsigned)((a.rows * a.split + kWarps - 1) / kWarps), kThreads, 0, st>>>(a);
     const cudaError_t e = cudaGetLastError();
     if (e == cudaSuccess) count_launch();
     return e;
   }
+  a.split = (int)std::max<int64_t>(1, std::min<int64_t>(want, rounds));
+  const int64_t blocks = (a.rows * a.split + kWarps - 1) / kWarps;
   const int n = (int)std::min<int64_t>(std::max<int64_t>(1, blocks), norm_blocks(a.num_sms));
   k_norm_rope_grad<T, S><<<n, kThreads, kWarps * 2 * a.dim * sizeof(float), st>>>(a);
   cudaError_t e = cudaGetLastError();
   if (e != cudaSuccess) return e;
   count_launch();
   if (!a.q_weight_grad && !a.k_weight_grad) return cudaSuccess;
-  k_norm_weights<T><<<(2 * a.dim + 31) / 32, 1024, 0, st>>>(a, n);
-  e = cudaGetLastError();
+  e = launch_early(k_norm_weights<T>, (2 * a.dim + 31) / 32, 1024, 0, st, a, n);
   if (e == cudaSuccess) count_launch();
   return e;
 }
