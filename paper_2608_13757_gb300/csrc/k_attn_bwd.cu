@@ -90,9 +90,10 @@ __device__ __forceinline__ void write_row(uint32_t acc, void* row, int c0, int c
       tmem_ld32(acc + c, x);
       wait_ld();
     }
+    uint32_t y[16];
 #pragma unroll
-    for (int e = 0; e < 32; ++e) x[e] = any ? x[e] * by : 0.f;
-    out.write<BF16>(x, c, dim);
+    for (int e = 0; e < 16; ++e) y[e] = any ? pack2<BF16>(x[2 * e] * by, x[2 * e + 1] * by) : 0;
+    out.write(y, 2 * c, 2 * dim);
   }
 }
 

@@ -53,6 +53,10 @@ struct Place {
   }
 };
 
+// Key tiles of an item that query tile t meets, and the first row of its
+// queries: of a dual item both have the first tile's, every other key tile.
+__device__ __forceinline__ int tiles_of(const AttnItem& it, int t) { return it.dual ? (it.n[0] + 1 - t) / 2 : it.n[t]; }
+
 template <int DP>
 struct Layout {
   static constexpr int kTileBytes = DP / 64 * kBlockBytes;
@@ -106,6 +110,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_fwd(const __grid_constant_
     bar_init_visible();
   }
   if (warp == 8) tmem_alloc<kCols>(smem_addr(shared_int));
+  const int i0 = uniform(a.block_first[blockIdx.x]), i1 = uniform(a.block_first[blockIdx.x + 1]);
+  asm volatile("prefetch.global.L1 [%0];" ::"l"(a.item + i0));
   fence_before();
   __syncthreads();
   fence_after();
@@ -113,7 +119,6 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_fwd(const __grid_constant_
 
   const int group = a.heads / a.kv_heads, packed_rows = kTile / group;
   if (threadIdx.x == 0) let_next_start();
-  const int i0 = uniform(a.block_first[blockIdx.x]), i1 = uniform(a.block_first[blockIdx.x + 1]);
 
   if (warp >= 8) {
     regs_down<kRegsFew>();
@@ -156,17 +161,17 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_fwd(const __grid_constant_
 #pragma unroll 1
       for (int i = i0; ok && i < i1; ++i) {
         const AttnItem it = a.item[i];
-        const int packed = uniform(it.packed), row = (int)it.q_row;
+        const int packed = uniform(it.packed), row = (int)it.q_row, apart = it.dual ? 0 : packed ? packed_rows : kTile;
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
-          if (!ok || !uniform(it.n[t])) continue;
+          if (!ok || !uniform(tiles_of(it, t))) continue;
           if (n[t] && !(ok = bar_wait(q_free + 8 * t, (n[t] - 1) & 1, a.error))) continue;
           if (leader) {
             bar_expect(q_full + 8 * t, DP / 64 * (packed ? packed_rows * group : kTile) * 128);
 #pragma unroll
             for (int c = 0; c < DP / 64; ++c)
               tma_load(base + t * L::kTileBytes + c * kBlockBytes, packed ? &qg_map : &q_map, q_full + 8 * t, 64 * c,
-                       it.head, row + t * (packed ? packed_rows : kTile));
+                       it.head, row + t * apart);
           }
           ++n[t];
         }
@@ -195,7 +200,18 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_fwd(const __grid_constant_
         at.next();
         return true;
       };
-      auto run = [&](int n, int all) {                      // n of the item's key tiles are this query tile's
+      auto skip = [&](int tiles) {                          // the other's: let go as they come
+#pragma unroll 1
+        for (int j = 0; j < tiles; ++j, at.next()) {
+          if (!arrived()) return false;
+          bar_arrive_warp(free_ + 8 * at.stage, leader);
+        }
+        return true;
+      };
+      // n of the item's key tiles are this query tile's: the first ones, or of
+      // a dual item every other one
+      auto run = [&](int n, int all, bool dual) {
+        if (dual && t && !skip(2)) return false;
 #pragma unroll 1
         for (int j = 0; j < n; ++j) {
           if (j == 0 && !scores(true, n == 1)) return false;
@@ -211,18 +227,15 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_fwd(const __grid_constant_
             commit(v_free);
             if (j + 1 == n) commit(o_full + 8 * t);
           }
-          if (j + 1 < n && !scores(false, j + 2 == n)) return false;
+          if (j + 1 < n && ((dual && !skip(2)) || !scores(false, j + 2 == n))) return false;
         }
-#pragma unroll 1
-        for (int j = 2 * n; j < 2 * all; ++j, at.next()) {   // the other's: let go as they come
-          if (!arrived()) return false;
-          bar_arrive_warp(free_ + 8 * at.stage, leader);
-        }
-        return true;
+        return skip(2 * (dual ? n && (all + t + 1) % 2 : all - n));
       };
 #pragma unroll 1
-      for (int i = i0; i < i1; ++i)
-        if (!run(uniform(a.item[i].n[t]), uniform(max(a.item[i].n[0], a.item[i].n[1])))) break;
+      for (int i = i0; i < i1; ++i) {
+        const AttnItem* const it = a.item + i;
+        if (!run(uniform(tiles_of(*it, t)), uniform(max(it->n[0], it->n[1])), uniform(it->dual))) break;
+      }
       if (leader) commit(done);
       bar_wait(done, 0, a.error);
     }
@@ -239,22 +252,23 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_fwd(const __grid_constant_
     for (int i = i0; i < i1; ++i) {
       const AttnItem* const at_item = a.item + i;
       if (i + 1 < i1) asm volatile("prefetch.global.L1 [%0];" ::"l"(at_item + 1));
-      const int packed = uniform(at_item->packed), n = uniform(at_item->n[t]), keys = uniform(at_item->keys);
+      const int packed = uniform(at_item->packed), dual = uniform(at_item->dual), keys = uniform(at_item->keys);
+      const int n = uniform(tiles_of(*at_item, t)), tq = dual ? 0 : t;
       const int per = packed ? packed_rows : kTile, rq = packed ? packed_q : r;
-      const int least = uniform(at_item->seen) + t * per;    // keys that the tile's first query sees
+      const int least = uniform(at_item->seen) + tq * per;   // keys that the tile's first query sees
       const int seen_all = min(least + rq, keys);            // and this row
-      const bool valid = rq < at_item->rows[t], busy = __any_sync(~0u, valid);
+      const bool valid = rq < at_item->rows[tq], busy = __any_sync(~0u, valid);
       float m = -INFINITY, l = 0.f;
       bool ok = true;
 #pragma unroll 1
       for (int j = 0; j < n; ++j) {
-        const int k0 = j * kTile;
+        const int g = dual ? 2 * j + t : j, k0 = g * kTile;
         if (!(ok = bar_wait(s_full + 8 * t, sn++ & 1, a.error))) break;
         if (k0 + kTile > keys) {
           // Values past the sequence's end belong to other sequences and may
           // be anything; a zero weight does not hide a NaN, so they are
           // cleared (both query tiles write the same zeros).
-          const uint32_t at = pos + 2 * j + 1, st = at % L::kStages;
+          const uint32_t at = pos + 2 * g + 1, st = at % L::kStages;
           if (!(ok = bar_wait(full + 8 * st, at / L::kStages & 1, a.error))) break;
           uint8_t* v = sm + L::kRing + st * L::kTileBytes;
 #pragma unroll 1
@@ -355,7 +369,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_fwd(const __grid_constant_
       const float by = __fdividef(1.f, l);
       const int slot = uniform(at_item->slot);
       const int head = at_item->head + (packed ? packed_h : 0);
-      const int64_t query = at_item->q_row + t * per + rq;
+      const int64_t query = at_item->q_row + tq * per + rq;
       if (valid) {
         const float lse2 = l == 0.f ? -INFINITY : fmaf(m, c2, __log2f(l));
         if (slot >= 0)
@@ -363,35 +377,27 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_fwd(const __grid_constant_
         else if (a.lse)
           a.lse[head * a.q.rows + query] = lse2 * 0.6931471805599453f;
       }
-      if (slot >= 0) {
-        // A piece of a split key range leaves its rows in 32 bits, scaled by
-        // its own sum: four columns of all rows side by side.
-        float* part = a.part_o + ((int64_t)slot * 2 + t) * kTile * DP + 4 * r;
+      // A piece of a split key range leaves its rows in 32 bits, scaled by its
+      // own sum; whole ranges are done.
+      const bool piece = slot >= 0;
+      const RowWriter out(piece ? reinterpret_cast<uint8_t*>(a.part_o + (((int64_t)slot * 2 + t) * kTile + r) * DP)
+                                : static_cast<uint8_t*>(a.o.data) + 2 * (query * a.o.row + head * a.o.head),
+                          valid);
 #pragma unroll 1
-        for (int c = 0; c < DP; c += 16) {
-          float o[16];
-          __syncwarp();
-          tmem_ld16(O + c, o);
-          wait_ld();
-#pragma unroll
-          for (int e = 0; e < 16; ++e) o[e] = some ? o[e] * by : 0.f;
-          if (valid)
-#pragma unroll
-            for (int e = 0; e < 16; e += 4)
-              *reinterpret_cast<float4*>(part + (c + e) * kTile) = make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
-        }
-        continue;
-      }
-      RowWriter out(static_cast<uint8_t*>(a.o.data) + 2 * (query * a.o.row + head * a.o.head), valid);
-#pragma unroll 1
-      for (int c = 0; c < DP; c += 32) {
+      for (int c = 0; c < DP; c += piece ? 16 : 32) {
         float o[32];
+        uint32_t y[16];
         __syncwarp();
-        tmem_ld32(O + c, o);
+        tmem_ld32(O + min(c, DP - 32), o);
         wait_ld();
+        if (piece) {                                         // (the last 16 columns come in the upper half)
 #pragma unroll
-        for (int e = 0; e < 32; ++e) o[e] = some ? o[e] * by : 0.f;
-        out.write<BF16>(o, c, a.dim);
+          for (int e = 0; e < 16; ++e) y[e] = some ? __float_as_uint(o[c > DP - 32 ? e + 16 : e] * by) : 0;
+        } else {
+#pragma unroll
+          for (int e = 0; e < 16; ++e) y[e] = some ? pack2<BF16>(o[2 * e] * by, o[2 * e + 1] * by) : 0;
+        }
+        out.write(y, piece ? 4 * c : 2 * c, piece ? 4 * DP : 2 * a.dim);
       }
     }
   }
@@ -412,19 +418,21 @@ __global__ void __launch_bounds__(256) k_attn_merge(const __grid_constant__ Attn
   const int n0 = s.rows[0] * heads, t = row >= n0;
   if (t) row -= n0;
   if (row >= s.rows[t] * heads) return;
+  // both results of a dual piece are of the first tile
+  const int pieces = s.dual ? 2 * s.pieces : s.pieces, apart = s.dual ? 1 : 2;
   const float* lse = a.part_lse + ((int64_t)s.slot * 2 + t) * kTile + row;
-  const float* part = a.part_o + ((int64_t)s.slot * 2 + t) * kTile * DP + lane % (DP / 4) * 4 * kTile + row * 4;
+  const float* part = a.part_o + (((int64_t)s.slot * 2 + t) * kTile + row) * DP + lane % (DP / 4) * 4;
   float top = -INFINITY;
-  for (int k = lane; k < s.pieces; k += 32) top = fmaxf(top, lse[(int64_t)k * 2 * kTile]);
+  for (int k = lane; k < pieces; k += 32) top = fmaxf(top, lse[(int64_t)k * apart * kTile]);
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, o));
   const float from = top == -INFINITY ? 0.f : top;
   float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
   float sum = 0.f;
 #pragma unroll 8
-  for (int k = 0; k < s.pieces; ++k) {
-    const float f = exp2_fast(lse[(int64_t)k * 2 * kTile] - from);
-    const float4 x = *reinterpret_cast<const float4*>(part + (int64_t)k * 2 * kTile * DP);
+  for (int k = 0; k < pieces; ++k) {
+    const float f = exp2_fast(lse[(int64_t)k * apart * kTile] - from);
+    const float4 x = *reinterpret_cast<const float4*>(part + (int64_t)k * apart * kTile * DP);
     sum += f;
     acc.x = fmaf(f, x.x, acc.x);
     acc.y = fmaf(f, x.y, acc.y);

@@ -263,10 +263,10 @@ __device__ __forceinline__ float2 unpack2(uint32_t r) {
   return f;
 }
 
-// Writes 128-row tiles whose rows lie one per lane, 32 columns at a time: four
-// lanes exchange their 16-byte pieces so that a store takes 64 bytes of 8 rows
-// instead of 16 bytes of 32.  (Those took some 5000 cycles per tile of 128
-// columns; these take 1000.)
+// Writes tiles whose rows lie one per lane, 64 bytes of each row at a time:
+// four lanes exchange their 16-byte pieces so that a store takes 64 bytes of 8
+// rows instead of 16 bytes of 32.  (Those took some 5000 cycles per tile of
+// 128 columns; these take 1000.)
 struct RowWriter {
   uint8_t* row[4];     // this lane's piece of the four rows of its group of lanes
   bool on[4];
@@ -279,12 +279,12 @@ struct RowWriter {
       on[e] = __shfl_sync(~0u, (int)valid, from);
     }
   }
-  template <bool BF16>
-  __device__ __forceinline__ void write(const float* x, int c, int dim) const {
+  // 16 words of this lane's row, from byte `at` of the row on; the row has `bytes`
+  __device__ __forceinline__ void write(const uint32_t* x, int at, int bytes) const {
     const int lane = threadIdx.x % 32;
     uint32_t v[4][4];                                        // piece, word
 #pragma unroll
-    for (int e = 0; e < 16; ++e) v[e / 4][e % 4] = pack2<BF16>(x[2 * e], x[2 * e + 1]);
+    for (int e = 0; e < 16; ++e) v[e / 4][e % 4] = x[e];
 #pragma unroll
     for (int bit = 2; bit; bit >>= 1)                        // lane i, piece j  <->  lane j, piece i
 #pragma unroll
@@ -300,7 +300,7 @@ struct RowWriter {
       }
 #pragma unroll
     for (int e = 0; e < 4; ++e)
-      if (on[e] && c + lane % 4 * 8 < dim) *reinterpret_cast<uint4*>(row[e] + 2 * c) = make_uint4(v[e][0], v[e][1], v[e][2], v[e][3]);
+      if (on[e] && at + lane % 4 * 16 < bytes) *reinterpret_cast<uint4*>(row[e] + at) = make_uint4(v[e][0], v[e][1], v[e][2], v[e][3]);
   }
 };
 
