@@ -249,11 +249,6 @@ struct ForwardWork {
 // key tiles that its query tiles meet and kItemCost for what it does besides
 // (a tile of one query tile takes about 0.8 us, an item's start and end 1.5).
 constexpr int64_t kItemCost = 4, kMinPiece = 2;
-// A query tile without a second one keeps half the block idle and waits for
-// each key tile's products; with this many key tiles in a block's share it pays
-// to let both halves take it, every other key tile each, and merge their
-// results.
-constexpr int kDualTiles = 4;
 
 template <class T>
 struct Draft {
@@ -293,7 +288,6 @@ ForwardWork forward_work(const sync_attn_desc* d, const std::vector<AttnSeq>& se
   const int group = d->heads / d->kv_heads;
   std::vector<Draft<AttnItem>> draft;
   int64_t total = 0;
-  bool dual = false;
   for (const AttnSeq& s : seq) {
     const bool packed = packs(s, group);
     const int32_t per = packed ? kTile / group : kTile;
@@ -316,33 +310,17 @@ ForwardWork forward_work(const sync_attn_desc* d, const std::vector<AttnSeq>& se
         total += draft.back().cost;
       }
   }
-  for (Draft<AttnItem>& x : draft) {
-    x.it.dual = x.it.rows[1] == 0 && std::min<int64_t>(x.it.n[0], total / num_sms) >= kDualTiles;
-    dual |= x.it.dual;
-  }
   ForwardWork w;
   std::vector<Draft<AttnItem>> whole = draft;
   const int64_t most = assign(whole, num_sms, w.item, w.block_first);
   const int64_t share = std::max((total + kItemCost * num_sms) / num_sms + 1, kMinPiece + kItemCost);
-  auto add_split = [&](AttnItem& it, int32_t slot, int32_t pieces) {
-    it.slot = slot;
-    w.split.push_back({it.q_row, it.head, it.packed, {it.rows[0], it.rows[1]}, slot, pieces, it.dual});
-    w.merge_rows = std::max(w.merge_rows, (it.rows[0] + it.rows[1]) * (it.packed ? group : 1));
-  };
   // Whole items balance well where there are many.  Where the fullest block
   // has 1/16 more than its share, the items are laid end to end and cut into
   // equal shares: an item that crosses a cut is split along its keys, and its
   // pieces' results are merged.  (At most one cut per block: split results
   // cost a write and a read in 32 bits.)
-  const bool balanced = most <= share + share / 16;
-  if (balanced && !dual) return w;
+  if (most <= share + share / 16) return w;
   w = ForwardWork{};
-  if (balanced) {                                              // whole items, the dual ones with their two results
-    for (Draft<AttnItem>& x : draft)
-      if (x.it.dual) add_split(x.it, w.slots++, 1);
-    assign(draft, num_sms, w.item, w.block_first);
-    return w;
-  }
   w.block_first.push_back(0);
   int64_t room = share;
   auto next_block = [&] {
@@ -378,7 +356,7 @@ ForwardWork forward_work(const sync_attn_desc* d, const std::vector<AttnSeq>& se
       it.seen -= from * kTile;
       it.keys -= from * kTile;
       for (int t = 0; t < 2; ++t) it.n[t] = std::max(0, std::min(x.it.n[t], to) - from);
-      const bool split = from > 0 || to < n || it.dual;
+      const bool split = from > 0 || to < n;
       if (split) it.slot = w.slots++;
       pieces += split;
       room -= cost(from, to);
@@ -387,8 +365,9 @@ ForwardWork forward_work(const sync_attn_desc* d, const std::vector<AttnSeq>& se
       from = to;
       if (to == n) break;
     }
-    AttnItem it = x.it;
-    if (pieces) add_split(it, slot0, pieces);
+    if (!pieces) continue;
+    w.split.push_back({x.it.q_row, x.it.head, x.it.packed, {x.it.rows[0], x.it.rows[1]}, slot0, pieces});
+    w.merge_rows = std::max(w.merge_rows, (x.it.rows[0] + x.it.rows[1]) * (x.it.packed ? group : 1));
   }
   w.block_first.push_back((int32_t)w.item.size());
   while (w.block_first.size() > 2 && w.block_first[w.block_first.size() - 2] == w.block_first.back()) w.block_first.pop_back();

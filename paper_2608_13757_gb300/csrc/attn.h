@@ -27,15 +27,13 @@ struct alignas(64) AttnItem {
   int32_t n[2];                    // key tiles that each meets
   int32_t seen;                    // keys of the range that the first query sees (may be negative); the next sees one more
   int32_t keys;                    // keys of the sequence from k_row on
-  int32_t dual;                    // 1: only the first tile has rows, and both halves of the block take it: the
-                                   // first the even key tiles, the second the odd ones
   int32_t slot;                    // where a piece of a split range leaves its result; -1: the range is whole
 };
 
 // A split key range: its pieces' results are at slot, slot + 1, ...
 struct AttnSplit {
   int64_t q_row;
-  int32_t head, packed, rows[2], slot, pieces, dual;
+  int32_t head, packed, rows[2], slot, pieces;
 };
 
 // A gradient item.  Key walk: a key tile of a key head against n query tiles

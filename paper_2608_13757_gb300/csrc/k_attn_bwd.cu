@@ -86,10 +86,8 @@ __device__ __forceinline__ void write_row(uint32_t acc, void* row, int c0, int c
   for (int c = c0; c < c1; c += 32) {
     float x[32];
     __syncwarp();
-    if (any) {
-      tmem_ld32(acc + c, x);
-      wait_ld();
-    }
+    tmem_ld32(acc + c, x);
+    wait_ld();
     uint32_t y[16];
 #pragma unroll
     for (int e = 0; e < 16; ++e) y[e] = any ? pack2<BF16>(x[2 * e] * by, x[2 * e + 1] * by) : 0;
@@ -116,7 +114,9 @@ struct Loader {
   const Bars<DP>& b;
   int* error;
   bool leader;
-  uint32_t pos = 0, fixed = 0;
+  Place<L::kStages> at;
+  bool first = true;             // of the ring, whose places are free
+  uint32_t fixed = 0;
   __device__ __forceinline__ void tile(uint32_t dst, const CUtensorMap* map, uint32_t bar, int head, int row) {
 #pragma unroll
     for (int c = 0; c < DP / 64; ++c) tma_load(dst + c * kBlockBytes, map, bar, 64 * c, head, row);
@@ -131,23 +131,110 @@ struct Loader {
     ++fixed;
     return true;
   }
-  __device__ __forceinline__ bool next(const CUtensorMap* map, int head, int row) {
-    const uint32_t st = pos % L::kStages;
-    if (pos >= L::kStages && !bar_wait(b.free_ + 8 * st, (pos / L::kStages - 1) & 1, error)) return false;
-    if (leader) {
-      bar_expect(b.full + 8 * st, L::kTileBytes);
-      tile(base + L::kRing + st * L::kTileBytes, map, b.full + 8 * st, head, row);
+  // n rows of tiles from `row` on, of two tensors in turn
+  __device__ __forceinline__ bool pairs(const CUtensorMap* m0, const CUtensorMap* m1, int head, int row, int n) {
+#pragma unroll 1
+    for (int j = 0; j < 2 * n; ++j) {
+      if (!first && !bar_wait(b.free_ + 8 * at.stage, at.parity ^ 1, error)) return false;
+      const uint32_t bar = b.full + 8 * at.stage;
+      if (leader) {
+        bar_expect(bar, L::kTileBytes);
+        tile(base + L::kRing + at.stage * L::kTileBytes, j % 2 ? m1 : m0, bar, head, row + j / 2 * kTile);
+      }
+      at.next();
+      first = first && at.stage;
     }
-    ++pos;
     return true;
   }
   __device__ __forceinline__ void finish() {                // nothing is in flight when the block ends
 #pragma unroll 1
-    for (uint32_t i = pos > L::kStages ? pos - L::kStages : 0; i < pos; ++i)
-      bar_wait(b.full + 8 * (i % L::kStages), i / L::kStages & 1, error);
+    for (uint32_t i = 0; i < L::kStages; ++i)
+      if (!first || i < at.stage) bar_wait(b.full + 8 * i, at.parity ^ (i >= at.stage), error);
     if (fixed) bar_wait(b.fixed_full, (fixed - 1) & 1, error);
   }
 };
+
+// Products of one block, by one warp, in the order of its ring of tiles.
+template <int DP, bool BF16>
+struct Products {
+  using L = Layout<DP>;
+  uint32_t ring, tmem;
+  const Bars<DP>& b;
+  int* error;
+  bool leader;
+  int ksteps;
+  uint32_t i_s, i_o;
+  Place<L::kStages> at;          // of the next tile
+  __device__ __forceinline__ Products(uint32_t base, uint32_t tmem, const Bars<DP>& b, int* error, int dim)
+      : ring(tile_desc(base + L::kRing)), tmem(tmem), b(b), error(error), leader(elect_one()), ksteps((dim + 15) / 16),
+        i_s(instr(BF16, kTile, false)), i_o(instr(BF16, ksteps * 16, true)) {}
+  __device__ __forceinline__ uint32_t tile(uint32_t stage) const { return ring + stage * (L::kTileBytes >> 4); }
+  __device__ __forceinline__ void done_with(uint32_t bar) const {
+    if (leader) commit(bar);
+  }
+  __device__ __forceinline__ void release(uint32_t stage) const { done_with(b.free_ + 8 * stage); }
+  __device__ __forceinline__ bool wait(uint32_t bar, uint32_t n) const {
+    const bool ok = bar_wait(bar, n & 1, error);
+    fence_after();
+    return ok;
+  }
+  // d = x y^T with the next tile y, whose stage it returns
+  __device__ __forceinline__ bool across(uint32_t d, uint32_t x, uint32_t bar, uint32_t& stage) {
+    if (!wait(b.full + 8 * at.stage, at.parity)) return false;
+    stage = at.stage;
+    if (leader) {
+      mma_along(tmem + d, x, tile(stage), i_s, ksteps);
+      commit(bar);
+    }
+    at.next();
+    return true;
+  }
+  // d (+)= x y with x of 128 columns in two runs of 64, each in its first 32 words
+  __device__ __forceinline__ void gradient(uint32_t d, uint32_t x, uint32_t stage, bool add) const {
+    if (!leader) return;
+#pragma unroll 1
+    for (int e = 0; e < 2; ++e) mma_rows(tmem + d, tmem + x + 64 * e, tile(stage) + step_rows(4 * e), i_o, add || e);
+  }
+};
+
+// Weights of 64 scores, exp2(s c2 - lse2), in place, with lse2 negated: one
+// value, or one for each column.
+__device__ __forceinline__ void weights(float* p, float c2, const float* minus_lse, bool by_column) {
+  const uint64_t c22 = pair_bits(c2, c2), all = pair_bits(*minus_lse, *minus_lse);
+#pragma unroll
+  for (int e = 0; e < 64; e += 4) {
+    ulonglong2 l = make_ulonglong2(all, all);
+    if (by_column) l = *reinterpret_cast<const ulonglong2*>(minus_lse + e);
+    pair_split(fma2(pair_bits(p[e], p[e + 1]), c22, l.x), p[e], p[e + 1]);
+    pair_split(fma2(pair_bits(p[e + 2], p[e + 3]), c22, l.y), p[e + 2], p[e + 3]);
+#pragma unroll
+    for (int f = 0; f < 4; ++f) p[e + f] = exp2_fast(p[e + f]);
+  }
+}
+// Their gradients p (d - delta), into d, with delta negated.
+__device__ __forceinline__ void weight_gradients(float* d, const float* p, const float* minus_delta, bool by_column) {
+  const uint64_t all = pair_bits(*minus_delta, *minus_delta);
+#pragma unroll
+  for (int e = 0; e < 64; e += 4) {
+    ulonglong2 l = make_ulonglong2(all, all);
+    if (by_column) l = *reinterpret_cast<const ulonglong2*>(minus_delta + e);
+    pair_split(mul2(pair_bits(p[e], p[e + 1]), add2(pair_bits(d[e], d[e + 1]), l.x)), d[e], d[e + 1]);
+    pair_split(mul2(pair_bits(p[e + 2], p[e + 3]), add2(pair_bits(d[e + 2], d[e + 3]), l.y)), d[e + 2], d[e + 3]);
+  }
+}
+// 64 values rounded to 16 bits, to tensor memory.
+template <bool BF16>
+__device__ __forceinline__ void put(uint32_t addr, const float* x) {
+  uint32_t y[32];
+#pragma unroll
+  for (int e = 0; e < 32; ++e) y[e] = pack2<BF16>(x[2 * e], x[2 * e + 1]);
+  tmem_st32(addr, y);
+}
+__device__ __forceinline__ void get(uint32_t addr, float* x) {
+  tmem_ld32(addr, x);
+  tmem_ld32(addr + 32, x + 32);
+  wait_ld();
+}
 
 template <int DP, bool BF16>
 __global__ void __launch_bounds__(kThreads, 1) k_attn_dkv(const __grid_constant__ AttnArgs a,
@@ -163,22 +250,20 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dkv(const __grid_constant_
   int* const shared_int = reinterpret_cast<int*>(sm + L::kInts);
   const int warp = uniform(threadIdx.x / 32);
   if (!swizzle_aligned(base, a.error)) return;
-  if (threadIdx.x == 0) {
-    b.init();
-  }
+  if (threadIdx.x == 0) b.init();
   if (warp == 9) tmem_alloc<512>(smem_addr(shared_int));
+  const int group = a.heads / a.kv_heads;
+  const int i0 = uniform(a.k_first[blockIdx.x]), i1 = uniform(a.k_first[blockIdx.x + 1]);
+  asm volatile("prefetch.global.L1 [%0];" ::"l"(a.k_tile + i0));
   fence_before();
   __syncthreads();
   fence_after();
   const uint32_t tmem = (uint32_t)shared_int[0];
-  const int group = a.heads / a.kv_heads;
-  const int i0 = uniform(a.k_first[blockIdx.x]), i1 = uniform(a.k_first[blockIdx.x + 1]);
 
   if (warp >= 8) {
     regs_down<kRegsFew>();
-    const bool leader = elect_one();
     if (warp == 8) {                                        // ---- loads
-      Loader<DP> load{base, b, a.error, leader};
+      Loader<DP> load{base, b, a.error, elect_one()};
       bool ok = true;
 #pragma unroll 1
       for (int i = i0; ok && i < i1; ++i) {
@@ -187,66 +272,39 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dkv(const __grid_constant_
         if (!n) continue;
         ok = load.stay(&k_map, &v_map, head, (int)it.k_row);
 #pragma unroll 1
-        for (int h = head * group; ok && h < (head + 1) * group; ++h)
-#pragma unroll 1
-          for (int t = 0; ok && t < n; ++t)
-            ok = load.next(&q_map, h, (int)it.q_row + t * kTile) && load.next(&do_map, h, (int)it.q_row + t * kTile);
+        for (int h = head * group; ok && h < (head + 1) * group; ++h) ok = load.pairs(&q_map, &do_map, h, (int)it.q_row, n);
       }
       load.finish();
     } else if (warp == 9) {                                 // ---- products
-      const int ksteps = (a.dim + 15) / 16;
-      const uint32_t i_s = instr(BF16, kTile, false), i_o = instr(BF16, ksteps * 16, true);
-      uint32_t pos = 0, fixed = 0, n = 0;                    // n: steps so far
-      auto tile = [&](uint32_t at) { return tile_desc(base + L::kRing + at % L::kStages * L::kTileBytes); };
-      auto arrived = [&](uint32_t at) { return bar_wait(b.full + 8 * (at % L::kStages), at / L::kStages & 1, a.error); };
-      auto done_with = [&](uint32_t bar) {
-        if (leader) commit(bar);
-      };
-      auto release = [&](uint32_t at) { done_with(b.free_ + 8 * (at % L::kStages)); };
-      auto across = [&](uint32_t d, uint32_t x, uint32_t at) {       // keys by queries
-        const uint32_t y = tile(at);
-        if (leader) mma_along(tmem + d, x, y, i_s, ksteps);
-      };
-      auto gradient = [&](uint32_t d, uint32_t x, uint32_t at, bool add) {
-        const uint32_t y = tile(at);
-        if (leader) {
-          mma_rows(tmem + d, tmem + x, y, i_o, add);
-          mma_rows(tmem + d, tmem + x + 64, y + step_rows(4), i_o, true);
-        }
-      };
+      Products<DP, BF16> m(base, tmem, b, a.error, a.dim);
       const uint32_t K = tile_desc(base), V = tile_desc(base + L::kTileBytes);
+      uint32_t fixed = 0, n = 0;                            // n: steps so far
+      // The scores and dO V^T of step j + 1 each follow the gradient product
+      // of step j that reads what they overwrite.
       auto run = [&](int steps) {
-        if (!bar_wait(b.fixed_full, fixed++ & 1, a.error) || !arrived(pos)) return false;
-        fence_after();
-        across(kS, K, pos);
-        done_with(b.s_full);
-        if (!arrived(pos + 1)) return false;
-        across(kDp, V, pos + 1);
-        done_with(b.dp_full);
-        if (steps == 1) done_with(b.fixed_free);
+        uint32_t q[2], g[2];                                // stages of Q and dO of this step and the next
 #pragma unroll 1
-        for (int j = 0; j < steps; ++j, pos += 2, ++n) {
-          if (!bar_wait(b.p_ready, n & 1, a.error)) return false;
-          fence_after();
-          gradient(kDv, kS, pos + 1, j > 0);
-          release(pos + 1);
-          if (j + 1 < steps) {
-            if (!arrived(pos + 2)) return false;
-            across(kS, K, pos + 2);
-            done_with(b.s_full);
+        for (int j = -1; j < steps; ++j) {
+          const bool more = j + 1 < steps;
+          if (j < 0) {
+            if (!m.wait(b.fixed_full, fixed++)) return false;
+          } else {
+            if (!m.wait(b.p_ready, n)) return false;
+            m.gradient(kDv, kS, g[0], j > 0);
+            m.release(g[0]);
           }
-          if (!bar_wait(b.ds_ready, n & 1, a.error)) return false;
-          fence_after();
-          gradient(kDk, kDp, pos, j > 0);
-          release(pos);
-          if (j + 1 < steps) {
-            if (!arrived(pos + 3)) return false;
-            across(kDp, V, pos + 3);
-            done_with(b.dp_full);
-            if (j + 2 == steps) done_with(b.fixed_free);
+          if (more && !m.across(kS, K, b.s_full, q[1])) return false;
+          if (j >= 0) {
+            if (!m.wait(b.ds_ready, n++)) return false;
+            m.gradient(kDk, kDp, q[0], j > 0);
+            m.release(q[0]);
           }
+          if (more && !m.across(kDp, V, b.dp_full, g[1])) return false;
+          if (j + 2 == steps) m.done_with(b.fixed_free);
+          q[0] = q[1];
+          g[0] = g[1];
         }
-        done_with(b.out_full);
+        m.done_with(b.out_full);
         return true;
       };
 #pragma unroll 1
@@ -254,40 +312,44 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dkv(const __grid_constant_
         const int steps = uniform(a.k_tile[i].n) * group;
         if (steps && !run(steps)) break;
       }
-      done_with(b.done);
+      m.done_with(b.done);
       bar_wait(b.done, 0, a.error);
-    } else if (warp == 10) {                                // ---- lse and delta of the query tiles
+    } else if (warp == 10) {                                // ---- lse and delta of the query tiles, negated
       const int lane = threadIdx.x % 32;
-      uint32_t n = 0;
-      bool ok = true;
+      const bool leader = elect_one();
+      Place<L::kStatStages> at;
+      bool ok = true, first = true;
       after_previous();                                      // delta is there
       let_next_start();
 #pragma unroll 1
       for (int i = i0; ok && i < i1; ++i) {
         const AttnTile it = a.k_tile[i];
-        const int tiles = uniform(it.n), head = uniform(it.head);
+        const int tiles = uniform(it.n), head = uniform(it.head), steps = tiles * group;
+        int t = 0, h = head * group;
 #pragma unroll 1
-        for (int h = head * group; ok && h < (head + 1) * group; ++h)
-#pragma unroll 1
-          for (int t = 0; t < tiles; ++t, ++n) {
-            const uint32_t st = n % L::kStatStages;
-            float lse[4], delta[4];
+        for (int j = 0; j < steps; ++j) {
+          float lse[4], delta[4];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const int q = t * kTile + lane + 32 * e;
-              lse[e] = q < it.rows ? __ldg(a.lse + h * a.q.rows + it.q_row + q) * kLog2e : -INFINITY;
-              delta[e] = q < it.rows ? a.delta[h * a.delta_rows + it.q_row + q] : 0.f;
-              if (lse[e] == -INFINITY) lse[e] = INFINITY;    // no weight for a row that sees nothing
-            }
-            if (n >= L::kStatStages && !(ok = bar_wait(b.stat_free + 8 * st, (n / L::kStatStages - 1) & 1, a.error))) break;
-            float* at = reinterpret_cast<float*>(sm + L::kStats + st * L::kStatBytes);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              at[lane + 32 * e] = lse[e];
-              at[kTile + lane + 32 * e] = delta[e];
-            }
-            bar_arrive_warp(b.stat_full + 8 * st, leader);
+          for (int e = 0; e < 4; ++e) {
+            const int q = t * kTile + lane + 32 * e;
+            lse[e] = q < it.rows ? __ldg(a.lse + h * a.q.rows + it.q_row + q) * kLog2e : -INFINITY;
+            delta[e] = q < it.rows ? a.delta[h * a.delta_rows + it.q_row + q] : 0.f;
           }
+          if (!first && !(ok = bar_wait(b.stat_free + 8 * at.stage, at.parity ^ 1, a.error))) break;
+          float* to = reinterpret_cast<float*>(sm + L::kStats + at.stage * L::kStatBytes);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            to[lane + 32 * e] = lse[e] == -INFINITY ? -INFINITY : -lse[e];    // no weight for a row that sees nothing
+            to[kTile + lane + 32 * e] = -delta[e];
+          }
+          bar_arrive_warp(b.stat_full + 8 * at.stage, leader);
+          at.next();
+          first = first && at.stage;
+          if (++t == tiles) {
+            t = 0;
+            ++h;
+          }
+        }
       }
     }
   } else {                                                  // ---- arithmetic: a key per lane, 64 queries
@@ -297,7 +359,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dkv(const __grid_constant_
     const uint32_t lanes = (uint32_t)(warp % 4 * 32) << 16;
     const uint32_t S = tmem + lanes + kS + c0, Dp = tmem + lanes + kDp + c0;
     const float c2 = a.scale * kLog2e;
-    uint32_t n = 0, pos = 0, items = 0;
+    Place<L::kStages> at;
+    Place<L::kStatStages> st;
+    uint32_t n = 0, items = 0;
 #pragma unroll 1
     for (int i = i0; i < i1; ++i) {
       const AttnTile it = a.k_tile[i];
@@ -306,73 +370,42 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dkv(const __grid_constant_
       bool ok = true;
       int t = 0;
 #pragma unroll 1
-      for (int j = 0; j < steps; ++j, ++n, pos += 2) {
-        const uint32_t st = n % L::kStatStages;
-        const float* stat = reinterpret_cast<const float*>(sm + L::kStats + st * L::kStatBytes) + c0;
+      for (int j = 0; j < steps; ++j, ++n) {
+        const float* stat = reinterpret_cast<const float*>(sm + L::kStats + st.stage * L::kStatBytes) + c0;
         // queries [from, to) of this half see the key
-        const int q0 = t * kTile, rows = queries - q0;
-        const int from = r + 1 - first_seen - q0 - c0, to = rows - c0;
+        const int q0 = t * kTile, rows = queries - q0, from = r + 1 - first_seen - q0 - c0, to = rows - c0;
         const bool tail = rows < kTile, masked = first_seen + q0 < kTile || tail;
+        const uint32_t q_stage = at.stage;
+        at.next();
         t = t + 1 < tiles ? t + 1 : 0;
-        float p[64];
-        if (!(ok = bar_wait(b.stat_full + 8 * st, n / L::kStatStages & 1, a.error) && bar_wait(b.s_full, n & 1, a.error))) break;
+        if (!(ok = bar_wait(b.stat_full + 8 * st.stage, st.parity, a.error) && bar_wait(b.s_full, n & 1, a.error))) break;
         fence_after();
-        tmem_ld32(S, p);
-        tmem_ld32(S + 32, p + 32);
-        wait_ld();
-#pragma unroll
-        for (int e = 0; e < 64; e += 4) {
-          const float4 l = *reinterpret_cast<const float4*>(stat + e);
-          p[e] = exp2_fast(fmaf(p[e], c2, -l.x));
-          p[e + 1] = exp2_fast(fmaf(p[e + 1], c2, -l.y));
-          p[e + 2] = exp2_fast(fmaf(p[e + 2], c2, -l.z));
-          p[e + 3] = exp2_fast(fmaf(p[e + 3], c2, -l.w));
-        }
-        if (masked)
-#pragma unroll
-          for (int e = 0; e < 64; ++e) p[e] = e >= from && e < to ? p[e] : 0.f;
-        {
-          uint32_t y[32];
-#pragma unroll
-          for (int e = 0; e < 32; ++e) y[e] = pack2<BF16>(p[2 * e], p[2 * e + 1]);
-          tmem_st32(S, y);
-        }
+        if (masked) keep(S, 64, from, to, -INFINITY);
+        float p[64];
+        get(S, p);
+        weights(p, c2, stat, true);
+        put<BF16>(S, p);
         if (tail) {
-          const uint32_t at = pos + 1, sg = at % L::kStages;
-          if (!(ok = bar_wait(b.full + 8 * sg, at / L::kStages & 1, a.error))) break;
-          clear_rows<DP>(sm + L::kRing + sg * L::kTileBytes, rows);
+          if (!(ok = bar_wait(b.full + 8 * at.stage, at.parity, a.error))) break;
+          clear_rows<DP>(sm + L::kRing + at.stage * L::kTileBytes, rows);
+          clear_rows<DP>(sm + L::kRing + q_stage * L::kTileBytes, rows);     // there since S is
         }
         wait_st();
         fence_before();
         bar_arrive_warp(b.p_ready, leader);
         if (!(ok = bar_wait(b.dp_full, n & 1, a.error))) break;
         fence_after();
+        if (tail) keep(Dp, 64, 0, to, 0.f);                   // of rows that may be anything
         float d[64];
-        tmem_ld32(Dp, d);
-        tmem_ld32(Dp + 32, d + 32);
-        wait_ld();
-#pragma unroll
-        for (int e = 0; e < 64; e += 4) {
-          const float4 l = *reinterpret_cast<const float4*>(stat + kTile + e);
-          d[e] = p[e] * (d[e] - l.x);
-          d[e + 1] = p[e + 1] * (d[e + 1] - l.y);
-          d[e + 2] = p[e + 2] * (d[e + 2] - l.z);
-          d[e + 3] = p[e + 3] * (d[e + 3] - l.w);
-        }
-        if (masked)
-#pragma unroll
-          for (int e = 0; e < 64; ++e) d[e] = e >= from && e < to ? d[e] : 0.f;
-        {
-          uint32_t y[32];
-#pragma unroll
-          for (int e = 0; e < 32; ++e) y[e] = pack2<BF16>(d[2 * e], d[2 * e + 1]);
-          tmem_st32(Dp, y);
-        }
-        if (tail) clear_rows<DP>(sm + L::kRing + pos % L::kStages * L::kTileBytes, rows);   // there since S is
+        get(Dp, d);
+        weight_gradients(d, p, stat + kTile, true);
+        put<BF16>(Dp, d);
         wait_st();
         fence_before();
         bar_arrive_warp(b.ds_ready, leader);
-        bar_arrive_warp(b.stat_free + 8 * st, leader);
+        bar_arrive_warp(b.stat_free + 8 * st.stage, leader);
+        at.next();
+        st.next();
       }
       if (!ok) break;
       if (steps) {
@@ -404,91 +437,62 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dq(const __grid_constant__
   int* const shared_int = reinterpret_cast<int*>(sm + L::kInts);
   const int warp = uniform(threadIdx.x / 32);
   if (!swizzle_aligned(base, a.error)) return;
-  if (threadIdx.x == 0) {
-    b.init();
-  }
+  if (threadIdx.x == 0) b.init();
   if (warp == 9) tmem_alloc<512>(smem_addr(shared_int));
+  const int group = a.heads / a.kv_heads;
+  const int i0 = uniform(a.q_first[blockIdx.x]), i1 = uniform(a.q_first[blockIdx.x + 1]);
+  asm volatile("prefetch.global.L1 [%0];" ::"l"(a.q_tile + i0));
   fence_before();
   __syncthreads();
   fence_after();
   const uint32_t tmem = (uint32_t)shared_int[0];
-  const int group = a.heads / a.kv_heads;
-  const int i0 = uniform(a.q_first[blockIdx.x]), i1 = uniform(a.q_first[blockIdx.x + 1]);
 
   if (warp >= 8) {
     regs_down<kRegsFew>();
-    const bool leader = elect_one();
     if (warp == 8) {                                        // ---- loads
-      Loader<DP> load{base, b, a.error, leader};
+      Loader<DP> load{base, b, a.error, elect_one()};
       bool ok = true;
 #pragma unroll 1
       for (int i = i0; ok && i < i1; ++i) {
         const AttnTile it = a.q_tile[i];
         const int n = uniform(it.n);
         if (!n) continue;
-        ok = load.stay(&q_map, &do_map, it.head, (int)it.q_row);
-#pragma unroll 1
-        for (int j = 0; ok && j < n; ++j)
-          ok = load.next(&k_map, it.head / group, (int)it.k_row + j * kTile) &&
-               load.next(&v_map, it.head / group, (int)it.k_row + j * kTile);
+        ok = load.stay(&q_map, &do_map, it.head, (int)it.q_row) && load.pairs(&k_map, &v_map, it.head / group, (int)it.k_row, n);
       }
       load.finish();
     } else if (warp == 9) {                                 // ---- products
-      const int ksteps = (a.dim + 15) / 16;
-      const uint32_t i_s = instr(BF16, kTile, false), i_o = instr(BF16, ksteps * 16, true);
-      uint32_t pos = 0, fixed = 0, n = 0;
-      auto tile = [&](uint32_t at) { return tile_desc(base + L::kRing + at % L::kStages * L::kTileBytes); };
-      auto arrived = [&](uint32_t at) { return bar_wait(b.full + 8 * (at % L::kStages), at / L::kStages & 1, a.error); };
-      auto done_with = [&](uint32_t bar) {
-        if (leader) commit(bar);
-      };
-      auto release = [&](uint32_t at) { done_with(b.free_ + 8 * (at % L::kStages)); };
+      Products<DP, BF16> m(base, tmem, b, a.error, a.dim);
       const uint32_t Q = tile_desc(base), dO = tile_desc(base + L::kTileBytes);
-      auto across = [&](uint32_t d, uint32_t x, uint32_t at) {       // queries by keys
-        const uint32_t y = tile(at);
-        if (leader) mma_along(tmem + d, x, y, i_s, ksteps);
-      };
-      auto scores = [&](uint32_t step, uint32_t at) {
-        across(kS + step % 2 * 128, Q, at);
-        done_with(b.s_full + 8 * (step % 2));
-      };
+      uint32_t fixed = 0, n = 0;
+      // dS replaces the scores in their buffer.  dO V^T of step j + 1 follows
+      // as soon as step j's is in registers, the scores of step j + 2 when the
+      // product with dS of step j is done with their buffer.
       auto run = [&](int steps) {
-        if (!bar_wait(b.fixed_full, fixed++ & 1, a.error) || !arrived(pos)) return false;
-        fence_after();
-        scores(n, pos);
-        if (!arrived(pos + 1)) return false;
-        across(kDp, dO, pos + 1);
-        done_with(b.dp_full);
-        release(pos + 1);
-        if (steps > 1) {
-          if (!arrived(pos + 2)) return false;
-          scores(n + 1, pos + 2);
-        } else {
-          done_with(b.fixed_free);
-        }
+        uint32_t k[3], v;                                   // stages of K of this step and the next two
 #pragma unroll 1
-        for (int j = 0; j < steps; ++j, pos += 2, ++n) {
-          if (!bar_wait(b.ds_ready, n & 1, a.error)) return false;
-          fence_after();
-          const uint32_t k = tile(pos);
-          if (leader) {
-            mma_rows(tmem + kDq, tmem + kDp, k, i_o, j > 0);
-            mma_rows(tmem + kDq, tmem + kDp + 64, k + step_rows(4), i_o, true);
+        for (int j = -2; j < steps; ++j) {
+          if (j == -2 && !m.wait(b.fixed_full, fixed++)) return false;
+          if (j >= -1 && j + 1 < steps) {
+            if (j >= 0 && !m.wait(b.p_ready, n)) return false;      // dO V^T was read
+            if (!m.across(kDp, dO, b.dp_full, v)) return false;
+            m.release(v);
           }
-          release(pos);
-          if (j + 1 < steps) {
-            if (!arrived(pos + 3)) return false;
-            across(kDp, dO, pos + 3);
-            done_with(b.dp_full);
-            release(pos + 3);
+          if (j >= 0) {
+            if (!m.wait(b.ds_ready, n)) return false;
+            m.gradient(kDq, kS + n % 2 * 128, k[0], j > 0);
+            m.release(k[0]);
+            ++n;
           }
           if (j + 2 < steps) {
-            if (!arrived(pos + 4)) return false;
-            scores(n + 2, pos + 4);
+            // before step 0 of an item, n is its number; then it is already that of step j + 1
+            const uint32_t s = (j < 0 ? n + j : n - 1) % 2;
+            if (!m.across(kS + s * 128, Q, b.s_full + 8 * s, k[2])) return false;
           }
-          if (j + 2 == steps) done_with(b.fixed_free);
+          if (j + 2 == steps) m.done_with(b.fixed_free);
+          k[0] = k[1];
+          k[1] = k[2];
         }
-        done_with(b.out_full);
+        m.done_with(b.out_full);
         return true;
       };
 #pragma unroll 1
@@ -496,7 +500,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dq(const __grid_constant__
         const int steps = uniform(a.q_tile[i].n);
         if (steps && !run(steps)) break;
       }
-      done_with(b.done);
+      m.done_with(b.done);
       bar_wait(b.done, 0, a.error);
     }
   } else {                                                  // ---- arithmetic: a query per lane, 64 keys
@@ -505,7 +509,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dq(const __grid_constant__
     const int half = warp / 4, r = threadIdx.x % 128, c0 = 64 * half;
     const uint32_t lanes = (uint32_t)(warp % 4 * 32) << 16, Dp = tmem + lanes + kDp + c0;
     const float c2 = a.scale * kLog2e;
-    uint32_t n = 0, pos = 0, items = 0;
+    uint32_t n = 0, items = 0;
+    Place<L::kStages> at;
 #pragma unroll 1
     for (int i = i0; i < i1; ++i) {
       const AttnTile it = a.q_tile[i];
@@ -513,47 +518,39 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dq(const __grid_constant__
       const int steps = uniform(it.n), first_seen = uniform(it.seen), keys = uniform(it.keys);
       const int64_t query = it.q_row + r;
       const bool valid = r < it.rows;
-      float lse = INFINITY, delta = 0.f;
+      float minus_lse = -INFINITY, minus_delta = 0.f;        // no weight for a row that sees nothing
       if (valid) {
-        lse = __ldg(a.lse + it.head * a.q.rows + query) * kLog2e;
-        delta = a.delta[it.head * a.delta_rows + query];
-        if (lse == -INFINITY) lse = INFINITY;                // no weight for a row that sees nothing
+        const float lse = __ldg(a.lse + it.head * a.q.rows + query) * kLog2e;
+        minus_lse = lse == -INFINITY ? -INFINITY : -lse;
+        minus_delta = -a.delta[it.head * a.delta_rows + query];
       }
       bool ok = true;
 #pragma unroll 1
-      for (int j = 0; j < steps; ++j, ++n, pos += 2) {
+      for (int j = 0; j < steps; ++j, ++n) {
         const uint32_t S = tmem + lanes + kS + n % 2 * 128 + c0;
-        const int seen = first_seen + r - j * kTile - c0;                   // keys of this half that the row sees
+        const int seen = first_seen + r - j * kTile - c0;                // keys of this half that the row sees
         const bool masked = (j + 1) * kTile > first_seen;
-        float p[64];
         if (!(ok = bar_wait(b.s_full + 8 * (n % 2), n / 2 & 1, a.error))) break;
         fence_after();
-        tmem_ld32(S, p);
-        tmem_ld32(S + 32, p + 32);
-        wait_ld();
-#pragma unroll
-        for (int e = 0; e < 64; ++e) p[e] = exp2_fast(fmaf(p[e], c2, -lse));
+        if (masked) keep(S, 64, 0, seen, -INFINITY);
+        float p[64];
+        get(S, p);
+        weights(p, c2, &minus_lse, false);
         if (!(ok = bar_wait(b.dp_full, n & 1, a.error))) break;
         fence_after();
+        if (masked) keep(Dp, 64, 0, seen, 0.f);               // of keys that may be anything
         float d[64];
-        tmem_ld32(Dp, d);
-        tmem_ld32(Dp + 32, d + 32);
-        wait_ld();
-#pragma unroll
-        for (int e = 0; e < 64; ++e) d[e] = p[e] * (d[e] - delta);
-        if (masked)
-#pragma unroll
-          for (int e = 0; e < 64; ++e) d[e] = e < seen ? d[e] : 0.f;
-        {
-          uint32_t y[32];
-#pragma unroll
-          for (int e = 0; e < 32; ++e) y[e] = pack2<BF16>(d[2 * e], d[2 * e + 1]);
-          tmem_st32(Dp, y);
-        }
-        if ((j + 1) * kTile > keys) clear_rows<DP>(sm + L::kRing + pos % L::kStages * L::kTileBytes, keys - j * kTile);
+        get(Dp, d);
+        fence_before();
+        bar_arrive_warp(b.p_ready, leader);
+        weight_gradients(d, p, &minus_delta, false);
+        put<BF16>(S, d);
+        if ((j + 1) * kTile > keys) clear_rows<DP>(sm + L::kRing + at.stage * L::kTileBytes, keys - j * kTile);
         wait_st();
         fence_before();
         bar_arrive_warp(b.ds_ready, leader);
+        at.next();
+        at.next();
       }
       if (!ok) break;
       if (steps) {

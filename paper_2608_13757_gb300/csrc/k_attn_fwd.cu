@@ -41,22 +41,6 @@ constexpr int kCols = 512;
 __device__ __forceinline__ constexpr uint32_t s_col(int t) { return 128 * t; }
 __device__ __forceinline__ constexpr uint32_t o_col(int t) { return 256 + 128 * t; }
 
-// A place in the ring of tiles and the parity of its use there.
-template <int STAGES>
-struct Place {
-  uint32_t stage = 0, parity = 0;
-  __device__ __forceinline__ void next() {
-    if (++stage == STAGES) {
-      stage = 0;
-      parity ^= 1;
-    }
-  }
-};
-
-// Key tiles of an item that query tile t meets, and the first row of its
-// queries: of a dual item both have the first tile's, every other key tile.
-__device__ __forceinline__ int tiles_of(const AttnItem& it, int t) { return it.dual ? (it.n[0] + 1 - t) / 2 : it.n[t]; }
-
 template <int DP>
 struct Layout {
   static constexpr int kTileBytes = DP / 64 * kBlockBytes;
@@ -66,16 +50,6 @@ struct Layout {
   static constexpr int kInts = kBars + 104 + 16 * kStages;  // after the barriers: dead, tensor memory
   static constexpr int kBytes = kInts + 8;
 };
-
-// Of 16 scores of a row, those from `seen` on become -inf.
-__device__ __forceinline__ void hide16(uint32_t addr, int seen) {
-  float x[16];
-  tmem_ld16(addr, x);
-  wait_ld();
-#pragma unroll
-  for (int c = 0; c < 16; ++c) x[c] = c < seen ? x[c] : -INFINITY;
-  tmem_st16(addr, reinterpret_cast<uint32_t*>(x));
-}
 
 template <int DP, bool BF16>
 __global__ void __launch_bounds__(kThreads, 1) k_attn_fwd(const __grid_constant__ AttnArgs a,
@@ -161,10 +135,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_fwd(const __grid_constant_
 #pragma unroll 1
       for (int i = i0; ok && i < i1; ++i) {
         const AttnItem it = a.item[i];
-        const int packed = uniform(it.packed), row = (int)it.q_row, apart = it.dual ? 0 : packed ? packed_rows : kTile;
+        const int packed = uniform(it.packed), row = (int)it.q_row, apart = packed ? packed_rows : kTile;
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
-          if (!ok || !uniform(tiles_of(it, t))) continue;
+          if (!ok || !uniform(it.n[t])) continue;
           if (n[t] && !(ok = bar_wait(q_free + 8 * t, (n[t] - 1) & 1, a.error))) continue;
           if (leader) {
             bar_expect(q_full + 8 * t, DP / 64 * (packed ? packed_rows * group : kTile) * 128);
@@ -200,18 +174,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_fwd(const __grid_constant_
         at.next();
         return true;
       };
-      auto skip = [&](int tiles) {                          // the other's: let go as they come
-#pragma unroll 1
-        for (int j = 0; j < tiles; ++j, at.next()) {
-          if (!arrived()) return false;
-          bar_arrive_warp(free_ + 8 * at.stage, leader);
-        }
-        return true;
-      };
-      // n of the item's key tiles are this query tile's: the first ones, or of
-      // a dual item every other one
-      auto run = [&](int n, int all, bool dual) {
-        if (dual && t && !skip(2)) return false;
+      auto run = [&](int n, int all) {                      // the first n of the item's key tiles are this query tile's
 #pragma unroll 1
         for (int j = 0; j < n; ++j) {
           if (j == 0 && !scores(true, n == 1)) return false;
@@ -227,14 +190,19 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_fwd(const __grid_constant_
             commit(v_free);
             if (j + 1 == n) commit(o_full + 8 * t);
           }
-          if (j + 1 < n && ((dual && !skip(2)) || !scores(false, j + 2 == n))) return false;
+          if (j + 1 < n && !scores(false, j + 2 == n)) return false;
         }
-        return skip(2 * (dual ? n && (all + t + 1) % 2 : all - n));
+#pragma unroll 1
+        for (int j = 2 * n; j < 2 * all; ++j, at.next()) {   // the other's: let go as they come
+          if (!arrived()) return false;
+          bar_arrive_warp(free_ + 8 * at.stage, leader);
+        }
+        return true;
       };
 #pragma unroll 1
       for (int i = i0; i < i1; ++i) {
         const AttnItem* const it = a.item + i;
-        if (!run(uniform(tiles_of(*it, t)), uniform(max(it->n[0], it->n[1])), uniform(it->dual))) break;
+        if (!run(uniform(it->n[t]), uniform(max(it->n[0], it->n[1])))) break;
       }
       if (leader) commit(done);
       bar_wait(done, 0, a.error);
@@ -252,23 +220,22 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_fwd(const __grid_constant_
     for (int i = i0; i < i1; ++i) {
       const AttnItem* const at_item = a.item + i;
       if (i + 1 < i1) asm volatile("prefetch.global.L1 [%0];" ::"l"(at_item + 1));
-      const int packed = uniform(at_item->packed), dual = uniform(at_item->dual), keys = uniform(at_item->keys);
-      const int n = uniform(tiles_of(*at_item, t)), tq = dual ? 0 : t;
+      const int packed = uniform(at_item->packed), n = uniform(at_item->n[t]), keys = uniform(at_item->keys);
       const int per = packed ? packed_rows : kTile, rq = packed ? packed_q : r;
-      const int least = uniform(at_item->seen) + tq * per;   // keys that the tile's first query sees
+      const int least = uniform(at_item->seen) + t * per;   // keys that the tile's first query sees
       const int seen_all = min(least + rq, keys);            // and this row
-      const bool valid = rq < at_item->rows[tq], busy = __any_sync(~0u, valid);
+      const bool valid = rq < at_item->rows[t], busy = __any_sync(~0u, valid);
       float m = -INFINITY, l = 0.f;
       bool ok = true;
 #pragma unroll 1
       for (int j = 0; j < n; ++j) {
-        const int g = dual ? 2 * j + t : j, k0 = g * kTile;
+        const int k0 = j * kTile;
         if (!(ok = bar_wait(s_full + 8 * t, sn++ & 1, a.error))) break;
         if (k0 + kTile > keys) {
           // Values past the sequence's end belong to other sequences and may
           // be anything; a zero weight does not hide a NaN, so they are
           // cleared (both query tiles write the same zeros).
-          const uint32_t at = pos + 2 * g + 1, st = at % L::kStages;
+          const uint32_t at = pos + 2 * j + 1, st = at % L::kStages;
           if (!(ok = bar_wait(full + 8 * st, at / L::kStages & 1, a.error))) break;
           uint8_t* v = sm + L::kRing + st * L::kTileBytes;
 #pragma unroll 1
@@ -286,7 +253,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_fwd(const __grid_constant_
         if (k0 + kTile > least) {                             // some row does not see the whole tile
           const int seen = seen_all - k0;
 #pragma unroll 1
-          for (int c = max(0, uniform(seen)) & ~15; c < kTile; c += 16) hide16(S + c, seen - c);
+          for (int c = max(0, uniform(seen)) & ~15; c < kTile; c += 16) keep16(S + c, 0, seen - c, -INFINITY);
           wait_st();
         }
         float x[kTile];
@@ -369,7 +336,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_fwd(const __grid_constant_
       const float by = __fdividef(1.f, l);
       const int slot = uniform(at_item->slot);
       const int head = at_item->head + (packed ? packed_h : 0);
-      const int64_t query = at_item->q_row + tq * per + rq;
+      const int64_t query = at_item->q_row + t * per + rq;
       if (valid) {
         const float lse2 = l == 0.f ? -INFINITY : fmaf(m, c2, __log2f(l));
         if (slot >= 0)
@@ -418,21 +385,19 @@ __global__ void __launch_bounds__(256) k_attn_merge(const __grid_constant__ Attn
   const int n0 = s.rows[0] * heads, t = row >= n0;
   if (t) row -= n0;
   if (row >= s.rows[t] * heads) return;
-  // both results of a dual piece are of the first tile
-  const int pieces = s.dual ? 2 * s.pieces : s.pieces, apart = s.dual ? 1 : 2;
   const float* lse = a.part_lse + ((int64_t)s.slot * 2 + t) * kTile + row;
   const float* part = a.part_o + (((int64_t)s.slot * 2 + t) * kTile + row) * DP + lane % (DP / 4) * 4;
   float top = -INFINITY;
-  for (int k = lane; k < pieces; k += 32) top = fmaxf(top, lse[(int64_t)k * apart * kTile]);
+  for (int k = lane; k < s.pieces; k += 32) top = fmaxf(top, lse[(int64_t)k * 2 * kTile]);
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, o));
   const float from = top == -INFINITY ? 0.f : top;
   float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
   float sum = 0.f;
-#pragma unroll 8
-  for (int k = 0; k < pieces; ++k) {
-    const float f = exp2_fast(lse[(int64_t)k * apart * kTile] - from);
-    const float4 x = *reinterpret_cast<const float4*>(part + (int64_t)k * apart * kTile * DP);
+#pragma unroll 4
+  for (int k = 0; k < s.pieces; ++k) {
+    const float f = exp2_fast(lse[(int64_t)k * 2 * kTile] - from);
+    const float4 x = *reinterpret_cast<const float4*>(part + (int64_t)k * 2 * kTile * DP);
     sum += f;
     acc.x = fmaf(f, x.x, acc.x);
     acc.y = fmaf(f, x.y, acc.y);

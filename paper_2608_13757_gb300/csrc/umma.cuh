@@ -99,6 +99,18 @@ __device__ __forceinline__ bool swizzle_aligned(uint32_t base, int* error) {
   return false;
 }
 
+// A place in a ring of tiles and the parity of its use there.
+template <int STAGES>
+struct Place {
+  uint32_t stage = 0, parity = 0;
+  __device__ __forceinline__ void next() {
+    if (++stage == STAGES) {
+      stage = 0;
+      parity ^= 1;
+    }
+  }
+};
+
 // ---- TMA ----
 // A box of a [rows][heads][entries] tensor at (entry, head, row).
 __device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap* map, uint32_t bar, int entry, int head,
@@ -202,6 +214,22 @@ __device__ __forceinline__ void tmem_st16(uint32_t addr, const uint32_t* r) {
 __device__ __forceinline__ void tmem_st32(uint32_t addr, const uint32_t* r) {
   asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31};" ::"r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]), "r"(addr)
                : "memory");
+}
+
+// Of 16 columns of a row, those outside [from, to) become `fill`.
+__device__ __forceinline__ void keep16(uint32_t addr, int from, int to, float fill) {
+  float x[16];
+  tmem_ld16(addr, x);
+  wait_ld();
+#pragma unroll
+  for (int c = 0; c < 16; ++c) x[c] = c >= from && c < to ? x[c] : fill;
+  tmem_st16(addr, reinterpret_cast<uint32_t*>(x));
+}
+// The same for `n` columns, 16 at a time.
+__device__ __forceinline__ void keep(uint32_t addr, int n, int from, int to, float fill) {
+#pragma unroll 1
+  for (int c = 0; c < n; c += 16) keep16(addr + c, from - c, to - c, fill);
+  wait_st();
 }
 
 // A warpgroup's registers per thread, given up or taken from what the block
