@@ -10,6 +10,11 @@
 // changes from run to run, and which cost a read and a write of dQ in L2 for
 // every pair of tiles.
 //
+// Products read shared memory at 128 bytes a cycle at most: 8 KB for a step of
+// 128 x 128 x 16 with both operands there, as long as the step takes.  So the
+// query walk keeps Q and dO, first operands that stay for an item, in tensor
+// memory (the key walk has no room there beside two accumulators).
+//
 // A walk takes one block per SM, tiles of 128 by 128.  The first operands of
 // the gradient products are P and dS in tensor memory, where they replace S
 // and dO V^T; the key walk computes both transposed (a lane has a key), so
@@ -50,16 +55,17 @@ struct Layout {
 template <int DP>
 struct Bars {
   using L = Layout<DP>;
-  uint32_t fixed_full, fixed_free, s_full, dp_full, p_ready, ds_ready, out_full, done, stat_full, stat_free, full, free_;
+  uint32_t fixed_full, fixed_free, s_full, fixed_ready, dp_full, p_ready, ds_ready, out_full, done, stat_full, stat_free, full, free_;
   __device__ __forceinline__ explicit Bars(uint32_t at)
-      : fixed_full(at), fixed_free(at + 8), s_full(at + 16), dp_full(at + 32), p_ready(at + 40), ds_ready(at + 48),
+      : fixed_full(at), fixed_free(at + 8), s_full(at + 16), fixed_ready(at + 24), dp_full(at + 32), p_ready(at + 40), ds_ready(at + 48),
         out_full(at + 56), done(at + 64), stat_full(at + 80), stat_free(stat_full + 8 * L::kStatStages),
         full(stat_free + 8 * L::kStatStages), free_(full + 8 * L::kStages) {}
-  __device__ __forceinline__ void init() const {
+  // fixed_users: arrivals that free the two tiles that stay
+  __device__ __forceinline__ void init(int fixed_users) const {
     bar_init(fixed_full, 1);
-    bar_init(fixed_free, 1);
+    bar_init(fixed_free, fixed_users);
+    bar_init(fixed_ready, 8);
     bar_init(s_full, 1);
-    bar_init(s_full + 8, 1);
     bar_init(dp_full, 1);
     bar_init(p_ready, 8);
     bar_init(ds_ready, 8);
@@ -178,12 +184,17 @@ struct Products {
     fence_after();
     return ok;
   }
-  // d = x y^T with the next tile y, whose stage it returns
+  // d = x y^T with the next tile y, whose stage it returns; x a tile in shared
+  // memory or (TMEM) in tensor memory
+  template <bool TMEM>
   __device__ __forceinline__ bool across(uint32_t d, uint32_t x, uint32_t bar, uint32_t& stage) {
     if (!wait(b.full + 8 * at.stage, at.parity)) return false;
     stage = at.stage;
     if (leader) {
-      mma_along(tmem + d, x, tile(stage), i_s, ksteps);
+      if (TMEM)
+        mma_tmem_along(tmem + d, tmem + x, tile(stage), i_s, ksteps);
+      else
+        mma_along(tmem + d, x, tile(stage), i_s, ksteps);
       commit(bar);
     }
     at.next();
@@ -230,6 +241,19 @@ __device__ __forceinline__ void put(uint32_t addr, const float* x) {
   for (int e = 0; e < 32; ++e) y[e] = pack2<BF16>(x[2 * e], x[2 * e + 1]);
   tmem_st32(addr, y);
 }
+// A row of a tile in shared memory, to tensor memory as a first operand.
+template <int DP>
+__device__ __forceinline__ void tile_to_tmem(uint32_t addr, const uint8_t* tile, int row) {
+#pragma unroll 1
+  for (int c = 0; c < DP / 64; ++c) {
+    uint4 x[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e)                              // 16-byte pieces lie at their number xor the row's
+      x[e] = *reinterpret_cast<const uint4*>(tile + c * kBlockBytes + row * 128 + (e ^ row % 8) * 16);
+    tmem_st32(addr + 32 * c, reinterpret_cast<const uint32_t*>(x));
+  }
+  wait_st();
+}
 __device__ __forceinline__ void get(uint32_t addr, float* x) {
   tmem_ld32(addr, x);
   tmem_ld32(addr + 32, x + 32);
@@ -250,7 +274,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dkv(const __grid_constant_
   int* const shared_int = reinterpret_cast<int*>(sm + L::kInts);
   const int warp = uniform(threadIdx.x / 32);
   if (!swizzle_aligned(base, a.error)) return;
-  if (threadIdx.x == 0) b.init();
+  if (threadIdx.x == 0) b.init(1);
   if (warp == 9) tmem_alloc<512>(smem_addr(shared_int));
   const int group = a.heads / a.kv_heads;
   const int i0 = uniform(a.k_first[blockIdx.x]), i1 = uniform(a.k_first[blockIdx.x + 1]);
@@ -293,13 +317,13 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dkv(const __grid_constant_
             m.gradient(kDv, kS, g[0], j > 0);
             m.release(g[0]);
           }
-          if (more && !m.across(kS, K, b.s_full, q[1])) return false;
+          if (more && !m.template across<false>(kS, K, b.s_full, q[1])) return false;
           if (j >= 0) {
             if (!m.wait(b.ds_ready, n++)) return false;
             m.gradient(kDk, kDp, q[0], j > 0);
             m.release(q[0]);
           }
-          if (more && !m.across(kDp, V, b.dp_full, g[1])) return false;
+          if (more && !m.template across<false>(kDp, V, b.dp_full, g[1])) return false;
           if (j + 2 == steps) m.done_with(b.fixed_free);
           q[0] = q[1];
           g[0] = g[1];
@@ -430,14 +454,14 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dq(const __grid_constant__
                                                          const __grid_constant__ CUtensorMap v_map,
                                                          const __grid_constant__ CUtensorMap do_map) {
   using L = Layout<DP>;
-  constexpr uint32_t kS = 0, kDp = 256, kDq = 384;          // two buffers of scores
+  constexpr uint32_t kS = 0, kDp = 128, kDq = 256, kQ = 384, kDo = 448;
   extern __shared__ __align__(1024) uint8_t sm[];
   const uint32_t base = smem_addr(sm);
   const Bars<DP> b(base + L::kBars);
   int* const shared_int = reinterpret_cast<int*>(sm + L::kInts);
   const int warp = uniform(threadIdx.x / 32);
   if (!swizzle_aligned(base, a.error)) return;
-  if (threadIdx.x == 0) b.init();
+  if (threadIdx.x == 0) b.init(8);
   if (warp == 9) tmem_alloc<512>(smem_addr(shared_int));
   const int group = a.heads / a.kv_heads;
   const int i0 = uniform(a.q_first[blockIdx.x]), i1 = uniform(a.q_first[blockIdx.x + 1]);
@@ -462,35 +486,29 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dq(const __grid_constant__
       load.finish();
     } else if (warp == 9) {                                 // ---- products
       Products<DP, BF16> m(base, tmem, b, a.error, a.dim);
-      const uint32_t Q = tile_desc(base), dO = tile_desc(base + L::kTileBytes);
       uint32_t fixed = 0, n = 0;
-      // dS replaces the scores in their buffer.  dO V^T of step j + 1 follows
-      // as soon as step j's is in registers, the scores of step j + 2 when the
-      // product with dS of step j is done with their buffer.
+      // The scores of step j + 1 follow as soon as step j's are in registers,
+      // its dO V^T when the product with dS of step j, which replaces dO V^T,
+      // is done.
       auto run = [&](int steps) {
-        uint32_t k[3], v;                                   // stages of K of this step and the next two
+        uint32_t k[2], v;                                   // stages of K of this step and the next
 #pragma unroll 1
-        for (int j = -2; j < steps; ++j) {
-          if (j == -2 && !m.wait(b.fixed_full, fixed++)) return false;
-          if (j >= -1 && j + 1 < steps) {
-            if (j >= 0 && !m.wait(b.p_ready, n)) return false;      // dO V^T was read
-            if (!m.across(kDp, dO, b.dp_full, v)) return false;
-            m.release(v);
+        for (int j = -1; j < steps; ++j) {
+          const bool more = j + 1 < steps;
+          if (more) {
+            if (!(j < 0 ? m.wait(b.fixed_ready, fixed++) : m.wait(b.p_ready, n))) return false;
+            if (!m.template across<true>(kS, kQ, b.s_full, k[1])) return false;
           }
           if (j >= 0) {
-            if (!m.wait(b.ds_ready, n)) return false;
-            m.gradient(kDq, kS + n % 2 * 128, k[0], j > 0);
+            if (!m.wait(b.ds_ready, n++)) return false;
+            m.gradient(kDq, kDp, k[0], j > 0);
             m.release(k[0]);
-            ++n;
           }
-          if (j + 2 < steps) {
-            // before step 0 of an item, n is its number; then it is already that of step j + 1
-            const uint32_t s = (j < 0 ? n + j : n - 1) % 2;
-            if (!m.across(kS + s * 128, Q, b.s_full + 8 * s, k[2])) return false;
+          if (more) {
+            if (!m.template across<true>(kDp, kDo, b.dp_full, v)) return false;
+            m.release(v);
           }
-          if (j + 2 == steps) m.done_with(b.fixed_free);
           k[0] = k[1];
-          k[1] = k[2];
         }
         m.done_with(b.out_full);
         return true;
@@ -507,7 +525,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dq(const __grid_constant__
     regs_up<kRegsMany>();
     const bool leader = elect_one();
     const int half = warp / 4, r = threadIdx.x % 128, c0 = 64 * half;
-    const uint32_t lanes = (uint32_t)(warp % 4 * 32) << 16, Dp = tmem + lanes + kDp + c0;
+    const uint32_t lanes = (uint32_t)(warp % 4 * 32) << 16, S = tmem + lanes + kS + c0, Dp = tmem + lanes + kDp + c0;
     const float c2 = a.scale * kLog2e;
     uint32_t n = 0, items = 0;
     Place<L::kStages> at;
@@ -525,26 +543,32 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dq(const __grid_constant__
         minus_delta = -a.delta[it.head * a.delta_rows + query];
       }
       bool ok = true;
+      if (steps) {                                            // half of the warps bring Q, half dO
+        if (!bar_wait(b.fixed_full, items & 1, a.error)) break;
+        tile_to_tmem<DP>(tmem + lanes + (half ? kDo : kQ), sm + half * L::kTileBytes, r);
+        fence_before();
+        bar_arrive_warp(b.fixed_ready, leader);
+        bar_arrive_warp(b.fixed_free, leader);
+      }
 #pragma unroll 1
       for (int j = 0; j < steps; ++j, ++n) {
-        const uint32_t S = tmem + lanes + kS + n % 2 * 128 + c0;
         const int seen = first_seen + r - j * kTile - c0;                // keys of this half that the row sees
         const bool masked = (j + 1) * kTile > first_seen;
-        if (!(ok = bar_wait(b.s_full + 8 * (n % 2), n / 2 & 1, a.error))) break;
+        if (!(ok = bar_wait(b.s_full, n & 1, a.error))) break;
         fence_after();
         if (masked) keep(S, 64, 0, seen, -INFINITY);
         float p[64];
         get(S, p);
+        fence_before();
+        bar_arrive_warp(b.p_ready, leader);
         weights(p, c2, &minus_lse, false);
         if (!(ok = bar_wait(b.dp_full, n & 1, a.error))) break;
         fence_after();
         if (masked) keep(Dp, 64, 0, seen, 0.f);               // of keys that may be anything
         float d[64];
         get(Dp, d);
-        fence_before();
-        bar_arrive_warp(b.p_ready, leader);
         weight_gradients(d, p, &minus_delta, false);
-        put<BF16>(S, d);
+        put<BF16>(Dp, d);
         if ((j + 1) * kTile > keys) clear_rows<DP>(sm + L::kRing + at.stage * L::kTileBytes, keys - j * kTile);
         wait_st();
         fence_before();

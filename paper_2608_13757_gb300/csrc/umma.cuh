@@ -188,6 +188,14 @@ __device__ __forceinline__ void mma_along(uint32_t d, uint32_t a, uint32_t b, ui
     for (int f = 0; f < 4; ++f)
       if (e + f < ksteps) mma(d, a + step_along(f), b + step_along(f), i, e + f > 0);
 }
+// The same with a in tensor memory.
+__device__ __forceinline__ void mma_tmem_along(uint32_t d, uint32_t a, uint32_t b, uint32_t i, int ksteps) {
+#pragma unroll 1
+  for (int e = 0; e < ksteps; e += 4, a += 32, b += kBlockBytes >> 4)
+#pragma unroll
+    for (int f = 0; f < 4; ++f)
+      if (e + f < ksteps) mma_tmem(d, a + 8 * f, b + step_along(f), i, e + f > 0);
+}
 // d (+)= a b over 64 contracted rows of a tile, a in tensor memory.
 __device__ __forceinline__ void mma_rows(uint32_t d, uint32_t a, uint32_t b, uint32_t i, bool add) {
 #pragma unroll
