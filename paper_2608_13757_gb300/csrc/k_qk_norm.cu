@@ -12,6 +12,7 @@
 #include <cuda_fp16.h>
 
 #include <algorithm>
+#include <cstring>
 
 #include "launch.cuh"
 #include "norm.h"
@@ -48,6 +49,19 @@ __device__ __forceinline__ void store(T* p, const float* f) {
   *reinterpret_cast<Pack<T, N>*>(p) = v;
 }
 
+// The value of 16 bits in a word
+template <class T>
+__device__ __forceinline__ float half_word(uint32_t w, bool high) {
+  const uint16_t bits = high ? w >> 16 : w & 0xffff;
+  T x;
+  memcpy(&x, &bits, 2);
+  return to_f(x);
+}
+template <>
+__device__ __forceinline__ float half_word<__nv_bfloat16>(uint32_t w, bool high) {
+  return __uint_as_float(high ? w & 0xffff0000u : w << 16);
+}
+
 // How a lane reads and writes its pairs: x[0..VEC) holds their first entries,
 // x[VEC..2*VEC) their second ones.
 //   VECTOR: VEC pairs that are all rotated or all not; two accesses of VEC
@@ -72,8 +86,45 @@ struct Shape {
   __device__ __forceinline__ int hi(int i) const {
     return lo(i) + (INTER ? 1 : first + i < half ? half : rest);
   }
-  template <class P>
-  __device__ __forceinline__ void read(const P* p, float* x) const {
+  // A lane's pairs as they were read: in their type where accesses are wide,
+  // which takes half the registers until they are used.
+  static constexpr bool kRaw = VECTOR && sizeof(T) == 2;
+  struct Values {
+    uint32_t w[kRaw ? VEC : 2 * VEC];
+    __device__ __forceinline__ void clear() {
+#pragma unroll
+      for (uint32_t& x : w) x = 0;
+    }
+    // the compiler unpacks again after this instead of keeping what it unpacked
+    __device__ __forceinline__ void keep() {
+#pragma unroll
+      for (uint32_t& x : w) asm volatile("" : "+r"(x));
+    }
+    __device__ __forceinline__ float operator[](int k) const {
+      if constexpr (kRaw) {
+        const int e = INTER ? 2 * (k % VEC) + k / VEC : k;
+        return half_word<T>(w[e / 2], e % 2);
+      } else {
+        return __uint_as_float(w[k]);
+      }
+    }
+  };
+  __device__ __forceinline__ void read(const T* p, Values& v) const {
+    if constexpr (kRaw) {
+      struct alignas(2 * VEC) Words {
+        uint32_t w[VEC / 2];
+      };
+      const Words a = *reinterpret_cast<const Words*>(p + lo(0)), b = *reinterpret_cast<const Words*>(p + (INTER ? lo(0) + VEC : hi(0)));
+#pragma unroll
+      for (int i = 0; i < VEC / 2; ++i) { v.w[i] = a.w[i]; v.w[VEC / 2 + i] = b.w[i]; }
+    } else {
+      float x[2 * VEC] = {};
+      read(p, x);
+#pragma unroll
+      for (int i = 0; i < 2 * VEC; ++i) v.w[i] = __float_as_uint(x[i]);
+    }
+  }
+  __device__ __forceinline__ void read(const T* p, float* x) const {
     if constexpr (VECTOR && INTER) {
       float y[2 * VEC];
       load<VEC>(p + lo(0), y);
@@ -89,8 +140,7 @@ struct Shape {
         if (has(i)) { x[i] = to_f(p[lo(i)]); x[VEC + i] = to_f(p[hi(i)]); }
     }
   }
-  template <class P>
-  __device__ __forceinline__ void write(P* p, const float* x) const {
+  __device__ __forceinline__ void write(T* p, const float* x) const {
     if constexpr (VECTOR && INTER) {
       float y[2 * VEC];
 #pragma unroll
@@ -142,11 +192,6 @@ __device__ __forceinline__ float sum_lanes(float v) {
   return v;
 }
 
-// Heads that a group of LANES lanes holds at a time: their loads are issued
-// together, before anything is stored (outputs may be inputs, so the compiler
-// cannot move a load over a store).
-constexpr int kAhead = 2;
-
 // Heads [h0, h1) of one token and one tensor, G at a time by the warp's groups.
 template <class T, class S>
 __device__ __forceinline__ void forward_heads(const NormArgs& a, const S& l, const NormTensor& in, const NormTensor& out,
@@ -159,36 +204,35 @@ __device__ __forceinline__ void forward_heads(const NormArgs& a, const S& l, con
   float w[2 * VEC];
   l.weights(weight, w);
 #pragma unroll 1
-  for (int hb = h0; hb < h1; hb += kAhead * G) {   // the same trips for every lane: the sums take whole warps
-    float v[kAhead][2 * VEC];
+  for (int hb = h0; hb < h1; hb += G) {   // the same trips for every lane: the sums take whole warps
+    const int h = hb + group;
+    const bool on = l.on() && h < h1;
+    typename S::Values v;
+    v.clear();
+    if (on) l.read(x + h * in.head, v);
+    float ss = 0.f;
 #pragma unroll
-    for (int k = 0; k < kAhead; ++k) {
+    for (int i = 0; i < 2 * VEC; ++i) ss += v[i] * v[i];
+    const float r = rsqrtf(sum_lanes<S::LANES>(ss) * a.inv_dim + a.eps);
+    v.keep();
+    float z[2 * VEC];
 #pragma unroll
-      for (int i = 0; i < 2 * VEC; ++i) v[k][i] = 0.f;
-      const int h = hb + k * G + group;
-      if (l.on() && h < h1) l.read(x + h * in.head, v[k]);
+    for (int i = 0; i < VEC; ++i) {
+      const float p = v[i] * r * w[i], q = v[VEC + i] * r * w[VEC + i];
+      z[i] = p * c[i] - q * s[i];
+      z[VEC + i] = q * c[i] + p * s[i];
     }
-#pragma unroll
-    for (int k = 0; k < kAhead; ++k) {
-      float ss = 0.f;
-#pragma unroll
-      for (int i = 0; i < 2 * VEC; ++i) ss += v[k][i] * v[k][i];
-      const float r = rsqrtf(sum_lanes<S::LANES>(ss) * a.inv_dim + a.eps);
-#pragma unroll
-      for (int i = 0; i < VEC; ++i) {
-        const float p = v[k][i] * r * w[i], q = v[k][VEC + i] * r * w[VEC + i];
-        v[k][i] = p * c[i] - q * s[i];
-        v[k][VEC + i] = q * c[i] + p * s[i];
-      }
-      const int h = hb + k * G + group;
-      if (l.on() && h < h1) l.write(y + h * out.head, v[k]);
-    }
+    if (on) l.write(y + h * out.head, z);
   }
 }
 
-// a.split warps share a token, a.per heads each (the query heads, then the key heads).
+// a.split warps share a token, a.per heads each (the query heads, then the key
+// heads).  Warps in flight count for more here than loads in flight per warp:
+// 64 registers a thread (32 warps per SM), one head per lane group at a time
+// take 61 us for 16411 tokens of 40 heads of 128 (5.6 TB/s); two heads at a
+// time in 92 registers took 81, 48 registers spill and took 89.
 template <class T, class S>
-__global__ void __launch_bounds__(kThreads) k_norm_rope(const __grid_constant__ NormArgs a) {
+__global__ void __launch_bounds__(kThreads, 4) k_norm_rope(const __grid_constant__ NormArgs a) {
   const int64_t warp = blockIdx.x * (int64_t)kWarps + threadIdx.x / 32;
   const int64_t t = warp / a.split;
   if (t >= a.rows) return;
@@ -205,6 +249,9 @@ __global__ void __launch_bounds__(kThreads) k_norm_rope(const __grid_constant__ 
 // in turn, once for the queries and once for the keys; the weights' sums stay
 // in registers until the end, go through shared memory in warp order and
 // leave as one row per block, so their order does not depend on the run.
+// 8192 tokens of 40 heads of 128: 59 us (4.3 TB/s) at 16 warps per SM; the
+// angles, weights and sums of a lane take 64 of its 128 registers, and 80
+// registers (24 warps) took 83.
 template <class T, class S>
 __device__ __forceinline__ void gradient_heads(const NormArgs& a, const S& l, const NormTensor& in, const NormTensor& grad,
                                                const NormTensor& out, int heads, const void* weight, float* row) {
@@ -227,43 +274,38 @@ __device__ __forceinline__ void gradient_heads(const NormArgs& a, const S& l, co
     float c[VEC], s[VEC];
     l.angles(a, t, c, s);
 #pragma unroll 1
-    for (int hb = h0; hb < h1; hb += kAhead * G) {
-      float v[kAhead][2 * VEC], d[kAhead][2 * VEC];
-#pragma unroll
-      for (int k = 0; k < kAhead; ++k) {
-#pragma unroll
-        for (int i = 0; i < 2 * VEC; ++i) v[k][i] = d[k][i] = 0.f;
-        const int h = hb + k * G + group;
-        if (l.on() && h < h1) {
-          l.read(x + h * in.head, v[k]);
-          l.read(dy + h * grad.head, d[k]);
-        }
+    for (int hb = h0; hb < h1; hb += G) {
+      const int h = hb + group;
+      const bool on = l.on() && h < h1;
+      typename S::Values v, d;
+      v.clear();
+      d.clear();
+      if (on) {
+        l.read(x + h * in.head, v);
+        l.read(dy + h * grad.head, d);
       }
+      float ss = 0.f, xd = 0.f;
 #pragma unroll
-      for (int k = 0; k < kAhead; ++k) {
-        float ss = 0.f, xd = 0.f;
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) {     // back through the rotation
-          const float p = d[k][i], q = d[k][VEC + i];
-          d[k][i] = p * c[i] + q * s[i];
-          d[k][VEC + i] = q * c[i] - p * s[i];
-        }
-#pragma unroll
-        for (int i = 0; i < 2 * VEC; ++i) {
-          ss += v[k][i] * v[k][i];
-          xd += v[k][i] * d[k][i] * w[i];
-        }
-        const float r = rsqrtf(sum_lanes<S::LANES>(ss) * a.inv_dim + a.eps);
-        const float m = sum_lanes<S::LANES>(xd) * a.inv_dim * r * r;
-        const int h = hb + k * G + group;
-        if (!(l.on() && h < h1)) continue;
-#pragma unroll
-        for (int i = 0; i < 2 * VEC; ++i) {
-          g[i] += d[k][i] * v[k][i] * r;
-          d[k][i] = r * (d[k][i] * w[i] - v[k][i] * m);
-        }
-        l.write(dx + h * out.head, d[k]);
+      for (int i = 0; i < VEC; ++i) {
+        const float p = d[i] * c[i] + d[VEC + i] * s[i], q = d[VEC + i] * c[i] - d[i] * s[i];   // turned back
+        ss += v[i] * v[i] + v[VEC + i] * v[VEC + i];
+        xd += v[i] * p * w[i] + v[VEC + i] * q * w[VEC + i];
       }
+      const float r = rsqrtf(sum_lanes<S::LANES>(ss) * a.inv_dim + a.eps);
+      const float m = sum_lanes<S::LANES>(xd) * a.inv_dim * r * r;
+      if (!on) continue;
+      v.keep();
+      d.keep();
+      float z[2 * VEC];
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) {
+        const float p = d[i] * c[i] + d[VEC + i] * s[i], q = d[VEC + i] * c[i] - d[i] * s[i];
+        g[i] += p * v[i] * r;
+        g[VEC + i] += q * v[VEC + i] * r;
+        z[i] = r * (p * w[i] - v[i] * m);
+        z[VEC + i] = r * (q * w[VEC + i] - v[VEC + i] * m);
+      }
+      l.write(dx + h * out.head, z);
     }
   }
 #pragma unroll
