@@ -4,7 +4,10 @@
 #include <cmath>
 #include <cstring>
 #include <functional>
+#include <initializer_list>
+#include <map>
 #include <memory>
+#include <mutex>
 #include <new>
 #include <queue>
 #include <string>
@@ -434,12 +437,77 @@ class Arena {
   std::vector<uint8_t> host_;
 };
 
+// Copies to the device on a stream of the library's own and waits for that
+// stream alone: the copy is complete for kernels on any stream, and the
+// caller's queued work is not waited for.
+void upload(int device, void* to, const void* from, size_t bytes) {
+  static std::mutex mu;
+  static std::map<int, cudaStream_t> streams;
+  cudaStream_t st = nullptr;
+  {
+    std::lock_guard<std::mutex> lock(mu);
+    auto at = streams.find(device);
+    if (at == streams.end()) {
+      cuda(cudaStreamCreateWithFlags(&st, cudaStreamNonBlocking), "cudaStreamCreate");
+      streams.emplace(device, st);
+    } else {
+      st = at->second;
+    }
+  }
+  cuda(cudaMemcpyAsync(to, from, bytes, cudaMemcpyHostToDevice, st), "sync_attn_plan");
+  cuda(cudaStreamSynchronize(st), "sync_attn_plan");
+}
+
 void check_gave_up(const sync_attn* plan) {
   if (*static_cast<volatile int*>(plan->error))
     fail(SYNC_ERR_CUDA, "an earlier call on this plan gave up waiting inside a kernel: its results are not valid");
 }
 
 }  // namespace
+
+// For tests on the host: the work lists of a plan for a GPU of num_sms SMs,
+// one row of `width` values per item.  which 0: forward items (block, q_row,
+// k_row, head, packed, rows of both tiles, key tiles of both, seen, keys,
+// slot); 1: split ranges (q_row, head, packed, rows of both, slot, pieces);
+// 2 and 3: query and key tiles of the gradients (block, q_row, k_row, head, n,
+// rows, keys, seen).  Returns the rows (written up to `capacity`), or a
+// negative status.
+extern "C" int64_t syncgb_attn_work(const sync_attn_desc* desc, int num_sms, int which, int64_t* out, int64_t capacity) {
+  int64_t n = 0;
+  const sync_status status = guarded([&] {
+    check_attn(desc);
+    sync_attn_sizes sz{};
+    const std::vector<AttnSeq> seq = sequences(desc, sz);
+    auto row = [&](std::initializer_list<int64_t> v) {
+      if (n < capacity) std::copy(v.begin(), v.end(), out + n * (int64_t)v.size());
+      ++n;
+    };
+    if (which < 2) {
+      const ForwardWork w = forward_work(desc, seq, num_sms);
+      if (which == 1) {
+        for (const AttnSplit& s : w.split) row({s.q_row, s.head, s.packed, s.rows[0], s.rows[1], s.slot, s.pieces});
+        return;
+      }
+      for (size_t b = 0; b + 1 < w.block_first.size(); ++b)
+        for (int32_t i = w.block_first[b]; i < w.block_first[b + 1]; ++i) {
+          const AttnItem& x = w.item[(size_t)i];
+          row({(int64_t)b, x.q_row, x.k_row, x.head, x.packed, x.rows[0], x.rows[1], x.n[0], x.n[1], x.seen, x.keys, x.slot});
+        }
+      return;
+    }
+    std::vector<Draft<AttnTile>> q, k;
+    gradient_work(desc, seq, q, k);
+    std::vector<AttnTile> tile;
+    std::vector<int32_t> first;
+    assign(which == 2 ? q : k, num_sms, tile, first);
+    for (size_t b = 0; b + 1 < first.size(); ++b)
+      for (int32_t i = first[b]; i < first[b + 1]; ++i) {
+        const AttnTile& x = tile[(size_t)i];
+        row({(int64_t)b, x.q_row, x.k_row, x.head, x.n, x.rows, x.keys, x.seen});
+      }
+  });
+  return status == SYNC_OK ? n : -(int64_t)status;
+}
 
 extern "C" {
 
@@ -526,7 +594,7 @@ sync_status sync_attn_plan(const sync_attn_desc* desc, int device, sync_attn** o
     *P->error = 0;
     a.error = P->error;
     cuda(cudaMalloc(&P->block, std::max<size_t>(m.size(), 1)), "sync_attn_plan");
-    cuda(cudaMemcpy(P->block, m.host().data(), m.host().size(), cudaMemcpyHostToDevice), "sync_attn_plan");
+    upload(device, P->block, m.host().data(), m.host().size());
     uint8_t* base = static_cast<uint8_t*>(P->block);
     a.item = reinterpret_cast<const AttnItem*>(base + at_item);
     a.block_first = reinterpret_cast<const int32_t*>(base + at_first);
