@@ -75,20 +75,10 @@ def _need(ok, what):
         raise _sg.SyncError(_sg.ERR_ARG, what)
 
 
-class _current:
-    """The device of a call that has no handle, made current where it is not."""
-
-    def __init__(self, device):
-        import torch
-        self.scope = torch.cuda.device(device) if torch.cuda.current_device() != device else None
-
-    def __enter__(self):
-        if self.scope is not None:
-            self.scope.__enter__()
-
-    def __exit__(self, *a):
-        if self.scope is not None:
-            self.scope.__exit__(*a)
+def _current_stream(device: int) -> int:
+    """The current stream's handle, without the object around it (a microsecond)."""
+    import torch
+    return torch._C._cuda_getCurrentRawStream(device)
 
 
 class _On:
@@ -111,10 +101,11 @@ class _On:
 
 def _rows(t, name, dtype, device, heads, dim) -> Rows:
     """A [rows, heads, dim] tensor's description, checked against the call's."""
-    if t.dim() != 3 or t.dtype is not dtype or t.get_device() != device:
-        _need(t.dim() == 3, f"{name} must be [rows, heads, dim]")
-        _need(t.dtype is dtype and t.get_device() == device, f"{name} must be {dtype} on GPU {device}")
-    n, h, d = t.shape
+    shape = t.shape
+    if len(shape) != 3 or t.dtype is not dtype or t.get_device() != device:
+        _need(len(shape) == 3, f"{name} must be [rows, heads, dim]")
+        _need(False, f"{name} must be {dtype} on GPU {device}")
+    n, h, d = shape
     rs, hs, ds = t.stride()
     if h != heads or d != dim or ds != 1:
         _need(h == heads and d == dim, f"{name} must have {heads} heads of {dim} entries")
@@ -154,18 +145,20 @@ def sync_qk_norm_rope(q, k, q_weight, k_weight, cos, sin, positions=None, eps: f
     angles of the token's position (int32; None: its row).  A position outside
     the table gives NaN.  Returns the pair of outputs; out=(q, k) works in place."""
     import torch
-    p = _norm_rope(q, k, q_weight, k_weight, cos, sin, positions, eps, interleaved)
     if stream is not None:
         with _On(q.device, stream):
             return sync_qk_norm_rope(q, k, q_weight, k_weight, cos, sin, positions, eps, interleaved, out)
+    p = _norm_rope(q, k, q_weight, k_weight, cos, sin, positions, eps, interleaved)
+    device, dtype = q.get_device(), q.dtype
+    if torch.cuda.current_device() != device:
+        with torch.cuda.device(device):
+            return sync_qk_norm_rope(q, k, q_weight, k_weight, cos, sin, positions, eps, interleaved, out)
     if out is None:
-        out = (torch.empty(q.shape, dtype=q.dtype, device=q.device),
-               torch.empty(k.shape, dtype=q.dtype, device=q.device))
-    device = q.get_device()
-    a = [_rows(t, name, q.dtype, device, h, p.dim) for t, name, h in ((out[0], "out[0]", p.heads),
-                                                                     (out[1], "out[1]", p.kv_heads))]
-    with _current(device):
-        _sg._check(_sg.lib().sync_qk_norm_rope(p, a[0], a[1], torch.cuda.current_stream(device).cuda_stream))
+        where = q.device
+        out = torch.empty(q.shape, dtype=dtype, device=where), torch.empty(k.shape, dtype=dtype, device=where)
+    _sg._check(_sg.lib().sync_qk_norm_rope(p, _rows(out[0], "out[0]", dtype, device, p.heads, p.dim),
+                                           _rows(out[1], "out[1]", dtype, device, p.kv_heads, p.dim),
+                                           _current_stream(device)))
     return out
 
 
@@ -175,26 +168,30 @@ def sync_qk_norm_rope_backward(q, k, dq_out, dk_out, q_weight, k_weight, cos, si
     its outputs' gradients; a weight that is None has None.  out=(dq, dk) may
     be the outputs' gradients themselves."""
     import torch
-    p = _norm_rope(q, k, q_weight, k_weight, cos, sin, positions, eps, interleaved)
     if stream is not None:
         with _On(q.device, stream):
             return sync_qk_norm_rope_backward(q, k, dq_out, dk_out, q_weight, k_weight, cos, sin, positions, eps,
                                               interleaved, out)
+    p = _norm_rope(q, k, q_weight, k_weight, cos, sin, positions, eps, interleaved)
+    device, dtype = q.get_device(), q.dtype
+    if torch.cuda.current_device() != device:
+        with torch.cuda.device(device):
+            return sync_qk_norm_rope_backward(q, k, dq_out, dk_out, q_weight, k_weight, cos, sin, positions, eps,
+                                              interleaved, out)
     if out is None:
-        out = (torch.empty(q.shape, dtype=q.dtype, device=q.device),
-               torch.empty(k.shape, dtype=q.dtype, device=q.device))
-    dw = [torch.empty(p.dim, dtype=q.dtype, device=q.device) if w is not None else None for w in (q_weight, k_weight)]
-    device = q.get_device()
-    a = [_rows(t, name, q.dtype, device, h, p.dim)
-         for t, name, h in ((dq_out, "dq_out", p.heads), (dk_out, "dk_out", p.kv_heads), (out[0], "out[0]", p.heads),
-                            (out[1], "out[1]", p.kv_heads))]
+        where = q.device
+        out = torch.empty(q.shape, dtype=dtype, device=where), torch.empty(k.shape, dtype=dtype, device=where)
+    heads, kv, dim = p.heads, p.kv_heads, p.dim
+    a = (_rows(dq_out, "dq_out", dtype, device, heads, dim), _rows(dk_out, "dk_out", dtype, device, kv, dim),
+         _rows(out[0], "out[0]", dtype, device, heads, dim), _rows(out[1], "out[1]", dtype, device, kv, dim))
+    dwq = torch.empty(dim, dtype=dtype, device=q.device) if q_weight is not None else None
+    dwk = torch.empty(dim, dtype=dtype, device=q.device) if k_weight is not None else None
     need = ctypes.c_int64()
-    with _current(device):
-        _sg._check(_sg.lib().sync_qk_norm_rope_workspace(p, need))
-        work = torch.empty(need.value, dtype=torch.uint8, device=q.device)
-        _sg._check(_sg.lib().sync_qk_norm_rope_backward(p, *a, _sg._ptr(dw[0]), _sg._ptr(dw[1]), _sg._ptr(work),
-                                                        need.value, torch.cuda.current_stream(device).cuda_stream))
-    return out[0], out[1], dw[0], dw[1]
+    _sg._check(_sg.lib().sync_qk_norm_rope_workspace(p, need))
+    work = torch.empty(need.value, dtype=torch.uint8, device=q.device)
+    _sg._check(_sg.lib().sync_qk_norm_rope_backward(p, *a, _sg._ptr(dwq), _sg._ptr(dwk), work.data_ptr(), need.value,
+                                                    _current_stream(device)))
+    return out[0], out[1], dwq, dwk
 
 
 class AttnPlan:
@@ -284,7 +281,7 @@ def sync_attn_forward(plan: AttnPlan, q, k, v, scale: float | None = None, out=N
             lse.fill_(-float("inf"))
     at = None if lse is False or lse is None else _vector(lse, "lse", device, heads * n, torch.float32)
     _sg._check(_sg.lib().sync_attn_forward(plan.handle, *a, dim ** -0.5 if scale is None else scale, o, at,
-                                           torch.cuda.current_stream(device).cuda_stream))
+                                           _current_stream(device)))
     return out if at is None and not isinstance(lse, torch.Tensor) else (out, lse)
 
 
@@ -295,14 +292,16 @@ def sync_attn_backward(plan: AttnPlan, q, k, v, o, lse, do, scale: float | None 
         with _On(plan.device, stream):
             return sync_attn_backward(plan, q, k, v, o, lse, do, scale, out)
     dtype, device, heads, kv, dim = plan.dtype, plan.index, plan.heads, plan.kv_heads, plan.head_dim
-    a = [_rows(t, name, dtype, device, h, dim) for t, name, h in ((q, "q", heads), (k, "k", kv), (v, "v", kv),
-                                                                 (o, "o", heads), (do, "do", heads))]
+    a = (_rows(q, "q", dtype, device, heads, dim), _rows(k, "k", dtype, device, kv, dim),
+         _rows(v, "v", dtype, device, kv, dim), _rows(o, "o", dtype, device, heads, dim))
+    g = _rows(do, "do", dtype, device, heads, dim)
     n, m = q.shape[0], k.shape[0]
     at = _vector(lse, "lse", device, heads * n, torch.float32)
     if out is None:
-        out = (_new(n, heads, plan, plan.n_queries), _new(m, kv, plan, plan.n_keys), _new(m, kv, plan, plan.n_keys))
-    d = [_rows(t, name, dtype, device, h, dim) for t, name, h in ((out[0], "dq", heads), (out[1], "dk", kv),
-                                                                 (out[2], "dv", kv))]
-    _sg._check(_sg.lib().sync_attn_backward(plan.handle, *a[:4], at, a[4], dim ** -0.5 if scale is None else scale, *d,
-                                            torch.cuda.current_stream(device).cuda_stream))
+        out = (_new(n, heads, plan, plan.n_queries), _new(m, kv, plan, plan.n_keys),
+               _new(m, kv, plan, plan.n_keys))
+    d = (_rows(out[0], "dq", dtype, device, heads, dim), _rows(out[1], "dk", dtype, device, kv, dim),
+         _rows(out[2], "dv", dtype, device, kv, dim))
+    _sg._check(_sg.lib().sync_attn_backward(plan.handle, *a, at, g, dim ** -0.5 if scale is None else scale, *d,
+                                            _current_stream(device)))
     return tuple(out)
