@@ -62,6 +62,23 @@ __device__ __forceinline__ float half_word<__nv_bfloat16>(uint32_t w, bool high)
   return __uint_as_float(high ? w & 0xffff0000u : w << 16);
 }
 
+// Copies of 8 or 16 bytes from global to shared memory.  A thread closes its
+// copies in groups and waits until N groups at most are on their way.
+template <int BYTES>
+__device__ __forceinline__ void copy_ahead(uint32_t dst, const void* src) {
+  if constexpr (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+  else asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void end_group() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void wait_groups() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+template <int BYTES>
+__device__ __forceinline__ void read_shared(uint32_t addr, uint32_t* x) {
+  if constexpr (BYTES == 16)
+    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(x[0]), "=r"(x[1]), "=r"(x[2]), "=r"(x[3]) : "r"(addr) : "memory");
+  else asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(x[0]), "=r"(x[1]) : "r"(addr) : "memory");
+}
+
 // How a lane reads and writes its pairs: x[0..VEC) holds their first entries,
 // x[VEC..2*VEC) their second ones.
 //   VECTOR: VEC pairs that are all rotated or all not; two accesses of VEC
@@ -71,6 +88,8 @@ __device__ __forceinline__ float half_word<__nv_bfloat16>(uint32_t w, bool high)
 template <class T, int VEC_, int LANES_, bool INTER, bool VECTOR>
 struct Shape {
   static constexpr int VEC = VEC_, LANES = LANES_;
+  static constexpr bool kWide = VECTOR;
+  static constexpr int kPiece = VEC * (int)sizeof(T);          // bytes of a wide access: 8 or 16
   int first, pairs, half, rest, rotated;
   __device__ __forceinline__ explicit Shape(const NormArgs& a)
       : first((int)(threadIdx.x % LANES) * VEC), pairs(a.dim / 2), half(a.rotated / 2),
@@ -161,6 +180,19 @@ struct Shape {
     for (int i = 0; i < 2 * VEC; ++i) x[i] = 1.f;
     if (w && on()) read(static_cast<const T*>(w), x);
   }
+  // Wide accesses by way of shared memory: a copy that does not wait, to this
+  // lane's place of a slot, and the read when it has come.
+  __device__ __forceinline__ void fetch(const T* p, uint32_t slot) const {
+    copy_ahead<kPiece>(slot, p + lo(0));
+    copy_ahead<kPiece>(slot + 32 * kPiece, p + (INTER ? lo(0) + VEC : hi(0)));
+  }
+  __device__ __forceinline__ void fetched(uint32_t slot, Values& v) const {
+    uint32_t y[2 * kPiece / 4];
+    read_shared<kPiece>(slot, y);
+    read_shared<kPiece>(slot + 32 * kPiece, y + kPiece / 4);
+#pragma unroll
+    for (int i = 0; i < 2 * kPiece / 4; ++i) v.w[!kRaw && INTER ? i / 2 + i % 2 * VEC : i] = y[i];
+  }
   // the angles of a token; NaN for a position outside the table
   __device__ __forceinline__ void angles(const NormArgs& a, int64_t t, float* c, float* s) const {
 #pragma unroll
@@ -244,32 +276,59 @@ __global__ void __launch_bounds__(kThreads, 4) k_norm_rope(const __grid_constant
   forward_heads<T>(a, l, a.k, a.k_out, a.k_weight, t, max(h0 - a.heads, 0), h1 - a.heads, c, s);
 }
 
-// Gradient, with xh = r x the normed head: dx = r (w dz - xh mean(w dz xh)),
-// dw = sum of dz xh, dz the output's gradient turned back.  Warps take tokens
-// in turn, once for the queries and once for the keys; the weights' sums stay
-// in registers until the end, go through shared memory in warp order and
-// leave as one row per block, so their order does not depend on the run.
-// 8192 tokens of 40 heads of 128: 59 us (4.3 TB/s) at 16 warps per SM; the
-// angles, weights and sums of a lane take 64 of its 128 registers, and 80
-// registers (24 warps) took 83.
+// Gradient, with xh = r x the normed head: dx = r (w dz xh - xh mean(w dz xh)),
+// dw = sum of dz xh, dz the output's gradient turned back.  Warps take equal
+// runs of rounds, a round being the G heads of a token that a warp holds at a
+// time, once of the queries and once of the keys; the weights' sums stay in
+// registers until the end, go through shared memory in warp order and leave as
+// one row per block, so their order does not depend on the run.
+// 8192 tokens of 40 heads of 128: 45 us (5.6 TB/s) at 16 warps per SM; the
+// angles, weights and sums of a lane take 64 of its 128 registers (80 registers
+// for 24 warps: 83).  Whole tokens in turn, 3 or 4 to a warp, took 59, equal
+// runs without the copies ahead 55, the next round held in registers 53; two
+// and four rounds ahead 48 and 46.
+
+// Bytes of a warp's slot: a round of inputs and one of gradients.
+template <class S>
+constexpr uint32_t kSlot = 4 * 32 * S::kPiece;
+
 template <class T, class S>
 __device__ __forceinline__ void gradient_heads(const NormArgs& a, const S& l, const NormTensor& in, const NormTensor& grad,
-                                               const NormTensor& out, int heads, const void* weight, float* row) {
+                                               const NormTensor& out, int heads, const void* weight, float* row, uint32_t slots) {
   constexpr int VEC = S::VEC, G = 32 / S::LANES;
   const int group = (threadIdx.x % 32) / S::LANES;
-  // with few tokens several warps share one, a whole number of rounds of G heads each
-  const int rounds = (heads + G - 1) / G, split = max(1, min(rounds, a.split)), per = (rounds + split - 1) / split * G;
-  const int64_t all = a.rows * split;
+  // rounds of G heads, over all tokens, in equal runs
+  const int rounds = (heads + G - 1) / G;
+  const int64_t all = a.rows * rounds, warps = gridDim.x * (int64_t)kWarps, warp = blockIdx.x * (int64_t)kWarps + threadIdx.x / 32;
+  int64_t left = all * (warp + 1) / warps - all * warp / warps, t = all * warp / warps / rounds;
+  int h0 = (int)(all * warp / warps - t * rounds) * G;
   float w[2 * VEC], g[2 * VEC];
   l.weights(weight, w);
 #pragma unroll
   for (int i = 0; i < 2 * VEC; ++i) g[i] = 0.f;
+  // One round ahead of the one that is computed, in two slots in turn.  A lane
+  // reads only what it copied itself.
+  int64_t ft = t, fleft = left;
+  int fh = h0;
+  uint32_t slot = slots + threadIdx.x % 32 * S::kPiece;
+  const uint32_t both = slot * 2 + kSlot<S>;
+  auto fetch = [&] {
+    if (fleft > 0 && l.on() && fh + group < heads) {
+      const int h = fh + group;
+      l.fetch(static_cast<const T*>(in.data) + ft * in.row + h * in.head, slot);
+      l.fetch(static_cast<const T*>(grad.data) + ft * grad.row + h * grad.head, slot + kSlot<S> / 2);
+    }
+    end_group();
+    --fleft;
+    fh += G;
+    if (fh >= heads) { fh = 0; ++ft; }
+    slot = both - slot;
+  };
+  if constexpr (S::kWide) fetch();
 #pragma unroll 1
-  for (int64_t warp = blockIdx.x * (int64_t)kWarps + threadIdx.x / 32; warp < all; warp += gridDim.x * (int64_t)kWarps) {
-    const int64_t t = warp / split;
-    const int h0 = (int)(warp - t * split) * per, h1 = min(heads, h0 + per);
-    const T* x = static_cast<const T*>(in.data) + t * in.row;
-    const T* dy = static_cast<const T*>(grad.data) + t * grad.row;
+  for (; left > 0; ++t, h0 = 0) {
+    const int h1 = (int)min((int64_t)heads, h0 + left * G);
+    left -= (h1 - h0 + G - 1) / G;
     T* dx = static_cast<T*>(out.data) + t * out.row;
     float c[VEC], s[VEC];
     l.angles(a, t, c, s);
@@ -280,9 +339,16 @@ __device__ __forceinline__ void gradient_heads(const NormArgs& a, const S& l, co
       typename S::Values v, d;
       v.clear();
       d.clear();
-      if (on) {
-        l.read(x + h * in.head, v);
-        l.read(dy + h * grad.head, d);
+      if constexpr (S::kWide) {
+        fetch();                          // the next round; the other slot has this one
+        wait_groups<1>();
+        if (on) {
+          l.fetched(slot, v);
+          l.fetched(slot + kSlot<S> / 2, d);
+        }
+      } else if (on) {
+        l.read(static_cast<const T*>(in.data) + t * in.row + h * in.head, v);
+        l.read(static_cast<const T*>(grad.data) + t * grad.row + h * grad.head, d);
       }
       float ss = 0.f, xd = 0.f;
 #pragma unroll
@@ -323,11 +389,14 @@ __device__ __forceinline__ void gradient_heads(const NormArgs& a, const S& l, co
 
 template <class T, class S>
 __global__ void __launch_bounds__(kThreads, 2) k_norm_rope_grad(const __grid_constant__ NormArgs a) {
-  extern __shared__ float part[];         // [kWarps][q, k][dim]
+  extern __shared__ __align__(16) float part[];         // [kWarps][q, k][dim]
   const S l(a);
   float* const row = part + threadIdx.x / 32 * 2 * a.dim;
-  gradient_heads<T>(a, l, a.q, a.q_out, a.dq, a.heads, a.q_weight, row);
-  gradient_heads<T>(a, l, a.k, a.k_out, a.dk, a.kv_heads, a.k_weight, row + a.dim);
+  uint32_t slots = 0;
+  if constexpr (S::kWide)
+    slots = (uint32_t)__cvta_generic_to_shared(part + kWarps * 2 * a.dim) + threadIdx.x / 32 * 2 * kSlot<S>;
+  gradient_heads<T>(a, l, a.q, a.q_out, a.dq, a.heads, a.q_weight, row, slots);
+  gradient_heads<T>(a, l, a.k, a.k_out, a.dk, a.kv_heads, a.k_weight, row + a.dim, slots);
   __syncthreads();
   for (int e = threadIdx.x; e < 2 * a.dim; e += kThreads) {
     float v = 0.f;
@@ -375,10 +444,10 @@ cudaError_t launch(NormArgs a, cudaStream_t st) {
     if (e == cudaSuccess) count_launch();
     return e;
   }
-  a.split = (int)std::max<int64_t>(1, std::min<int64_t>(want, rounds));
-  const int64_t blocks = (a.rows * a.split + kWarps - 1) / kWarps;
+  const int64_t blocks = (a.rows * rounds + kWarps - 1) / kWarps;
   const int n = (int)std::min<int64_t>(std::max<int64_t>(1, blocks), norm_blocks(a.num_sms));
-  k_norm_rope_grad<T, S><<<n, kThreads, kWarps * 2 * a.dim * sizeof(float), st>>>(a);
+  const int shared = kWarps * (2 * a.dim * (int)sizeof(float) + (S::kWide ? 2 * (int)kSlot<S> : 0));   // 48 KB at most
+  k_norm_rope_grad<T, S><<<n, kThreads, shared, st>>>(a);
   cudaError_t e = cudaGetLastError();
   if (e != cudaSuccess) return e;
   count_launch();
