@@ -224,62 +224,96 @@ __device__ __forceinline__ float sum_lanes(float v) {
   return v;
 }
 
-// Heads [h0, h1) of one token and one tensor, G at a time by the warp's groups.
-template <class T, class S>
-__device__ __forceinline__ void forward_heads(const NormArgs& a, const S& l, const NormTensor& in, const NormTensor& out,
-                                              const void* weight, int64_t t, int h0, int h1, const float* c,
-                                              const float* s) {
-  constexpr int VEC = S::VEC, G = 32 / S::LANES;
-  const int group = (threadIdx.x % 32) / S::LANES;
-  const T* x = static_cast<const T*>(in.data) + t * in.row;
-  T* y = static_cast<T*>(out.data) + t * out.row;
-  float w[2 * VEC];
-  l.weights(weight, w);
-#pragma unroll 1
-  for (int hb = h0; hb < h1; hb += G) {   // the same trips for every lane: the sums take whole warps
-    const int h = hb + group;
-    const bool on = l.on() && h < h1;
-    typename S::Values v;
-    v.clear();
-    if (on) l.read(x + h * in.head, v);
-    float ss = 0.f;
-#pragma unroll
-    for (int i = 0; i < 2 * VEC; ++i) ss += v[i] * v[i];
-    const float r = rsqrtf(sum_lanes<S::LANES>(ss) * a.inv_dim + a.eps);
-    v.keep();
-    float z[2 * VEC];
-#pragma unroll
-    for (int i = 0; i < VEC; ++i) {
-      const float p = v[i] * r * w[i], q = v[VEC + i] * r * w[VEC + i];
-      z[i] = p * c[i] - q * s[i];
-      z[VEC + i] = q * c[i] + p * s[i];
-    }
-    if (on) l.write(y + h * out.head, z);
-  }
-}
+// Bytes of a warp's slot for a round of one or two tensors.
+template <class S>
+constexpr uint32_t kSlot = 2 * 32 * S::kPiece;
+template <class S>
+constexpr uint32_t kSlot2 = 2 * kSlot<S>;
 
-// a.split warps share a token, a.per heads each (the query heads, then the key
-// heads).  Warps in flight count for more here than loads in flight per warp:
-// 64 registers a thread (32 warps per SM), one head per lane group at a time
-// take 61 us for 16411 tokens of 40 heads of 128 (5.6 TB/s); two heads at a
-// time in 92 registers took 81, 48 registers spill and took 89.
+// A round is the G heads of a token that a warp holds at a time, the queries'
+// rounds before the keys'; warps take equal runs of rounds.  One round is
+// copied ahead of the one that is computed, in two slots in turn; a lane reads
+// only what it copied itself.  Reads in flight without registers are what it
+// takes: 16411 tokens of 40 heads of 128 take 56 us (6.1 TB/s) with 80
+// registers a thread (24 warps per SM); 59 with 16 warps, 67 with 32, which
+// spill.  Read straight into registers by 32 warps a token each: 61.
 template <class T, class S>
-__global__ void __launch_bounds__(kThreads, 4) k_norm_rope(const __grid_constant__ NormArgs a) {
-  const int64_t warp = blockIdx.x * (int64_t)kWarps + threadIdx.x / 32;
-  const int64_t t = warp / a.split;
-  if (t >= a.rows) return;
-  const int h0 = (int)(warp - t * a.split) * a.per, h1 = min(a.heads + a.kv_heads, h0 + a.per);
+__global__ void __launch_bounds__(kThreads, 3) k_norm_rope(const __grid_constant__ NormArgs a) {
+  extern __shared__ __align__(16) float part[];   // [kWarps] two slots
+  constexpr int VEC = S::VEC, G = 32 / S::LANES;
   const S l(a);
-  float c[S::VEC], s[S::VEC];
-  l.angles(a, t, c, s);
-  forward_heads<T>(a, l, a.q, a.q_out, a.q_weight, t, h0, min(h1, a.heads), c, s);
-  forward_heads<T>(a, l, a.k, a.k_out, a.k_weight, t, max(h0 - a.heads, 0), h1 - a.heads, c, s);
+  const int group = (threadIdx.x % 32) / S::LANES;
+  const int q_rounds = (a.heads + G - 1) / G, rounds = q_rounds + (a.kv_heads + G - 1) / G;
+  const int64_t all = a.rows * rounds, warps = gridDim.x * (int64_t)kWarps, warp = blockIdx.x * (int64_t)kWarps + threadIdx.x / 32;
+  int64_t left = all * (warp + 1) / warps - all * warp / warps, t = all * warp / warps / rounds;
+  int i = (int)(all * warp / warps - t * rounds);
+  int64_t ft = t, fleft = left;
+  int fi = i;
+  uint32_t slot = 0, both = 0;
+  if constexpr (S::kWide) {
+    slot = (uint32_t)__cvta_generic_to_shared(part) + threadIdx.x / 32 * 2 * kSlot<S> + threadIdx.x % 32 * S::kPiece;
+    both = slot * 2 + kSlot<S>;
+  }
+  auto fetch = [&] {
+    const bool key = fi >= q_rounds;
+    const NormTensor& in = key ? a.k : a.q;
+    const int h = (key ? fi - q_rounds : fi) * G + group;
+    if (fleft > 0 && l.on() && h < (key ? a.kv_heads : a.heads)) l.fetch(static_cast<const T*>(in.data) + ft * in.row + h * in.head, slot);
+    end_group();
+    --fleft;
+    if (++fi == rounds) { fi = 0; ++ft; }
+    slot = both - slot;
+  };
+  if constexpr (S::kWide) fetch();
+#pragma unroll 1
+  while (left > 0) {
+    float c[VEC], s[VEC];
+    l.angles(a, t, c, s);
+#pragma unroll 1
+    while (true) {
+      const bool key = i >= q_rounds;
+      const int first = key ? q_rounds : 0, n = (int)min(left, (int64_t)(key ? rounds : q_rounds) - i), heads = key ? a.kv_heads : a.heads;
+      const NormTensor &in = key ? a.k : a.q, &out = key ? a.k_out : a.q_out;
+      float w[2 * VEC];
+      l.weights(key ? a.k_weight : a.q_weight, w);
+      left -= n;
+#pragma unroll 1
+      for (const int end = i + n; i < end; ++i) {
+        const int h = (i - first) * G + group;
+        const bool on = l.on() && h < heads;
+        typename S::Values v;
+        v.clear();
+        if constexpr (S::kWide) {
+          fetch();
+          wait_groups<1>();
+          if (on) l.fetched(slot, v);
+        } else if (on) {
+          l.read(static_cast<const T*>(in.data) + t * in.row + h * in.head, v);
+        }
+        float ss = 0.f;
+#pragma unroll
+        for (int e = 0; e < 2 * VEC; ++e) ss += v[e] * v[e];
+        const float r = rsqrtf(sum_lanes<S::LANES>(ss) * a.inv_dim + a.eps);
+        v.keep();
+        float z[2 * VEC];
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) {
+          const float p = v[e] * r * w[e], q = v[VEC + e] * r * w[VEC + e];
+          z[e] = p * c[e] - q * s[e];
+          z[VEC + e] = q * c[e] + p * s[e];
+        }
+        if (on) l.write(static_cast<T*>(out.data) + t * out.row + h * out.head, z);
+      }
+      if (left <= 0 || i == rounds) break;
+    }
+    i = 0;
+    ++t;
+  }
 }
 
 // Gradient, with xh = r x the normed head: dx = r (w dz xh - xh mean(w dz xh)),
 // dw = sum of dz xh, dz the output's gradient turned back.  Warps take equal
-// runs of rounds, a round being the G heads of a token that a warp holds at a
-// time, once of the queries and once of the keys; the weights' sums stay in
+// runs of rounds, once of the queries and once of the keys; the weights' sums stay in
 // registers until the end, go through shared memory in warp order and leave as
 // one row per block, so their order does not depend on the run.
 // 8192 tokens of 40 heads of 128: 45 us (5.6 TB/s) at 16 warps per SM; the
@@ -287,11 +321,6 @@ __global__ void __launch_bounds__(kThreads, 4) k_norm_rope(const __grid_constant
 // for 24 warps: 83).  Whole tokens in turn, 3 or 4 to a warp, took 59, equal
 // runs without the copies ahead 55, the next round held in registers 53; two
 // and four rounds ahead 48 and 46.
-
-// Bytes of a warp's slot: a round of inputs and one of gradients.
-template <class S>
-constexpr uint32_t kSlot = 4 * 32 * S::kPiece;
-
 template <class T, class S>
 __device__ __forceinline__ void gradient_heads(const NormArgs& a, const S& l, const NormTensor& in, const NormTensor& grad,
                                                const NormTensor& out, int heads, const void* weight, float* row, uint32_t slots) {
@@ -311,12 +340,12 @@ __device__ __forceinline__ void gradient_heads(const NormArgs& a, const S& l, co
   int64_t ft = t, fleft = left;
   int fh = h0;
   uint32_t slot = slots + threadIdx.x % 32 * S::kPiece;
-  const uint32_t both = slot * 2 + kSlot<S>;
+  const uint32_t both = slot * 2 + kSlot2<S>;
   auto fetch = [&] {
     if (fleft > 0 && l.on() && fh + group < heads) {
       const int h = fh + group;
       l.fetch(static_cast<const T*>(in.data) + ft * in.row + h * in.head, slot);
-      l.fetch(static_cast<const T*>(grad.data) + ft * grad.row + h * grad.head, slot + kSlot<S> / 2);
+      l.fetch(static_cast<const T*>(grad.data) + ft * grad.row + h * grad.head, slot + kSlot<S>);
     }
     end_group();
     --fleft;
@@ -344,7 +373,7 @@ __device__ __forceinline__ void gradient_heads(const NormArgs& a, const S& l, co
         wait_groups<1>();
         if (on) {
           l.fetched(slot, v);
-          l.fetched(slot + kSlot<S> / 2, d);
+          l.fetched(slot + kSlot<S>, d);
         }
       } else if (on) {
         l.read(static_cast<const T*>(in.data) + t * in.row + h * in.head, v);
@@ -394,7 +423,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_norm_rope_grad(const __grid_con
   float* const row = part + threadIdx.x / 32 * 2 * a.dim;
   uint32_t slots = 0;
   if constexpr (S::kWide)
-    slots = (uint32_t)__cvta_generic_to_shared(part + kWarps * 2 * a.dim) + threadIdx.x / 32 * 2 * kSlot<S>;
+    slots = (uint32_t)__cvta_generic_to_shared(part + kWarps * 2 * a.dim) + threadIdx.x / 32 * 2 * kSlot2<S>;
   gradient_heads<T>(a, l, a.q, a.q_out, a.dq, a.heads, a.q_weight, row, slots);
   gradient_heads<T>(a, l, a.k, a.k_out, a.dk, a.kv_heads, a.k_weight, row + a.dim, slots);
   __syncthreads();
@@ -429,24 +458,18 @@ __global__ void __launch_bounds__(1024) k_norm_weights(const __grid_constant__ N
 
 template <class T, class S>
 cudaError_t launch(NormArgs a, cudaStream_t st) {
-  // A token's heads go to as many warps as it takes to fill the GPU (32 warps
-  // per SM are resident, about), in whole rounds of G heads.
   constexpr int G = 32 / S::LANES;
-  const int rounds = (a.heads + a.kv_heads + G - 1) / G;
-  const int64_t want = (int64_t)a.num_sms * 32 / std::max<int64_t>(1, a.rows);
+  const int64_t rounds = a.rows * ((a.heads + G - 1) / G + (a.kv_heads + G - 1) / G), blocks = (rounds + kWarps - 1) / kWarps;
   if (!a.grad) {
     if (a.rows == 0) return cudaSuccess;
-    const int split = (int)std::min<int64_t>(rounds, std::max<int64_t>(1, want));
-    a.per = (rounds + split - 1) / split * G;
-    a.split = (a.heads + a.kv_heads + a.per - 1) / a.per;
-    k_norm_rope<T, S><<<(unsigned)((a.rows * a.split + kWarps - 1) / kWarps), kThreads, 0, st>>>(a);
+    const int n = (int)std::min<int64_t>(blocks, 3 * a.num_sms);
+    k_norm_rope<T, S><<<n, kThreads, S::kWide ? kWarps * 2 * kSlot<S> : 0, st>>>(a);
     const cudaError_t e = cudaGetLastError();
     if (e == cudaSuccess) count_launch();
     return e;
   }
-  const int64_t blocks = (a.rows * rounds + kWarps - 1) / kWarps;
   const int n = (int)std::min<int64_t>(std::max<int64_t>(1, blocks), norm_blocks(a.num_sms));
-  const int shared = kWarps * (2 * a.dim * (int)sizeof(float) + (S::kWide ? 2 * (int)kSlot<S> : 0));   // 48 KB at most
+  const int shared = kWarps * (2 * a.dim * (int)sizeof(float) + (S::kWide ? 2 * (int)kSlot2<S> : 0));   // 48 KB at most
   k_norm_rope_grad<T, S><<<n, kThreads, shared, st>>>(a);
   cudaError_t e = cudaGetLastError();
   if (e != cudaSuccess) return e;

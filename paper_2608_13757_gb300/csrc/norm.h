@@ -29,7 +29,6 @@ struct NormArgs {
   const int32_t* positions = nullptr;
   float* partial = nullptr;      // [norm_blocks][q, k][dim]
   int num_sms = 0;
-  int split = 1, per = 0;        // warps per token, heads per warp (set by the launch)
 };
 
 // Most blocks of the gradient kernel: two per SM, which keeps every SM full.
