@@ -64,10 +64,11 @@ __device__ __forceinline__ float half_word<__nv_bfloat16>(uint32_t w, bool high)
 
 // Copies of 8 or 16 bytes from global to shared memory.  A thread closes its
 // copies in groups and waits until N groups at most are on their way.
-template <int BYTES>
+// CACHED where two copies share 32-byte sectors, which then come once.
+template <int BYTES, bool CACHED>
 __device__ __forceinline__ void copy_ahead(uint32_t dst, const void* src) {
-  if constexpr (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
-  else asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(dst), "l"(src) : "memory");
+  if constexpr (BYTES == 16 && !CACHED) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+  else asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(dst), "l"(src), "n"(BYTES) : "memory");
 }
 __device__ __forceinline__ void end_group() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N>
@@ -183,8 +184,8 @@ struct Shape {
   // Wide accesses by way of shared memory: a copy that does not wait, to this
   // lane's place of a slot, and the read when it has come.
   __device__ __forceinline__ void fetch(const T* p, uint32_t slot) const {
-    copy_ahead<kPiece>(slot, p + lo(0));
-    copy_ahead<kPiece>(slot + 32 * kPiece, p + (INTER ? lo(0) + VEC : hi(0)));
+    copy_ahead<kPiece, INTER>(slot, p + lo(0));
+    copy_ahead<kPiece, INTER>(slot + 32 * kPiece, p + (INTER ? lo(0) + VEC : hi(0)));
   }
   __device__ __forceinline__ void fetched(uint32_t slot, Values& v) const {
     uint32_t y[2 * kPiece / 4];
