@@ -295,7 +295,7 @@ bool cut(const std::vector<Draft<AttnItem>>& all, int group, int num_sms, int64_
   w = ForwardWork{};
   std::vector<std::vector<AttnItem>> of((size_t)num_sms);
   std::set<std::pair<int64_t, int32_t>> rooms;                 // (room, -block): the first of equal ones is the last
-  for (int32_t b = 0; b < num_sms; ++b) rooms.insert({most, -b});
+  for (int32_t b = num_sms - 1; b >= 0; --b) rooms.emplace_hint(rooms.end(), most, -b);
   for (const Draft<AttnItem>& x : all) {
     const int32_t n = std::max(x.it.n[0], x.it.n[1]), slot0 = w.slots;
     auto cost = [&](int32_t a, int32_t b) {                    // of key tiles [a, b)
@@ -309,7 +309,8 @@ bool cut(const std::vector<Draft<AttnItem>>& all, int group, int num_sms, int64_
       auto at = rooms.lower_bound({cost(from, n), -num_sms});
       if (at == rooms.end()) {
         at = std::prev(at);
-        while (to > from && (n - to < kMinPiece || cost(from, to) > at->first)) --to;
+        to = (int32_t)std::min(n - kMinPiece, from + at->first - kItemCost);       // a tile costs 1 or 2
+        while (to > from && cost(from, to) > at->first) --to;
         if (to - from < kMinPiece) return false;
       }
       AttnItem it = x.it;
@@ -318,11 +319,10 @@ bool cut(const std::vector<Draft<AttnItem>>& all, int group, int num_sms, int64_
       it.keys -= from * kTile;
       for (int t = 0; t < 2; ++t) it.n[t] = std::max(0, std::min(x.it.n[t], to) - from);
       if (from > 0 || to < n) it.slot = w.slots++;
-      const int64_t left = at->first - cost(from, to);
-      const int32_t b = -at->second;
-      of[(size_t)b].push_back(it);
-      rooms.erase(at);
-      rooms.insert({left, -b});
+      auto room = rooms.extract(at);
+      room.value().first -= cost(from, to);
+      of[(size_t)-room.value().second].push_back(it);
+      rooms.insert(std::move(room));
       from = to;
     } while (from < n);
     if (w.slots == slot0) continue;
