@@ -624,12 +624,19 @@ __global__ void __launch_bounds__(256) k_attn_delta(const __grid_constant__ Attn
 // The walks start early: the key walk's loads and products run before delta is
 // there, and the query walk, which needs nothing of the key walk, takes the
 // SMs that its last blocks leave.  (The key walk's blocks let it start only
-// once delta is there.)
+// once delta is there.)  Tiles that meet nothing are written as zeros at once,
+// so a walk starts early only behind the kernel that it expects: the key walk
+// behind delta, which started in the plain way, when all earlier work of the
+// stream was done, and the query walk behind the key walk.  Without queries
+// there is no delta, and what comes before may still read the memory that dk
+// and dv now are; without keys delta itself comes before the query walk, which
+// reads it.
 template <class K>
-cudaError_t walk(K kernel, int blocks, int bytes, std::atomic<uint64_t>& allowed, const AttnArgs& a, const AttnMaps& m, cudaStream_t st) {
+cudaError_t walk(K kernel, int blocks, int bytes, bool early, std::atomic<uint64_t>& allowed, const AttnArgs& a, const AttnMaps& m, cudaStream_t st) {
   cudaError_t e = allow_smem(kernel, bytes, allowed);
   if (e != cudaSuccess) return e;
-  e = launch_early(kernel, blocks, kThreads, bytes, st, a, m.q, m.k, m.v, m.d_o);
+  e = early ? launch_early(kernel, blocks, kThreads, bytes, st, a, m.q, m.k, m.v, m.d_o)
+            : launch_plain(kernel, blocks, kThreads, bytes, st, a, m.q, m.k, m.v, m.d_o);
   if (e == cudaSuccess) count_launch();
   return e;
 }
@@ -646,8 +653,8 @@ cudaError_t launch(const AttnArgs& a, const AttnMaps& m, cudaStream_t st) {
     if ((e = cudaGetLastError()) != cudaSuccess) return e;
     count_launch();
   }
-  if (a.n_k_blocks && (e = walk(k_attn_dkv<DP, BF16>, a.n_k_blocks, L::kBytes, dkv_allowed, a, m, st)) != cudaSuccess) return e;
-  if (a.n_q_blocks && (e = walk(k_attn_dq<DP, BF16>, a.n_q_blocks, L::kBytes, dq_allowed, a, m, st)) != cudaSuccess) return e;
+  if (a.n_k_blocks && (e = walk(k_attn_dkv<DP, BF16>, a.n_k_blocks, L::kBytes, a.delta_rows > 0, dkv_allowed, a, m, st)) != cudaSuccess) return e;
+  if (a.n_q_blocks && (e = walk(k_attn_dq<DP, BF16>, a.n_q_blocks, L::kBytes, a.n_k_blocks > 0, dq_allowed, a, m, st)) != cudaSuccess) return e;
   return cudaSuccess;
 }
 
