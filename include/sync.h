@@ -524,11 +524,12 @@ typedef struct {
   float eps;
   sync_rows q, k;             /* inputs                                        */
   const void *q_weight, *k_weight;  /* [dim] each, or NULL for weights of 1    */
-  const float *cos, *sin;     /* [n_positions][rotated/2]                      */
+  const float *cos, *sin;     /* [n_positions][rotated/2]; not read where
+                                 rotated is 0                                  */
   int64_t n_positions;
   const int32_t *positions;   /* [rows], or NULL: the row's index.  A position
                                  outside 0..n_positions-1 makes its token's
-                                 outputs NaN                                   */
+                                 outputs NaN.  Not read where rotated is 0     */
 } sync_norm_rope;
 
 /* Writes the outputs y of q and k (rows, strides as given; either may be its

@@ -143,7 +143,8 @@ def sync_qk_norm_rope(q, k, q_weight, k_weight, cos, sin, positions=None, eps: f
     """Root-mean-square norm of every head of q and k, times its weights (or
     None), with the first 2 * cos.shape[1] entries of each head rotated by the
     angles of the token's position (int32; None: its row).  A position outside
-    the table gives NaN.  Returns the pair of outputs; out=(q, k) works in place."""
+    the table gives NaN; where nothing is rotated (tables of width 0, of any
+    length) positions are not looked at.  Returns the pair of outputs; out=(q, k) works in place."""
     import torch
     if stream is not None:
         with _On(q.device, stream):

@@ -194,10 +194,12 @@ struct Shape {
 #pragma unroll
     for (int i = 0; i < 2 * kPiece / 4; ++i) v.w[!kRaw && INTER ? i / 2 + i % 2 * VEC : i] = y[i];
   }
-  // the angles of a token; NaN for a position outside the table
+  // the angles of a token; NaN for a position outside the table.  Where nothing
+  // is rotated no position is looked at: the table may be absent.
   __device__ __forceinline__ void angles(const NormArgs& a, int64_t t, float* c, float* s) const {
 #pragma unroll
     for (int i = 0; i < VEC; ++i) { c[i] = 1.f; s[i] = 0.f; }
+    if (half == 0) return;
     const int64_t pos = a.positions ? (int64_t)__ldg(a.positions + t) : t;
     if (pos < 0 || pos >= a.n_positions) {
 #pragma unroll
