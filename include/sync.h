@@ -590,6 +590,15 @@ sync_status sync_attn_plan(const sync_attn_desc *desc, int device, sync_attn **o
 
 sync_status sync_attn_query(const sync_attn *plan, sync_attn_sizes *out);
 
+/* Whether a kernel of this plan has given up.  The kernels' warps wait for one
+ * another; a wait that does not end within about a second is a defect, of the
+ * library or of the device, and ends the kernel with results that are not
+ * valid.  The call that launched it has returned SYNC_OK by then.  This asks
+ * for the calls (and graph replays) that are done on the GPU: synchronise
+ * first.  SYNC_OK, or SYNC_ERR_CUDA from then on, also from every later forward
+ * and backward call of the plan, which is of no further use. */
+sync_status sync_attn_status(const sync_attn *plan);
+
 /* o = softmax(scale * q k^T over the visible keys) v, for every query row of
  * every sequence; rows outside the sequences are not written, and a query
  * that sees no key gets zeros.  q, o: [q_rows][heads][head_dim]; k, v:

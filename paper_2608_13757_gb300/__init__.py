@@ -40,7 +40,7 @@ EXPORTS = ("sync_load_programs", "sync_query", "sync_pair_offsets", "sync_eval_t
            "sync_check_minimal", "sync_simulate", "sync_simulate_fused", "sync_simulate_noalloc",
            "sync_free_programs", "sync_last_error", "sync_kernel_launches", "sync_validate_programs",
            "sync_qk_norm_rope", "sync_qk_norm_rope_workspace", "sync_qk_norm_rope_backward",
-           "sync_attn_plan", "sync_attn_query", "sync_attn_forward", "sync_attn_backward", "sync_attn_free")
+           "sync_attn_plan", "sync_attn_query", "sync_attn_status", "sync_attn_forward", "sync_attn_backward", "sync_attn_free")
 NOALLOC_SCRATCH_BYTES = 64 << 20
 CODE_BYTES_PER_INSTR = 16
 

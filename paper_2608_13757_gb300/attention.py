@@ -55,6 +55,7 @@ def declare(lib: ctypes.CDLL):
     lib.sync_qk_norm_rope_backward.argtypes = [P(NormRope), rows, rows, rows, rows, vp, vp, vp, ctypes.c_int64, vp]
     lib.sync_attn_plan.argtypes = [P(AttnDesc), ctypes.c_int, P(vp)]
     lib.sync_attn_query.argtypes = [vp, P(AttnSizes)]
+    lib.sync_attn_status.argtypes = [vp]
     lib.sync_attn_forward.argtypes = [vp, rows, rows, rows, ctypes.c_float, rows, vp, vp]
     lib.sync_attn_backward.argtypes = [vp, rows, rows, rows, rows, vp, rows, ctypes.c_float, rows, rows, rows, vp]
     lib.sync_attn_free.argtypes = [vp]
@@ -211,6 +212,12 @@ class AttnPlan:
         if not self._h:
             raise ValueError("plan already freed")
         return self._h
+
+    def check(self):
+        """Raises if a kernel of a call on this plan that is done on the GPU gave
+        up waiting, so that its results are not valid.  (Synchronise first; the
+        plan's later calls raise too.)"""
+        _sg._check(_sg.lib().sync_attn_status(self.handle))
 
     def close(self):
         if self._h:

@@ -463,7 +463,7 @@ void upload(int device, void* to, const void* from, size_t bytes) {
 
 void check_gave_up(const sync_attn* plan) {
   if (*static_cast<volatile int*>(plan->error))
-    fail(SYNC_ERR_CUDA, "an earlier call on this plan gave up waiting inside a kernel: its results are not valid");
+    fail(SYNC_ERR_CUDA, "a call on this plan gave up waiting inside a kernel: its results are not valid");
 }
 
 }  // namespace
@@ -510,6 +510,15 @@ extern "C" int64_t syncgb_attn_work(const sync_attn_desc* desc, int num_sms, int
       }
   });
   return status == SYNC_OK ? n : -(int64_t)status;
+}
+
+// For tests: a kernel of the plan whose waits run out after `tries` tries.
+extern "C" sync_status syncgb_attn_wait_in_vain(const sync_attn* plan, int tries, void* stream) {
+  return guarded([&] {
+    need(plan && tries >= 1, "plan must not be NULL, tries at least 1");
+    DeviceScope scope(plan->device);
+    cuda(launch_wait_in_vain(plan->error, tries, static_cast<cudaStream_t>(stream)), "syncgb_attn_wait_in_vain");
+  });
 }
 
 extern "C" {
@@ -623,6 +632,13 @@ sync_status sync_attn_query(const sync_attn* plan, sync_attn_sizes* out) {
   return guarded([&] {
     need(plan && out, "plan and out must not be NULL");
     *out = plan->sz;
+  });
+}
+
+sync_status sync_attn_status(const sync_attn* plan) {
+  return guarded([&] {
+    need(plan, "plan must not be NULL");
+    check_gave_up(plan);
   });
 }
 

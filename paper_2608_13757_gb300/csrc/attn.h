@@ -82,6 +82,7 @@ struct AttnMaps {
 
 cudaError_t launch_attn_forward(const AttnArgs& a, const AttnMaps& m, cudaStream_t st);
 cudaError_t launch_attn_backward(const AttnArgs& a, const AttnMaps& m, cudaStream_t st);
+cudaError_t launch_wait_in_vain(int* error, int tries, cudaStream_t st);   // for tests
 
 }  // namespace syncgb
 

@@ -423,6 +423,22 @@ __global__ void __launch_bounds__(256) k_attn_merge(const __grid_constant__ Attn
   if (a.lse && lane == 0) a.lse[head * a.q.rows + query] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * 0.6931471805599453f;
 }
 
+// For tests: a wait for a barrier that nobody arrives on, by the first of two
+// warps, and one by the second for the first's arrival, which then never comes.
+__global__ void __launch_bounds__(64) k_wait_in_vain(int* error, int tries) {
+  __shared__ __align__(8) uint64_t bars[2];
+  const uint32_t bar = smem_addr(bars);
+  const int warp = uniform(threadIdx.x / 32);
+  if (threadIdx.x == 0) {
+    bar_init(bar, 1);
+    bar_init(bar + 8, 1);
+    bar_init_visible();
+  }
+  __syncthreads();
+  if (bar_wait(bar + 8 * warp, 0, error, tries) && warp == 0) bar_arrive_warp(bar + 8, elect_one());
+  __syncthreads();
+}
+
 template <int DP, bool BF16>
 cudaError_t launch(const AttnArgs& a, const AttnMaps& m, cudaStream_t st) {
   using L = Layout<DP>;
@@ -439,6 +455,11 @@ cudaError_t launch(const AttnArgs& a, const AttnMaps& m, cudaStream_t st) {
 }
 
 }  // namespace
+
+cudaError_t launch_wait_in_vain(int* error, int tries, cudaStream_t st) {
+  k_wait_in_vain<<<1, 64, 0, st>>>(error, std::min(tries, kTries));
+  return cudaGetLastError();
+}
 
 cudaError_t launch_attn_forward(const AttnArgs& a, const AttnMaps& m, cudaStream_t st) {
   if (a.dim <= 64) return a.bf16 ? launch<64, true>(a, m, st) : launch<64, false>(a, m, st);
