@@ -196,9 +196,17 @@ def sync_qk_norm_rope_backward(q, k, dq_out, dk_out, q_weight, k_weight, cos, si
     return out[0], out[1], dwq, dwk
 
 
+# Handles of plans that were dropped without close().  Freeing one waits for the
+# device and would invalidate a capture, and a finaliser may run anywhere: it
+# only leaves the handle here, for the next sync_attn_plan.
+_dropped = []
+
+
 class AttnPlan:
-    """The work of a packed batch on one GPU (owns device memory; freed on
-    close / GC).  Calls on one plan must not overlap on the GPU."""
+    """The work of a packed batch on one GPU.  Owns device memory, which close()
+    frees, waiting for the device; that of a plan that is dropped instead is
+    freed by the next sync_attn_plan.  Keep it as long as a graph that captured
+    its calls.  Calls on one plan must not overlap on the GPU."""
 
     def __init__(self, handle, device, heads, kv_heads, head_dim, dtype):
         self._h = handle
@@ -225,10 +233,9 @@ class AttnPlan:
             self._h = None
 
     def __del__(self):
-        try:
-            self.close()
-        except Exception:
-            pass
+        h, self._h = getattr(self, "_h", None), None
+        if h:
+            _dropped.append(h)
 
 
 def sync_attn_plan(q_lens, k_lens, heads: int, kv_heads: int, head_dim: int, dtype, q_starts=None, k_starts=None,
@@ -255,6 +262,11 @@ def sync_attn_plan(q_lens, k_lens, heads: int, kv_heads: int, head_dim: int, dty
                                  ("k_start", ctypes.c_int64)), arrays):
         if a is not None:
             setattr(d, field, a.ctypes.data_as(ctypes.POINTER(kind)))
+    try:
+        while True:
+            _sg.lib().sync_attn_free(_dropped.pop())
+    except IndexError:                      # none left (another thread may have taken the last)
+        pass
     h = ctypes.c_void_p()
     _sg._check(_sg.lib().sync_attn_plan(ctypes.byref(d), index, ctypes.byref(h)))
     return AttnPlan(h, torch.device("cuda", index), heads, kv_heads, head_dim, dtype)
