@@ -495,7 +495,8 @@ void sync_free_programs(sync_programs *h);
  * Tensors are caller-owned device memory of one type, described by their
  * strides in elements; the entries of one head are contiguous.  Calls run
  * asynchronously on `stream`; arguments are checked on the host before
- * anything is launched.  Results are deterministic: every sum has a fixed
+ * anything is launched, every pointer for its type's alignment among them.
+ * Results are deterministic: every sum has a fixed
  * order, no result depends on which block ran first. */
 
 typedef enum { SYNC_BF16 = 0, SYNC_FP16 = 1, SYNC_FP32 = 2 } sync_dtype;

@@ -80,6 +80,12 @@ int sm_count(int device) {
   return n;
 }
 
+int current_sms() {
+  int device = 0;
+  cuda(cudaGetDevice(&device), "cudaGetDevice");
+  return sm_count(device);
+}
+
 // ---- norm and rotation ----------------------------------------------------
 
 void check_norm(const sync_norm_rope* p) {
@@ -93,11 +99,18 @@ void check_norm(const sync_norm_rope* p) {
   need(p->q.rows <= INT32_MAX, "more than INT32_MAX rows");
 }
 
+// A pointer that is NULL or a multiple of its type's size.
+void need_aligned(const void* p, int size, const char* what) {
+  need(reinterpret_cast<uintptr_t>(p) % size == 0, what);
+}
+
+int entry_size(const sync_norm_rope* p) { return p->dtype == SYNC_FP32 ? 4 : 2; }
+
 NormTensor norm_tensor(const sync_rows* t, const sync_norm_rope* p, const char* what) {
   need(t, what);
   need(t->rows == p->q.rows, "every tensor must have the rows of q");
   need(t->data || t->rows == 0, what);
-  need(reinterpret_cast<uintptr_t>(t->data) % (p->dtype == SYNC_FP32 ? 4 : 2) == 0, "a tensor is not aligned to its type");
+  need_aligned(t->data, entry_size(p), "a tensor is not aligned to its type");
   NormTensor r;
   r.data = t->data;
   r.row = t->row_stride;
@@ -109,6 +122,11 @@ NormArgs norm_args(const sync_norm_rope* p) {
   NormArgs a;
   need(p->rotated == 0 || p->q.rows == 0 || (p->cos && p->sin), "cos and sin must not be NULL");
   need(p->n_positions >= 0, "n_positions must not be negative");
+  need_aligned(p->q_weight, entry_size(p), "q_weight is not aligned to its type");
+  need_aligned(p->k_weight, entry_size(p), "k_weight is not aligned to its type");
+  need_aligned(p->cos, 4, "cos is not aligned to its type");
+  need_aligned(p->sin, 4, "sin is not aligned to its type");
+  need_aligned(p->positions, 4, "positions is not aligned to its type");
   a.dtype = p->dtype;
   a.heads = p->heads;
   a.kv_heads = p->kv_heads;
@@ -126,9 +144,6 @@ NormArgs norm_args(const sync_norm_rope* p) {
   a.cos = p->cos;
   a.sin = p->sin;
   a.positions = p->positions;
-  int device = 0;
-  cuda(cudaGetDevice(&device), "cudaGetDevice");
-  a.num_sms = sm_count(device);
   return a;
 }
 
@@ -529,6 +544,7 @@ sync_status sync_qk_norm_rope(const sync_norm_rope* p, const sync_rows* q_out, c
     NormArgs a = norm_args(p);
     a.q_out = norm_tensor(q_out, p, "q_out must not be NULL");
     a.k_out = norm_tensor(k_out, p, "k_out must not be NULL");
+    a.num_sms = current_sms();
     cuda(launch_norm_rope(a, static_cast<cudaStream_t>(stream)), "sync_qk_norm_rope");
   });
 }
@@ -537,9 +553,7 @@ sync_status sync_qk_norm_rope_workspace(const sync_norm_rope* p, int64_t* bytes)
   return guarded([&] {
     check_norm(p);
     need(bytes, "bytes must not be NULL");
-    int device = 0;
-    cuda(cudaGetDevice(&device), "cudaGetDevice");
-    *bytes = norm_workspace(p, sm_count(device));
+    *bytes = norm_workspace(p, current_sms());
   });
 }
 
@@ -555,6 +569,9 @@ sync_status sync_qk_norm_rope_backward(const sync_norm_rope* p, const sync_rows*
     a.dq = norm_tensor(dq, p, "dq must not be NULL");
     a.dk = norm_tensor(dk, p, "dk must not be NULL");
     need(!p->q_weight == !dq_weight && !p->k_weight == !dk_weight, "a weight and its gradient must both be given or both be NULL");
+    need_aligned(dq_weight, entry_size(p), "dq_weight is not aligned to its type");
+    need_aligned(dk_weight, entry_size(p), "dk_weight is not aligned to its type");
+    a.num_sms = current_sms();
     need(workspace && workspace_bytes >= norm_workspace(p, a.num_sms) && reinterpret_cast<uintptr_t>(workspace) % 16 == 0,
          "the workspace is NULL, too small or not 16-byte aligned");
     a.q_weight_grad = dq_weight;
@@ -647,6 +664,7 @@ sync_status sync_attn_forward(const sync_attn* plan, const sync_rows* q, const s
   return guarded([&] {
     need(plan, "plan must not be NULL");
     need(std::isfinite(scale) && scale > 0.f, "scale must be positive and finite");
+    need_aligned(lse, 4, "lse is not aligned to its type");
     AttnArgs a = plan->args;
     a.scale = scale;
     a.q = attn_tensor(q, plan->sz.q_rows, "q must not be NULL");
@@ -677,6 +695,7 @@ sync_status sync_attn_backward(const sync_attn* plan, const sync_rows* q, const 
     need(plan->train, "the plan was made without train set");
     need(std::isfinite(scale) && scale > 0.f, "scale must be positive and finite");
     need(lse || plan->sz.q_rows == 0, "lse must not be NULL");
+    need_aligned(lse, 4, "lse is not aligned to its type");
     AttnArgs a = plan->args;
     a.scale = scale;
     a.q = attn_tensor(q, plan->sz.q_rows, "q must not be NULL");

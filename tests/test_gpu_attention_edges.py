@@ -60,3 +60,21 @@ def test_gradients_wait_for_the_call_before(sg):
         assert int(torch.count_nonzero(a)) == 0 and int(torch.count_nonzero(b)) == 0
     plan.close()
     keys.close()
+
+
+def test_lse_off_its_type(sg):
+    """Through the C calls: a misaligned lse is refused before any launch."""
+    A = sg.attention
+    q, k, v = normal(1, 5, 4, 64), normal(2, 5, 2, 64), normal(3, 5, 2, 64)
+    plan = sg.sync_attn_plan([5], [5], 4, 2, 64, torch.bfloat16, train=True)
+    room = torch.empty(64, device="cuda")
+    stream = torch.cuda.current_stream().cuda_stream
+
+    def rows(t):
+        return A.Rows(t.data_ptr(), t.shape[0], t.stride(0), t.stride(1))
+    before = sg.kernel_launches()
+    bad = room.data_ptr() + 2
+    assert sg.lib().sync_attn_forward(plan.handle, rows(q), rows(k), rows(v), 0.1, rows(q.clone()), bad, stream) == sg.ERR_ARG
+    assert sg.lib().sync_attn_backward(plan.handle, rows(q), rows(k), rows(v), rows(q), bad, rows(q), 0.1, rows(q.clone()), rows(k.clone()), rows(v.clone()), stream) == sg.ERR_ARG
+    assert "lse" in sg.lib().sync_last_error().decode() and sg.kernel_launches() == before
+    plan.close()
