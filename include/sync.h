@@ -496,7 +496,8 @@ void sync_free_programs(sync_programs *h);
  * strides in elements; the entries of one head are contiguous.  Calls run
  * asynchronously on `stream`; arguments are checked on the host before
  * anything is launched, every pointer for its type's alignment among them.
- * Results are deterministic: every sum has a fixed
+ * Inputs may repeat a row or a head in the norms (a stride of 0), outputs may
+ * not.  Results are deterministic: every sum has a fixed
  * order, no result depends on which block ran first. */
 
 typedef enum { SYNC_BF16 = 0, SYNC_FP16 = 1, SYNC_FP32 = 2 } sync_dtype;

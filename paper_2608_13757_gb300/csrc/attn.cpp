@@ -118,6 +118,14 @@ NormTensor norm_tensor(const sync_rows* t, const sync_norm_rope* p, const char* 
   return r;
 }
 
+// Inputs may repeat a row or a head (a stride of 0); outputs may not, since
+// warps in no order would write it.
+NormTensor norm_output(const sync_rows* t, const sync_norm_rope* p, int32_t heads, const char* what) {
+  const NormTensor r = norm_tensor(t, p, what);
+  need((t->rows <= 1 || r.row) && (heads <= 1 || r.head), "an output's rows and heads must not share memory");
+  return r;
+}
+
 NormArgs norm_args(const sync_norm_rope* p) {
   NormArgs a;
   need(p->rotated == 0 || p->q.rows == 0 || (p->cos && p->sin), "cos and sin must not be NULL");
@@ -542,8 +550,8 @@ sync_status sync_qk_norm_rope(const sync_norm_rope* p, const sync_rows* q_out, c
   return guarded([&] {
     check_norm(p);
     NormArgs a = norm_args(p);
-    a.q_out = norm_tensor(q_out, p, "q_out must not be NULL");
-    a.k_out = norm_tensor(k_out, p, "k_out must not be NULL");
+    a.q_out = norm_output(q_out, p, p->heads, "q_out must not be NULL");
+    a.k_out = norm_output(k_out, p, p->kv_heads, "k_out must not be NULL");
     a.num_sms = current_sms();
     cuda(launch_norm_rope(a, static_cast<cudaStream_t>(stream)), "sync_qk_norm_rope");
   });
@@ -566,8 +574,8 @@ sync_status sync_qk_norm_rope_backward(const sync_norm_rope* p, const sync_rows*
     a.grad = true;
     a.q_out = norm_tensor(dq_out, p, "dq_out must not be NULL");
     a.k_out = norm_tensor(dk_out, p, "dk_out must not be NULL");
-    a.dq = norm_tensor(dq, p, "dq must not be NULL");
-    a.dk = norm_tensor(dk, p, "dk must not be NULL");
+    a.dq = norm_output(dq, p, p->heads, "dq must not be NULL");
+    a.dk = norm_output(dk, p, p->kv_heads, "dk must not be NULL");
     need(!p->q_weight == !dq_weight && !p->k_weight == !dk_weight, "a weight and its gradient must both be given or both be NULL");
     need_aligned(dq_weight, entry_size(p), "dq_weight is not aligned to its type");
     need_aligned(dk_weight, entry_size(p), "dk_weight is not aligned to its type");

@@ -42,3 +42,12 @@ def test_pointers_off_their_type(sg, field, address, dtype):
 def test_weight_gradients_off_their_type(sg, name, address, dtype):
     assert backward(sg, description(sg, dtype), **{name: address}) == sg.ERR_ARG
     assert "aligned" in sg.lib().sync_last_error().decode()
+
+
+@pytest.mark.parametrize("name,rows", [("q", (256, 5, 0, 64)), ("k", (256, 5, 0, 64)), ("q", (256, 5, 256, 0)), ("k", (256, 5, 128, 0))])
+def test_outputs_that_share_memory(sg, name, rows):
+    p = description(sg)
+    assert forward(sg, p, **{name + "_out": rows}) == sg.ERR_ARG
+    assert "share" in sg.lib().sync_last_error().decode()
+    assert backward(sg, p, **{"d" + name: rows}) == sg.ERR_ARG
+    assert "share" in sg.lib().sync_last_error().decode()
