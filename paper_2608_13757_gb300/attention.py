@@ -244,7 +244,12 @@ def sync_attn_plan(q_lens, k_lens, heads: int, kv_heads: int, head_dim: int, dty
     k_lens[i] tokens whose keys it attends to, causally.  Starts are rows of the
     query and key tensors (None: packed without gaps)."""
     import torch
-    index = torch.cuda.current_device() if device is None else device if isinstance(device, int) else torch.device(device).index
+    index = device if device is None or isinstance(device, int) else torch.device(device)
+    if isinstance(index, torch.device):
+        _need(index.type == "cuda", f"device must be a GPU, not {index}")
+        index = index.index
+    if index is None:
+        index = torch.cuda.current_device()
     arrays = []
     for v, kind, name in ((q_lens, np.int32, "q_lens"), (k_lens, np.int32, "k_lens"), (q_starts, np.int64, "q_starts"),
                           (k_starts, np.int64, "k_starts")):

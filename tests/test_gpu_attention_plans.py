@@ -61,3 +61,12 @@ def test_dropped_plans_are_freed_by_the_next_one(sg):
         plan = make()
     assert torch.cuda.mem_get_info()[0] > free - (64 << 20)
     plan.close()
+
+
+@pytest.mark.parametrize("device", [None, 0, "cuda", "cuda:0", torch.device("cuda"), torch.device("cuda", 0)], ids=str)
+def test_names_of_a_device(sg, device):
+    plan = sg.sync_attn_plan([3], [3], 4, 2, 64, torch.bfloat16, device=device)
+    assert plan.device == torch.device("cuda", 0)
+    x = torch.ones(3, 4, 64, device="cuda", dtype=torch.bfloat16)
+    assert torch.equal(sg.sync_attn_forward(plan, x, x[:, :2], x[:, :2]), x)
+    plan.close()
