@@ -256,7 +256,10 @@ def sync_attn_plan(q_lens, k_lens, heads: int, kv_heads: int, head_dim: int, dty
         if v is None:
             arrays.append(None)
             continue
-        w = np.asarray(v, dtype=np.int64)
+        given = np.asarray(v)
+        if given.dtype.kind == "f":
+            _need(bool(np.all(np.isfinite(given) & (given == np.floor(given)))), f"{name} must be whole numbers")
+        w = given.astype(np.int64)
         _need(w.ndim == 1 and len(w) == len(q_lens), f"{name} must have one entry per sequence")
         _need(kind is np.int64 or w.size == 0 or (w.min() >= -1 << 31 and w.max() < 1 << 31), f"{name} must fit 32 bits")
         arrays.append(np.ascontiguousarray(w, dtype=kind))
