@@ -55,13 +55,32 @@ sync_status guarded(F&& f) {
   }
 }
 
+// A function of the driver, or null.
+template <class F>
+F driver_function(const char* name, unsigned version) {
+  void* p = nullptr;
+  cudaDriverEntryPointQueryResult r;
+  if (cudaGetDriverEntryPointByVersion(name, &p, version, cudaEnableDefault, &r) != cudaSuccess || r != cudaDriverEntryPointSuccess)
+    p = nullptr;
+  return reinterpret_cast<F>(p);
+}
+
+// Whether this thread has a context.  One that has made no call of the runtime
+// yet has none (a framework's backward pass runs on such threads), and encoding
+// a tile map needs one, which it does not make itself.
+bool has_context() {
+  static const auto f = driver_function<decltype(&cuCtxGetCurrent)>("cuCtxGetCurrent", 4000);
+  CUcontext c = nullptr;
+  return f && f(&c) == CUDA_SUCCESS && c;
+}
+
 // The device that a call works on, set for its duration.
 class DeviceScope {
  public:
   explicit DeviceScope(int device) {
     cuda(cudaGetDevice(&was_), "cudaGetDevice");
-    if (was_ != device) cuda(cudaSetDevice(device), "cudaSetDevice");
     set_ = was_ != device;
+    if (set_ || !has_context()) cuda(cudaSetDevice(device), "cudaSetDevice");
   }
   ~DeviceScope() {
     if (set_) cudaSetDevice(was_);
@@ -228,17 +247,8 @@ AttnTensor attn_tensor(const sync_rows* t, int64_t rows, const char* what) {
   return r;
 }
 
-using EncodeTiled = decltype(&cuTensorMapEncodeTiled);
-
-EncodeTiled encode_tiled() {
-  static const EncodeTiled f = [] {
-    void* p = nullptr;
-    cudaDriverEntryPointQueryResult r;
-    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &r) != cudaSuccess ||
-        r != cudaDriverEntryPointSuccess)
-      p = nullptr;
-    return reinterpret_cast<EncodeTiled>(p);
-  }();
+auto encode_tiled() {
+  static const auto f = driver_function<decltype(&cuTensorMapEncodeTiled)>("cuTensorMapEncodeTiled", 12000);
   if (!f) fail(SYNC_ERR_CUDA, "the driver has no cuTensorMapEncodeTiled");
   return f;
 }
