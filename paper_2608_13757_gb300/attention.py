@@ -7,10 +7,15 @@ strides on.  Tensors are ``[rows, heads, dim]`` with the last dimension
 contiguous; outputs are new contiguous tensors unless given.  Calls run on
 the current stream, or on ``stream``; outputs that a call allocates belong to
 the stream it runs on.
+
+Nothing is recorded for autograd: outputs carry no gradient, and the gradients
+are calls of their own.  A forward call warns of inputs that require one while
+gradients are recorded.
 """
 from __future__ import annotations
 
 import ctypes
+import warnings
 
 import numpy as np
 
@@ -74,6 +79,14 @@ def _code(dtype) -> int:
 def _need(ok, what):
     if not ok:
         raise _sg.SyncError(_sg.ERR_ARG, what)
+
+
+def _not_recorded(name):
+    """Says that a call drops the gradient that an input of it requires."""
+    import torch
+    if torch.is_grad_enabled():
+        warnings.warn(f"{name} records nothing for autograd: its outputs carry no gradient to the inputs that require one "
+                      f"(use {name.replace('_forward', '')}_backward, and torch.no_grad() around this call)", stacklevel=3)
 
 
 def _current_stream(device: int) -> int:
@@ -155,6 +168,9 @@ def sync_qk_norm_rope(q, k, q_weight, k_weight, cos, sin, positions=None, eps: f
     if torch.cuda.current_device() != device:
         with torch.cuda.device(device):
             return sync_qk_norm_rope(q, k, q_weight, k_weight, cos, sin, positions, eps, interleaved, out)
+    if q.requires_grad or k.requires_grad or q_weight is not None and q_weight.requires_grad or \
+            k_weight is not None and k_weight.requires_grad:
+        _not_recorded("sync_qk_norm_rope")
     if out is None:
         where = q.device
         out = torch.empty(q.shape, dtype=dtype, device=where), torch.empty(k.shape, dtype=dtype, device=where)
@@ -297,6 +313,8 @@ def sync_attn_forward(plan: AttnPlan, q, k, v, scale: float | None = None, out=N
     dtype, device, heads, kv, dim = plan.dtype, plan.index, plan.heads, plan.kv_heads, plan.head_dim
     a = (_rows(q, "q", dtype, device, heads, dim), _rows(k, "k", dtype, device, kv, dim),
          _rows(v, "v", dtype, device, kv, dim))
+    if q.requires_grad or k.requires_grad or v.requires_grad:
+        _not_recorded("sync_attn_forward")
     n = q.shape[0]
     if out is None:
         out = _new(n, heads, plan, plan.n_queries)
