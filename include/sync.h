@@ -609,9 +609,11 @@ sync_status sync_attn_status(const sync_attn *plan);
  * each row's sum of exponentials (-inf for a query that sees no key).
  * Products are summed in 32 bits, the softmax's maximum and sum are held in
  * 32 bits, and its unnormalised weights are rounded to dtype for the second
- * product.  Keys and values of other sequences never reach a row, whatever
- * they hold; within a sequence, a NaN or an infinity in the value of a key
- * may reach earlier queries too. */
+ * product.  Scores, scale * q k^T, stay below 2^27 in size (above it, half a
+ * unit in the last place of a score is a factor that the weights may not hold).
+ * Keys and values of other sequences never reach a row, whatever they hold;
+ * within a sequence, a NaN or an infinity in the value of a key may reach
+ * earlier queries too. */
 sync_status sync_attn_forward(const sync_attn *plan, const sync_rows *q, const sync_rows *k,
                               const sync_rows *v, float scale, const sync_rows *o, float *lse,
                               void *stream);
@@ -619,8 +621,16 @@ sync_status sync_attn_forward(const sync_attn *plan, const sync_rows *q, const s
 /* Gradients of sync_attn_forward for a plan with train set, from its inputs,
  * its outputs o and lse, and o's gradient d_o.  dq is written for every query
  * row, dk and dv (summed over the query heads of their key head) for every
- * key row of the sequences.  The weights and their gradients are rounded to
- * dtype for the products, sums are held in 32 bits. */
+ * key row of the sequences.  Sums are held in 32 bits.  The weights, recomputed
+ * from lse (a relative error of about 2^-23 |lse|), and their gradients
+ * dS = P (d_o v^T - rowsum(o d_o)) are rounded to dtype for the products, and o
+ * is what the forward call rounded.  So in SYNC_FP16 entries of dS below 2^-14
+ * lose bits and those above 65504 overflow.  The gradients are linear in d_o:
+ * scale it, as the loss of fp16 training usually is, to keep dS (|d_o| |v| times
+ * a weight, about one over the keys seen) inside that range.  Rows of q and d_o of
+ * other sequences never reach a gradient; within a sequence, a NaN or an
+ * infinity in one, also of a query that sees no key, may reach the gradient of
+ * any key. */
 sync_status sync_attn_backward(const sync_attn *plan, const sync_rows *q, const sync_rows *k,
                                const sync_rows *v, const sync_rows *o, const float *lse,
                                const sync_rows *d_o, float scale, const sync_rows *dq,

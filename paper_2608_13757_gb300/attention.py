@@ -6,7 +6,8 @@ has that a pointer does not (device, type, shape), allocate outputs and pass
 strides on.  Tensors are ``[rows, heads, dim]`` with the last dimension
 contiguous; outputs are new contiguous tensors unless given.  Calls run on
 the current stream, or on ``stream``; outputs that a call allocates belong to
-the stream it runs on.
+the stream it runs on.  Inputs that belong to another one are the caller's to
+order and to keep until the call is done (``Tensor.record_stream``).
 
 Nothing is recorded for autograd: outputs carry no gradient, and the gradients
 are calls of their own.  A forward call warns of inputs that require one while

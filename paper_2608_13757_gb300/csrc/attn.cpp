@@ -415,6 +415,10 @@ ForwardWork forward_work(const sync_attn_desc* d, const std::vector<AttnSeq>& se
 
 // Tiles of the gradients' two walks: key tiles with the query tiles that see
 // them, over all heads of their group, and query tiles with the keys they see.
+// These are not cut: the fullest block of the key walk has at least the steps of the
+// first key tile of the longest sequence, for the whole group, which leaves SMs idle
+// where key tiles and key heads are few (8192 tokens, 16 heads on 1 key head:
+// 1024 steps where the mean is 219, a gradient of 1.47 ms against 0.86 on 2).
 void gradient_work(const sync_attn_desc* d, const std::vector<AttnSeq>& seq, std::vector<Draft<AttnTile>>& q,
                    std::vector<Draft<AttnTile>>& k) {
   const int64_t group = d->heads / d->kv_heads;

@@ -236,7 +236,9 @@ __device__ __forceinline__ void weight_gradients(float* d, const float* p, const
     pair_split(mul2(pair_bits(p[e + 2], p[e + 3]), add2(pair_bits(d[e + 2], d[e + 3]), l.y)), d[e + 2], d[e + 3]);
   }
 }
-// 64 values rounded to 16 bits, to tensor memory.
+// 64 values rounded to 16 bits, to tensor memory: P and dS, each rounded once as
+// an operand of the next product.  float16 holds dS in steps of 2^-24 at the
+// least and up to 65504; the caller scales d_o (include/sync.h).
 template <bool BF16>
 __device__ __forceinline__ void put(uint32_t addr, const float* x) {
   uint32_t y[32];
@@ -595,7 +597,11 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dq(const __grid_constant__
   after_previous();                                          // no later kernel overtakes the key walk
 }
 
-// delta of every row and head, eight entries per lane; LANES lanes a head.
+// delta of every row and head, eight entries per lane; LANES lanes a head.  It
+// is of the rounded output, the one that the forward pass leaves: an unrounded
+// copy would be twice its bytes, and rowsum(P dP), which equals it, a third walk.
+// Its error is shared by a row's dS: in bf16 dq is off by 3.2e-3 at 8 keys and
+// 2.5e-3 at 1024 where rounding dq alone takes 1.7e-3.
 // Bound by memory: 8192 rows of 32 heads of 128 take 24 us (5.6 TB/s).
 template <int LANES, bool BF16>
 __global__ void __launch_bounds__(256) k_attn_delta(const __grid_constant__ AttnArgs a) {

@@ -20,8 +20,9 @@
 // twice at 4096 a cycle), which is also what shared memory takes to deliver
 // their operands and to receive the next tiles (128 KB at 128 bytes a cycle),
 // and 512 of exponentials.  Measured on 8192 tokens, 32 heads of 128: 370 us,
-// 1490 TFLOP/s of the visible pairs, 1550 cycles a pair of tiles, the tensor
-// pipe busy 66% of them; the rest is the way from a tile's scores to its
+// 1490 TFLOP/s of the visible pairs (alone; 397 when passes follow one another
+// and the power limit holds), 1550 cycles a pair of tiles, the tensor pipe busy
+// 66% of them; the rest is the way from a tile's scores to its
 // weights (700 cycles of exponentials of one row per thread, 100 for the
 // scores, barriers on both sides) where the other query tile's products do
 // not cover it.  Half a row per thread on twice the warps took 414 us, whole
@@ -267,6 +268,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_fwd(const __grid_constant_
 #pragma unroll
         for (int c = 0; c < kTile; c += 32) tmem_ld32(S + c, x + c);
         wait_ld();
+        // (The weights are rounded to the operands' type, which is what the
+        // second product takes; their sum is of the unrounded ones.)
         // The weights of the first half with the maximum known so far, while
         // the tile's own is found (the one keeps the special function unit
         // busy, the other the integer unit).
