@@ -251,7 +251,7 @@ class AttnPlan:
 
     def __del__(self):
         h, self._h = getattr(self, "_h", None), None
-        if h:
+        if h and _dropped is not None:      # (None while the interpreter ends)
             _dropped.append(h)
 
 

@@ -70,3 +70,18 @@ def test_names_of_a_device(sg, device):
     x = torch.ones(3, 4, 64, device="cuda", dtype=torch.bfloat16)
     assert torch.equal(sg.sync_attn_forward(plan, x, x[:, :2], x[:, :2]), x)
     plan.close()
+
+
+def test_a_plan_at_the_interpreter_s_end(sg):
+    """A plan that is still there when the program ends leaves quietly."""
+    import os
+    import subprocess
+    import sys
+    code = ("import torch, paper_2608_13757_gb300 as sg\n"
+            "class Holder: pass\n"
+            "h = Holder(); h.me = h\n"
+            "h.plan = sg.sync_attn_plan([3], [3], 4, 2, 64, torch.bfloat16)\n"
+            "sys = __import__('sys'); sys.keep = sg.sync_attn_plan([3], [3], 4, 2, 64, torch.bfloat16)\n")
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-c", code], cwd=root, capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0 and "ignored" not in r.stderr, r.stderr
