@@ -590,6 +590,15 @@ typedef struct sync_attn sync_attn;   /* opaque; owns device memory */
  * SYNC_ERR_OVERFLOW for rows past INT32_MAX. */
 sync_status sync_attn_plan(const sync_attn_desc *desc, int device, sync_attn **out);
 
+/* The same for attention to the states of another sequence, as a decoder's to
+ * its encoder's: query and key lengths have nothing to do with one another, and
+ * every query of a sequence sees all k_len[i] keys of it (none where k_len[i]
+ * is 0).  Sequences that share their keys (several decoders of one encoder's
+ * states) give the same k_start, unless train is set.  The plan serves the same
+ * calls; it depends on the lengths alone, so one serves every step of decoding
+ * against the same states. */
+sync_status sync_cross_attn_plan(const sync_attn_desc *desc, int device, sync_attn **out);
+
 sync_status sync_attn_query(const sync_attn *plan, sync_attn_sizes *out);
 
 /* Whether a kernel of this plan has given up.  The kernels' warps wait for one

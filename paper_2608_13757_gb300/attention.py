@@ -1,5 +1,6 @@
 """Operators of an attention block: head norms with the position rotation, and
-causal attention over packed sequences, each with its gradient.
+attention over packed sequences, causal or to another sequence's states, each
+with its gradient.
 
 Thin wrappers over the calls of ``include/sync.h``: they check what a tensor
 has that a pointer does not (device, type, shape), allocate outputs and pass
@@ -60,6 +61,7 @@ def declare(lib: ctypes.CDLL):
     lib.sync_qk_norm_rope_workspace.argtypes = [P(NormRope), P(ctypes.c_int64)]
     lib.sync_qk_norm_rope_backward.argtypes = [P(NormRope), rows, rows, rows, rows, vp, vp, vp, ctypes.c_int64, vp]
     lib.sync_attn_plan.argtypes = [P(AttnDesc), ctypes.c_int, P(vp)]
+    lib.sync_cross_attn_plan.argtypes = lib.sync_attn_plan.argtypes
     lib.sync_attn_query.argtypes = [vp, P(AttnSizes)]
     lib.sync_attn_status.argtypes = [vp]
     lib.sync_attn_forward.argtypes = [vp, rows, rows, rows, ctypes.c_float, rows, vp, vp]
@@ -256,10 +258,11 @@ class AttnPlan:
 
 
 def sync_attn_plan(q_lens, k_lens, heads: int, kv_heads: int, head_dim: int, dtype, q_starts=None, k_starts=None,
-                   train: bool = False, device=None) -> AttnPlan:
+                   train: bool = False, device=None, causal: bool = True) -> AttnPlan:
     """Plan of a packed batch: sequence i has q_lens[i] queries, the last of the
     k_lens[i] tokens whose keys it attends to, causally.  Starts are rows of the
-    query and key tensors (None: packed without gaps)."""
+    query and key tensors (None: packed without gaps).  causal=False: the keys are
+    of another sequence (an encoder's states), every query sees all of them."""
     import torch
     index = device if device is None or isinstance(device, int) else torch.device(device)
     if isinstance(index, torch.device):
@@ -293,7 +296,8 @@ def sync_attn_plan(q_lens, k_lens, heads: int, kv_heads: int, head_dim: int, dty
     except IndexError:                      # none left (another thread may have taken the last)
         pass
     h = ctypes.c_void_p()
-    _sg._check(_sg.lib().sync_attn_plan(ctypes.byref(d), index, ctypes.byref(h)))
+    make = _sg.lib().sync_attn_plan if causal else _sg.lib().sync_cross_attn_plan
+    _sg._check(make(ctypes.byref(d), index, ctypes.byref(h)))
     return AttnPlan(h, torch.device("cuda", index), heads, kv_heads, head_dim, dtype)
 
 
@@ -305,7 +309,7 @@ def _new(rows, heads, plan, covered):
 
 
 def sync_attn_forward(plan: AttnPlan, q, k, v, scale: float | None = None, out=None, lse=False, stream=None):
-    """Causal attention of a planned batch.  With lse=True (or a float32 tensor
+    """Attention of a planned batch.  With lse=True (or a float32 tensor
     [heads, rows of q] to write) returns (o, lse), as the gradient needs."""
     import torch
     if stream is not None:

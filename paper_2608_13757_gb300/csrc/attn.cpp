@@ -194,7 +194,9 @@ struct AttnSeq {
   int32_t lq, lk;
 };
 
-std::vector<AttnSeq> sequences(const sync_attn_desc* d, sync_attn_sizes& sz) {
+// Queries see the keys of their sequence up to their own place, or (not
+// causal) all of them.
+std::vector<AttnSeq> sequences(const sync_attn_desc* d, bool causal, sync_attn_sizes& sz) {
   std::vector<AttnSeq> seq((size_t)d->n_seqs);
   int64_t q = 0, k = 0;
   for (int32_t i = 0; i < d->n_seqs; ++i) {
@@ -215,7 +217,7 @@ std::vector<AttnSeq> sequences(const sync_attn_desc* d, sync_attn_sizes& sz) {
     sz.n_queries += s.lq;
     sz.n_keys += s.lk;
     const int64_t seeing = std::min(s.lq, s.lk);
-    sz.pairs += seeing * (s.lk - seeing) + seeing * (seeing + 1) / 2;
+    sz.pairs += causal ? seeing * (s.lk - seeing) + seeing * (seeing + 1) / 2 : (int64_t)s.lq * s.lk;
   }
   // ranges of rows that are written must be disjoint
   auto disjoint = [&](int64_t AttnSeq::*start, int32_t AttnSeq::*len, const char* what) {
@@ -371,7 +373,7 @@ bool cut(const std::vector<Draft<AttnItem>>& all, int group, int num_sms, int64_
   return true;
 }
 
-ForwardWork forward_work(const sync_attn_desc* d, const std::vector<AttnSeq>& seq, int num_sms) {
+ForwardWork forward_work(const sync_attn_desc* d, bool causal, const std::vector<AttnSeq>& seq, int num_sms) {
   const int group = d->heads / d->kv_heads;
   std::vector<Draft<AttnItem>> draft;
   int64_t total = 0;
@@ -385,12 +387,12 @@ ForwardWork forward_work(const sync_attn_desc* d, const std::vector<AttnSeq>& se
         it.k_row = s.k0;
         it.head = h;
         it.packed = packed;
-        it.seen = (int32_t)(q0 + s.lk - s.lq + 1);
+        it.seen = causal ? (int32_t)(q0 + s.lk - s.lq + 1) : s.lk;
         it.keys = s.lk;
         it.slot = -1;
         for (int t = 0; t < 2; ++t) {
           it.rows[t] = (int32_t)std::max<int64_t>(0, std::min<int64_t>(per, s.lq - q0 - t * per));
-          const int64_t most = (int64_t)it.seen + t * per + it.rows[t] - 1;      // keys that the last query sees
+          const int64_t most = std::min<int64_t>((int64_t)it.seen + t * per + it.rows[t] - 1, s.lk);   // keys that the last query sees
           it.n[t] = it.rows[t] && most > 0 ? (int32_t)((most + kTile - 1) / kTile) : 0;
         }
         draft.push_back({it, it.n[0] + it.n[1] + kItemCost});
@@ -419,7 +421,7 @@ ForwardWork forward_work(const sync_attn_desc* d, const std::vector<AttnSeq>& se
 // first key tile of the longest sequence, for the whole group, which leaves SMs idle
 // where key tiles and key heads are few (8192 tokens, 16 heads on 1 key head:
 // 1024 steps where the mean is 219, a gradient of 1.47 ms against 0.86 on 2).
-void gradient_work(const sync_attn_desc* d, const std::vector<AttnSeq>& seq, std::vector<Draft<AttnTile>>& q,
+void gradient_work(const sync_attn_desc* d, bool causal, const std::vector<AttnSeq>& seq, std::vector<Draft<AttnTile>>& q,
                    std::vector<Draft<AttnTile>>& k) {
   const int64_t group = d->heads / d->kv_heads;
   for (const AttnSeq& s : seq) {
@@ -427,26 +429,26 @@ void gradient_work(const sync_attn_desc* d, const std::vector<AttnSeq>& seq, std
     AttnTile it{};
     for (int32_t h = 0; h < d->heads; ++h)
       for (int64_t q0 = 0; q0 < s.lq; q0 += kTile) {
-        const int64_t most = std::min<int64_t>(q0 + kTile, s.lq) + offset;       // keys that the last query sees
+        const int64_t most = causal ? std::min<int64_t>(q0 + kTile, s.lq) + offset : s.lk;       // keys that the last query sees
         it.q_row = s.q0 + q0;
         it.k_row = s.k0;
         it.head = h;
         it.n = (int32_t)(most > 0 ? (most + kTile - 1) / kTile : 0);
         it.rows = (int32_t)(s.lq - q0);
         it.keys = s.lk;
-        it.seen = (int32_t)(q0 + offset + 1);
+        it.seen = causal ? (int32_t)(q0 + offset + 1) : s.lk;
         q.push_back({it, it.n + kItemCost});
       }
     for (int32_t h = 0; h < d->kv_heads; ++h)
       for (int64_t k0 = 0; k0 < s.lk; k0 += kTile) {
-        const int64_t first = std::min(tiles, std::max<int64_t>(0, k0 - offset) / kTile);   // the first tile that sees key k0
+        const int64_t first = causal ? std::min(tiles, std::max<int64_t>(0, k0 - offset) / kTile) : 0;   // the first tile that sees key k0
         it.q_row = s.q0 + first * kTile;
         it.k_row = s.k0 + k0;
         it.head = h;
         it.n = (int32_t)(tiles - first);
         it.rows = (int32_t)(s.lq - first * kTile);
         it.keys = (int32_t)(s.lk - k0);
-        it.seen = (int32_t)(first * kTile + offset + 1 - k0);
+        it.seen = causal ? (int32_t)(first * kTile + offset + 1 - k0) : kTile;   // (all of the tile)
         k.push_back({it, it.n * group + kItemCost});
       }
   }
@@ -512,18 +514,18 @@ void check_gave_up(const sync_attn* plan) {
 // 2 and 3: query and key tiles of the gradients (block, q_row, k_row, head, n,
 // rows, keys, seen).  Returns the rows (written up to `capacity`), or a
 // negative status.
-extern "C" int64_t syncgb_attn_work(const sync_attn_desc* desc, int num_sms, int which, int64_t* out, int64_t capacity) {
+static int64_t work_rows(const sync_attn_desc* desc, bool causal, int num_sms, int which, int64_t* out, int64_t capacity) {
   int64_t n = 0;
   const sync_status status = guarded([&] {
     check_attn(desc);
     sync_attn_sizes sz{};
-    const std::vector<AttnSeq> seq = sequences(desc, sz);
+    const std::vector<AttnSeq> seq = sequences(desc, causal, sz);
     auto row = [&](std::initializer_list<int64_t> v) {
       if (n < capacity) std::copy(v.begin(), v.end(), out + n * (int64_t)v.size());
       ++n;
     };
     if (which < 2) {
-      const ForwardWork w = forward_work(desc, seq, num_sms);
+      const ForwardWork w = forward_work(desc, causal, seq, num_sms);
       if (which == 1) {
         for (const AttnSplit& s : w.split) row({s.q_row, s.head, s.packed, s.rows[0], s.rows[1], s.slot, s.pieces});
         return;
@@ -536,7 +538,7 @@ extern "C" int64_t syncgb_attn_work(const sync_attn_desc* desc, int num_sms, int
       return;
     }
     std::vector<Draft<AttnTile>> q, k;
-    gradient_work(desc, seq, q, k);
+    gradient_work(desc, causal, seq, q, k);
     std::vector<AttnTile> tile;
     std::vector<int32_t> first;
     assign(which == 2 ? q : k, num_sms, tile, first);
@@ -547,6 +549,12 @@ extern "C" int64_t syncgb_attn_work(const sync_attn_desc* desc, int num_sms, int
       }
   });
   return status == SYNC_OK ? n : -(int64_t)status;
+}
+extern "C" int64_t syncgb_attn_work(const sync_attn_desc* desc, int num_sms, int which, int64_t* out, int64_t capacity) {
+  return work_rows(desc, true, num_sms, which, out, capacity);
+}
+extern "C" int64_t syncgb_cross_attn_work(const sync_attn_desc* desc, int num_sms, int which, int64_t* out, int64_t capacity) {
+  return work_rows(desc, false, num_sms, which, out, capacity);
 }
 
 // For tests: a kernel of the plan whose waits run out after `tries` tries.
@@ -603,13 +611,13 @@ sync_status sync_qk_norm_rope_backward(const sync_norm_rope* p, const sync_rows*
   });
 }
 
-sync_status sync_attn_plan(const sync_attn_desc* desc, int device, sync_attn** out) {
+static sync_status make_plan(const sync_attn_desc* desc, bool causal, int device, sync_attn** out) {
   return guarded([&] {
     need(out, "out must not be NULL");
     *out = nullptr;
     check_attn(desc);
     sync_attn_sizes sz{};
-    const std::vector<AttnSeq> seq = sequences(desc, sz);
+    const std::vector<AttnSeq> seq = sequences(desc, causal, sz);
     DeviceScope scope(device);
     std::unique_ptr<sync_attn, void (*)(sync_attn*)> P(new sync_attn, sync_attn_free);
     P->device = device;
@@ -621,13 +629,13 @@ sync_status sync_attn_plan(const sync_attn_desc* desc, int device, sync_attn** o
     a.kv_heads = desc->kv_heads;
     a.dim = desc->head_dim;
     a.num_sms = P->num_sms;
-    const ForwardWork w = forward_work(desc, seq, P->num_sms);
+    const ForwardWork w = forward_work(desc, causal, seq, P->num_sms);
     a.n_blocks = (int)w.block_first.size() - 1;
     std::vector<AttnTile> qt, kt;
     std::vector<int32_t> q_first, k_first;
     if (P->train) {
       std::vector<Draft<AttnTile>> q, k;
-      gradient_work(desc, seq, q, k);
+      gradient_work(desc, causal, seq, q, k);
       assign(q, P->num_sms, qt, q_first);
       assign(k, P->num_sms, kt, k_first);
       a.n_q_blocks = (int)q_first.size() - 1;
@@ -665,6 +673,14 @@ sync_status sync_attn_plan(const sync_attn_desc* desc, int device, sync_attn** o
     P->sz = sz;
     *out = P.release();
   });
+}
+
+sync_status sync_attn_plan(const sync_attn_desc* desc, int device, sync_attn** out) {
+  return make_plan(desc, true, device, out);
+}
+
+sync_status sync_cross_attn_plan(const sync_attn_desc* desc, int device, sync_attn** out) {
+  return make_plan(desc, false, device, out);
 }
 
 sync_status sync_attn_query(const sync_attn* plan, sync_attn_sizes* out) {

@@ -557,7 +557,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dq(const __grid_constant__
       }
 #pragma unroll 1
       for (int j = 0; j < steps; ++j, ++n) {
-        const int seen = first_seen + r - j * kTile - c0;                // keys of this half that the row sees
+        const int seen = min(first_seen + r, keys) - j * kTile - c0;     // keys of this half that the row sees
         const bool masked = (j + 1) * kTile > first_seen;
         if (!(ok = bar_wait(b.s_full, n & 1, a.error))) break;
         fence_after();

@@ -230,7 +230,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_fwd(const __grid_constant_
       if (i + 1 < i1) asm volatile("prefetch.global.L1 [%0];" ::"l"(at_item + 1));
       const int packed = uniform(at_item->packed), n = uniform(at_item->n[t]), keys = uniform(at_item->keys);
       const int per = packed ? packed_rows : kTile, rq = packed ? packed_q : r;
-      const int least = uniform(at_item->seen) + t * per;   // keys that the tile's first query sees
+      const int least = min(uniform(at_item->seen) + t * per, keys);   // keys that the tile's first query sees
       const int seen_all = min(least + rq, keys);            // and this row
       const bool valid = rq < at_item->rows[t], busy = __any_sync(~0u, valid);
       float m = -INFINITY, l = 0.f;
