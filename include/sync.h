@@ -649,6 +649,131 @@ sync_status sync_attn_backward(const sync_attn *plan, const sync_rows *q, const 
  * sync_free_programs does. */
 void sync_attn_free(sync_attn *plan);
 
+/* ---------------------------------------------------------------------------
+ * Rotation by positions, and a paged cache of keys and values with the
+ * attention that reads it: an attention block's work while it answers, token by
+ * token.  Conventions are those of the attention block's operators above. */
+
+/* How heads are turned.  Pair j < rotated/2 of a head (entries as in
+ * sync_norm_rope) is turned by the angle in row p, column j of the tables, where
+ * p is the token's position on the pair's axis: one axis for text, several for
+ * a video's time, height and width.  A p outside 0..n_positions-1 makes the
+ * token's heads NaN in that pair.  Products and sums are rounded to 32 bits one
+ * by one, the result once to the tensors' type. */
+typedef struct {
+  int32_t rotated;            /* even, in 0..dim; 0: nothing is turned         */
+  int32_t interleaved;        /* 0: pairs (j, j + rotated/2); 1: (2j, 2j + 1)  */
+  int32_t n_axes;             /* 1..4                                          */
+  const uint8_t *pair_axis;   /* host, [rotated/2], each below n_axes; NULL:
+                                 axis 0 for all                                */
+  const float *cos, *sin;     /* [n_positions][rotated/2]                      */
+  int64_t n_positions;
+  const int32_t *positions;   /* row r's position on axis a is
+                                 positions[a * position_stride + r]; NULL (one
+                                 axis only): r itself, in the cache's calls the
+                                 token's place in its sequence                 */
+  int64_t position_stride;
+} sync_rotation;
+
+typedef struct {
+  int32_t dtype;              /* sync_dtype of all tensors                     */
+  int32_t heads, kv_heads, dim;   /* dim even and in 2..256                    */
+  sync_rows q, k;             /* the same number of rows                       */
+  sync_rotation turn;
+} sync_rope_desc;
+
+/* Turns every query and key head (rows and strides as given; an output may be
+ * its own input). */
+sync_status sync_rope(const sync_rope_desc *p, const sync_rows *q_out, const sync_rows *k_out, void *stream);
+
+/* Gradient of sync_rope: p's q and k are the outputs' gradients, dq and dk (which
+ * may be the same) the inputs'.  A rotation's gradient is the rotation back. */
+sync_status sync_rope_backward(const sync_rope_desc *p, const sync_rows *dq, const sync_rows *dk, void *stream);
+
+/* Keys and values of many sequences in pages of `page` tokens, caller-owned
+ * device memory, contiguous and 16-byte aligned.  16 bits:
+ *   k, v              [n_pages][kv_heads][page][head_dim] of dtype.
+ * 4 bits, with g = head_dim / 32 groups of 32 entries a row:
+ *   k, v              [n_pages][kv_heads][page][head_dim / 2] bytes,
+ *   k_scale, v_scale  [n_pages][kv_heads][page][g] float16;
+ * entry 32 w + 8 c + e (w < g, c < 4, e < 8) of a row is bits 4 e .. 4 e + 3 of
+ * its little-endian 32-bit word g c + w, and stands for (bits - 8) * scale[w].
+ * A row is written with scale = max |x| / 7 of the group, rounded to float16 (at
+ * most 65504), and bits = x / scale, rounded to even and limited to -7..7, plus
+ * 8; a group with a NaN or an infinity reads as NaN. */
+typedef struct {
+  int32_t dtype;              /* SYNC_BF16 or SYNC_FP16                        */
+  int32_t bits;               /* 16 or 4                                       */
+  int32_t kv_heads, head_dim; /* 16 bits: a multiple of 8 in 8..128; 4: of 32  */
+  int32_t page;               /* a power of two in 16..1024                    */
+  int32_t n_pages;            /* n_pages * page is at most INT32_MAX           */
+  void *k, *v, *k_scale, *v_scale;
+} sync_cache;
+
+/* The sequences of a step, all arrays on the device (nothing is read back, so a
+ * captured call follows what the arrays hold when it is replayed).  Token p of
+ * sequence s is in page page_table[s * table_stride + p / page], at p % page.
+ * lens[s] counts its tokens, the step's new ones included.  Sequence s has rows
+ * row_starts[s] .. row_starts[s + 1] - 1 of the step's tensors, its last tokens in
+ * order (row_starts does not fall, from 0 on); NULL: one row each.  Rows from
+ * row_starts[n_seqs] on belong to no sequence: padding.
+ * Pages of tokens that are written belong to one sequence; others may be shared.
+ * (A slot that one call writes twice holds either row, or parts of both.) */
+typedef struct {
+  int32_t n_seqs, max_pages;
+  const int32_t *page_table;
+  int64_t table_stride;
+  const int32_t *lens;
+  const int32_t *row_starts;
+} sync_cache_seqs;
+
+/* Writes the step's new keys, turned, and values, as they are, to the cache, and
+ * the step's queries, turned, to q_out; q and q_out may both be NULL, or be the
+ * same memory.  k, v: [rows][kv_heads][head_dim]; q: [rows][heads][head_dim].
+ * turn: NULL turns nothing.  A row whose place the table does not have (a page
+ * number outside 0..n_pages-1, a position below 0 or past max_pages) is not
+ * written.  Rows of no sequence: nothing goes to the cache; q_out keeps what it
+ * has, or (zero_rest) becomes zero. */
+sync_status sync_cache_append(const sync_cache *cache, const sync_cache_seqs *seqs, const sync_rows *k,
+                              const sync_rows *v, int32_t heads, const sync_rows *q, const sync_rows *q_out,
+                              const sync_rotation *turn, int32_t zero_rest, void *stream);
+
+/* Reads tokens back as packed rows of dtype: tokens 0, 1, .. of sequence s to
+ * rows row_starts[s] .. row_starts[s + 1] - 1 (here row_starts says where a
+ * sequence's whole context goes, and is not NULL).  Rows past a sequence's
+ * length become zero, tokens on pages that the cache does not have NaN; values of 4
+ * bits are rounded to dtype, in SYNC_FP16 to 65504 in size at most; rows of no
+ * sequence keep what they have, or (zero_rest) become zero.  Strides multiples
+ * of 8, data 16-byte aligned. */
+sync_status sync_cache_read(const sync_cache *cache, const sync_cache_seqs *seqs, const sync_rows *k,
+                            const sync_rows *v, int32_t zero_rest, void *stream);
+
+/* Bytes of device workspace (16-byte aligned, contents irrelevant) that
+ * sync_cache_attn needs on the current device. */
+sync_status sync_cache_attn_workspace(const sync_cache *cache, int32_t heads, int32_t max_new, int64_t *bytes);
+
+/* Attention of the step's rows over the cache, after sync_cache_append: row i of
+ * the n rows of sequence s sees tokens 0 .. lens[s] - n + i.
+ *   o = softmax(scale * q k^T over these) v
+ * with the values that the cache stands for; query head h reads key head
+ * h / (heads / kv_heads).  A row that sees nothing gets zeros (lse: -inf), every
+ * row of a sequence that has a seen token on a page that the cache does not have,
+ * or more tokens than max_pages hold, NaN.  Rows of no sequence keep what they
+ * have, or (zero_rest) become zero.  q, o: [rows][heads][head_dim], data 16-byte
+ * aligned, strides multiples of 8; lse: NULL, or [heads][rows] float.  max_new:
+ * how many rows a sequence has at most, for the choice of the tile alone: results
+ * are right for more.
+ * Scores, maxima and sums are held in 32 bits.  16 bits: the unnormalised weights
+ * are rounded to dtype for the second product.  4 bits: codes enter the products
+ * exactly; queries are scaled by a power of two to float16 (entries below 2^-21
+ * of their head's largest lose bits), weights are rounded to float16 before and
+ * after their value's scale.  Scores stay below 2^27 in size.  In 16 bits a NaN or an
+ * infinity in the value of a token that some of a sequence's rows see may reach
+ * its other rows; nothing past lens[s] or of other sequences ever does. */
+sync_status sync_cache_attn(const sync_cache *cache, const sync_cache_seqs *seqs, int32_t heads, const sync_rows *q,
+                            float scale, int32_t max_new, const sync_rows *o, float *lse, int32_t zero_rest,
+                            void *workspace, int64_t workspace_bytes, void *stream);
+
 /* Message for the last non-OK status returned on this thread ("" if none). */
 const char *sync_last_error(void);
 

@@ -18,6 +18,12 @@ are in ``attention`` and re-exported here:
     plan = sg.sync_attn_plan(lengths, lengths, heads, kv_heads, head_dim, q.dtype, train=True)
     o, lse = sg.sync_attn_forward(plan, q, k, v, lse=True)
     dq, dk, dv = sg.sync_attn_backward(plan, q, k, v, o, lse, do)
+
+and those of its decoding, on a paged cache, in ``cache``:
+
+    cache = sg.sync_kv_cache(n_pages, 64, kv_heads, head_dim, q.dtype, bits=4)
+    q = sg.sync_cache_append(cache, k, v, page_table, lens, q=q, cos=cos, sin=sin)
+    o = sg.sync_cache_attn(cache, q, page_table, lens)
 """
 from __future__ import annotations
 
@@ -40,7 +46,8 @@ EXPORTS = ("sync_load_programs", "sync_query", "sync_pair_offsets", "sync_eval_t
            "sync_check_minimal", "sync_simulate", "sync_simulate_fused", "sync_simulate_noalloc",
            "sync_free_programs", "sync_last_error", "sync_kernel_launches", "sync_validate_programs",
            "sync_qk_norm_rope", "sync_qk_norm_rope_workspace", "sync_qk_norm_rope_backward",
-           "sync_attn_plan", "sync_cross_attn_plan", "sync_attn_query", "sync_attn_status", "sync_attn_forward", "sync_attn_backward", "sync_attn_free")
+           "sync_attn_plan", "sync_cross_attn_plan", "sync_attn_query", "sync_attn_status", "sync_attn_forward", "sync_attn_backward", "sync_attn_free",
+           "sync_rope", "sync_rope_backward", "sync_cache_append", "sync_cache_read", "sync_cache_attn_workspace", "sync_cache_attn")
 NOALLOC_SCRATCH_BYTES = 64 << 20
 CODE_BYTES_PER_INSTR = 16
 
@@ -112,6 +119,7 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.sync_kernel_launches.argtypes = []
     lib.sync_kernel_launches.restype = ctypes.c_int64
     attention.declare(lib)
+    cache.declare(lib)
     for f in EXPORTS:
         if f not in ("sync_free_programs", "sync_attn_free", "sync_last_error", "sync_kernel_launches"):
             getattr(lib, f).restype = ctypes.c_int
@@ -359,6 +367,8 @@ def sync_free_programs(h: Programs):
     h.close()
 
 
-from . import attention  # noqa: E402  (uses the binding above)
+from . import attention, cache  # noqa: E402  (use the binding above)
 from .attention import (AttnPlan, sync_attn_backward, sync_attn_forward, sync_attn_plan,  # noqa: E402,F401
                         sync_qk_norm_rope, sync_qk_norm_rope_backward)
+from .cache import (KVCache, sync_cache_append, sync_cache_attn, sync_cache_read, sync_kv_cache,  # noqa: E402,F401
+                    sync_rope, sync_rope_backward)

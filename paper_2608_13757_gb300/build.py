@@ -24,9 +24,9 @@ CUDA_HOME = os.environ.get("CUDA_HOME", "/usr/local/cuda")
 NVCC = os.path.join(CUDA_HOME, "bin", "nvcc")
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 CU = ["k_tiles.cu", "k_load.cu", "k_thresholds.cu", "k_simulate.cu", "k_sweep.cu", "k_sweep_maps.cu", "k_bar.cu", "k_piece.cu", "k_noalloc.cu",
-      "k_qk_norm.cu", "k_attn_fwd.cu", "k_attn_bwd.cu"]
-CPP = ["capi.cpp", "attn.cpp"]
-HEADERS = [os.path.join(CSRC, "enc.h"), os.path.join(CSRC, "progbuild.cuh"), os.path.join(CSRC, "cost.cuh"), os.path.join(CSRC, "sweep.cuh"), os.path.join(CSRC, "bar.cuh"), os.path.join(CSRC, "trip.cuh"), os.path.join(CSRC, "handle.h"), os.path.join(CSRC, "waitval.cuh"), os.path.join(CSRC, "attn.h"), os.path.join(CSRC, "umma.cuh"), os.path.join(CSRC, "launch.cuh"), os.path.join(CSRC, "norm.h"), os.path.join(ROOT, "include", "sync.h")]
+      "k_qk_norm.cu", "k_attn_fwd.cu", "k_attn_bwd.cu", "k_rope.cu", "k_cache.cu", "k_cache_attn.cu"]
+CPP = ["capi.cpp", "attn.cpp", "cache.cpp"]
+HEADERS = [os.path.join(CSRC, "enc.h"), os.path.join(CSRC, "progbuild.cuh"), os.path.join(CSRC, "cost.cuh"), os.path.join(CSRC, "sweep.cuh"), os.path.join(CSRC, "bar.cuh"), os.path.join(CSRC, "trip.cuh"), os.path.join(CSRC, "handle.h"), os.path.join(CSRC, "waitval.cuh"), os.path.join(CSRC, "attn.h"), os.path.join(CSRC, "umma.cuh"), os.path.join(CSRC, "launch.cuh"), os.path.join(CSRC, "norm.h"), os.path.join(CSRC, "abi.h"), os.path.join(CSRC, "cache.h"), os.path.join(CSRC, "division.h"), os.path.join(CSRC, "rotate.cuh"), os.path.join(CSRC, "paged.cuh"), os.path.join(ROOT, "include", "sync.h")]
 
 
 def _sources():
