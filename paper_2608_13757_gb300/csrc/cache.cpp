@@ -93,6 +93,7 @@ CacheArgs cache_args(const sync_cache* c) {
        c->bits == 4 ? "head_dim must be a multiple of 32 in 32..128 in 4 bits" : "head_dim must be a multiple of 8 in 8..128");
   need(c->page >= 16 && c->page <= 1024 && (c->page & (c->page - 1)) == 0, "page must be a power of two in 16..1024");
   need(c->n_pages >= 0 && (int64_t)c->n_pages * c->page <= INT32_MAX, "n_pages * page must be in 0..INT32_MAX");
+  need((int64_t)c->n_pages * c->page / 16 * c->kv_heads <= UINT32_MAX, "the cache has more than 16 * UINT32_MAX rows");
   CacheArgs a;
   a.bf16 = c->dtype == SYNC_BF16;
   a.bits = c->bits;
@@ -140,37 +141,31 @@ int checked_heads(const sync_cache* c, int32_t heads) {
 
 }  // namespace
 
-// For tests on the host: the pieces that `blocks` blocks take of a step with
-// `group` query heads per key head and passes of `rows` rows, one row of 13 values
-// per piece: block, sequence, key head, first row, tokens, first token's row,
-// length, bad, tiles [from, to) of tiles; and the block's header (before, open).
-// Returns the rows (written up to `capacity`).
+// For tests on the host: the pieces that `warps` warps take of a step with
+// `group` query heads per key head, passes of `rows` rows and tiles of `tile` keys,
+// 11 values per piece: warp, sequence, key head, first row, tokens, first token's
+// row, length, bad, tiles [from, to) of tiles.  Returns the number of pieces
+// (written up to `capacity`).
 extern "C" int64_t syncgb_cache_attn_work(int n_seqs, const int32_t* lens, const int32_t* row_starts, int64_t all_rows, int room,
-                                          int kv_heads, int group, int rows, int blocks, int64_t* out, int64_t capacity) {
+                                          int kv_heads, int group, int rows, int tile, int warps, int64_t* out, int64_t capacity) {
   auto shape_of = [&](int s) {
-    return division::shape(row_starts ? row_starts[s] : s, row_starts ? row_starts[s + 1] : s + 1, all_rows, lens[s], room, group, kv_heads, rows);
+    return division::shape(row_starts ? row_starts[s] : s, row_starts ? row_starts[s + 1] : s + 1, all_rows, lens[s], room, group, kv_heads, rows, tile);
   };
   int64_t total = 0, n = 0;
   for (int s = 0; s < n_seqs; ++s) total += shape_of(s).cost;
-  const int takers = division::takers(total, blocks);
-  for (int b = 0; b < blocks; ++b) {
-    int64_t from = division::bound(total, takers, b);
-    const int64_t run = division::bound(total, takers, b + 1) - from;
+  const int takers = division::takers(total, warps);
+  for (int w = 0; w < warps; ++w) {
+    int64_t from = division::bound(total, takers, w);
+    const int64_t run = division::bound(total, takers, w + 1) - from;
     if (!run) continue;
     int s = 0;
     for (; from >= shape_of(s).cost; ++s) from -= shape_of(s).cost;
     division::Lister l;
     l.start(shape_of(s), s, from, run);
     division::Piece x;
-    const int64_t first = n;
-    while (l.next(shape_of, n_seqs, kv_heads, rows, x)) {
-      const int64_t row[13] = {b, x.s, x.head, x.first, x.n, x.row0, x.len, x.bad, x.from, x.to, x.tiles, 0, 0};
-      if (n < capacity) std::copy(row, row + 13, out + 13 * n);
-      ++n;
-    }
-    for (int64_t i = first; i < std::min(n, capacity); ++i) {
-      out[13 * i + 11] = l.header.before;
-      out[13 * i + 12] = l.header.open;
+    for (; l.next(shape_of, n_seqs, kv_heads, rows, x); ++n) {
+      const int64_t row[11] = {w, x.s, x.head, x.first, x.n, x.row0, x.len, x.bad, x.from, x.to, x.tiles};
+      if (n < capacity) std::copy(row, row + 11, out + 11 * n);
     }
   }
   return n;

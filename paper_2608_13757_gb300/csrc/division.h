@@ -2,9 +2,9 @@
 // the device and, for tests, on the host.
 //
 // The work is a list: sequence > key head > pass (of `rows` query rows) > tile
-// of 64 keys, every pass counting kUnitCost tiles more for its start and end.
-// A block has an equal run of it.  A pass that a block begins but does not end
-// is continued by the blocks that follow.
+// of `tile` keys, every pass counting kUnitCost tiles more for its start and end.
+// A warp has an equal run of it.  A pass that a warp begins but does not end is
+// continued by the warps that follow.
 #pragma once
 
 #include <cuda_runtime.h>
@@ -19,8 +19,7 @@ namespace division {
 #define SYNCGB_BOTH inline
 #endif
 
-constexpr int kTile = 64;
-constexpr int kUnitCost = 1, kLeast = 2;   // tiles that a pass costs besides; that a block takes at least
+constexpr int kUnitCost = 1, kLeast = 2;   // tiles that a pass costs besides; that a warp takes at least
 
 SYNCGB_BOTH int64_t less(int64_t a, int64_t b) { return a < b ? a : b; }
 SYNCGB_BOTH int64_t more(int64_t a, int64_t b) { return a > b ? a : b; }
@@ -31,7 +30,8 @@ struct Shape {
   int row0, n, len, bad, tiles, passes;
   int64_t cost;
 };
-SYNCGB_BOTH Shape shape(int64_t begin, int64_t end, int64_t all_rows, int len, int room, int group, int kv_heads, int rows) {
+SYNCGB_BOTH Shape shape(int64_t begin, int64_t end, int64_t all_rows, int len, int room, int group, int kv_heads, int rows,
+                        int tile) {
   Shape x;
   begin = less(more(begin, 0), all_rows);
   end = less(more(end, begin), all_rows);
@@ -39,40 +39,33 @@ SYNCGB_BOTH Shape shape(int64_t begin, int64_t end, int64_t all_rows, int len, i
   x.n = (int)(end - begin);
   x.bad = len > room;
   x.len = (int)less(more(len, 0), room);
-  x.tiles = (x.len + kTile - 1) / kTile;
+  x.tiles = (x.len + tile - 1) / tile;
   x.passes = (int)(((int64_t)x.n * group + rows - 1) / rows);
   x.cost = (int64_t)x.passes * kv_heads * (x.tiles + kUnitCost);
   return x;
 }
 
-// Blocks that take work, and the run [from, to) of one.
-SYNCGB_BOTH int takers(int64_t total, int blocks) { return (int)more(1, less(blocks, total / kLeast)); }
-SYNCGB_BOTH int64_t bound(int64_t total, int takers, int block) {
-  block = (int)less(block, takers);
-  return total / takers * block + total % takers * block / takers;   // (no product as large as total * block)
+// Warps that take work, and where the run of one begins (and the last one's ends).
+SYNCGB_BOTH int takers(int64_t total, int warps) { return (int)more(1, less(warps, total / kLeast)); }
+SYNCGB_BOTH int64_t bound(int64_t total, int takers, int warp) {
+  warp = (int)less(warp, takers);
+  if (total < (int64_t)1 << 32 && (uint64_t)total * (uint32_t)takers < (uint64_t)1 << 32) return (uint32_t)total * (uint32_t)warp / (uint32_t)takers;
+  return total / takers * warp + total % takers * warp / takers;   // (no product as large as total * warp)
 }
 
-// A block's part of a pass.
+// A warp's part of a pass.
 struct Piece {
   int s, head;                             // sequence, key head
   int first, n, row0;                      // first row of the pass among the n * group rows; tokens; row of the first token
   int len, bad;                            // tokens in the cache; more than its pages hold
-  int from, to, tiles;                     // tiles of the block, and of the pass
+  int from, to, tiles;                     // tiles of the warp, and of the pass
 };
 
-// What a block leaves for the kernel that joins the pieces.
-struct alignas(32) Header {
-  int before;                              // it has a piece of a pass that began before; 2: and ends it
-  int open;                                // it has begun a pass that it does not end:
-  int row0, n, head, first;                // as in Piece
-};
-
-// The pieces of a block, one after the other.
+// The pieces of a warp, one after the other.
 struct Lister {
   Shape now;
   int s, unit;                             // unit: key head * passes + pass
   int64_t into, left;                      // tiles into the unit, tiles left of the run
-  Header header;
   // into: of the sequence's work
   SYNCGB_BOTH void start(const Shape& x, int seq, int64_t into_seq, int64_t run) {
     now = x;
@@ -80,7 +73,6 @@ struct Lister {
     unit = (int)(into_seq / (x.tiles + kUnitCost));
     into = into_seq % (x.tiles + kUnitCost);
     left = run;
-    header = Header{0, 0, 0, 0, 0, 0};
   }
   template <class F>
   SYNCGB_BOTH bool next(F&& shape_of, int n_seqs, int kv_heads, int rows, Piece& x) {
@@ -95,11 +87,7 @@ struct Lister {
       const int64_t to = less(now.tiles + kUnitCost, into + left);
       const int a = (int)more(0, into - kUnitCost), b = (int)more(0, to - kUnitCost);
       const bool some = b > a || (now.tiles == 0 && into == 0);
-      if (some) {
-        x = Piece{s, unit / now.passes, unit % now.passes * rows, now.n, now.row0, now.len, now.bad, a, b, now.tiles};
-        if (a > 0) header.before = b == now.tiles ? 2 : 1;
-        else if (b < now.tiles) header = Header{header.before, 1, x.row0, x.n, x.head, x.first};
-      }
+      if (some) x = Piece{s, unit / now.passes, unit % now.passes * rows, now.n, now.row0, now.len, now.bad, a, b, now.tiles};
       left -= to - into;
       into = 0;
       ++unit;

@@ -18,6 +18,7 @@ namespace {
 using namespace rotate;
 
 constexpr int kThreads = 256, kTokens = 8;       // most tokens of a block: one per warp
+constexpr int kAhead = 4;                        // pieces that a thread reads before it writes the first
 
 // 8 entries of a row, by one access or entry by entry
 template <class T>
@@ -122,32 +123,40 @@ __global__ void __launch_bounds__(kThreads) k_append(const __grid_constant__ Cac
   }
   __syncthreads();
   if (a.heads) {                                            // queries, as k_rope turns them
-    const int pairs = a.dim / 2, runs = pairs / QVEC, each = a.heads * runs;
-    for (int i = threadIdx.x; i < n * each; i += kThreads) {
-      const int t = i / each, r = i - t * each, h = r / runs, p = (r - h * runs) * QVEC;
-      const int64_t row = row0 + t;
-      T* out = static_cast<T*>(a.q_out.data) + row * a.q_out.row + h * a.q_out.head;
-      Pairs<T, QVEC, INTER> x;
-      if (!mine[t]) {
-        if (!a.fill) continue;
+    const int pairs = a.dim / 2;
+    Walk w(threadIdx.x, kThreads, a.heads, pairs / QVEC);
+    while (w.t < n) {
+      Pairs<T, QVEC, INTER> x[kAhead];
+      Walk at = w;
 #pragma unroll
-        for (int e = 0; e < 2 * QVEC; ++e) from_f(x.x[e], 0.f);
-      } else {
-        x.read(static_cast<const T*>(a.q.data) + row * a.q.row + h * a.q.head, p, half, pairs);
-        const float* c = angles + 2 * t * half + p;
-        if (p < half) x.by(c, c + half);
+      for (int e = 0; e < kAhead; ++e, at.next()) {
+        if (at.t >= n) break;
+        if (mine[at.t]) x[e].read(static_cast<const T*>(a.q.data) + (row0 + at.t) * a.q.row + at.h * a.q.head, at.r * QVEC, half, pairs);
       }
-      x.write(out, p, half, pairs);
+#pragma unroll
+      for (int e = 0; e < kAhead; ++e, w.next()) {
+        if (w.t >= n) break;
+        const int p = w.r * QVEC;
+        if (!mine[w.t]) {
+          if (!a.fill) continue;
+#pragma unroll
+          for (int i = 0; i < 2 * QVEC; ++i) from_f(x[e].x[i], 0.f);
+        } else if (p < half) {
+          const float* c = angles + 2 * w.t * half + p;
+          x[e].by(c, c + half);
+        }
+        x[e].write(static_cast<T*>(a.q_out.data) + (row0 + w.t) * a.q_out.row + w.h * a.q_out.head, p, half, pairs);
+      }
     }
   }
   // keys, then values: 8 entries per thread
-  const int runs = a.dim / 8, each = 2 * a.kv_heads * runs, g = a.dim / kGroup;
-  for (int i = threadIdx.x; i < n * each; i += kThreads) {
-    // (each is a multiple of 4 where the cache has 4 bits: the lanes of a group agree)
-    const int t = i / each, r = i - t * each, hh = r / runs, e = r - hh * runs, d = 8 * e;
+  // (a row has a multiple of 4 runs where the cache has 4 bits: the lanes of a group agree)
+  const int g = a.dim / kGroup;
+  for (Walk w(threadIdx.x, kThreads, 2 * a.kv_heads, a.dim / 8); w.t < n; w.next()) {
+    const int t = w.t, e = w.r, d = 8 * e;
     if (place[t] < 0) continue;
-    const bool is_v = hh >= a.kv_heads;
-    const int h = is_v ? hh - a.kv_heads : hh;
+    const bool is_v = w.h >= a.kv_heads;
+    const int h = is_v ? w.h - a.kv_heads : w.h;
     const HeadTensor& in = is_v ? a.v_rows : a.k_rows;
     const T* head = static_cast<const T*>(in.data) + (row0 + t) * in.row + h * in.head;
     const int64_t at = paged::row_of(a, place[t], h);
@@ -189,36 +198,49 @@ __global__ void __launch_bounds__(kThreads) k_read(const __grid_constant__ Cache
     }
   }
   __syncthreads();
-  const int runs = a.dim / 8, each = 2 * a.kv_heads * runs, g = a.dim / kGroup;
-#pragma unroll 4
-  for (int i = threadIdx.x; i < n * each; i += kThreads) {
-    const int t = i / each, r = i - t * each, hh = r / runs, e = r - hh * runs;
-    const bool is_v = hh >= a.kv_heads;
-    const int h = is_v ? hh - a.kv_heads : hh;
-    const int64_t from = place[t];
-    if (from == -2 && !a.fill) continue;
-    const HeadTensor& out = is_v ? a.v_rows : a.k_rows;
-    Pack<T, 8> y;
-    if (from < 0) {
+  const int g = a.dim / kGroup;
+  Walk w(threadIdx.x, kThreads, 2 * a.kv_heads, a.dim / 8);
+  while (w.t < n) {
+    Pack<T, 8> y[kAhead];                                   // 16 bits: the entries; 4: a word of codes and its scale
+    Walk at = w;
 #pragma unroll
-      for (int k = 0; k < 8; ++k) from_f(y.x[k], from == -3 ? __int_as_float(0x7fffffff) : 0.f);
-    } else {
-      const int64_t at = paged::row_of(a, from, h);
+    for (int e = 0; e < kAhead; ++e, at.next()) {
+      if (at.t >= n) break;
+      if (place[at.t] < 0) continue;
+      const bool is_v = at.h >= a.kv_heads;
+      const int64_t row = paged::row_of(a, place[at.t], is_v ? at.h - a.kv_heads : at.h);
       if (a.bits == 16) {
-        y = *reinterpret_cast<const Pack<T, 8>*>((is_v ? a.v : a.k) + (at * a.dim + 8 * e) * 2);
+        y[e] = *reinterpret_cast<const Pack<T, 8>*>((is_v ? a.v : a.k) + (row * a.dim + 8 * at.r) * 2);
       } else {
-        const uint32_t word = *reinterpret_cast<const uint32_t*>((is_v ? a.v : a.k) + at * (a.dim / 2) + 4 * paged::word_of(e, g));
-        const float scale = __half2float(reinterpret_cast<const __half*>(is_v ? a.v_scale : a.k_scale)[at * g + e / 4]);
+        uint32_t* in = reinterpret_cast<uint32_t*>(&y[e]);
+        in[0] = __ldg(reinterpret_cast<const uint32_t*>((is_v ? a.v : a.k) + row * (a.dim / 2)) + paged::word_of(at.r, g));
+        in[1] = __ldg(reinterpret_cast<const uint16_t*>(is_v ? a.v_scale : a.k_scale) + row * g + at.r / 4);
+      }
+    }
+#pragma unroll
+    for (int e = 0; e < kAhead; ++e, w.next()) {
+      if (w.t >= n) break;
+      const int64_t from = place[w.t];
+      if (from == -2 && !a.fill) continue;
+      if (from < 0) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) from_f(y[e].x[k], from == -3 ? __int_as_float(0x7fffffff) : 0.f);
+      } else if (a.bits == 4) {
+        const uint32_t* in = reinterpret_cast<const uint32_t*>(&y[e]);
+        const uint32_t word = in[0];
+        const float scale = __half2float(__ushort_as_half((uint16_t)in[1]));
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
           float x = (float)((int)(word >> (4 * k) & 15) - 8) * scale;
           // 7 scales may be past float16's end where the row's largest entry was not: the scale was rounded
           if (!a.bf16) x = x > 65504.f ? 65504.f : x < -65504.f ? -65504.f : x;
-          from_f(y.x[k], x);
+          from_f(y[e].x[k], x);
         }
       }
+      const bool is_v = w.h >= a.kv_heads;
+      const HeadTensor& out = is_v ? a.v_rows : a.k_rows;
+      *reinterpret_cast<Pack<T, 8>*>(static_cast<T*>(out.data) + (row0 + w.t) * out.row + (is_v ? w.h - a.kv_heads : w.h) * out.head + 8 * w.r) = y[e];
     }
-    *reinterpret_cast<Pack<T, 8>*>(static_cast<T*>(out.data) + (row0 + t) * out.row + h * out.head + 8 * e) = y;
   }
 }
 

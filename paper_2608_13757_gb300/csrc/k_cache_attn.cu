@@ -39,8 +39,6 @@
 namespace syncgb {
 namespace {
 
-using division::Header;
-using division::kTile;
 using division::Lister;
 using division::Piece;
 using division::Shape;
@@ -50,17 +48,27 @@ using umma::smem_addr;
 using umma::unpack2;
 
 constexpr int kWarps = 4, kThreads = 32 * kWarps, kKeys = 16;
-static_assert(kTile == kWarps * kKeys, "a warp has 16 keys of a tile");
-constexpr int kPieces = 16;                // of a block's list that are laid out at a time
+constexpr int kPieces = 8;                 // of a warp's list that are laid out at a time
 
 // Blocks per SM
-constexpr int per_sm(int bits, int nt) { return bits == 4 && nt == 1 ? 4 : 2; }
+constexpr int per_sm(int bits, int nt) { return bits == 4 && nt == 1 ? 3 : 2; }
+
+// What a block leaves for the kernel that joins the pieces.
+struct alignas(32) Header {
+  int before;                              // it has a piece of a pass that began before; 2: and ends it
+  int open;                                // it has begun a pass that it does not end:
+  int row0, n, head, first;                // as in Piece
+};
 
 template <int DP, int ROWS>
 struct Parts {                             // the workspace
   static constexpr int kRow = DP + 4;      // a row's entries, then its maximum and sum
+  static constexpr int kFloats = ROWS * kRow;
   static __host__ __device__ size_t header(int blocks) { return ((size_t)blocks * sizeof(Header) + 255) / 256 * 256; }
-  static __host__ __device__ size_t bytes(int blocks) { return header(blocks) + (size_t)2 * blocks * ROWS * kRow * sizeof(float); }
+  // two slots per block, then one per warp
+  static __device__ int64_t slot(int i) { return (int64_t)i * kFloats; }
+  static __device__ int64_t warp_slot(int blocks, int i) { return (int64_t)(2 * blocks + i) * kFloats; }
+  static constexpr int kSlots = 2 + kWarps;   // per block
 };
 
 // ---- instructions ----
@@ -88,20 +96,47 @@ __device__ __forceinline__ uint32_t transposed(uint32_t x) {
   asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
   return y;
 }
-// 16 bytes to shared memory without waiting; zeros where `on` is false
+// 16 bytes to shared memory without waiting; zeros where `on` is false.  Offsets
+// that are known go into the instructions.
+template <int TO, int FROM>
+__device__ __forceinline__ void copy16(uint32_t dst, const uint8_t* src) {
+  asm volatile("cp.async.cg.shared.global [%0 + %2], [%1 + %3], 16;" ::"r"(dst), "l"(src), "n"(TO), "n"(FROM) : "memory");
+}
 __device__ __forceinline__ void copy16(uint32_t dst, const uint8_t* src, bool on) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(on ? 16 : 0) : "memory");
 }
 __device__ __forceinline__ void end_group() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N>
 __device__ __forceinline__ void wait_groups() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
-template <int N>
+template <int N, int AT>
 __device__ __forceinline__ void read_words(uint32_t addr, uint32_t* x) {
-  if constexpr (N == 4) asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(x[0]), "=r"(x[1]), "=r"(x[2]), "=r"(x[3]) : "r"(addr) : "memory");
-  else if constexpr (N == 2) asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(x[0]), "=r"(x[1]) : "r"(addr) : "memory");
-  else
-#pragma unroll
-    for (int i = 0; i < N; ++i) asm volatile("ld.shared.u32 %0, [%1];" : "=r"(x[i]) : "r"(addr + 4 * i) : "memory");
+  if constexpr (N == 4) asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4 + %5];" : "=r"(x[0]), "=r"(x[1]), "=r"(x[2]), "=r"(x[3]) : "r"(addr), "n"(AT) : "memory");
+  else if constexpr (N == 2) asm volatile("ld.shared.v2.u32 {%0, %1}, [%2 + %3];" : "=r"(x[0]), "=r"(x[1]) : "r"(addr), "n"(AT) : "memory");
+  else {                                   // one by one: three words are aligned to one
+    asm volatile("ld.shared.u32 %0, [%1 + %2];" : "=r"(x[0]) : "r"(addr), "n"(AT) : "memory");
+    if constexpr (N == 3) {
+      read_words<1, AT + 4>(addr, x + 1);
+      read_words<1, AT + 8>(addr, x + 2);
+    }
+  }
+}
+template <int AT>
+__device__ __forceinline__ uint32_t read_half(uint32_t addr) {
+  uint16_t x;
+  asm volatile("ld.shared.u16 %0, [%1 + %2];" : "=h"(x) : "r"(addr), "n"(AT) : "memory");
+  return x;
+}
+// f with 0, 1, .. as constants
+template <int I>
+struct Constant {
+  static constexpr int value = I;
+};
+template <int N, int I = 0, class F>
+__device__ __forceinline__ void unrolled(F&& f) {
+  if constexpr (I < N) {
+    f(Constant<I>());
+    unrolled<N, I + 1>(f);
+  }
 }
 __device__ __forceinline__ __half2 as_half2(uint32_t x) { return *reinterpret_cast<__half2*>(&x); }
 __device__ __forceinline__ uint32_t as_word(__half2 x) { return *reinterpret_cast<uint32_t*>(&x); }
@@ -112,33 +147,56 @@ __device__ __forceinline__ uint32_t as_word(__half2 x) { return *reinterpret_cas
 
 template <int DP_, int NT, bool BF16>
 struct Wide {                              // 16 bits
-  static constexpr int DP = DP_, kStages = 3, kSide = kKeys * DP * 2, kStage = 2 * kSide;
+  static constexpr int kBits = 16;
+  static constexpr int DP = DP_, MT = 1, kStages = 3, kSide = kKeys * DP * 2, kStage = 2 * kSide;
   uint32_t q[DP / 16][NT][2];
   float o[DP / 16][NT][4], f;
 
-  __device__ __forceinline__ void fetch(const CacheArgs& a, uint32_t stage, int64_t row, int keys) const {
-    const int lane = threadIdx.x % 32, chunks = a.dim / 8;
+  // What the copies of a tile of 16 keys, the row16-th of the cache, start from.
+  const uint8_t *k, *v;
+  uint32_t to;
+  __device__ __forceinline__ void begin(const CacheArgs& a, uint32_t ring) {
+    const int lane = threadIdx.x % 32, key = lane / (DP / 8), j = lane % (DP / 8);
+    k = a.k + key * a.dim * 2 + 16 * j;
+    v = a.v + key * a.dim * 2 + 16 * j;
+    to = key * DP * 2 + ((j ^ key) * 16);
+    if (a.dim < DP)                        // entries that the heads do not have: zero, and never written again
+      for (int i = lane; i < kStages * kStage / 16; i += 32) asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(ring + 16 * i), "r"(0) : "memory");
+    __syncwarp();
+  }
+  template <int T>
+  __device__ __forceinline__ void fetch(const CacheArgs& a, uint32_t stage, uint32_t row16, int keys) const {
+    constexpr int kStep = 256 / DP;        // keys that the lanes copy at a time
+    const int lane = threadIdx.x % 32, key = lane / (DP / 8), j = lane % (DP / 8);
+    if (j >= a.dim / 8) return;
+    const uint8_t *from_k = k + (uint64_t)row16 * (uint32_t)(32 * a.dim), *from_v = v + (uint64_t)row16 * (uint32_t)(32 * a.dim);
 #pragma unroll
-    for (int e = 0; e < kKeys * DP / 8 / 32; ++e) {
-      const int i = lane + 32 * e, key = i / (DP / 8), j = i % (DP / 8);
-      const bool on = key < keys && j < chunks;
-      const int64_t from = ((row + key) * a.dim + 8 * j) * 2;
-      const uint32_t to = stage + key * DP * 2 + ((j ^ key % 8) * 16);
-      copy16(to, on ? a.k + from : a.k, on);
-      copy16(to + kSide, on ? a.v + from : a.v, on);
+    for (int e = 0; e < kKeys / kStep; ++e) {
+      const uint32_t at = stage + e * kStep * DP * 2 + (to ^ (e * kStep % 8 * 16));
+      const int step = e * kStep * a.dim * 2;
+      if (keys >= kKeys) {
+        copy16<0, 0>(at, from_k + step);
+        copy16<kSide, 0>(at, from_v + step);
+      } else {                             // past the sequence's end anything may lie, and a zero weight does not hide a NaN
+        copy16(at, from_k + step, key + e * kStep < keys);
+        copy16(at + kSide, from_v + step, key + e * kStep < keys);
+      }
     }
   }
-  // the query row of column lane / 4; null: none
-  __device__ __forceinline__ void queries(const CacheArgs& a, int nt, const uint8_t* row) {
+  // the query row of column lane / 4 as it is read (null: none), and taken
+  static constexpr int kRaw = DP / 8;
+  static __device__ __forceinline__ void read(const CacheArgs& a, const uint8_t* row, uint32_t* x) {
     const int c = threadIdx.x % 4;
+#pragma unroll
+    for (int i = 0; i < kRaw; ++i) {
+      const int d = 8 * i + 2 * c;
+      x[i] = row && d < a.dim ? __ldg(reinterpret_cast<const uint32_t*>(row + 2 * d)) : 0;
+    }
+  }
+  __device__ __forceinline__ void queries(const CacheArgs& a, int nt, const uint32_t* x) {
     f = a.scale * 1.4426950408889634f;
 #pragma unroll
-    for (int k = 0; k < DP / 16; ++k)
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const int d = 16 * k + 8 * e + 2 * c;
-        q[k][nt][e] = row && d < a.dim ? __ldg(reinterpret_cast<const uint32_t*>(row + 2 * d)) : 0;
-      }
+    for (int i = 0; i < kRaw; ++i) q[i / 2][nt][i % 2] = x[i];
   }
   __device__ __forceinline__ void clear() {
 #pragma unroll
@@ -149,6 +207,7 @@ struct Wide {                              // 16 bits
         for (int e = 0; e < 4; ++e) o[i][nt][e] = 0.f;
   }
   __device__ __forceinline__ float factor(int, int) const { return f; }
+  template <int T>
   __device__ __forceinline__ void scores(uint32_t stage, float (*s)[4]) const {
     const int lane = threadIdx.x % 32, key = lane % 16;
 #pragma unroll
@@ -163,8 +222,9 @@ struct Wide {                              // 16 bits
       for (int nt = 0; nt < NT; ++nt) mma<BF16>(s[nt], x, q[k][nt][0], q[k][nt][1], s[nt]);
     }
   }
-  __device__ __forceinline__ void outputs(uint32_t stage, int, const float (*p)[4]) {
+  __device__ __forceinline__ void outputs(uint32_t stage, int, const float (*p1)[NT][4]) {
     const int lane = threadIdx.x % 32, key = lane % 8 + lane / 16 * 8;
+    const float(*p)[4] = p1[0];
     uint32_t b[NT][2];
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
@@ -186,7 +246,7 @@ struct Wide {                              // 16 bits
       o[i][nt][j + 2] *= by;
     }
   }
-  // f(entry, column 2 c + j, value) for all of this lane's outputs
+  // put(entry, column 2 c + j, value) for all of this lane's outputs
   template <class F>
   __device__ __forceinline__ void each(int nt, F&& put) const {
     const int r = threadIdx.x % 32 / 4;
@@ -195,58 +255,97 @@ struct Wide {                              // 16 bits
 #pragma unroll
       for (int e = 0; e < 4; ++e) put(16 * i + r + e / 2 * 8, e % 2, o[i][nt][e]);
   }
+  // the outputs of column lane / 4, times its factor, to its row (null: none)
+  __device__ __forceinline__ void store(const CacheArgs& a, int nt, const float* by, uint8_t* row) const {
+    const int c = threadIdx.x % 4;
+#pragma unroll
+    for (int i = 0; i < DP / 16; ++i)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const uint32_t x = transposed(pack2<BF16>(o[i][nt][2 * h] * by[0], o[i][nt][2 * h + 1] * by[1]));
+        const int d = 16 * i + 8 * h + 2 * c;
+        if (row && d < a.dim) *reinterpret_cast<uint32_t*>(row + 2 * d) = x;
+      }
+  }
 };
 
 template <int G, int NT, bool BF16>
 struct Narrow {                            // 4 bits, G groups of 32 entries
-  static constexpr int DP = 32 * G, kStages = 4, kSide = kKeys * 16 * G, kScales = kKeys * 2 * G, kStage = 2 * (kSide + kScales);
-  uint32_t q[2 * G][NT][2];
-  float start[G][NT][2];                   // -8 sum q of a group
+  static constexpr int kBits = 4;
+  // Two times 16 keys at once where there are registers for them: what is done
+  // once per tile counts half, and one's instructions cover the other's.
+  static constexpr int DP = 32 * G, MT = NT == 1 ? 2 : 1, kStages = MT == 2 ? 3 : 4, kSide = kKeys * 16 * G, kScales = kKeys * 2 * G;
+  static constexpr int kPart = 2 * (kSide + kScales), kStage = MT * kPart;
+  uint32_t q[2 * G][NT][2], start[NT][2];  // start: -8 sum q of each group, as sums of two float16
   float o[2 * G][NT][4], off[NT][4];       // off: row w has -8 sum p s of group w
   float f[NT][2];
   uint32_t by;                             // 1 / bound twice, in float16
   float bound;                             // a power of two that no scale so far reaches
 
-  __device__ __forceinline__ void fetch(const CacheArgs& a, uint32_t stage, int64_t row, int keys) const {
-    const int lane = threadIdx.x % 32;
-#pragma unroll
-    for (int e = 0; e < (kKeys * G + 31) / 32; ++e) {
-      const int i = lane + 32 * e, key = i / G, j = i % G;
-      if (i >= kKeys * G) break;
-      const bool on = key < keys;
-      const int64_t from = (row + key) * (16 * G) + 16 * j;
-      copy16(stage + 16 * i, on ? a.k + from : a.k, on);
-      // rows of values: even keys first, so that the four keys of a product's slots lie side by side
-      copy16(stage + kSide + (key / 2 + key % 2 * 8) * 16 * G + 16 * j, on ? a.v + from : a.v, on);
-    }
-    if (lane < 4 * G) {                    // 2 G pieces of 16 bytes for keys, then for values
-      const bool is_v = lane >= 2 * G;
-      const int i = is_v ? lane - 2 * G : lane;
-      const uint8_t* from = (is_v ? a.v_scale : a.k_scale) + row * (2 * G) + 16 * i;
-      copy16(stage + 2 * kSide + (is_v ? kScales : 0) + 16 * i, from, true);
-    }
+  const uint8_t *k, *v, *scale;            // what the copies of 16 keys start from
+  uint32_t to_v, to_scale;
+  uint32_t at_k, at_v, at_scale;           // where this lane reads
+  __device__ __forceinline__ void begin(const CacheArgs& a, uint32_t) {
+    const int lane = threadIdx.x % 32, key = lane / G, j = lane % G, i = lane % (2 * G), r = lane / 4, c = lane % 4;
+    k = a.k + 16 * lane;
+    v = a.v + 16 * lane;
+    // rows of values: even keys first, so that the four keys of a product's slots lie side by side
+    to_v = kSide + (key / 2 + key % 2 * 8) * 16 * G + 16 * j;
+    scale = (lane < 2 * G ? a.k_scale : a.v_scale) + 16 * i;
+    to_scale = 2 * kSide + (lane < 2 * G ? 0 : kScales) + 16 * i;
+    at_k = r * 16 * G + 4 * G * c;
+    at_v = kSide + c * 16 * G + 4 * G * (r / 2);
+    at_scale = 2 * kSide + r * 2 * G;
   }
-  __device__ __forceinline__ void queries(const CacheArgs& a, int nt, const uint8_t* row) {
-    const int lane = threadIdx.x % 32, c = lane % 4;
-    float x[G][8];
-    float top = 0.f;
+  // (Rows past the sequence's end come too: codes are numbers whatever they are,
+  // and outputs() leaves out their scales.)
+  template <int T>
+  __device__ __forceinline__ void fetch(const CacheArgs&, uint32_t stage, uint32_t row16, int) const {
+    const int lane = threadIdx.x % 32;
+    const uint8_t *from_k = k + (uint64_t)row16 * (256 * G), *from_v = v + (uint64_t)row16 * (256 * G);
+    const uint32_t put_k = stage + 16 * lane, put_v = stage + to_v;
+    unrolled<(kKeys * G + 31) / 32>([&](auto step) {
+      constexpr int E = 32 * decltype(step)::value;
+      if (E + 32 <= kKeys * G || lane < kKeys * G - E) {
+        copy16<T * kPart + 16 * E, 16 * E>(put_k, from_k);
+        if constexpr (32 % (2 * G) == 0) { // 32 pieces further is a whole, even number of keys further
+          copy16<T * kPart + E / (2 * G) * 16 * G, 16 * E>(put_v, from_v);
+        } else {
+          const int key = (lane + E) / G, j = (lane + E) % G;
+          copy16<T * kPart + kSide, 16 * E>(stage + (key / 2 + key % 2 * 8) * 16 * G + 16 * j, from_v);
+        }
+      }
+    });
+    if (lane < 4 * G) copy16<T * kPart, 0>(stage + to_scale, scale + (uint64_t)row16 * (32 * G));   // 2 G pieces for keys, then for values
+  }
+  static constexpr int kRaw = 4 * G;
+  static __device__ __forceinline__ void read(const CacheArgs&, const uint8_t* row, uint32_t* x) {
+    const int c = threadIdx.x % 4;
 #pragma unroll
     for (int w = 0; w < G; ++w) {
       uint4 v = make_uint4(0, 0, 0, 0);
       if (row) v = __ldg(reinterpret_cast<const uint4*>(row + 2 * (32 * w + 8 * c)));
-      const uint32_t words[4] = {v.x, v.y, v.z, v.w};
+      x[4 * w] = v.x;
+      x[4 * w + 1] = v.y;
+      x[4 * w + 2] = v.z;
+      x[4 * w + 3] = v.w;
+    }
+  }
+  __device__ __forceinline__ void queries(const CacheArgs& a, int nt, const uint32_t* raw) {
+    const int c = threadIdx.x % 4;
+    float x[G][8];
+    float top = 0.f;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const float2 y = unpack2<BF16>(words[e]);
-        x[w][2 * e] = y.x;
-        x[w][2 * e + 1] = y.y;
-        top = fmaxf(top, fmaxf(fabsf(y.x), fabsf(y.y)));
-      }
+    for (int i = 0; i < kRaw; ++i) {
+      const float2 y = unpack2<BF16>(raw[i]);
+      x[i / 4][2 * (i % 4)] = y.x;
+      x[i / 4][2 * (i % 4) + 1] = y.y;
+      top = fmaxf(top, fmaxf(fabsf(y.x), fabsf(y.y)));
     }
     top = fmaxf(top, __shfl_xor_sync(~0u, top, 1));
     top = fmaxf(top, __shfl_xor_sync(~0u, top, 2));
-    // the head's largest entry into 2^11 .. 2^12
-    const int k = min(100, 11 + 127 - (int)(__float_as_uint(top) >> 23));
+    // the head's largest entry into 2^14 .. 2^15
+    const int k = min(100, 14 + 127 - (int)(__float_as_uint(top) >> 23));
     const float up = __uint_as_float((uint32_t)(127 + k) << 23), down = __uint_as_float((uint32_t)(127 - k) << 23);
 #pragma unroll
     for (int w = 0; w < G; ++w)
@@ -256,16 +355,30 @@ struct Narrow {                            // 4 bits, G groups of 32 entries
         q[2 * w + h][nt][1] = pack2<false>(x[w][2 * h + 1] * up * 0.0625f, x[w][2 * h + 5] * up * 0.0625f);
       }
 #pragma unroll
-    for (int j = 0; j < 2; ++j) f[nt][j] = a.scale * 1.4426950408889634f * 16777216.f * __shfl_sync(~0u, down, (2 * c + j) * 4);
-    const uint32_t eight[4] = {0x80088008u, 0x80088008u, 0x80808080u, 0x80808080u};   // -8, and -8 times 16
+    for (int j = 0; j < 2; ++j)            // (not 0, which would make a NaN of a hidden score)
+      f[nt][j] = fmaxf(a.scale * 1.4426950408889634f * 16777216.f * __shfl_sync(~0u, down, (2 * c + j) * 4), 1.17549435e-38f);
+    // -8 sum q of the groups, to lanes c = 0 (groups 0, 1) and 1 (2, 3), and what
+    // their rounding leaves to lanes c = 2 and 3
+    float sum[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int w = 0; w < G; ++w) {
-      float d[4] = {0.f, 0.f, 0.f, 0.f};
-      mma<false>(d, eight, q[2 * w][nt][0], q[2 * w][nt][1], d);
-      mma<false>(d, eight, q[2 * w + 1][nt][0], q[2 * w + 1][nt][1], d);
-      start[w][nt][0] = d[0];
-      start[w][nt][1] = d[1];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const float2 u = unpack2<false>(q[2 * w + h][nt][0]), t = unpack2<false>(q[2 * w + h][nt][1]);
+        sum[w] += u.x + u.y + 16.f * (t.x + t.y);
+      }
+      sum[w] += __shfl_xor_sync(~0u, sum[w], 1);
+      sum[w] += __shfl_xor_sync(~0u, sum[w], 2);
+      sum[w] *= -8.f / 16777216.f;
     }
+    float s0 = c % 2 ? sum[2] : sum[0], s1 = c % 2 ? sum[3] : sum[1];
+    if (c >= 2) {
+      const float2 t = unpack2<false>(pack2<false>(s0, s1));
+      s0 -= t.x;
+      s1 -= t.y;
+    }
+    start[nt][0] = pack2<false>(s0, s1);
+    start[nt][1] = 0;
   }
   __device__ __forceinline__ void clear() {
     by = 0;
@@ -281,34 +394,35 @@ struct Narrow {                            // 4 bits, G groups of 32 entries
   }
   __device__ __forceinline__ float factor(int nt, int j) const { return f[nt][j]; }
   // the scales of keys r and r + 8, as they lie: G halves each
+  template <int AT>
   static __device__ __forceinline__ void scales(uint32_t at, uint32_t (*x)[(G + 1) / 2]) {
-    const int r = threadIdx.x % 32 / 4;
-#pragma unroll
-    for (int e = 0; e < 2; ++e) {
-      const uint32_t from = at + (r + 8 * e) * 2 * G;
-      if constexpr (G % 2 == 0) {
-        read_words<G / 2>(from, x[e]);
-      } else {
-#pragma unroll
-        for (int i = 0; i < (G + 1) / 2; ++i) {
-          uint16_t lo, hi = 0;
-          asm volatile("ld.shared.u16 %0, [%1];" : "=h"(lo) : "r"(from + 4 * i) : "memory");
-          if (2 * i + 1 < G) asm volatile("ld.shared.u16 %0, [%1];" : "=h"(hi) : "r"(from + 4 * i + 2) : "memory");
-          x[e][i] = lo | (uint32_t)hi << 16;
-        }
+    if constexpr (G % 2 == 0) {
+      read_words<G / 2, AT>(at, x[0]);
+      read_words<G / 2, AT + 16 * G>(at, x[1]);
+    } else {
+      x[0][0] = read_half<AT>(at);
+      x[1][0] = read_half<AT + 16 * G>(at);
+      if constexpr (G == 3) {
+        x[0][0] |= read_half<AT + 2>(at) << 16;
+        x[1][0] |= read_half<AT + 2 + 16 * G>(at) << 16;
+        x[0][1] = read_half<AT + 4>(at);
+        x[1][1] = read_half<AT + 4 + 16 * G>(at);
       }
     }
   }
+  template <int T>
   __device__ __forceinline__ void scores(uint32_t stage, float (*s)[4]) const {
-    const int lane = threadIdx.x % 32, r = lane / 4, c = lane % 4;
+    const int c = threadIdx.x % 4;
     uint32_t x[2][G], sc[2][(G + 1) / 2];
-    read_words<G>(stage + r * 16 * G + 4 * G * c, x[0]);
-    read_words<G>(stage + (r + 8) * 16 * G + 4 * G * c, x[1]);
-    scales(stage + 2 * kSide, sc);
+    read_words<G, T * kPart>(stage + at_k, x[0]);
+    read_words<G, T * kPart + 8 * 16 * G>(stage + at_k, x[1]);
+    scales<T * kPart>(stage + at_scale, sc);
+    // the sums' start: scales by -8 sum q
+    const bool odd = c % 2;
+    const uint32_t both[4] = {G > 2 && odd ? sc[0][(G + 1) / 2 - 1] : odd ? 0 : sc[0][0], G > 2 && odd ? sc[1][(G + 1) / 2 - 1] : odd ? 0 : sc[1][0], 0, 0};
+    const float zero[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) s[nt][e] = 0.f;
+    for (int nt = 0; nt < NT; ++nt) mma<false>(s[nt], both, start[nt][0], start[nt][1], zero);
 #pragma unroll
     for (int w = 0; w < G; ++w) {
       const uint32_t lo[4] = {x[0][w] & 0x000f000fu, x[1][w] & 0x000f000fu, x[0][w] & 0x00f000f0u, x[1][w] & 0x00f000f0u};
@@ -318,8 +432,8 @@ struct Narrow {                            // 4 bits, G groups of 32 entries
       const float u0 = w % 2 ? k0.y : k0.x, u1 = w % 2 ? k1.y : k1.x;
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
-        float d[4] = {start[w][nt][0], start[w][nt][1], start[w][nt][0], start[w][nt][1]};
-        mma<false>(d, lo, q[2 * w][nt][0], q[2 * w][nt][1], d);
+        float d[4];
+        mma<false>(d, lo, q[2 * w][nt][0], q[2 * w][nt][1], zero);
         mma<false>(d, hi, q[2 * w + 1][nt][0], q[2 * w + 1][nt][1], d);
         s[nt][0] = fmaf(u0, d[0], s[nt][0]);
         s[nt][1] = fmaf(u0, d[1], s[nt][1]);
@@ -328,18 +442,25 @@ struct Narrow {                            // 4 bits, G groups of 32 entries
       }
     }
   }
-  __device__ __forceinline__ void outputs(uint32_t stage, int keys, const float (*p)[4]) {
-    const int lane = threadIdx.x % 32, r = lane / 4, c = lane % 4;
-    uint32_t sc[2][(G + 1) / 2];
-    scales(stage + 2 * kSide + kScales, sc);
-    if (keys < kKeys) {                    // past the sequence's end a scale may be anything, and a zero weight does not hide a NaN
+  __device__ __forceinline__ void outputs(uint32_t stage, int keys, const float (*p)[NT][4]) {
+    const int r = threadIdx.x % 32 / 4;
+    uint32_t sc[MT][2][(G + 1) / 2];
+    unrolled<MT>([&](auto t) { scales<decltype(t)::value * kPart + kScales>(stage + at_scale, sc[decltype(t)::value]); });
+    if (keys < MT * kKeys) {               // past the sequence's end a scale may be anything, and a zero weight does not hide a NaN
+#pragma unroll
+      for (int t = 0; t < MT; ++t)
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+#pragma unroll
+          for (int i = 0; i < (G + 1) / 2; ++i) sc[t][e][i] = 16 * t + r + 8 * e < keys ? sc[t][e][i] : 0;
+    }
+    __half2 most = as_half2(sc[0][0][0]);
+#pragma unroll
+    for (int t = 0; t < MT; ++t)
 #pragma unroll
       for (int e = 0; e < 2; ++e)
 #pragma unroll
-        for (int i = 0; i < (G + 1) / 2; ++i) sc[e][i] = r + 8 * e < keys ? sc[e][i] : 0;
-    }
-    __half2 most = __hmax2(as_half2(sc[0][0]), as_half2(sc[1][0]));
-    if constexpr (G > 2) most = __hmax2(most, __hmax2(as_half2(sc[0][1]), as_half2(sc[1][1])));
+        for (int i = 0; i < (G + 1) / 2; ++i) most = __hmax2(most, as_half2(sc[t][e][i]));
     float top = fmaxf(__low2float(most), __high2float(most));
     if (__any_sync(~0u, top >= bound)) {                     // a larger scale than any so far (or the first tile)
 #pragma unroll
@@ -358,44 +479,48 @@ struct Narrow {                            // 4 bits, G groups of 32 entries
           for (int i = 0; i < 2 * G; ++i) o[i][nt][e] *= ratio;
         }
     }
-    __half2 rel[2][(G + 1) / 2];
-#pragma unroll
-    for (int e = 0; e < 2; ++e)
-#pragma unroll
-      for (int i = 0; i < (G + 1) / 2; ++i) rel[e][i] = __hmul2(as_half2(sc[e][i]), as_half2(by));
-    __half2 h[NT][2];
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-      h[nt][0] = as_half2(pack2<false>(p[nt][0], p[nt][1]));
-      h[nt][1] = as_half2(pack2<false>(p[nt][2], p[nt][3]));
-    }
-    uint32_t x[4][G];                                        // keys 2 c, 2 c + 1, 2 c + 8, 2 c + 9
-#pragma unroll
-    for (int e = 0; e < 4; ++e) read_words<G>(stage + kSide + (c + e / 2 * 4 + e % 2 * 8) * 16 * G + 4 * G * (r / 2), x[e]);
     const uint32_t halves = r % 2 ? 0x7632u : 0x5410u;
+    unrolled<MT>([&](auto part) {
+      constexpr int T = decltype(part)::value;
+      __half2 rel[2][(G + 1) / 2], h[NT][2];
 #pragma unroll
-    for (int w = 0; w < G; ++w) {
-      uint32_t b[NT][2];
-      const __half2 r0 = w % 2 ? __high2half2(rel[0][w / 2]) : __low2half2(rel[0][w / 2]);
-      const __half2 r1 = w % 2 ? __high2half2(rel[1][w / 2]) : __low2half2(rel[1][w / 2]);
-      const uint32_t mark = r == w ? 0x80088008u : 0u;       // -8 in row w
-      const uint32_t eight[4] = {mark, 0u, mark, 0u};
+      for (int e = 0; e < 2; ++e)
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt) {
-        b[nt][0] = transposed(as_word(__hmul2(h[nt][0], r0)));
-        b[nt][1] = transposed(as_word(__hmul2(h[nt][1], r1)));
-        mma<false>(off[nt], eight, b[nt][0], b[nt][1], off[nt]);
-      }
-      const uint32_t y0 = __byte_perm(x[0][w], x[1][w], halves), y1 = __byte_perm(x[2][w], x[3][w], halves);
-      const uint32_t lo[4] = {y0 & 0x000f000fu, y0 & 0x00f000f0u, y1 & 0x000f000fu, y1 & 0x00f000f0u};
-      const uint32_t z0 = y0 >> 8, z1 = y1 >> 8;
-      const uint32_t hi[4] = {z0 & 0x000f000fu, z0 & 0x00f000f0u, z1 & 0x000f000fu, z1 & 0x00f000f0u};
+        for (int i = 0; i < (G + 1) / 2; ++i) rel[e][i] = __hmul2(as_half2(sc[T][e][i]), as_half2(by));
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
-        mma<false>(o[2 * w][nt], lo, b[nt][0], b[nt][1], o[2 * w][nt]);
-        mma<false>(o[2 * w + 1][nt], hi, b[nt][0], b[nt][1], o[2 * w + 1][nt]);
+        h[nt][0] = as_half2(pack2<false>(p[T][nt][0], p[T][nt][1]));
+        h[nt][1] = as_half2(pack2<false>(p[T][nt][2], p[T][nt][3]));
       }
-    }
+      uint32_t x[4][G];                                      // keys 2 c, 2 c + 1, 2 c + 8, 2 c + 9
+      unrolled<4>([&](auto key) {
+        constexpr int E = decltype(key)::value;
+        read_words<G, T * kPart + (E / 2 * 4 + E % 2 * 8) * 16 * G>(stage + at_v, x[E]);
+      });
+#pragma unroll
+      for (int w = 0; w < G; ++w) {
+        uint32_t b[NT][2];
+        const __half2 r0 = w % 2 ? __high2half2(rel[0][w / 2]) : __low2half2(rel[0][w / 2]);
+        const __half2 r1 = w % 2 ? __high2half2(rel[1][w / 2]) : __low2half2(rel[1][w / 2]);
+        const uint32_t mark = r == w ? 0x80088008u : 0u;     // -8 in row w
+        const uint32_t eight[4] = {mark, 0u, mark, 0u};
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+          b[nt][0] = transposed(as_word(__hmul2(h[nt][0], r0)));
+          b[nt][1] = transposed(as_word(__hmul2(h[nt][1], r1)));
+          mma<false>(off[nt], eight, b[nt][0], b[nt][1], off[nt]);
+        }
+        const uint32_t y0 = __byte_perm(x[0][w], x[1][w], halves), y1 = __byte_perm(x[2][w], x[3][w], halves);
+        const uint32_t lo[4] = {y0 & 0x000f000fu, y0 & 0x00f000f0u, y1 & 0x000f000fu, y1 & 0x00f000f0u};
+        const uint32_t z0 = y0 >> 8, z1 = y1 >> 8;
+        const uint32_t hi[4] = {z0 & 0x000f000fu, z0 & 0x00f000f0u, z1 & 0x000f000fu, z1 & 0x00f000f0u};
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+          mma<false>(o[2 * w][nt], lo, b[nt][0], b[nt][1], o[2 * w][nt]);
+          mma<false>(o[2 * w + 1][nt], hi, b[nt][0], b[nt][1], o[2 * w + 1][nt]);
+        }
+      }
+    });
   }
   __device__ __forceinline__ void rescale(int nt, int j, float by_) {
     off[nt][j] *= by_;
@@ -404,6 +529,10 @@ struct Narrow {                            // 4 bits, G groups of 32 entries
       o[i][nt][j] *= by_;
       o[i][nt][j + 2] *= by_;
     }
+  }
+  // output entries 32 w + 4 r + 2 h (s = 0) and the one after it (s = 1) of column 2 c + j
+  __device__ __forceinline__ float output(int w, int h, int s, int nt, int j, float minus, float unit) const {
+    return s ? fmaf(o[2 * w + h][nt][j + 2], 0.0625f, minus) * unit : (o[2 * w + h][nt][j] + minus) * unit;
   }
   template <class F>
   __device__ __forceinline__ void each(int nt, F&& put) const {
@@ -415,307 +544,451 @@ struct Narrow {                            // 4 bits, G groups of 32 entries
       for (int j = 0; j < 2; ++j) {
         const float minus = __shfl_sync(~0u, off[nt][j], 4 * w + c);
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          put(32 * w + 4 * r + 2 * h, j, (o[2 * w + h][nt][j] + minus) * unit);
-          put(32 * w + 4 * r + 2 * h + 1, j, fmaf(o[2 * w + h][nt][j + 2], 0.0625f, minus) * unit);
-        }
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int s = 0; s < 2; ++s) put(32 * w + 4 * r + 2 * h + s, j, output(w, h, s, nt, j, minus, unit));
       }
+  }
+  __device__ __forceinline__ void store(const CacheArgs&, int nt, const float* by, uint8_t* row) const {
+    const int c = threadIdx.x % 4;
+    const float unit = bound * 16777216.f;
+#pragma unroll
+    for (int w = 0; w < G; ++w) {
+      const float m0 = __shfl_sync(~0u, off[nt][0], 4 * w + c), m1 = __shfl_sync(~0u, off[nt][1], 4 * w + c);
+      uint32_t x[2][2];                    // entries 8 c + 2 h + s and 8 c + 4 + 2 h + s of column r
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+          x[h][s] = transposed(pack2<BF16>(output(w, h, s, nt, 0, m0, unit) * by[0], output(w, h, s, nt, 1, m1, unit) * by[1]));
+      if (row)
+        *reinterpret_cast<uint4*>(row + 2 * (32 * w + 8 * c)) =
+            make_uint4(__byte_perm(x[0][0], x[0][1], 0x5410), __byte_perm(x[1][0], x[1][1], 0x5410),
+                       __byte_perm(x[0][0], x[0][1], 0x7632), __byte_perm(x[1][0], x[1][1], 0x7632));
+    }
   }
 };
 
 // ---- division of the work ----
-__device__ __forceinline__ Shape shape_of(const CacheArgs& a, int s, int rows) {
+__device__ __forceinline__ Shape shape_of(const CacheArgs& a, int s, int rows, int tile) {
   const int64_t begin = a.starts ? __ldg(a.starts + s) : s, end = a.starts ? __ldg(a.starts + s + 1) : s + 1;
-  return division::shape(begin, end, a.rows, __ldg(a.lens + s), a.max_pages << a.page_shift, a.heads / a.kv_heads, a.kv_heads, rows);
+  return division::shape(begin, end, a.rows, __ldg(a.lens + s), a.max_pages << a.page_shift, a.heads / a.kv_heads, a.kv_heads, rows, tile);
 }
 
-// Where a block's run of the list begins: the sequence, and how far into its
-// work.  left: the length of the run.
-struct Start {
-  int s;
-  int64_t into, left;
+// The runs of a block's warps: their bounds in the list, and the sequences where
+// they begin with how far into them.
+struct Runs {
+  int64_t sum[kWarps], bound[kWarps + 1], into[kWarps];
+  int s[kWarps];
 };
 
-template <int ROWS>
-__device__ __forceinline__ Start find_start(const CacheArgs& a, int64_t* shared) {
-  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-  int64_t total = 0;
-  for (int s = threadIdx.x; s < a.n_seqs; s += kThreads) total += shape_of(a, s, ROWS).cost;
+__device__ __forceinline__ int64_t summed_up(int64_t x) {     // over the lanes up to this one
 #pragma unroll
-  for (int o = 16; o; o >>= 1) total += __shfl_xor_sync(~0u, total, o);
-  if (lane == 0) shared[warp] = total;
-  if (threadIdx.x == 0) shared[4] = -1;
+  for (int o = 1; o < 32; o *= 2) {
+    const int64_t up = __shfl_up_sync(~0u, x, o);
+    if (threadIdx.x % 32 >= o) x += up;
+  }
+  return x;
+}
+
+template <int ROWS, int TILE>
+__device__ __forceinline__ void find_runs(const CacheArgs& a, Runs& runs) {
+  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  const bool few = a.n_seqs <= kThreads;
+  int64_t cost = 0;
+  for (int s = threadIdx.x; s < a.n_seqs; s += kThreads) cost += shape_of(a, s, ROWS, TILE).cost;
+  int64_t sum = summed_up(cost);
+  if (lane == 31) runs.sum[warp] = sum;
   __syncthreads();
-  total = shared[0] + shared[1] + shared[2] + shared[3];
-  Start r;
-  const int takers = division::takers(total, gridDim.x);
-  const int64_t x0 = division::bound(total, takers, blockIdx.x);
-  r.left = division::bound(total, takers, blockIdx.x + 1) - x0;
-  r.s = 0;
-  r.into = 0;
-  if (r.left == 0) return r;               // (the same for the whole block)
+  if (threadIdx.x <= kWarps) {
+    const int64_t total = runs.sum[0] + runs.sum[1] + runs.sum[2] + runs.sum[3];
+    runs.bound[threadIdx.x] = division::bound(total, division::takers(total, gridDim.x * kWarps), blockIdx.x * kWarps + threadIdx.x);
+  }
+  __syncthreads();
+  if (runs.bound[0] == runs.bound[kWarps]) return;
   int64_t before = 0;
   for (int s0 = 0; s0 < a.n_seqs; s0 += kThreads) {
     const int s = s0 + threadIdx.x;
-    const int64_t cost = s < a.n_seqs ? shape_of(a, s, ROWS).cost : 0;
-    int64_t sum = cost;
-#pragma unroll
-    for (int o = 1; o < 32; o *= 2) {
-      const int64_t up = __shfl_up_sync(~0u, sum, o);
-      if (lane >= o) sum += up;
+    if (!few) {
+      cost = s < a.n_seqs ? shape_of(a, s, ROWS, TILE).cost : 0;
+      sum = summed_up(cost);
+      __syncthreads();
+      if (lane == 31) runs.sum[warp] = sum;
+      __syncthreads();
     }
-    __syncthreads();
-    if (lane == 31) shared[warp] = sum;
-    __syncthreads();
     int64_t mine = before + sum - cost;
-    for (int w = 0; w < warp; ++w) mine += shared[w];
-    before += shared[0] + shared[1] + shared[2] + shared[3];
-    if (cost && mine <= x0 && x0 < mine + cost) {
-      shared[4] = s;
-      shared[5] = x0 - mine;
+    for (int w = 0; w < kWarps; ++w) {
+      if (w < warp) mine += runs.sum[w];
+      before += runs.sum[w];
     }
-    __syncthreads();
-    if (shared[4] >= 0) break;
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) {
+      const int64_t at = runs.bound[w];
+      if (at < runs.bound[w + 1] && mine <= at && at < mine + cost) {
+        runs.s[w] = s;
+        runs.into[w] = at - mine;
+      }
+    }
+    if (before > runs.bound[kWarps - 1]) break;
   }
-  r.s = (int)max(shared[4], (int64_t)0);
-  r.into = shared[5];
   __syncthreads();
-  return r;
 }
 
+// What a warp leaves of passes that it did not do alone: the end of one that
+// began before (its rows are in the workspace), and one that it did not end (in
+// the warp's shared memory).
+struct Left {
+  int before;
+  int open;                                // 1: that it began; 2: that began before
+  int row0[2], n[2], head[2], first[2];    // of either, as in Piece
+};
+
 template <class K, int NT, bool BF16>
-__global__ void __launch_bounds__(kThreads, per_sm(K::kStages == 4 ? 4 : 16, NT)) k_cache_attn(const __grid_constant__ CacheArgs a) {
-  constexpr int DP = K::DP, ROWS = 8 * NT, S = K::kStages;
+__global__ void __launch_bounds__(kThreads, per_sm(K::kBits, NT)) k_cache_attn(const __grid_constant__ CacheArgs a) {
+  constexpr int DP = K::DP, MT = K::MT, ROWS = 8 * NT, S = K::kStages, kTile = MT * kKeys, kRing = S * K::kStage;
   using P = Parts<DP, ROWS>;
+  static_assert(P::kFloats * 4 <= kRing, "a warp's shared memory holds a pass");
   extern __shared__ __align__(16) uint8_t ring[];
-  __shared__ float joined[2][8][DP + 4];
-  __shared__ float stat[kWarps][ROWS][2];
-  __shared__ Piece list[kPieces];
-  __shared__ int64_t scan[6];
-  __shared__ int listed;
-  __shared__ Lister lister;
+  __shared__ Piece lists[kWarps][kPieces];
+  __shared__ Lister listers[kWarps];
+  __shared__ Left lefts[kWarps];
+  __shared__ Runs runs;
   let_next_start();
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, r = lane / 4, c = lane % 4;
   const int group = a.heads / a.kv_heads;
-  const uint32_t mine = smem_addr(ring) + warp * S * K::kStage;
-  Header* const headers = reinterpret_cast<Header*>(a.work);
+  const uint32_t mine = smem_addr(ring) + warp * kRing;
   float* const parts = reinterpret_cast<float*>(a.work + P::header(gridDim.x));
+  auto out_row = [&](const int64_t row, int head) { return static_cast<uint8_t*>(a.q_out.data) + 2 * (row * a.q_out.row + head * a.q_out.head); };
 
   if (a.fill) {                            // padding behind the last sequence
     const int64_t end = a.starts ? min(max((int64_t)__ldg(a.starts + a.n_seqs), (int64_t)0), a.rows) : a.rows;
     for (int64_t row = end + blockIdx.x; row < a.rows; row += gridDim.x)
       for (int i = threadIdx.x; i < a.heads * (a.dim / 8); i += kThreads) {
         const int h = i / (a.dim / 8), d = i % (a.dim / 8) * 8;
-        *reinterpret_cast<uint4*>(static_cast<uint8_t*>(a.q_out.data) + 2 * (row * a.q_out.row + h * a.q_out.head + d)) = make_uint4(0, 0, 0, 0);
+        *reinterpret_cast<uint4*>(out_row(row, h) + 2 * d) = make_uint4(0, 0, 0, 0);
         if (a.lse && d == 0) a.lse[h * a.rows + row] = -INFINITY;
       }
   }
 
-  // the list of pieces is laid out by one thread, kPieces at a time
-  const Start at = find_start<ROWS>(a, scan);
-  if (threadIdx.x == 0) {
-    lister.left = 0;
-    lister.header = Header{0, 0, 0, 0, 0, 0};
-    if (at.left) lister.start(shape_of(a, at.s, ROWS), at.s, at.into, at.left);
+  find_runs<ROWS, kTile>(a, runs);
+  Lister& lister = listers[warp];
+  Piece* const list = lists[warp];
+  Left& left = lefts[warp];
+  if (lane == 0) {
+    left.before = left.open = 0;
+    lister.left = runs.bound[warp + 1] - runs.bound[warp];
+    if (lister.left) lister.start(shape_of(a, runs.s[warp], ROWS, kTile), runs.s[warp], runs.into[warp], lister.left);
   }
   K k;
-  for (;;) {
-    if (threadIdx.x == 0) {
-      int n = 0;
-      while (n < kPieces && lister.next([&](int s) { return shape_of(a, s, ROWS); }, a.n_seqs, a.kv_heads, ROWS, list[n])) ++n;
-      listed = n;
+  k.begin(a, mine);
+
+  // The next piece of this warp, in a ring of kPieces (the copies are at most S
+  // tiles, and so pieces, ahead).  Passes without keys are done here.
+  int made = 0;
+  bool done = false;
+  auto make = [&] {
+    for (;;) {
+      if (done) return false;
+      int ok = 0;
+      if (lane == 0) ok = lister.next([&](int s) { return shape_of(a, s, ROWS, kTile); }, a.n_seqs, a.kv_heads, ROWS, list[made % kPieces]);
+      __syncwarp();
+      done = !__shfl_sync(~0u, ok, 0);
+      if (done) return false;
+      const Piece& x = list[made % kPieces];
+      if (x.from < x.to) {
+        ++made;
+        return true;
+      }
+      const uint32_t fill = x.bad ? 0x7fff7fffu : 0u;        // NaN in both types
+      for (int i = lane; i < ROWS * (a.dim / 8); i += 32) {
+        const int row = x.first + i / (a.dim / 8), d = i % (a.dim / 8) * 8, head = x.head * group + row % group;
+        if (row >= x.n * group) break;
+        *reinterpret_cast<uint4*>(out_row(x.row0 + row / group, head) + 2 * d) = make_uint4(fill, fill, fill, fill);
+        if (a.lse && d == 0) a.lse[head * a.rows + x.row0 + row / group] = x.bad ? __int_as_float(0x7fffffff) : -INFINITY;
+      }
+      __syncwarp();
     }
-    __syncthreads();
-    const int pieces = listed;
-    if (pieces == 0) break;
+  };
 
-    // Tiles ahead: (ap, t) is the next one to copy, its page looked up one tile
-    // before.
-    int ap = 0, t = list[0].from, page = -1;
-    bool bad = false;
-    auto settle = [&] {                    // past pieces without tiles
-      while (ap < pieces && t >= list[ap].to)
-        if (++ap < pieces) t = list[ap].from;
-    };
-    auto look = [&] {
-      if (ap >= pieces) return;
-      const int pos = t * kTile + warp * kKeys;
-      page = pos < list[ap].len ? __ldg(a.table + list[ap].s * a.table_stride + (pos >> a.page_shift)) : -1;
-    };
-    int put = 0;
-    uint32_t lost = 0;                     // stages whose page the cache does not have
-    auto ahead = [&] {
-      if (ap < pieces) {
-        const int pos = t * kTile + warp * kKeys, keys = list[ap].len - pos;
-        if (keys > 0) {
-          const bool has = (unsigned)page < (unsigned)a.n_pages;
-          lost = has ? lost & ~(1u << put) : lost | 1u << put;
-          const int64_t row = (((int64_t)(has ? page : 0) * a.kv_heads + list[ap].head) << a.page_shift) + (pos & ((1 << a.page_shift) - 1));
-          if (has) k.fetch(a, mine + put * K::kStage, row, min(keys, kKeys));
-        }
-        ++t;
-        settle();
-        look();
+  // Tiles ahead: the next one to copy, whose page was looked up one tile before.
+  int ap = 0, at_tile = 0, at_to = 0, at_len = 0, at_head = 0, page[MT];
+  const int32_t* at_table = nullptr;
+  auto piece = [&] {                       // at_len 0 behind the last
+    at_len = 0;
+    if (ap == made && !make()) return;
+    const Piece& x = list[ap++ % kPieces];
+    at_tile = x.from;
+    at_to = x.to;
+    at_len = x.len;
+    at_head = x.head;
+    at_table = a.table + x.s * a.table_stride;
+  };
+  auto look = [&] {
+    const int pos = at_tile * kTile;
+    if (at_len) page[0] = __ldg(at_table + (pos >> a.page_shift));
+    if (MT == 2 && a.page_shift == 4 && pos + kKeys < at_len) page[MT - 1] = __ldg(at_table + (pos >> a.page_shift) + 1);
+  };
+  uint32_t put = mine, lost = 0;           // lost: stages whose page the cache does not have
+  auto ahead = [&] {
+    if (at_len) {
+      const int pos = at_tile * kTile;
+      auto row16 = [&](int t) {
+        return (((uint32_t)page[t] * a.kv_heads + at_head) << (a.page_shift - 4)) + (pos / kKeys & ((1 << (a.page_shift - 4)) - 1));
+      };
+      const bool two = MT == 2 && pos + kKeys < at_len, apart = a.page_shift == 4;
+      bool has = (unsigned)page[0] < (unsigned)a.n_pages;
+      const uint32_t first = row16(0);
+      if (has) k.template fetch<0>(a, put, first, at_len - pos);
+      if (two && apart) {
+        has = has && (unsigned)page[MT - 1] < (unsigned)a.n_pages;
+        if (has) k.template fetch<MT - 1>(a, put, row16(MT - 1), at_len - pos - kKeys);
+      } else if (two && has) {
+        k.template fetch<MT - 1>(a, put, first + 1, at_len - pos - kKeys);
       }
-      end_group();
-      put = put + 1 == S ? 0 : put + 1;
-    };
-    settle();
-    look();
-    __syncwarp();
+      if (!has) lost |= 1u << (put - mine) / K::kStage;
+      if (++at_tile >= at_to) piece();
+      look();
+    }
+    end_group();
+    put = put + K::kStage == mine + kRing ? mine : put + K::kStage;
+  };
+  piece();
+  look();
+  __syncwarp();
 #pragma unroll 1
-    for (int i = 0; i < S - 1; ++i) ahead();
-    int get = 0;
+  for (int i = 0; i < S - 1; ++i) ahead();
+  uint32_t get = mine;
 
+  // the query of a column: head and token of a row of the pass
+  auto split = [&](const Piece& x, int row, int& token, int& head) {
+    token = x.n == 1 ? 0 : row / group;
+    head = x.head * group + (x.n == 1 ? row : row - token * group);
+  };
+  auto query = [&](const Piece& x, int nt) -> const uint8_t* {
+    const int row = x.first + 8 * nt + r;
+    int token, head;
+    split(x, row, token, head);
+    return row < x.n * group ? static_cast<const uint8_t*>(a.q.data) + 2 * ((x.row0 + token) * a.q.row + head * a.q.head) : nullptr;
+  };
+  uint32_t raw[K::kRaw];                   // the next piece's queries, where there are registers for them
+  if (NT == 1 && made) K::read(a, query(list[0], 0), raw);
+  // (the copies, a tile ahead at least, have asked for the next piece before one is done)
 #pragma unroll 1
-    for (int ip = 0; ip < pieces; ++ip) {
-      const Piece x = list[ip];
-      float m[NT][2], l[NT][2];
-      int limit[NT][2];                    // tokens that a column's row sees
-      int least = x.len;
+  for (int ip = 0; ip < made; ++ip) {
+    const Piece& x = list[ip % kPieces];
+    const int len = x.len, to = x.to;
+    float m[NT][2], l[NT][2], shift[NT][2];   // shift: m, or 0 where nothing was seen
+    int limit[NT][2];                      // tokens that a column's row sees
+    int least = len;
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt) {
-        const int row = x.first + 8 * nt + r;
-        const bool is = row < x.n * group;
-        const int token = row / group, head = x.head * group + row % group;
-        k.queries(a, nt, is ? static_cast<const uint8_t*>(a.q.data) + 2 * ((x.row0 + token) * a.q.row + head * a.q.head) : nullptr);
+    for (int nt = 0; nt < NT; ++nt) {
+      if (NT > 1) K::read(a, query(x, nt), raw);
+      k.queries(a, nt, raw);
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          m[nt][j] = -INFINITY;
-          l[nt][j] = 0.f;
-          limit[nt][j] = x.len - x.n + min((x.first + 8 * nt + 2 * c + j) / group, x.n - 1) + 1;
-          least = min(least, limit[nt][j]);
-        }
+      for (int j = 0; j < 2; ++j) {
+        int token, head;
+        split(x, x.first + 8 * nt + 2 * c + j, token, head);
+        m[nt][j] = -INFINITY;
+        l[nt][j] = shift[nt][j] = 0.f;
+        limit[nt][j] = len - x.n + min(token, x.n - 1) + 1;
+        least = min(least, limit[nt][j]);
       }
-      k.clear();
-      bad = x.bad;
-      const bool all = __all_sync(~0u, least == x.len);
+    }
+    k.clear();
+    bool bad = x.bad;
+    // from this token on some row does not see a tile whole
+    const int whole_to = __all_sync(~0u, least == len) ? len - kTile : -1;
 #pragma unroll 1
-      for (int tile = x.from; tile < x.to; ++tile) {
-        __syncwarp();
-        ahead();
-        wait_groups<S - 1>();
-        __syncwarp();
-        const uint32_t stage = mine + get * K::kStage;
-        const int pos = tile * kTile + warp * kKeys;
-        const bool gone = lost >> get & 1;
-        get = get + 1 == S ? 0 : get + 1;
-        if (pos >= x.len) continue;
-        if (gone) {
+    for (int tile = x.from; tile < to; ++tile) {
+      __syncwarp();
+      ahead();
+      wait_groups<S - 1>();
+      __syncwarp();
+      const uint32_t stage = get;
+      const int pos = tile * kTile;
+      get = get + K::kStage == mine + kRing ? mine : get + K::kStage;
+      if (lost) {
+        const uint32_t bit = 1u << (stage - mine) / K::kStage;
+        if (lost & bit) {
+          lost &= ~bit;
           bad = true;
           continue;
         }
-        float s[NT][4];
-        k.scores(stage, s);
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) s[nt][e] *= k.factor(nt, e % 2);
-        if (!all || pos + kKeys > x.len) {
-#pragma unroll
-          for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) s[nt][e] = pos + r + e / 2 * 8 < limit[nt][e % 2] ? s[nt][e] : -INFINITY;
-        }
-        // The running maximum follows only rises of more than 2^8 in the weights.
-        bool rises = false;
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-          for (int j = 0; j < 2; ++j) rises = rises || fmaxf(s[nt][j], s[nt][j + 2]) > m[nt][j] + 8.f;
-        if (__any_sync(~0u, rises)) {
-#pragma unroll
-          for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-              float top = fmaxf(s[nt][j], s[nt][j + 2]);
-#pragma unroll
-              for (int o = 4; o < 32; o *= 2) top = fmaxf(top, __shfl_xor_sync(~0u, top, o));
-              if (top > m[nt][j] + 8.f) {
-                const float by = exp2_fast(m[nt][j] - top);
-                m[nt][j] = top;
-                l[nt][j] *= by;
-                k.rescale(nt, j, by);
-              }
-            }
-        }
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const float shift = m[nt][e % 2] == -INFINITY ? 0.f : m[nt][e % 2];
-            s[nt][e] = exp2_fast(s[nt][e] - shift);
-            l[nt][e % 2] += s[nt][e];
-          }
-        k.outputs(stage, x.len - pos, s);
       }
-      // ---- the warps' results joined
-      const bool any_bad = __any_sync(~0u, bad);
+      float s[MT][NT][4];
+      unrolled<MT>([&](auto t) { k.template scores<decltype(t)::value>(stage, s[decltype(t)::value]); });
+      if (pos > whole_to) {
+#pragma unroll
+        for (int t = 0; t < MT; ++t)
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              s[t][nt][e] = pos + kKeys * t + r + e / 2 * 8 < limit[nt][e % 2] ? s[t][nt][e] : -INFINITY;
+      }
+      // The running maximum follows only rises of more than 2^8 in the weights.
+      float top[NT][2];
+      bool rises = false;
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
+          top[nt][j] = fmaxf(s[0][nt][j], s[0][nt][j + 2]);
 #pragma unroll
-          for (int o = 4; o < 32; o *= 2) l[nt][j] += __shfl_xor_sync(~0u, l[nt][j], o);
-          if (any_bad) l[nt][j] = __int_as_float(0x7fffffff);
-          if (r == 0) {
-            stat[warp][8 * nt + 2 * c + j][0] = m[nt][j];
-            stat[warp][8 * nt + 2 * c + j][1] = l[nt][j];
+          for (int t = 1; t < MT; ++t) top[nt][j] = fmaxf(top[nt][j], fmaxf(s[t][nt][j], s[t][nt][j + 2]));
+          top[nt][j] *= k.factor(nt, j);
+          rises = rises || top[nt][j] > m[nt][j] + 8.f;
+        }
+      if (__any_sync(~0u, rises)) {
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+#pragma unroll
+            for (int o = 4; o < 32; o *= 2) top[nt][j] = fmaxf(top[nt][j], __shfl_xor_sync(~0u, top[nt][j], o));
+            if (top[nt][j] > m[nt][j] + 8.f) {
+              const float by = exp2_fast(m[nt][j] - top[nt][j]);
+              m[nt][j] = shift[nt][j] = top[nt][j];
+              l[nt][j] *= by;
+              k.rescale(nt, j, by);
+            }
           }
-        }
-      __syncthreads();
-      const bool whole = x.from == 0 && x.to == x.tiles;
-      const int slot = 2 * blockIdx.x + (x.from == 0);
+      }
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt) {                      // warps 2 and 3, then 0 and 1 on top of them
-        float w[2];
+      for (int t = 0; t < MT; ++t)
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          const int col = 8 * nt + 2 * c + j;
-          const float top = fmaxf(fmaxf(stat[0][col][0], stat[1][col][0]), fmaxf(stat[2][col][0], stat[3][col][0]));
-          w[j] = m[nt][j] == -INFINITY ? 0.f : exp2_fast(m[nt][j] - top);
-        }
-        if (warp >= 2) k.each(nt, [&](int d, int j, float v) { joined[warp - 2][2 * c + j][d] = v * w[j]; });
-        __syncthreads();
-        if (warp < 2) k.each(nt, [&](int d, int j, float v) { joined[warp][2 * c + j][d] += v * w[j]; });
-        __syncthreads();
-        constexpr int kEach = DP / 16;
-        const int col = threadIdx.x / 16, d0 = threadIdx.x % 16 * kEach, row = x.first + 8 * nt + col;
-        float top = -INFINITY, sum = 0.f;
+        for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-        for (int i = 0; i < kWarps; ++i) top = fmaxf(top, stat[i][8 * nt + col][0]);
-#pragma unroll
-        for (int i = 0; i < kWarps; ++i) {
-          const float mi = stat[i][8 * nt + col][0], li = stat[i][8 * nt + col][1];
-          sum += mi == -INFINITY ? li : li * exp2_fast(mi - top);      // (li is 0 or NaN then)
-        }
-        if (!whole) {
-          float* to = parts + ((int64_t)slot * ROWS + 8 * nt + col) * P::kRow;
-#pragma unroll
-          for (int i = 0; i < kEach; ++i) to[d0 + i] = joined[0][col][d0 + i] + joined[1][col][d0 + i];
-          if (d0 == 0) {
-            to[DP] = top;
-            to[DP + 1] = sum;
+          for (int e = 0; e < 4; ++e) {
+            s[t][nt][e] = exp2_fast(fmaf(s[t][nt][e], k.factor(nt, e % 2), -shift[nt][e % 2]));
+            l[nt][e % 2] += s[t][nt][e];
           }
-        } else if (row < x.n * group) {
-          const int64_t at_row = x.row0 + row / group;
-          const int head = x.head * group + row % group;
-          uint8_t* to = static_cast<uint8_t*>(a.q_out.data) + 2 * (at_row * a.q_out.row + head * a.q_out.head);
-          const float by = sum == 0.f ? 0.f : 1.f / sum;
+      k.outputs(stage, len - pos, s);
+    }
+    if (NT == 1 && ip + 1 < made) K::read(a, query(list[(ip + 1) % kPieces], 0), raw);
 #pragma unroll
-          for (int i = 0; i < kEach; i += 2)
-            if (d0 + i < a.dim)
-              *reinterpret_cast<uint32_t*>(to + 2 * (d0 + i)) =
-                  pack2<BF16>((joined[0][col][d0 + i] + joined[1][col][d0 + i]) * by, (joined[0][col][d0 + i + 1] + joined[1][col][d0 + i + 1]) * by);
-          if (a.lse && d0 == 0) a.lse[head * a.rows + at_row] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * 0.6931471805599453f;
-        }
-        __syncthreads();
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+#pragma unroll
+        for (int o = 4; o < 32; o *= 2) l[nt][j] += __shfl_xor_sync(~0u, l[nt][j], o);
+        if (bad) l[nt][j] = __int_as_float(0x7fffffff);
+      }
+    if (x.from == 0 && to == x.tiles) {    // all of the pass
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        const float by[2] = {l[nt][0] == 0.f ? 0.f : 1.f / l[nt][0], l[nt][1] == 0.f ? 0.f : 1.f / l[nt][1]};
+        const int row = x.first + 8 * nt + r;
+        int token, head;
+        split(x, row, token, head);
+        k.store(a, nt, by, row < x.n * group ? out_row(x.row0 + token, head) : nullptr);
+        if (a.lse && r == 0)
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            split(x, x.first + 8 * nt + 2 * c + j, token, head);
+            if (x.first + 8 * nt + 2 * c + j < x.n * group)
+              a.lse[head * a.rows + x.row0 + token] = l[nt][j] == 0.f ? -INFINITY : (m[nt][j] + log2f(l[nt][j])) * 0.6931471805599453f;
+          }
+      }
+    } else {
+      const int open = to < x.tiles;       // the warp's last piece: its shared memory is free
+      float* const part = open ? reinterpret_cast<float*>(ring + warp * kRing) : parts + P::warp_slot(gridDim.x, blockIdx.x * kWarps + warp);
+      if (open) {
+        wait_groups<0>();
+        __syncwarp();
+      }
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        k.each(nt, [&](int d, int j, float v) { part[(8 * nt + 2 * c + j) * P::kRow + d] = v; });
+        if (r == 0)
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            part[(8 * nt + 2 * c + j) * P::kRow + DP] = m[nt][j];
+            part[(8 * nt + 2 * c + j) * P::kRow + DP + 1] = l[nt][j];
+          }
+      }
+      if (lane == 0) {
+        if (open) left.open = x.from ? 2 : 1;
+        else left.before = 1;
+        left.row0[open] = x.row0;
+        left.n[open] = x.n;
+        left.head[open] = x.head;
+        left.first[open] = x.first;
       }
     }
-    wait_groups<0>();
-    __syncthreads();
+    __syncwarp();
   }
-  if (threadIdx.x == 0) headers[blockIdx.x] = lister.header;
+  wait_groups<0>();
+  __syncthreads();
+
+  // Passes of which several warps have pieces, in the order of the warps: a chain
+  // from a warp's open pass over those that it goes on in to one that ends it.
+  // What is still open at either end of the block goes to the second kernel.
+  Header header{0, 0, 0, 0, 0, 0};
+  auto join = [&](int a0, int b, bool ended, bool led) {
+    const Left& of = lefts[ended ? b : a0];
+    const int which = ended ? 0 : 1, row0 = of.row0[which], n = of.n[which], head = of.head[which], first = of.first[which];
+    const bool whole = ended && !led;
+    const int slot = 2 * blockIdx.x + (ended || led ? 0 : 1);
+    if (led) header.before = ended ? 2 : 1;
+    else if (!ended) header = Header{header.before, 1, row0, n, head, first};
+    for (int row = warp; row < ROWS && first + row < n * group; row += kWarps) {
+      const float* p[kWarps + 1];
+      float top = -INFINITY, sum = 0.f, acc[DP / 32];
+#pragma unroll
+      for (int e = 0; e < DP / 32; ++e) acc[e] = 0.f;
+#pragma unroll
+      for (int w = 0; w <= kWarps; ++w) {
+        p[w] = w < kWarps ? (w >= a0 && w < b ? reinterpret_cast<const float*>(ring + w * kRing) + row * P::kRow : nullptr)
+                          : ended ? parts + P::warp_slot(gridDim.x, blockIdx.x * kWarps + b) + row * P::kRow : nullptr;
+        if (p[w]) top = fmaxf(top, p[w][DP]);
+      }
+#pragma unroll
+      for (int w = 0; w <= kWarps; ++w)
+        if (p[w]) {
+          const float m = p[w][DP], l = p[w][DP + 1], f = m == -INFINITY ? 0.f : exp2_fast(m - top);
+          sum += m == -INFINITY ? l : l * f;                 // (l is 0 or NaN where nothing was seen)
+#pragma unroll
+          for (int e = 0; e < DP / 32; ++e) acc[e] = fmaf(f, p[w][lane + 32 * e], acc[e]);
+        }
+      if (whole) {
+        const int token = (first + row) / group, h = head * group + (first + row) % group;
+        uint8_t* to = out_row(row0 + token, h);
+        const float by = sum == 0.f ? 0.f : 1.f / sum;
+#pragma unroll
+        for (int e = 0; e < DP / 32; ++e)
+          if (lane + 32 * e < a.dim) reinterpret_cast<uint16_t*>(to)[lane + 32 * e] = (uint16_t)pack2<BF16>(acc[e] * by, 0.f);
+        if (a.lse && lane == 0) a.lse[h * a.rows + row0 + token] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * 0.6931471805599453f;
+      } else {
+        float* to = parts + P::slot(slot) + row * P::kRow;
+#pragma unroll
+        for (int e = 0; e < DP / 32; ++e) to[lane + 32 * e] = acc[e];
+        if (lane == 0) {
+          to[DP] = top;
+          to[DP + 1] = sum;
+        }
+      }
+    }
+  };
+  bool going = false, led = false;
+  int a0 = 0, last = 0;
+#pragma unroll 1
+  for (int w = 0; w < kWarps; ++w) {
+    if (lefts[w].before) {
+      join(going ? a0 : w, w, true, going ? led : true);
+      going = false;
+    }
+    if (lefts[w].open) {
+      if (!going) {
+        a0 = w;
+        led = lefts[w].open == 2;
+      }
+      going = true;
+      last = w;
+    }
+  }
+  if (going) join(a0, last + 1, false, led);
+  if (threadIdx.x == 0) reinterpret_cast<Header*>(a.work)[blockIdx.x] = header;
 }
 
 // Passes that were cut, from their pieces in order: a block for each block of
@@ -741,7 +1014,7 @@ __global__ void __launch_bounds__(kThreads) k_cache_merge(const __grid_constant_
     }
   }
   last = min(last, blocks - 1);
-  auto part = [&](int b) { return parts + (int64_t)(2 * b + (b == (int)blockIdx.x)) * ROWS * P::kRow; };
+  auto part = [&](int b) { return parts + P::slot(2 * b + (b == (int)blockIdx.x)); };
   float top = -INFINITY;
   for (int b = blockIdx.x + lane; b <= last; b += 32) top = fmaxf(top, part(b)[DP]);
 #pragma unroll
@@ -819,7 +1092,7 @@ int cache_attn_blocks(int bits, int most_rows, int num_sms) { return per_sm(bits
 int64_t cache_attn_workspace(int dim, int most_rows, int blocks) {
   const int dp = dim <= 64 ? 64 : 128;
   const size_t header = Parts<128, 32>::header(blocks);
-  return (int64_t)(header + (size_t)2 * blocks * most_rows * (dp + 4) * sizeof(float));
+  return (int64_t)(header + (size_t)Parts<128, 32>::kSlots * blocks * most_rows * (dp + 4) * sizeof(float));
 }
 
 cudaError_t launch_cache_attn(const CacheArgs& a, cudaStream_t st) {

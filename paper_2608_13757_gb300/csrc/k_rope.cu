@@ -19,43 +19,41 @@ using namespace rotate;
 constexpr int kThreads = 256, kAhead = 4;
 
 template <class T, int VEC, bool INTER>
-__global__ void __launch_bounds__(kThreads) k_rope(const __grid_constant__ RopeArgs a, int tokens) {
+__global__ void __launch_bounds__(kThreads, 3) k_rope(const __grid_constant__ RopeArgs a, int tokens) {
   extern __shared__ __align__(16) float angles[];          // [tokens][cos, sin][half]
-  const int half = a.turn.half, pairs = a.dim / 2, runs = pairs / VEC, heads = a.heads + a.kv_heads;
+  const int half = a.turn.half, pairs = a.dim / 2, heads = a.heads + a.kv_heads;
   const int64_t row0 = blockIdx.x * (int64_t)tokens;
   const int n = (int)min((int64_t)tokens, a.rows - row0);
+  Walk w(threadIdx.x, kThreads, heads, pairs / VEC);
+  Pairs<T, VEC, INTER> x[kAhead];
+  auto read = [&](Walk at) {                                // the next runs
+#pragma unroll
+    for (int e = 0; e < kAhead; ++e, at.next()) {
+      if (at.t >= n) break;
+      const HeadTensor& in = at.h < a.heads ? a.q : a.k;
+      x[e].read(static_cast<const T*>(in.data) + (row0 + at.t) * in.row + (at.h < a.heads ? at.h : at.h - a.heads) * in.head,
+                at.r * VEC, half, pairs);
+    }
+  };
+  read(w);                                                  // under the way to the angles
   for (int i = threadIdx.x; i < n * half; i += kThreads) {
     const int t = i / half, j = i - t * half;
-    const float2 x = angle(a.turn, position(a.turn, row0 + t, row0 + t, j), j);
-    angles[2 * t * half + j] = x.x;
-    angles[(2 * t + 1) * half + j] = x.y;
+    const float2 y = angle(a.turn, position(a.turn, row0 + t, row0 + t, j), j);
+    angles[2 * t * half + j] = y.x;
+    angles[(2 * t + 1) * half + j] = y.y;
   }
   __syncthreads();
-  const int each = heads * runs, all = n * each;
-  for (int i0 = threadIdx.x; i0 < all; i0 += kAhead * kThreads) {
-    Pairs<T, VEC, INTER> x[kAhead];
-    T* to[kAhead];
-    int p[kAhead], t[kAhead];
+  while (w.t < n) {
 #pragma unroll
-    for (int e = 0; e < kAhead; ++e) {
-      const int i = i0 + e * kThreads;
-      if (i >= all) break;
-      t[e] = i / each;
-      const int r = i - t[e] * each, h = r / runs;
-      p[e] = (r - h * runs) * VEC;
-      const bool is_q = h < a.heads;
-      const HeadTensor &in = is_q ? a.q : a.k, &out = is_q ? a.q_out : a.k_out;
-      const int64_t row = row0 + t[e], head = is_q ? h : h - a.heads;
-      to[e] = static_cast<T*>(out.data) + row * out.row + head * out.head;
-      x[e].read(static_cast<const T*>(in.data) + row * in.row + head * in.head, p[e], half, pairs);
+    for (int e = 0; e < kAhead; ++e, w.next()) {
+      if (w.t >= n) break;
+      const int p = w.r * VEC;
+      const float* c = angles + 2 * w.t * half + p;
+      if (p < half) x[e].by(c, c + half);
+      const HeadTensor& out = w.h < a.heads ? a.q_out : a.k_out;
+      x[e].write(static_cast<T*>(out.data) + (row0 + w.t) * out.row + (w.h < a.heads ? w.h : w.h - a.heads) * out.head, p, half, pairs);
     }
-#pragma unroll
-    for (int e = 0; e < kAhead; ++e) {
-      if (i0 + e * kThreads >= all) break;
-      const float* c = angles + 2 * t[e] * half + p[e];
-      if (p[e] < half) x[e].by(c, c + half);
-      x[e].write(to[e], p[e], half, pairs);
-    }
+    if (w.t < n) read(w);
   }
 }
 

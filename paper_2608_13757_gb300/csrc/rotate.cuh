@@ -78,6 +78,35 @@ struct Pairs {
   }
 };
 
+// Items (token, head, run of a head) of a block in steps of its threads, counted
+// on instead of divided out.
+struct Walk {
+  int t, h, r;
+  int dt, dh, dr, heads, runs;
+  __device__ __forceinline__ Walk(int from, int step, int heads_, int runs_) : heads(heads_), runs(runs_) {
+    const int each = heads * runs;
+    t = from / each;
+    h = (from - t * each) / runs;
+    r = from - t * each - h * runs;
+    dt = step / each;
+    dh = (step - dt * each) / runs;
+    dr = step - dt * each - dh * runs;
+  }
+  __device__ __forceinline__ void next() {
+    r += dr;
+    h += dh;
+    t += dt;
+    if (r >= runs) {
+      r -= runs;
+      ++h;
+    }
+    if (h >= heads) {
+      h -= heads;
+      ++t;
+    }
+  }
+};
+
 // The widest run of pairs, of up to 16 bytes, that sizes, strides and
 // addresses of all `n` tensors allow, in entries of `size` bytes; 1 always goes.
 inline int widest(const HeadTensor* t, int n, int size, int half, int dim) {
