@@ -63,7 +63,7 @@ Rotation rotation(const sync_rotation* t, int dim, int64_t rows) {
 RopeArgs rope_args(const sync_rope_desc* p, const sync_rows* q_out, const sync_rows* k_out) {
   need(p, "the description must not be NULL");
   need(p->dtype == SYNC_BF16 || p->dtype == SYNC_FP16 || p->dtype == SYNC_FP32, "dtype must be a sync_dtype");
-  need(p->heads >= 1 && p->kv_heads >= 1 && (int64_t)p->heads + p->kv_heads <= INT32_MAX / 4096, "heads and kv_heads must be at least 1");
+  need(p->heads >= 1 && p->kv_heads >= 1 && p->heads <= 65536 && p->kv_heads <= 65536, "heads and kv_heads must be in 1..65536");
   need(p->dim >= 2 && p->dim <= 2 * kMostPairs && p->dim % 2 == 0, "dim must be even and in 2..256");
   need(p->q.rows >= 0 && p->q.rows <= INT32_MAX, "the number of rows must be in 0..INT32_MAX");
   need(p->turn.rotated >= 0, "rotated must be even and in 0..dim");

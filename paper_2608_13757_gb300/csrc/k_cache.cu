@@ -1,11 +1,11 @@
 // Rows into and out of the paged cache (include/sync.h, sync_cache_append and
 // sync_cache_read).
 //
-// Both are one pass over the rows, bound by memory.  A block takes a few tokens;
-// a warp per token finds its sequence, its position and its place first, the
-// angles are staged in shared memory (rotate.cuh), and the threads then take
-// pieces of 16 bytes of the tokens' heads in turn.
-#include <algorithm>
+// Both are one pass over the rows, bound by memory, in the manner of rotate.cuh:
+// a thread has a column of 16 bytes for all tokens of its block.  Sequences,
+// positions and places of the block's tokens (reads that depend on one another)
+// are found first, a thread per token, for kFound tokens at a time.
+#include <type_traits>
 
 #include "cache.h"
 #include "paged.cuh"
@@ -17,55 +17,63 @@ namespace {
 
 using namespace rotate;
 
-constexpr int kThreads = 256, kTokens = 8;       // most tokens of a block: one per warp
-constexpr int kAhead = 4;                        // pieces that a thread reads before it writes the first
+constexpr int kReadAhead = 8;            // pieces of a column that a thread of k_read has in flight
+constexpr int kReadResident = 768;       // its threads of an SM
+// Columns of a block of k_append, tokens that its threads have in flight, and its
+// threads of an SM: several blocks, which do not wait for one another's angles.
+constexpr int kAppendThreads = 256, kAppendAhead = 2, kAppendResident = 1024;
+constexpr int kFound = 512;              // tokens whose places a block knows
 
 // 8 entries of a row, by one access or entry by entry
 template <class T>
-__device__ __forceinline__ void load8(const T* p, bool wide, float* x) {
+__device__ __forceinline__ void load8(const T* p, bool wide, uint32_t* w) {
   if (wide) {
-    const Pack<T, 8> v = *reinterpret_cast<const Pack<T, 8>*>(p);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = to_f(v.x[i]);
+    *reinterpret_cast<Pack<uint32_t, 4>*>(w) = *reinterpret_cast<const Pack<uint32_t, 4>*>(p);
   } else {
+    const uint16_t* x = reinterpret_cast<const uint16_t*>(p);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = to_f(p[i]);
+    for (int i = 0; i < 4; ++i) w[i] = x[2 * i] | (uint32_t)x[2 * i + 1] << 16;
+  }
+}
+template <class T>
+__device__ __forceinline__ void unpack8(const uint32_t* w, float* x) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float2 y = unpack<T>(w[i]);
+    x[2 * i] = y.x;
+    x[2 * i + 1] = y.y;
   }
 }
 
-// Entries d .. d + 7 of a key head after the rotation.  c: cosines of the
-// token's pairs, then its sines.
-template <class T>
-__device__ __forceinline__ void turned8(const T* head, int d, bool wide, int half, bool interleaved, const float* c, float* x) {
+// Entries d .. d + 7 of a key head, whose words are w, after the rotation: by
+// their own pairs (interleaved) or with the entries half a rotation further or
+// back (other).  c: cosines of the token's pairs, then its sines.
+template <class T, bool INTER>
+__device__ __forceinline__ void turned8(const T* head, const uint32_t* w, const uint32_t* other, int d, int half, const float* c, float* x) {
   const float* s = c + half;
-  if (interleaved) {
-    load8(head + d, wide, x);
+  unpack8<T>(w, x);
+  if (d >= 2 * half) return;
+  if (INTER) {
 #pragma unroll
     for (int i = 0; i < 8; i += 2)
       if (d + i < 2 * half) turn(x[i], x[i + 1], c[(d + i) / 2], s[(d + i) / 2]);
-  } else if (wide && half % 8 == 0) {
-    load8(head + d, wide, x);
-    if (d >= 2 * half) return;
+  } else if (half % 8 == 0) {
     float y[8];
+    unpack8<T>(other, y);
     const int j = d < half ? d : d - half;
-    load8(head + (d < half ? d + half : j), wide, y);
+    const uint32_t sign = d < half ? 0x80000000u : 0u;      // a c - b s, or b c + a s
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      if (d < half) turn(x[i], y[i], c[j + i], s[j + i]);
-      else turn(y[i], x[i], c[j + i], s[j + i]);
-    }
-  } else {
+    for (int i = 0; i < 8; ++i)
+      x[i] = __fadd_rn(__fmul_rn(x[i], c[j + i]), __fmul_rn(__uint_as_float(__float_as_uint(y[i]) ^ sign), s[j + i]));
+  } else {                                                  // 8 entries that are not all on one side
 #pragma unroll 1
     for (int i = 0; i < 8; ++i) {
       const int e = d + i, j = e < half ? e : e - half;
-      float v = to_f(head[e]);
-      if (e < 2 * half) {
-        float u = to_f(head[e < half ? e + half : j]);
-        if (e < half) turn(v, u, c[j], s[j]);
-        else turn(u, v, c[j], s[j]);
-      }
+      if (e >= 2 * half) break;
+      float u = to_f(head[j]), v = to_f(head[j + half]);
+      turn(u, v, c[j], s[j]);
 #pragma unroll
-      for (int k = 0; k < 8; ++k) x[k] = k == i ? v : x[k];
+      for (int k = 0; k < 8; ++k) x[k] = k != i ? x[k] : e < half ? u : v;
     }
   }
 }
@@ -83,178 +91,329 @@ __device__ __forceinline__ uint32_t codes8(const float* x, __half& scale, uint32
   top = max(top, __shfl_xor_sync(lanes, top, 2));
   scale = top >= 0x7f800000u ? __ushort_as_half(0x7fff) : __float2half(fminf(__fdiv_rn(__uint_as_float(top), 7.f), 65504.f));
   const float by = __half2float(scale);
+  if (!(by > 0.f)) return 0x88888888u;
+  // Quotients by the reciprocal, off by less than 7 * 2^-22 from those of the
+  // division: where one is so near to a half that this could matter, all are
+  // divided.
+  const float inverse = __fdiv_rn(1.f, by);
+  float far = 0.f;                                          // from the whole number next to it
   uint32_t word = 0;
+  auto codes = [&](auto quotient) {
+    word = 0;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const int code = by > 0.f ? min(7, max(-7, __float2int_rn(__fdiv_rn(x[i], by)))) : 0;
-    word |= (uint32_t)(code + 8) << (4 * i);
-  }
+    for (int i = 0; i < 8; ++i) {
+      const float t = fminf(7.f, fmaxf(-7.f, quotient(x[i]))), m = t + 12582920.f;   // 1.5 * 2^23 + 8: its last bits are the code
+      far = fmaxf(far, fabsf(t - (m - 12582920.f)));
+      word |= (__float_as_uint(m) & 15u) << (4 * i);
+    }
+  };
+  codes([&](float v) { return v * inverse; });
+  if (far > 0.4999f) codes([&](float v) { return __fdiv_rn(v, by); });
   return word;
 }
 
-// New tokens into the cache.  T: their type.  QVEC: pairs of a query head that
-// a thread takes at a time.
+// Where a row's token is.  place: counted in rows of the cache for key head 0
+// (head h is h << page_shift further); -1: nowhere.
+struct Where {
+  int64_t place;
+  int pos;
+  int mine;                                                 // a sequence has the row
+};
+// The groups of a block's next kFound tokens: group, group + gridDim.x, ..; how many.
+__device__ __forceinline__ int known_groups(const Columns& c, int64_t group) {
+  const int64_t left = (c.groups - group + gridDim.x - 1) / gridDim.x;
+  return (int)min(left, (int64_t)(kFound / c.tokens()));
+}
+
+// What a thread of k_append has of a token: runs of pairs of a query head, or
+// 8 entries of a key or value head.
 template <class T, int QVEC, bool INTER>
-__global__ void __launch_bounds__(kThreads) k_append(const __grid_constant__ CacheArgs a, int tokens, bool kv_wide) {
-  extern __shared__ __align__(16) float angles[];           // [tokens][cos, sin][half]
-  __shared__ int64_t place[kTokens], pos[kTokens];
-  __shared__ bool mine[kTokens];                            // a sequence has the row
-  const int half = a.turn.half, warp = threadIdx.x / 32;
-  const int64_t row0 = blockIdx.x * (int64_t)tokens;
-  const int n = (int)min((int64_t)tokens, a.rows - row0);
-  if (warp < n) {
-    const int64_t row = row0 + warp;
-    const int s = paged::sequence_of(a, row);
-    if (threadIdx.x % 32 == 0) {
-      int64_t at = -1;
-      if (s >= 0) at = a.starts ? (int64_t)__ldg(a.lens + s) - __ldg(a.starts + s + 1) + row : (int64_t)__ldg(a.lens + s) - 1;
-      mine[warp] = s >= 0;
-      pos[warp] = at;
-      place[warp] = s >= 0 ? paged::place_of(a, s, at) : -1;
+struct QueryItem {
+  static constexpr int kAhead = kAppendAhead;               // tokens in flight
+  Pairs<T, QVEC, INTER> x[kAhead];
+  const T* from;
+  T* to;
+  int p, half, pairs;
+  int64_t in_row, out_row;
+  bool fill;
+  __device__ __forceinline__ bool begin(const CacheArgs& a, int column) {
+    half = a.turn.half;
+    pairs = a.dim / 2;
+    const int runs = pairs / QVEC, head = column / runs;
+    p = (column - head * runs) * QVEC;
+    in_row = a.q.row;
+    out_row = a.q_out.row;
+    from = static_cast<const T*>(a.q.data) + head * a.q.head;
+    to = static_cast<T*>(a.q_out.data) + head * a.q_out.head;
+    fill = a.fill;
+    return column < a.heads * runs;
+  }
+  __device__ __forceinline__ void read(int e, int64_t row) { x[e].read(from + row * in_row, p, half, pairs); }
+  __device__ __forceinline__ void write(int e, int64_t row, const Where& w, const float* cs) {
+    if (w.mine) {
+      if (p < half) x[e].by(cs + p, cs + half + p);
+    } else {
+      if (!fill) return;
+#pragma unroll
+      for (uint32_t& z : x[e].w) z = 0;
     }
+    x[e].write(to + row * out_row, p, half, pairs);
   }
-  __syncthreads();
-  for (int i = threadIdx.x; i < n * half; i += kThreads) {
-    const int t = i / half, j = i - t * half;
-    if (!mine[t]) continue;
-    const float2 x = angle(a.turn, position(a.turn, row0 + t, pos[t], j), j);
-    angles[2 * t * half + j] = x.x;
-    angles[(2 * t + 1) * half + j] = x.y;
-  }
-  __syncthreads();
-  if (a.heads) {                                            // queries, as k_rope turns them
-    const int pairs = a.dim / 2;
-    Walk w(threadIdx.x, kThreads, a.heads, pairs / QVEC);
-    while (w.t < n) {
-      Pairs<T, QVEC, INTER> x[kAhead];
-      Walk at = w;
-#pragma unroll
-      for (int e = 0; e < kAhead; ++e, at.next()) {
-        if (at.t >= n) break;
-        if (mine[at.t]) x[e].read(static_cast<const T*>(a.q.data) + (row0 + at.t) * a.q.row + at.h * a.q.head, at.r * QVEC, half, pairs);
-      }
-#pragma unroll
-      for (int e = 0; e < kAhead; ++e, w.next()) {
-        if (w.t >= n) break;
-        const int p = w.r * QVEC;
-        if (!mine[w.t]) {
-          if (!a.fill) continue;
-#pragma unroll
-          for (int i = 0; i < 2 * QVEC; ++i) from_f(x[e].x[i], 0.f);
-        } else if (p < half) {
-          const float* c = angles + 2 * w.t * half + p;
-          x[e].by(c, c + half);
-        }
-        x[e].write(static_cast<T*>(a.q_out.data) + (row0 + w.t) * a.q_out.row + w.h * a.q_out.head, p, half, pairs);
-      }
-    }
-  }
-  // keys, then values: 8 entries per thread
-  // (a row has a multiple of 4 runs where the cache has 4 bits: the lanes of a group agree)
-  const int g = a.dim / kGroup;
-  for (Walk w(threadIdx.x, kThreads, 2 * a.kv_heads, a.dim / 8); w.t < n; w.next()) {
-    const int t = w.t, e = w.r, d = 8 * e;
-    if (place[t] < 0) continue;
-    const bool is_v = w.h >= a.kv_heads;
-    const int h = is_v ? w.h - a.kv_heads : w.h;
+};
+
+template <class T, int BITS, bool INTER>
+struct KeyItem {
+  static constexpr int kAhead = kAppendAhead;
+  uint32_t x[kAhead][8];                                    // 8 entries, and of a key those that they turn with
+  const T* from;
+  uint8_t *data, *scales;
+  int d, half, row_bytes, g, other;
+  int64_t in_row;
+  bool is_v, wide, paired;
+  __device__ __forceinline__ bool begin(const CacheArgs& a, bool kv_wide, int column) {
+    const int runs = a.dim / 8, at = column / runs;
+    is_v = at >= a.kv_heads;
+    const int head = is_v ? at - a.kv_heads : at;
     const HeadTensor& in = is_v ? a.v_rows : a.k_rows;
-    const T* head = static_cast<const T*>(in.data) + (row0 + t) * in.row + h * in.head;
-    const int64_t at = paged::row_of(a, place[t], h);
-    float x[8];
-    if (is_v) load8(head + d, kv_wide, x);
-    else turned8(head, d, kv_wide, half, INTER, angles + 2 * t * half, x);
-    if (a.bits == 16) {
-      Pack<T, 8> y;
+    const int64_t head_rows = (int64_t)head << a.page_shift;
+    half = a.turn.half;
+    g = a.dim / kGroup;
+    d = (column - at * runs) * 8;
+    from = static_cast<const T*>(in.data) + head * in.head;
+    in_row = in.row;
+    row_bytes = BITS == 16 ? 2 * a.dim : a.dim / 2;
+    data = (is_v ? a.v : a.k) + head_rows * row_bytes + (BITS == 16 ? 2 * d : 4 * paged::word_of(d / 8, g));
+    scales = BITS == 16 ? nullptr : (is_v ? a.v_scale : a.k_scale) + 2 * (head_rows * g + d / kGroup);
+    wide = kv_wide;
+    paired = !INTER && !is_v && half % 8 == 0 && d < 2 * half;
+    other = d < half ? half : -half;
+    return column < 2 * a.kv_heads * runs;
+  }
+  __device__ __forceinline__ void read(int e, int64_t row) {
+    const T* head = from + row * in_row + d;
+    load8(head, wide, x[e]);
+    if (paired) load8(head + other, wide, x[e] + 4);
+  }
+  __device__ __forceinline__ void write(int e, int64_t row, const Where& w, const float* cs) {
+    if (w.place < 0) return;
 #pragma unroll
-      for (int k = 0; k < 8; ++k) from_f(y.x[k], x[k]);
-      *reinterpret_cast<Pack<T, 8>*>((is_v ? a.v : a.k) + (at * a.dim + d) * 2) = y;
+    for (uint32_t& z : x[e]) asm volatile("" : "+r"(z));     // (unpacked from here on, not where they were read)
+    uint8_t* const to = data + w.place * row_bytes;
+    if (BITS == 16 && (is_v || d >= 2 * half)) {
+      *reinterpret_cast<Pack<uint32_t, 4>*>(to) = *reinterpret_cast<const Pack<uint32_t, 4>*>(x[e]);
+      return;
+    }
+    float y[8];
+    if (is_v) unpack8<T>(x[e], y);
+    else turned8<T, INTER>(from + row * in_row, x[e], x[e] + 4, d, half, cs, y);
+    if (BITS == 16) {
+      Pack<uint32_t, 4> z;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) z.x[i] = pack<T>(y[2 * i], y[2 * i + 1]);
+      *reinterpret_cast<Pack<uint32_t, 4>*>(to) = z;
     } else {
       __half scale;
-      const uint32_t word = codes8(x, scale, 0xfu << (threadIdx.x % 32 / 4 * 4));
-      *reinterpret_cast<uint32_t*>((is_v ? a.v : a.k) + at * (a.dim / 2) + 4 * paged::word_of(e, g)) = word;
-      if (e % 4 == 0) reinterpret_cast<__half*>(is_v ? a.v_scale : a.k_scale)[at * g + e / 4] = scale;
+      *reinterpret_cast<uint32_t*>(to) = codes8(y, scale, 0xfu << (threadIdx.x % 32 / 4 * 4));
+      if (d % kGroup == 0) *reinterpret_cast<__half*>(scales + w.place * (2 * g)) = scale;
     }
+  }
+};
+
+// All tokens of this block through `item`, which has this thread's column.
+template <class Item>
+__device__ __forceinline__ void through(const CacheArgs& a, const Columns& c, float* angles, Where* where, bool on, Item& item) {
+  constexpr int kAhead = Item::kAhead;
+  const int half = a.turn.half, tokens = c.tokens(), sub = threadIdx.x / c.each;
+  auto here = [&](int64_t group) {                          // tokens of this thread in a group
+    const int64_t left = a.rows - group * tokens - sub;
+    return on && left > 0 ? (int)min((int64_t)c.ahead, (left + c.par - 1) / c.par) : 0;
+  };
+  auto read = [&](int64_t group) {
+    const int n = here(group);
+#pragma unroll
+    for (int e = 0; e < kAhead; ++e)
+      if (e < n) item.read(e, group * tokens + sub + e * c.par);
+  };
+  auto search = [&](int64_t group, int groups) {            // into where, for that many groups
+    for (int i = threadIdx.x; i < groups * tokens; i += blockDim.x) {
+      const int64_t row = (group + (int64_t)(i / tokens) * gridDim.x) * tokens + i % tokens;
+      Where w{-1, -1, 0};
+      const int s = row < a.rows ? paged::sequence_of(a, (int)row) : -1;
+      if (s >= 0) {
+        w.mine = 1;
+        w.pos = (int)(a.starts ? (int64_t)__ldg(a.lens + s) - __ldg(a.starts + s + 1) + row : (int64_t)__ldg(a.lens + s) - 1);
+        const int64_t at = paged::place_of(a, s, w.pos);
+        if (at >= 0) w.place = paged::row_of(a, at, 0);
+      }
+      where[i] = w;
+    }
+  };
+  int t[kStaged], j[kStaged];                                 // staged entries of this thread: pair j of token t
+  float2 turned[kStaged];
+#pragma unroll
+  for (int e = 0; e < kStaged; ++e) {
+    const int i = threadIdx.x + e * blockDim.x;
+    t[e] = i < tokens * half ? i / half : -1;
+    j[e] = i - t[e] * half;
+  }
+  auto find = [&](int64_t group, int at) {                  // angles of a group, whose tokens are at `at` of where
+#pragma unroll
+    for (int e = 0; e < kStaged; ++e) {
+      if (t[e] < 0) continue;
+      const Where& w = where[at + t[e]];
+      if (w.mine) turned[e] = angle(a.turn, position(a.turn, group * tokens + t[e], w.pos, j[e]), j[e]);
+    }
+  };
+  auto put = [&](int which) {
+#pragma unroll
+    for (int e = 0; e < kStaged; ++e)
+      if (t[e] >= 0) {
+        float* to = angles + ((which * tokens + t[e]) * 2) * half + j[e];
+        to[0] = turned[e].x;
+        to[half] = turned[e].y;
+      }
+  };
+  int64_t group = blockIdx.x;
+  read(group);
+  while (group < c.groups) {
+    const int known = known_groups(c, group);
+    search(group, known);
+    __syncthreads();
+    find(group, 0);
+    put(0);
+    __syncthreads();
+#pragma unroll 1
+    for (int n = 0; n < known; ++n, group += gridDim.x) {
+      const bool more = n + 1 < known;
+      if (more) find(group + gridDim.x, (n + 1) * tokens);
+      const int mine = here(group);
+#pragma unroll
+      for (int e = 0; e < kAhead; ++e) {
+        const int token = sub + e * c.par;
+        if (e < mine) item.write(e, group * tokens + token, where[n * tokens + token], angles + ((n % 2 * tokens + token) * 2) * half);
+      }
+      if (group + gridDim.x < c.groups) read(group + gridDim.x);
+      if (more) put((n + 1) % 2);
+      __syncthreads();
+    }
+  }
+}
+
+// New tokens into the cache: blocks [0, kv_blocks) of a group take its keys and
+// values, the others its queries.  T: their type; QVEC: pairs of a query head that
+// a thread takes at a time.
+template <class T, int QVEC, int BITS, bool INTER>
+__global__ void __launch_bounds__(kAppendResident, 1) k_append(const __grid_constant__ CacheArgs a, const __grid_constant__ Columns c, int kv_blocks, bool kv_wide) {
+  extern __shared__ __align__(16) float angles[];           // [2][tokens][cos, sin][half]
+  __shared__ Where where[kFound];
+  const bool on = (int)threadIdx.x / c.each < c.par;
+  const int column = threadIdx.x % c.each;
+  if ((int)blockIdx.y < kv_blocks) {
+    KeyItem<T, BITS, INTER> item;
+    const bool has = item.begin(a, kv_wide, blockIdx.y * c.each + column);
+    through(a, c, angles, where, on && has, item);
+  } else {
+    QueryItem<T, QVEC, INTER> item;
+    const bool has = item.begin(a, (blockIdx.y - kv_blocks) * c.each + column);
+    through(a, c, angles, where, on && has, item);
   }
 }
 
 // Cached tokens back to rows of 16 bits: the tokens of sequence s from its first
 // one on go to rows starts[s] .. starts[s + 1]; zeros past its length.
-template <class T>
-__global__ void __launch_bounds__(kThreads) k_read(const __grid_constant__ CacheArgs a, int tokens) {
-  __shared__ int64_t place[kTokens];                        // -1: no such token, -2: not a sequence's row, -3: no such page
-  const int64_t row0 = blockIdx.x * (int64_t)tokens;
-  const int n = (int)min((int64_t)tokens, a.rows - row0), warp = threadIdx.x / 32;
-  if (warp < n) {
-    const int64_t row = row0 + warp;
-    const int s = paged::sequence_of(a, row);
-    if (threadIdx.x % 32 == 0) {
-      int64_t at = -2;
+template <class T, int BITS>
+__global__ void __launch_bounds__(kReadResident, 1) k_read(const __grid_constant__ CacheArgs a, const __grid_constant__ Columns c) {
+  __shared__ int64_t places[kFound];                        // as in Where; -1: no such token, -2: no sequence's row, -3: no such page
+  const int tokens = c.tokens(), runs = a.dim / 8, g = a.dim / kGroup;
+  const int sub = threadIdx.x / c.each, column = blockIdx.y * c.each + threadIdx.x % c.each;
+  const bool on = sub < c.par && column < 2 * a.kv_heads * runs;
+  const int at = column / runs, run = column - at * runs;
+  const bool is_v = at >= a.kv_heads;
+  const int head = is_v ? at - a.kv_heads : at;
+  const HeadTensor& out = is_v ? a.v_rows : a.k_rows;
+  T* const to = static_cast<T*>(out.data) + head * out.head + 8 * run;
+  const int64_t out_row = out.row, out_step = out_row * c.par, head_rows = (int64_t)head << a.page_shift;
+  // this column's piece of the cache's rows
+  const int row_bytes = BITS == 16 ? 2 * a.dim : a.dim / 2;
+  const uint8_t* const data = (is_v ? a.v : a.k) + head_rows * row_bytes + (BITS == 16 ? 16 * run : 4 * paged::word_of(run, g));
+  const uint8_t* const scales = BITS == 16 ? nullptr : (is_v ? a.v_scale : a.k_scale) + (head_rows * g + run / 4) * 2;
+
+  int64_t group = blockIdx.x;
+  while (group < c.groups) {
+    const int known = known_groups(c, group);
+    for (int i = threadIdx.x; i < known * tokens; i += blockDim.x) {
+      const int64_t row = (group + (int64_t)(i / tokens) * gridDim.x) * tokens + i % tokens;
+      const int s = row < a.rows ? paged::sequence_of(a, (int)row) : -1;
+      int64_t p = -2;
       if (s >= 0) {
-        const int64_t p = row - (a.starts ? __ldg(a.starts + s) : row);
-        at = p < __ldg(a.lens + s) ? paged::place_of(a, s, p) : -1;
-        if (at < 0 && p < __ldg(a.lens + s)) at = -3;
-      }
-      place[warp] = at;
-    }
-  }
-  __syncthreads();
-  const int g = a.dim / kGroup;
-  Walk w(threadIdx.x, kThreads, 2 * a.kv_heads, a.dim / 8);
-  while (w.t < n) {
-    Pack<T, 8> y[kAhead];                                   // 16 bits: the entries; 4: a word of codes and its scale
-    Walk at = w;
-#pragma unroll
-    for (int e = 0; e < kAhead; ++e, at.next()) {
-      if (at.t >= n) break;
-      if (place[at.t] < 0) continue;
-      const bool is_v = at.h >= a.kv_heads;
-      const int64_t row = paged::row_of(a, place[at.t], is_v ? at.h - a.kv_heads : at.h);
-      if (a.bits == 16) {
-        y[e] = *reinterpret_cast<const Pack<T, 8>*>((is_v ? a.v : a.k) + (row * a.dim + 8 * at.r) * 2);
-      } else {
-        uint32_t* in = reinterpret_cast<uint32_t*>(&y[e]);
-        in[0] = __ldg(reinterpret_cast<const uint32_t*>((is_v ? a.v : a.k) + row * (a.dim / 2)) + paged::word_of(at.r, g));
-        in[1] = __ldg(reinterpret_cast<const uint16_t*>(is_v ? a.v_scale : a.k_scale) + row * g + at.r / 4);
-      }
-    }
-#pragma unroll
-    for (int e = 0; e < kAhead; ++e, w.next()) {
-      if (w.t >= n) break;
-      const int64_t from = place[w.t];
-      if (from == -2 && !a.fill) continue;
-      if (from < 0) {
-#pragma unroll
-        for (int k = 0; k < 8; ++k) from_f(y[e].x[k], from == -3 ? __int_as_float(0x7fffffff) : 0.f);
-      } else if (a.bits == 4) {
-        const uint32_t* in = reinterpret_cast<const uint32_t*>(&y[e]);
-        const uint32_t word = in[0];
-        const float scale = __half2float(__ushort_as_half((uint16_t)in[1]));
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          float x = (float)((int)(word >> (4 * k) & 15) - 8) * scale;
-          // 7 scales may be past float16's end where the row's largest entry was not: the scale was rounded
-          if (!a.bf16) x = x > 65504.f ? 65504.f : x < -65504.f ? -65504.f : x;
-          from_f(y[e].x[k], x);
+        const int64_t pos = row - __ldg(a.starts + s);
+        p = -1;
+        if (pos < __ldg(a.lens + s)) {
+          p = paged::place_of(a, s, pos);
+          p = p < 0 ? -3 : paged::row_of(a, p, 0);
         }
       }
-      const bool is_v = w.h >= a.kv_heads;
-      const HeadTensor& out = is_v ? a.v_rows : a.k_rows;
-      *reinterpret_cast<Pack<T, 8>*>(static_cast<T*>(out.data) + (row0 + w.t) * out.row + (is_v ? w.h - a.kv_heads : w.h) * out.head + 8 * w.r) = y[e];
+      places[i] = p;
     }
+    __syncthreads();
+#pragma unroll 1
+    for (int n = 0; n < known; ++n, group += gridDim.x) {
+      const int64_t row = group * tokens + sub, left = a.rows - row;
+      const int mine = on && left > 0 ? (int)min((int64_t)c.ahead, (left + c.par - 1) / c.par) : 0;
+      const int64_t* const place = places + n * tokens + sub;
+      Pack<uint32_t, 4> x[kReadAhead];                      // 16 bits: the entries; 4: a word of codes and its scale
+#pragma unroll
+      for (int e = 0; e < kReadAhead; ++e) {
+        if (e >= mine) break;
+        const int64_t p = place[e * c.par];
+        if (p < 0) continue;
+        if (BITS == 16) {
+          x[e] = *reinterpret_cast<const Pack<uint32_t, 4>*>(data + p * row_bytes);
+        } else {
+          x[e].x[0] = __ldg(reinterpret_cast<const uint32_t*>(data + p * row_bytes));
+          x[e].x[1] = __ldg(reinterpret_cast<const uint16_t*>(scales + p * (2 * g)));
+        }
+      }
+      T* o = to + row * out_row;
+#pragma unroll
+      for (int e = 0; e < kReadAhead; ++e, o += out_step) {
+        if (e >= mine) break;
+        const int64_t p = place[e * c.par];
+        if (p < 0) {
+          if (p == -2 && !a.fill) continue;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) x[e].x[i] = p == -3 ? 0x7fff7fffu : 0u;   // NaN in both types
+        } else if (BITS == 4) {
+          const uint32_t word = x[e].x[0];
+          const float scale = __half2float(__ushort_as_half((uint16_t)x[e].x[1]));
+          float y[8];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {                     // 2^23 + code, as bits, less 2^23 + 8
+            y[i] = (__uint_as_float((word >> (4 * i) & 15) | 0x4b000000u) - 8388616.f) * scale;
+            // 7 scales may be past float16's end where the row's largest entry was not: the scale was rounded
+            if (std::is_same<T, __half>::value) y[i] = y[i] > 65504.f ? 65504.f : y[i] < -65504.f ? -65504.f : y[i];
+          }
+#pragma unroll
+          for (int i = 0; i < 4; ++i) x[e].x[i] = pack<T>(y[2 * i], y[2 * i + 1]);
+        }
+        *reinterpret_cast<Pack<uint32_t, 4>*>(o) = x[e];
+      }
+    }
+    __syncthreads();
   }
 }
 
-// Tokens of a block: enough for its threads to have several pieces in flight,
-// as long as every SM has blocks.
-int tokens_of(int64_t rows, int num_sms) { return (int)std::max<int64_t>(1, std::min<int64_t>(kTokens, rows / (4 * num_sms))); }
-
-template <class T, int QVEC>
+template <class T, int QVEC, int BITS>
 cudaError_t append(const CacheArgs& a, bool kv_wide, cudaStream_t st) {
-  const int tokens = tokens_of(a.rows, a.num_sms);
-  const unsigned blocks = (unsigned)((a.rows + tokens - 1) / tokens);
-  const size_t smem = (size_t)tokens * 2 * a.turn.half * sizeof(float);
-  if (a.turn.interleaved) k_append<T, QVEC, true><<<blocks, kThreads, smem, st>>>(a, tokens, kv_wide);
-  else k_append<T, QVEC, false><<<blocks, kThreads, smem, st>>>(a, tokens, kv_wide);
+  const int kv = 2 * a.kv_heads * (a.dim / 8), q = a.heads * (a.dim / 2 / QVEC);
+  Columns c = columns_of(a.rows, std::min(kAppendThreads, std::max(kv, q)), kAppendAhead, a.turn.half, a.num_sms, kAppendThreads, kAppendResident);
+  const int kv_blocks = (kv + c.each - 1) / c.each;
+  c.blocks_y = kv_blocks + (q + c.each - 1) / c.each;
+  c.blocks_x = std::max(1, std::min(c.blocks_x, a.num_sms * std::max(1, kAppendResident / c.threads) / c.blocks_y));
+  const dim3 grid((unsigned)c.blocks_x, (unsigned)c.blocks_y);
+  const size_t smem = (size_t)4 * c.tokens() * a.turn.half * sizeof(float);
+  if (a.turn.interleaved) k_append<T, QVEC, BITS, true><<<grid, c.threads, smem, st>>>(a, c, kv_blocks, kv_wide);
+  else k_append<T, QVEC, BITS, false><<<grid, c.threads, smem, st>>>(a, c, kv_blocks, kv_wide);
   const cudaError_t e = cudaGetLastError();
   if (e == cudaSuccess) count_launch();
   return e;
@@ -267,9 +426,11 @@ cudaError_t append_type(const CacheArgs& a, cudaStream_t st) {
     wide = wide && reinterpret_cast<uintptr_t>(t->data) % 16 == 0 && t->row % 8 == 0 && t->head % 8 == 0;
   const HeadTensor q[2] = {a.q, a.q_out};
   const int vec = a.heads ? widest(q, 2, 2, a.turn.half, a.dim) : 8;
-  if (vec == 8) return append<T, 8>(a, wide, st);
-  if (vec == 4) return append<T, 4>(a, wide, st);
-  return append<T, 1>(a, wide, st);
+  auto with = [&](auto bits) {
+    constexpr int kBits = decltype(bits)::value;
+    return vec == 8 ? append<T, 8, kBits>(a, wide, st) : vec == 4 ? append<T, 4, kBits>(a, wide, st) : append<T, 1, kBits>(a, wide, st);
+  };
+  return a.bits == 16 ? with(std::integral_constant<int, 16>()) : with(std::integral_constant<int, 4>());
 }
 
 }  // namespace
@@ -281,10 +442,11 @@ cudaError_t launch_cache_append(const CacheArgs& a, cudaStream_t st) {
 
 cudaError_t launch_cache_read(const CacheArgs& a, cudaStream_t st) {
   if (!a.rows) return cudaSuccess;
-  const int tokens = tokens_of(a.rows, a.num_sms);
-  const unsigned blocks = (unsigned)((a.rows + tokens - 1) / tokens);
-  if (a.bf16) k_read<__nv_bfloat16><<<blocks, kThreads, 0, st>>>(a, tokens);
-  else k_read<__half><<<blocks, kThreads, 0, st>>>(a, tokens);
+  const Columns c = columns_of(a.rows, 2 * a.kv_heads * (a.dim / 8), kReadAhead, 0, a.num_sms, kMostThreads, kReadResident);
+  const dim3 grid((unsigned)c.blocks_x, (unsigned)c.blocks_y);
+  if (a.bits == 16) k_read<__nv_bfloat16, 16><<<grid, c.threads, 0, st>>>(a, c);   // (whichever type: the bits are copied)
+  else if (a.bf16) k_read<__nv_bfloat16, 4><<<grid, c.threads, 0, st>>>(a, c);
+  else k_read<__half, 4><<<grid, c.threads, 0, st>>>(a, c);
   const cudaError_t e = cudaGetLastError();
   if (e == cudaSuccess) count_launch();
   return e;

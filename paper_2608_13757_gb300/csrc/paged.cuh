@@ -8,23 +8,17 @@
 namespace syncgb {
 namespace paged {
 
-// The sequence that has `row`, by a warp: the last s with starts[s] <= row, if
-// row < starts[s + 1] too; -1: none.  32 starts are looked at in a step.
-__device__ __forceinline__ int sequence_of(const CacheArgs& a, int64_t row) {
-  if (!a.starts) return row < a.n_seqs ? (int)row : -1;
-  const int lane = threadIdx.x % 32;
-  int lo = 0, hi = a.n_seqs;
-  if (hi == 0) return -1;
-  do {
-    const int step = (hi - lo + 31) / 32, at = lo + lane * step;
-    const uint32_t before = __ballot_sync(~0u, at < hi && __ldg(a.starts + min(at, hi - 1)) <= row);
-    // (only the run of lanes from the first on counts, should starts not rise)
-    const int n = __ffs(~before) ? __ffs(~before) - 1 : 32;
-    if (n == 0) return -1;
-    lo += (n - 1) * step;
-    hi = min(hi, lo + step);
-  } while (hi - lo > 1);
-  return row < __ldg(a.starts + lo + 1) ? lo : -1;
+// The sequence that has `row`: the last s with starts[s] <= row, if row <
+// starts[s + 1] too; -1: none.
+__device__ __forceinline__ int sequence_of(const CacheArgs& a, int row) {
+  if (!a.starts) return row < a.n_seqs ? row : -1;
+  int lo = 0, hi = a.n_seqs;                                // starts[lo] <= row < starts[hi], as far as they rise
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) / 2;
+    if (mid < a.n_seqs && __ldg(a.starts + mid) <= row) lo = mid;
+    else hi = mid - 1;
+  }
+  return a.n_seqs > 0 && __ldg(a.starts + lo) <= row && row < __ldg(a.starts + lo + 1) ? lo : -1;
 }
 
 // The place of a token in the cache, counted in tokens of one head: page number
