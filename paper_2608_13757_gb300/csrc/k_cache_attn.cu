@@ -634,6 +634,47 @@ __device__ __forceinline__ void find_runs(const CacheArgs& a, Runs& runs) {
   __syncthreads();
 }
 
+// N entries of a piece's row, a multiple of N from its start, in wide accesses.
+template <int N>
+struct Entries {
+  static constexpr int kVec = N % 4 == 0 ? 4 : 2;
+  static __device__ __forceinline__ void load(const float* p, float* x) {
+#pragma unroll
+    for (int e = 0; e < N; e += kVec) {
+      if constexpr (kVec == 4) {
+        const float4 v = *reinterpret_cast<const float4*>(p + e);
+        x[e] = v.x;
+        x[e + 1] = v.y;
+        x[e + 2] = v.z;
+        x[e + 3] = v.w;
+      } else {
+        const float2 v = *reinterpret_cast<const float2*>(p + e);
+        x[e] = v.x;
+        x[e + 1] = v.y;
+      }
+    }
+  }
+  static __device__ __forceinline__ void store(float* p, const float* x) {
+#pragma unroll
+    for (int e = 0; e < N; e += kVec) {
+      if constexpr (kVec == 4) *reinterpret_cast<float4*>(p + e) = make_float4(x[e], x[e + 1], x[e + 2], x[e + 3]);
+      else *reinterpret_cast<float2*>(p + e) = make_float2(x[e], x[e + 1]);
+    }
+  }
+};
+
+// DP / 16 entries of an output row from d0 on, from their sums with weights of
+// maximum `top` and sum `sum`.
+template <int DP, bool BF16>
+__device__ __forceinline__ void finish_row(const CacheArgs& a, int64_t row, int head, int d0, const float* acc, float top, float sum) {
+  uint8_t* const to = static_cast<uint8_t*>(a.q_out.data) + 2 * (row * a.q_out.row + head * a.q_out.head);
+  const float by = sum == 0.f ? 0.f : 1.f / sum;
+#pragma unroll
+  for (int e = 0; e < DP / 16; e += 2)
+    if (d0 + e < a.dim) *reinterpret_cast<uint32_t*>(to + 2 * (d0 + e)) = pack2<BF16>(acc[e] * by, acc[e + 1] * by);
+  if (a.lse && d0 == 0) a.lse[head * a.rows + row] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * 0.6931471805599453f;
+}
+
 // What a warp leaves of passes that it did not do alone: the end of one that
 // began before (its rows are in the workspace), and one that it did not end (in
 // the warp's shared memory).
@@ -924,6 +965,7 @@ __global__ void __launch_bounds__(kThreads, per_sm(K::kBits, NT)) k_cache_attn(c
   // Passes of which several warps have pieces, in the order of the warps: a chain
   // from a warp's open pass over those that it goes on in to one that ends it.
   // What is still open at either end of the block goes to the second kernel.
+  constexpr int kEach = DP / 16;
   Header header{0, 0, 0, 0, 0, 0};
   auto join = [&](int a0, int b, bool ended, bool led) {
     const Left& of = lefts[ended ? b : a0];
@@ -932,38 +974,41 @@ __global__ void __launch_bounds__(kThreads, per_sm(K::kBits, NT)) k_cache_attn(c
     const int slot = 2 * blockIdx.x + (ended || led ? 0 : 1);
     if (led) header.before = ended ? 2 : 1;
     else if (!ended) header = Header{header.before, 1, row0, n, head, first};
-    for (int row = warp; row < ROWS && first + row < n * group; row += kWarps) {
-      const float* p[kWarps + 1];
-      float top = -INFINITY, sum = 0.f, acc[DP / 32];
+    // 16 threads a row, for all rows at once: what they wait for is one read of
+    // the pieces' maxima and one of their entries
 #pragma unroll
-      for (int e = 0; e < DP / 32; ++e) acc[e] = 0.f;
+    for (int nt = 0; nt < NT; ++nt) {
+      const int row = 8 * nt + threadIdx.x / 16, d0 = threadIdx.x % 16 * kEach;
+      if (first + row >= n * group) continue;
+      const float* p[kWarps + 1];
+      float m[kWarps + 1], l[kWarps + 1], top = -INFINITY, sum = 0.f, acc[kEach];
 #pragma unroll
       for (int w = 0; w <= kWarps; ++w) {
         p[w] = w < kWarps ? (w >= a0 && w < b ? reinterpret_cast<const float*>(ring + w * kRing) + row * P::kRow : nullptr)
                           : ended ? parts + P::warp_slot(gridDim.x, blockIdx.x * kWarps + b) + row * P::kRow : nullptr;
-        if (p[w]) top = fmaxf(top, p[w][DP]);
+        m[w] = p[w] ? p[w][DP] : -INFINITY;
+        l[w] = p[w] ? p[w][DP + 1] : 0.f;
+        top = fmaxf(top, m[w]);
       }
+#pragma unroll
+      for (int e = 0; e < kEach; ++e) acc[e] = 0.f;
 #pragma unroll
       for (int w = 0; w <= kWarps; ++w)
         if (p[w]) {
-          const float m = p[w][DP], l = p[w][DP + 1], f = m == -INFINITY ? 0.f : exp2_fast(m - top);
-          sum += m == -INFINITY ? l : l * f;                 // (l is 0 or NaN where nothing was seen)
+          const float f = m[w] == -INFINITY ? 0.f : exp2_fast(m[w] - top);
+          sum += m[w] == -INFINITY ? l[w] : l[w] * f;         // (l is 0 or NaN where nothing was seen)
+          float v[kEach];
+          Entries<kEach>::load(p[w] + d0, v);
 #pragma unroll
-          for (int e = 0; e < DP / 32; ++e) acc[e] = fmaf(f, p[w][lane + 32 * e], acc[e]);
+          for (int e = 0; e < kEach; ++e) acc[e] = fmaf(f, v[e], acc[e]);
         }
       if (whole) {
         const int token = (first + row) / group, h = head * group + (first + row) % group;
-        uint8_t* to = out_row(row0 + token, h);
-        const float by = sum == 0.f ? 0.f : 1.f / sum;
-#pragma unroll
-        for (int e = 0; e < DP / 32; ++e)
-          if (lane + 32 * e < a.dim) reinterpret_cast<uint16_t*>(to)[lane + 32 * e] = (uint16_t)pack2<BF16>(acc[e] * by, 0.f);
-        if (a.lse && lane == 0) a.lse[h * a.rows + row0 + token] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * 0.6931471805599453f;
+        finish_row<DP, BF16>(a, row0 + token, h, d0, acc, top, sum);
       } else {
         float* to = parts + P::slot(slot) + row * P::kRow;
-#pragma unroll
-        for (int e = 0; e < DP / 32; ++e) to[lane + 32 * e] = acc[e];
-        if (lane == 0) {
+        Entries<kEach>::store(to + d0, acc);
+        if (d0 == 0) {
           to[DP] = top;
           to[DP + 1] = sum;
         }
@@ -991,20 +1036,22 @@ __global__ void __launch_bounds__(kThreads, per_sm(K::kBits, NT)) k_cache_attn(c
   if (threadIdx.x == 0) reinterpret_cast<Header*>(a.work)[blockIdx.x] = header;
 }
 
-// Passes that were cut, from their pieces in order: a block for each block of
-// the first kernel that began one, and each of its rows.
+// Passes that several blocks have pieces of, from these in order: a block for
+// each block of the first kernel, if it began such a pass, and each of its rows;
+// 16 threads on pieces in turn.  (Small blocks, which find room beside the first
+// kernel's and wait there: of 512 threads they cost 5 us more.)
+constexpr int kMergers = 8;
 template <int DP, int ROWS, bool BF16>
-__global__ void __launch_bounds__(kThreads) k_cache_merge(const __grid_constant__ CacheArgs a, int blocks) {
+__global__ void __launch_bounds__(16 * kMergers) k_cache_merge(const __grid_constant__ CacheArgs a, int blocks) {
   using P = Parts<DP, ROWS>;
-  constexpr int kEach = DP / 32;
-  __shared__ float sums[kWarps][DP + 2];
+  constexpr int kEach = DP / 16;
+  __shared__ __align__(16) float sums[kMergers][DP + 4];
   after_previous();
   const Header* const headers = reinterpret_cast<const Header*>(a.work);
   const Header x = headers[blockIdx.x];
   const int group = a.heads / a.kv_heads, row = x.first + (int)blockIdx.y;
   if (!x.open || row >= x.n * group) return;
-  const float* const parts = reinterpret_cast<const float*>(a.work + P::header(blocks)) + blockIdx.y * P::kRow;
-  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  const int lane = threadIdx.x % 32;
   int last = blockIdx.x + 1;                                // the block that ends the pass
   for (; last < blocks; last += 32) {
     const uint32_t ends = __ballot_sync(~0u, last + lane < blocks && headers[last + lane].before == 2);
@@ -1014,35 +1061,42 @@ __global__ void __launch_bounds__(kThreads) k_cache_merge(const __grid_constant_
     }
   }
   last = min(last, blocks - 1);
+  const int mine = threadIdx.x / 16, l16 = threadIdx.x % 16, d0 = l16 * kEach;
+  const float* const parts = reinterpret_cast<const float*>(a.work + P::header(blocks)) + blockIdx.y * P::kRow;
   auto part = [&](int b) { return parts + P::slot(2 * b + (b == (int)blockIdx.x)); };
   float top = -INFINITY;
-  for (int b = blockIdx.x + lane; b <= last; b += 32) top = fmaxf(top, part(b)[DP]);
+  for (int b = blockIdx.x + l16; b <= last; b += 16) top = fmaxf(top, part(b)[DP]);
 #pragma unroll
-  for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, o));
+  for (int o = 8; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, o));
   float acc[kEach], sum = 0.f;
 #pragma unroll
   for (int e = 0; e < kEach; ++e) acc[e] = 0.f;
 #pragma unroll 4
-  for (int b = blockIdx.x + warp; b <= last; b += kWarps) {
+  for (int b = blockIdx.x + mine; b <= last; b += kMergers) {
     const float* p = part(b);
     const float m = p[DP], f = m == -INFINITY ? 0.f : exp2_fast(m - top), l = p[DP + 1];
     sum += m == -INFINITY ? l : l * f;
+    float v[kEach];
+    Entries<kEach>::load(p + d0, v);
 #pragma unroll
-    for (int e = 0; e < kEach; ++e) acc[e] = fmaf(f, p[lane * kEach + e], acc[e]);
+    for (int e = 0; e < kEach; ++e) acc[e] = fmaf(f, v[e], acc[e]);
   }
-#pragma unroll
-  for (int e = 0; e < kEach; ++e) sums[warp][lane * kEach + e] = acc[e];
-  if (lane == 0) sums[warp][DP] = sum;
+  Entries<kEach>::store(&sums[mine][d0], acc);
+  if (l16 == 0) sums[mine][DP] = sum;
   __syncthreads();
-  sum = (sums[0][DP] + sums[1][DP]) + (sums[2][DP] + sums[3][DP]);
-  const float by = sum == 0.f ? 0.f : 1.f / sum;
-  const int64_t at_row = x.row0 + row / group;
-  const int head = x.head * group + row % group, d = 2 * threadIdx.x;
-  if (d < a.dim) {
-    const float u = (sums[0][d] + sums[1][d]) + (sums[2][d] + sums[3][d]), v = (sums[0][d + 1] + sums[1][d + 1]) + (sums[2][d + 1] + sums[3][d + 1]);
-    *reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(a.q_out.data) + 2 * (at_row * a.q_out.row + head * a.q_out.head + d)) = pack2<BF16>(u * by, v * by);
+  if (mine) return;
+  sum = 0.f;
+#pragma unroll
+  for (int e = 0; e < kEach; ++e) acc[e] = 0.f;
+#pragma unroll
+  for (int i = 0; i < kMergers; ++i) {
+    float v[kEach];
+    Entries<kEach>::load(&sums[i][d0], v);
+    sum += sums[i][DP];
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) acc[e] += v[e];
   }
-  if (a.lse && threadIdx.x == 0) a.lse[head * a.rows + at_row] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * 0.6931471805599453f;
+  finish_row<DP, BF16>(a, x.row0 + row / group, x.head * group + row % group, d0, acc, top, sum);
 }
 
 template <class K, int NT, bool BF16>
@@ -1054,7 +1108,7 @@ cudaError_t launch(const CacheArgs& a, cudaStream_t st) {
   k_cache_attn<K, NT, BF16><<<a.blocks, kThreads, kBytes, st>>>(a);
   if ((e = cudaGetLastError()) != cudaSuccess) return e;
   count_launch();
-  e = launch_early(k_cache_merge<K::DP, 8 * NT, BF16>, dim3((unsigned)a.blocks, 8 * NT), kThreads, 0, st, a, a.blocks);
+  e = launch_early(k_cache_merge<K::DP, 8 * NT, BF16>, dim3((unsigned)a.blocks, 8 * NT), 16 * kMergers, 0, st, a, a.blocks);
   if (e == cudaSuccess) count_launch();
   return e;
 }
