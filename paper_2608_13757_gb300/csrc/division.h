@@ -19,7 +19,7 @@ namespace division {
 #define SYNCGB_BOTH inline
 #endif
 
-constexpr int kUnitCost = 1, kLeast = 2;   // tiles that a pass costs besides; that a warp takes at least
+constexpr int kUnitCost = 3, kLeast = 2;   // tiles that a pass costs besides; that a warp takes at least
 
 SYNCGB_BOTH int64_t less(int64_t a, int64_t b) { return a < b ? a : b; }
 SYNCGB_BOTH int64_t more(int64_t a, int64_t b) { return a > b ? a : b; }
@@ -70,8 +70,9 @@ struct Lister {
   SYNCGB_BOTH void start(const Shape& x, int seq, int64_t into_seq, int64_t run) {
     now = x;
     s = seq;
-    unit = (int)(into_seq / (x.tiles + kUnitCost));
-    into = into_seq % (x.tiles + kUnitCost);
+    const int cost = x.tiles + kUnitCost;
+    unit = into_seq < (int64_t)1 << 31 ? (int)((uint32_t)into_seq / (uint32_t)cost) : (int)(into_seq / cost);
+    into = into_seq - (int64_t)unit * cost;
     left = run;
   }
   template <class F>

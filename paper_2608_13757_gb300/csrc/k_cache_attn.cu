@@ -580,6 +580,7 @@ __device__ __forceinline__ Shape shape_of(const CacheArgs& a, int s, int rows, i
 struct Runs {
   int64_t sum[kWarps], bound[kWarps + 1], into[kWarps];
   int s[kWarps];
+  Shape shape[kWarps];                     // of that sequence
 };
 
 __device__ __forceinline__ int64_t summed_up(int64_t x) {     // over the lanes up to this one
@@ -596,7 +597,11 @@ __device__ __forceinline__ void find_runs(const CacheArgs& a, Runs& runs) {
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
   const bool few = a.n_seqs <= kThreads;
   int64_t cost = 0;
-  for (int s = threadIdx.x; s < a.n_seqs; s += kThreads) cost += shape_of(a, s, ROWS, TILE).cost;
+  Shape x{};
+  for (int s = threadIdx.x; s < a.n_seqs; s += kThreads) {
+    x = shape_of(a, s, ROWS, TILE);
+    cost += x.cost;
+  }
   int64_t sum = summed_up(cost);
   if (lane == 31) runs.sum[warp] = sum;
   __syncthreads();
@@ -610,7 +615,8 @@ __device__ __forceinline__ void find_runs(const CacheArgs& a, Runs& runs) {
   for (int s0 = 0; s0 < a.n_seqs; s0 += kThreads) {
     const int s = s0 + threadIdx.x;
     if (!few) {
-      cost = s < a.n_seqs ? shape_of(a, s, ROWS, TILE).cost : 0;
+      if (s < a.n_seqs) x = shape_of(a, s, ROWS, TILE);
+      cost = s < a.n_seqs ? x.cost : 0;
       sum = summed_up(cost);
       __syncthreads();
       if (lane == 31) runs.sum[warp] = sum;
@@ -627,6 +633,7 @@ __device__ __forceinline__ void find_runs(const CacheArgs& a, Runs& runs) {
       if (at < runs.bound[w + 1] && mine <= at && at < mine + cost) {
         runs.s[w] = s;
         runs.into[w] = at - mine;
+        runs.shape[w] = x;
       }
     }
     if (before > runs.bound[kWarps - 1]) break;
@@ -689,7 +696,8 @@ __global__ void __launch_bounds__(kThreads, per_sm(K::kBits, NT)) k_cache_attn(c
   constexpr int DP = K::DP, MT = K::MT, ROWS = 8 * NT, S = K::kStages, kTile = MT * kKeys, kRing = S * K::kStage;
   using P = Parts<DP, ROWS>;
   static_assert(P::kFloats * 4 <= kRing, "a warp's shared memory holds a pass");
-  extern __shared__ __align__(16) uint8_t ring[];
+  // (aligned: a copy of 32 bytes by two lanes to halves of two such pieces reads them twice from L2)
+  extern __shared__ __align__(128) uint8_t ring[];
   __shared__ Piece lists[kWarps][kPieces];
   __shared__ Lister listers[kWarps];
   __shared__ Left lefts[kWarps];
@@ -718,7 +726,7 @@ __global__ void __launch_bounds__(kThreads, per_sm(K::kBits, NT)) k_cache_attn(c
   if (lane == 0) {
     left.before = left.open = 0;
     lister.left = runs.bound[warp + 1] - runs.bound[warp];
-    if (lister.left) lister.start(shape_of(a, runs.s[warp], ROWS, kTile), runs.s[warp], runs.into[warp], lister.left);
+    if (lister.left) lister.start(runs.shape[warp], runs.s[warp], runs.into[warp], lister.left);
   }
   K k;
   k.begin(a, mine);
