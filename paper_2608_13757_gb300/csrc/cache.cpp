@@ -143,9 +143,9 @@ int checked_heads(const sync_cache* c, int32_t heads) {
 
 // For tests on the host: the pieces that `warps` warps take of a step with
 // `group` query heads per key head, passes of `rows` rows and tiles of `tile` keys,
-// 11 values per piece: warp, sequence, key head, first row, tokens, first token's
-// row, length, bad, tiles [from, to) of tiles.  Returns the number of pieces
-// (written up to `capacity`).
+// 12 values per piece: warp, sequence, key head, first row, tokens, first token's
+// row, length, bad, tiles [from, to) of tiles, the warp of the pass's last tile.
+// Returns the number of pieces (written up to `capacity`).
 extern "C" int64_t syncgb_cache_attn_work(int n_seqs, const int32_t* lens, const int32_t* row_starts, int64_t all_rows, int room,
                                           int kv_heads, int group, int rows, int tile, int warps, int64_t* out, int64_t capacity) {
   auto shape_of = [&](int s) {
@@ -155,17 +155,18 @@ extern "C" int64_t syncgb_cache_attn_work(int n_seqs, const int32_t* lens, const
   for (int s = 0; s < n_seqs; ++s) total += shape_of(s).cost;
   const int takers = division::takers(total, warps);
   for (int w = 0; w < warps; ++w) {
-    int64_t from = division::bound(total, takers, w);
-    const int64_t run = division::bound(total, takers, w + 1) - from;
+    const int64_t begin = division::bound(total, takers, w), run = division::bound(total, takers, w + 1) - begin;
     if (!run) continue;
     int s = 0;
+    int64_t from = begin;
     for (; from >= shape_of(s).cost; ++s) from -= shape_of(s).cost;
     division::Lister l;
-    l.start(shape_of(s), s, from, run);
+    l.start(shape_of(s), s, begin, from, run);
     division::Piece x;
     for (; l.next(shape_of, n_seqs, kv_heads, rows, x); ++n) {
-      const int64_t row[11] = {w, x.s, x.head, x.first, x.n, x.row0, x.len, x.bad, x.from, x.to, x.tiles};
-      if (n < capacity) std::copy(row, row + 11, out + 11 * n);
+      const int64_t row[12] = {w, x.s, x.head, x.first, x.n, x.row0, x.len, x.bad, x.from, x.to, x.tiles,
+                               x.tiles ? division::holder(total, takers, x.last_tile()) : w};
+      if (n < capacity) std::copy(row, row + 12, out + 12 * n);
     }
   }
   return n;

@@ -53,27 +53,38 @@ SYNCGB_BOTH int64_t bound(int64_t total, int takers, int warp) {
   return total / takers * warp + total % takers * warp / takers;   // (no product as large as total * warp)
 }
 
+// The warp whose run has the tile at x < total.
+SYNCGB_BOTH int holder(int64_t total, int takers, int64_t x) {
+  int w = (int)less((int64_t)((double)x / (double)total * takers), takers - 1);
+  while (bound(total, takers, w) > x) --w;
+  while (bound(total, takers, w + 1) <= x) ++w;
+  return w;
+}
+
 // A warp's part of a pass.
 struct Piece {
   int s, head;                             // sequence, key head
   int first, n, row0;                      // first row of the pass among the n * group rows; tokens; row of the first token
   int len, bad;                            // tokens in the cache; more than its pages hold
   int from, to, tiles;                     // tiles of the warp, and of the pass
+  int64_t at;                              // where the pass is in the list
+  SYNCGB_BOTH int64_t last_tile() const { return at + kUnitCost + tiles - 1; }
 };
 
 // The pieces of a warp, one after the other.
 struct Lister {
   Shape now;
   int s, unit;                             // unit: key head * passes + pass
-  int64_t into, left;                      // tiles into the unit, tiles left of the run
-  // into: of the sequence's work
-  SYNCGB_BOTH void start(const Shape& x, int seq, int64_t into_seq, int64_t run) {
+  int64_t into, left, at;                  // tiles into the unit, tiles left of the run; where the unit begins
+  // The run of `run` tiles from `begin` on, which is into_seq into the sequence's work.
+  SYNCGB_BOTH void start(const Shape& x, int seq, int64_t begin, int64_t into_seq, int64_t run) {
     now = x;
     s = seq;
     const int cost = x.tiles + kUnitCost;
     unit = into_seq < (int64_t)1 << 31 ? (int)((uint32_t)into_seq / (uint32_t)cost) : (int)(into_seq / cost);
     into = into_seq - (int64_t)unit * cost;
     left = run;
+    at = begin - into;
   }
   template <class F>
   SYNCGB_BOTH bool next(F&& shape_of, int n_seqs, int kv_heads, int rows, Piece& x) {
@@ -88,9 +99,10 @@ struct Lister {
       const int64_t to = less(now.tiles + kUnitCost, into + left);
       const int a = (int)more(0, into - kUnitCost), b = (int)more(0, to - kUnitCost);
       const bool some = b > a || (now.tiles == 0 && into == 0);
-      if (some) x = Piece{s, unit / now.passes, unit % now.passes * rows, now.n, now.row0, now.len, now.bad, a, b, now.tiles};
+      if (some) x = Piece{s, unit / now.passes, unit % now.passes * rows, now.n, now.row0, now.len, now.bad, a, b, now.tiles, at};
       left -= to - into;
       into = 0;
+      at += now.tiles + kUnitCost;
       ++unit;
       if (some) return true;
     }

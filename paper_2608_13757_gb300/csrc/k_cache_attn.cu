@@ -53,11 +53,11 @@ constexpr int kPieces = 8;                 // of a warp's list that are laid out
 // Blocks per SM
 constexpr int per_sm(int bits, int nt) { return bits == 4 && nt == 1 ? 3 : 2; }
 
-// What a block leaves for the kernel that joins the pieces.
+// What a block leaves for the kernel that joins the pieces: the pass that it has
+// begun and does not end, and the block that does.
 struct alignas(32) Header {
-  int before;                              // it has a piece of a pass that began before; 2: and ends it
-  int open;                                // it has begun a pass that it does not end:
-  int row0, n, head, first;                // as in Piece
+  int open;                                // 0: none
+  int last, row0, n, head, first;          // as in Piece
 };
 
 template <int DP, int ROWS>
@@ -578,8 +578,8 @@ __device__ __forceinline__ Shape shape_of(const CacheArgs& a, int s, int rows, i
 // The runs of a block's warps: their bounds in the list, and the sequences where
 // they begin with how far into them.
 struct Runs {
-  int64_t sum[kWarps], bound[kWarps + 1], into[kWarps];
-  int s[kWarps];
+  int64_t sum[kWarps], bound[kWarps + 1], into[kWarps], total;
+  int s[kWarps], takers;
   Shape shape[kWarps];                     // of that sequence
 };
 
@@ -607,7 +607,12 @@ __device__ __forceinline__ void find_runs(const CacheArgs& a, Runs& runs) {
   __syncthreads();
   if (threadIdx.x <= kWarps) {
     const int64_t total = runs.sum[0] + runs.sum[1] + runs.sum[2] + runs.sum[3];
-    runs.bound[threadIdx.x] = division::bound(total, division::takers(total, gridDim.x * kWarps), blockIdx.x * kWarps + threadIdx.x);
+    const int takers = division::takers(total, gridDim.x * kWarps);
+    runs.bound[threadIdx.x] = division::bound(total, takers, blockIdx.x * kWarps + threadIdx.x);
+    if (threadIdx.x == 0) {
+      runs.total = total;
+      runs.takers = takers;
+    }
   }
   __syncthreads();
   if (runs.bound[0] == runs.bound[kWarps]) return;
@@ -689,6 +694,7 @@ struct Left {
   int before;
   int open;                                // 1: that it began; 2: that began before
   int row0[2], n[2], head[2], first[2];    // of either, as in Piece
+  int last;                                // of the open one: the block that ends it
 };
 
 template <class K, int NT, bool BF16>
@@ -726,7 +732,7 @@ __global__ void __launch_bounds__(kThreads, per_sm(K::kBits, NT)) k_cache_attn(c
   if (lane == 0) {
     left.before = left.open = 0;
     lister.left = runs.bound[warp + 1] - runs.bound[warp];
-    if (lister.left) lister.start(runs.shape[warp], runs.s[warp], runs.into[warp], lister.left);
+    if (lister.left) lister.start(runs.shape[warp], runs.s[warp], runs.bound[warp], runs.into[warp], lister.left);
   }
   K k;
   k.begin(a, mine);
@@ -963,6 +969,7 @@ __global__ void __launch_bounds__(kThreads, per_sm(K::kBits, NT)) k_cache_attn(c
         left.n[open] = x.n;
         left.head[open] = x.head;
         left.first[open] = x.first;
+        if (open) left.last = division::holder(runs.total, runs.takers, x.last_tile()) / kWarps;
       }
     }
     __syncwarp();
@@ -980,8 +987,7 @@ __global__ void __launch_bounds__(kThreads, per_sm(K::kBits, NT)) k_cache_attn(c
     const int which = ended ? 0 : 1, row0 = of.row0[which], n = of.n[which], head = of.head[which], first = of.first[which];
     const bool whole = ended && !led;
     const int slot = 2 * blockIdx.x + (ended || led ? 0 : 1);
-    if (led) header.before = ended ? 2 : 1;
-    else if (!ended) header = Header{header.before, 1, row0, n, head, first};
+    if (!led && !ended) header = Header{1, of.last, row0, n, head, first};
     // 16 threads a row, for all rows at once: what they wait for is one read of
     // the pieces' maxima and one of their entries
 #pragma unroll
@@ -1048,7 +1054,7 @@ __global__ void __launch_bounds__(kThreads, per_sm(K::kBits, NT)) k_cache_attn(c
 // each block of the first kernel, if it began such a pass, and each of its rows;
 // 16 threads on pieces in turn.  (Small blocks, which find room beside the first
 // kernel's and wait there: of 512 threads they cost 5 us more.)
-constexpr int kMergers = 8;
+constexpr int kMergers = 8, kAtOnce = 3;
 template <int DP, int ROWS, bool BF16>
 __global__ void __launch_bounds__(16 * kMergers) k_cache_merge(const __grid_constant__ CacheArgs a, int blocks) {
   using P = Parts<DP, ROWS>;
@@ -1059,50 +1065,64 @@ __global__ void __launch_bounds__(16 * kMergers) k_cache_merge(const __grid_cons
   const Header x = headers[blockIdx.x];
   const int group = a.heads / a.kv_heads, row = x.first + (int)blockIdx.y;
   if (!x.open || row >= x.n * group) return;
-  const int lane = threadIdx.x % 32;
-  int last = blockIdx.x + 1;                                // the block that ends the pass
-  for (; last < blocks; last += 32) {
-    const uint32_t ends = __ballot_sync(~0u, last + lane < blocks && headers[last + lane].before == 2);
-    if (ends) {
-      last += __ffs(ends) - 1;
-      break;
-    }
-  }
-  last = min(last, blocks - 1);
   const int mine = threadIdx.x / 16, l16 = threadIdx.x % 16, d0 = l16 * kEach;
   const float* const parts = reinterpret_cast<const float*>(a.work + P::header(blocks)) + blockIdx.y * P::kRow;
   auto part = [&](int b) { return parts + P::slot(2 * b + (b == (int)blockIdx.x)); };
-  float top = -INFINITY;
-  for (int b = blockIdx.x + l16; b <= last; b += 16) top = fmaxf(top, part(b)[DP]);
-#pragma unroll
-  for (int o = 8; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, o));
-  float acc[kEach], sum = 0.f;
+  // this thread's pieces with the maximum so far: all reads of a few pieces at once
+  float acc[kEach], sum = 0.f, top = -INFINITY;
 #pragma unroll
   for (int e = 0; e < kEach; ++e) acc[e] = 0.f;
-#pragma unroll 4
-  for (int b = blockIdx.x + mine; b <= last; b += kMergers) {
-    const float* p = part(b);
-    const float m = p[DP], f = m == -INFINITY ? 0.f : exp2_fast(m - top), l = p[DP + 1];
-    sum += m == -INFINITY ? l : l * f;
-    float v[kEach];
-    Entries<kEach>::load(p + d0, v);
+#pragma unroll 1
+  for (int b0 = blockIdx.x + mine; b0 <= x.last; b0 += kMergers * kAtOnce) {
+    float m[kAtOnce], l[kAtOnce], v[kAtOnce][kEach], now = top;
 #pragma unroll
-    for (int e = 0; e < kEach; ++e) acc[e] = fmaf(f, v[e], acc[e]);
+    for (int i = 0; i < kAtOnce; ++i) {
+      const int b = b0 + i * kMergers;
+      m[i] = -INFINITY;
+      l[i] = 0.f;
+      if (b > x.last) continue;
+      const float* p = part(b);
+      m[i] = p[DP];
+      l[i] = p[DP + 1];
+      Entries<kEach>::load(p + d0, v[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < kAtOnce; ++i) now = fmaxf(now, m[i]);
+    const float f = top == -INFINITY ? 0.f : exp2_fast(top - now);
+    top = now;
+    sum *= f;
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) acc[e] *= f;
+#pragma unroll
+    for (int i = 0; i < kAtOnce; ++i) {
+      if (b0 + i * kMergers > x.last) continue;
+      const float g = m[i] == -INFINITY ? 0.f : exp2_fast(m[i] - top);
+      sum += m[i] == -INFINITY ? l[i] : l[i] * g;           // (l is 0 or NaN where nothing was seen)
+#pragma unroll
+      for (int e = 0; e < kEach; ++e) acc[e] = fmaf(g, v[i][e], acc[e]);
+    }
   }
   Entries<kEach>::store(&sums[mine][d0], acc);
-  if (l16 == 0) sums[mine][DP] = sum;
+  if (l16 == 0) {
+    sums[mine][DP] = top;
+    sums[mine][DP + 1] = sum;
+  }
   __syncthreads();
   if (mine) return;
+  top = -INFINITY;
+#pragma unroll
+  for (int i = 0; i < kMergers; ++i) top = fmaxf(top, sums[i][DP]);
   sum = 0.f;
 #pragma unroll
   for (int e = 0; e < kEach; ++e) acc[e] = 0.f;
 #pragma unroll
   for (int i = 0; i < kMergers; ++i) {
+    const float m = sums[i][DP], l = sums[i][DP + 1], f = m == -INFINITY ? 0.f : exp2_fast(m - top);
     float v[kEach];
     Entries<kEach>::load(&sums[i][d0], v);
-    sum += sums[i][DP];
+    sum += m == -INFINITY ? l : l * f;
 #pragma unroll
-    for (int e = 0; e < kEach; ++e) acc[e] += v[e];
+    for (int e = 0; e < kEach; ++e) acc[e] = fmaf(f, v[e], acc[e]);
   }
   finish_row<DP, BF16>(a, x.row0 + row / group, x.head * group + row % group, d0, acc, top, sum);
 }

@@ -120,7 +120,7 @@ def work(sg, lens, starts, rows_all, room, kv, group, rows, tile, warps):
     b = None if starts is None else np.array(starts, dtype=np.int32)
     args = (len(lens), a.ctypes.data, None if b is None else b.ctypes.data, rows_all, room, kv, group, rows, tile, warps)
     n = f(*args, None, 0)
-    out = np.zeros((n, 11), dtype=np.int64)
+    out = np.zeros((n, 12), dtype=np.int64)
     assert f(*args, out.ctypes.data, n) == n
     return out
 
@@ -154,7 +154,7 @@ def test_pieces_cover_every_tile_once(sg):
                         at = x[9]
                     assert at == tiles
                     b = [int(x[0]) for x in pieces]                # warps that follow one another
-                    assert b == list(range(b[0], b[0] + len(b)))
+                    assert b == list(range(b[0], b[0] + len(b))) and all(x[11] == b[-1] for x in pieces)
         assert want == len(units)
         # a warp has at most one piece that began before (its first) and one that it leaves open (its last)
         for b in set(got[:, 0]):
