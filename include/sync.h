@@ -749,7 +749,9 @@ sync_status sync_cache_read(const sync_cache *cache, const sync_cache_seqs *seqs
                             const sync_rows *v, int32_t zero_rest, void *stream);
 
 /* Bytes of device workspace (16-byte aligned, contents irrelevant) that
- * sync_cache_attn needs on the current device. */
+ * sync_cache_attn needs on the current device, for sequences of any length.  Where
+ * max_pages * page is at most SYNC_CACHE_SHORT it needs none. */
+#define SYNC_CACHE_SHORT 128
 sync_status sync_cache_attn_workspace(const sync_cache *cache, int32_t heads, int32_t max_new, int64_t *bytes);
 
 /* Attention of the step's rows over the cache, after sync_cache_append: row i of

@@ -17,6 +17,9 @@ import paper_2608_13757_gb300 as _sg
 from .attention import _On, Rows, _code, _current_stream, _need, _not_recorded, _rows, _vector
 
 
+SHORT = 128      # tokens of max_pages pages up to which attention takes no workspace
+
+
 class Rotation(ctypes.Structure):
     _fields_ = [("rotated", ctypes.c_int32), ("interleaved", ctypes.c_int32), ("n_axes", ctypes.c_int32),
                 ("pair_axis", ctypes.c_char_p), ("cos", ctypes.c_void_p), ("sin", ctypes.c_void_p),
@@ -49,6 +52,12 @@ def declare(lib: ctypes.CDLL):
     lib.sync_cache_attn.argtypes = [cache, seqs, i32, rows, ctypes.c_float, i32, rows, vp, i32, vp, ctypes.c_int64, vp]
 
 
+def _current_device() -> int:
+    """torch.cuda.current_device() where a GPU is in use already."""
+    import torch
+    return torch._C._cuda_getDevice()
+
+
 def _rotation(cos, sin, positions, axes, interleaved, n, device) -> Rotation:
     """The description of a rotation of n rows."""
     import torch
@@ -69,7 +78,7 @@ def _rotation(cos, sin, positions, axes, interleaved, n, device) -> Rotation:
     if axes is not None:
         _need(len(axes) == half, "axes must name an axis for every pair")
         try:
-            axes = axes if isinstance(axes, bytes) else bytes(list(axes))
+            axes = bytes(axes if isinstance(axes, (bytes, list, tuple)) else list(axes))
         except (TypeError, ValueError):
             _need(False, "axes must be whole numbers from 0 on")
     else:
@@ -86,7 +95,7 @@ def _rope(name, f, q, k, cos, sin, positions, axes, interleaved, out, stream):
     _need(q.dim() == 3 and k.dim() == 3, "q and k must be [rows, heads, dim]")
     _need(q.is_cuda, "q must be on a GPU")
     device, dtype = q.get_device(), q.dtype
-    if torch.cuda.current_device() != device:
+    if _current_device() != device:
         with torch.cuda.device(device):
             return _rope(name, f, q, k, cos, sin, positions, axes, interleaved, out, None)
     n, heads, dim = q.shape
@@ -197,7 +206,7 @@ def sync_cache_append(cache: KVCache, k, v, page_table, lens, row_starts=None, q
         with _On(cache.device, stream):
             return sync_cache_append(cache, k, v, page_table, lens, row_starts, q, cos, sin, positions, axes, interleaved, out)
     device, dtype, kv, dim = cache.index, cache.dtype, cache.kv_heads, cache.head_dim
-    if torch.cuda.current_device() != device:
+    if _current_device() != device:
         with torch.cuda.device(device):
             return sync_cache_append(cache, k, v, page_table, lens, row_starts, q, cos, sin, positions, axes, interleaved, out)
     a, b = _rows(k, "k", dtype, device, kv, dim), _rows(v, "v", dtype, device, kv, dim)
@@ -227,7 +236,7 @@ def sync_cache_read(cache: KVCache, page_table, lens, row_starts, rows: int | No
         with _On(cache.device, stream):
             return sync_cache_read(cache, page_table, lens, row_starts, rows, out)
     device, dtype, kv, dim = cache.index, cache.dtype, cache.kv_heads, cache.head_dim
-    if torch.cuda.current_device() != device:
+    if _current_device() != device:
         with torch.cuda.device(device):
             return sync_cache_read(cache, page_table, lens, row_starts, rows, out)
     _need(row_starts is not None, "row_starts must be given")
@@ -253,7 +262,7 @@ def sync_cache_attn(cache: KVCache, q, page_table, lens, row_starts=None, max_ne
         with _On(cache.device, stream):
             return sync_cache_attn(cache, q, page_table, lens, row_starts, max_new, scale, out, lse)
     device, dtype, dim = cache.index, cache.dtype, cache.head_dim
-    if torch.cuda.current_device() != device:
+    if _current_device() != device:
         with torch.cuda.device(device):
             return sync_cache_attn(cache, q, page_table, lens, row_starts, max_new, scale, out, lse)
     heads = q.shape[1] if q.dim() == 3 else 0
@@ -269,9 +278,12 @@ def sync_cache_attn(cache: KVCache, q, page_table, lens, row_starts=None, max_ne
         if not fill and row_starts is not None:
             lse.fill_(-float("inf"))
     at = None if lse is False or lse is None else _vector(lse, "lse", device, heads * n, torch.float32)
-    work = torch.empty(cache.workspace(heads, max_new), dtype=torch.uint8, device=cache.device)
+    work, size = None, 0
+    if page_table.shape[-1] * cache.page > SHORT:
+        size = cache.workspace(heads, max_new)
+        work = torch.empty(size, dtype=torch.uint8, device=cache.device)
     _sg._check(_sg.lib().sync_cache_attn(cache.desc, _seqs(page_table, lens, row_starts, device), heads, a,
                                          dim ** -0.5 if scale is None else scale, max_new,
-                                         _rows(out, "out", dtype, device, heads, dim), at, fill, work.data_ptr(),
-                                         work.numel(), _current_stream(device)))
+                                         _rows(out, "out", dtype, device, heads, dim), at, fill,
+                                         None if work is None else work.data_ptr(), size, _current_stream(device)))
     return out if at is None and not isinstance(lse, torch.Tensor) else (out, lse)

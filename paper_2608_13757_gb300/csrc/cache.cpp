@@ -147,13 +147,13 @@ int checked_heads(const sync_cache* c, int32_t heads) {
 // row, length, bad, tiles [from, to) of tiles, the warp of the pass's last tile.
 // Returns the number of pieces (written up to `capacity`).
 extern "C" int64_t syncgb_cache_attn_work(int n_seqs, const int32_t* lens, const int32_t* row_starts, int64_t all_rows, int room,
-                                          int kv_heads, int group, int rows, int tile, int warps, int64_t* out, int64_t capacity) {
+                                          int kv_heads, int group, int rows, int tile, int whole, int warps, int64_t* out, int64_t capacity) {
   auto shape_of = [&](int s) {
-    return division::shape(row_starts ? row_starts[s] : s, row_starts ? row_starts[s + 1] : s + 1, all_rows, lens[s], room, group, kv_heads, rows, tile);
+    return division::shape(row_starts ? row_starts[s] : s, row_starts ? row_starts[s + 1] : s + 1, all_rows, lens[s], room, group, kv_heads, rows, tile, whole != 0);
   };
   int64_t total = 0, n = 0;
   for (int s = 0; s < n_seqs; ++s) total += shape_of(s).cost;
-  const int takers = division::takers(total, warps);
+  const int takers = division::takers(total, warps, whole != 0);
   for (int w = 0; w < warps; ++w) {
     const int64_t begin = division::bound(total, takers, w), run = division::bound(total, takers, w + 1) - begin;
     if (!run) continue;
@@ -163,9 +163,9 @@ extern "C" int64_t syncgb_cache_attn_work(int n_seqs, const int32_t* lens, const
     division::Lister l;
     l.start(shape_of(s), s, begin, from, run);
     division::Piece x;
-    for (; l.next(shape_of, n_seqs, kv_heads, rows, x); ++n) {
+    for (; l.next(shape_of, n_seqs, kv_heads, rows, whole != 0, x); ++n) {
       const int64_t row[12] = {w, x.s, x.head, x.first, x.n, x.row0, x.len, x.bad, x.from, x.to, x.tiles,
-                               x.tiles ? division::holder(total, takers, x.last_tile()) : w};
+                               x.tiles && !whole ? division::holder(total, takers, x.last_tile()) : w};
       if (n < capacity) std::copy(row, row + 12, out + 12 * n);
     }
   }
@@ -261,13 +261,14 @@ sync_status sync_cache_attn(const sync_cache* cache, const sync_cache_seqs* seqs
     a.scale = scale;
     a.lse = lse;
     a.fill = zero_rest != 0;
+    a.whole = (int64_t)seqs->max_pages * cache->page <= SYNC_CACHE_SHORT;
+    need(a.whole || (workspace && reinterpret_cast<uintptr_t>(workspace) % 16 == 0), "the workspace is NULL or not 16-byte aligned");
+    if (!a.rows) return;
     a.num_sms = current_sms();
     a.most_rows = cache_attn_rows(a.bits, a.heads / a.kv_heads, max_new);
     a.blocks = cache_attn_blocks(a.bits, a.most_rows, a.num_sms);
-    need(workspace && workspace_bytes >= cache_attn_workspace(a.dim, a.most_rows, a.blocks) && reinterpret_cast<uintptr_t>(workspace) % 16 == 0,
-         "the workspace is NULL, too small or not 16-byte aligned");
+    need(a.whole || workspace_bytes >= cache_attn_workspace(a.dim, a.most_rows, a.blocks), "the workspace is too small");
     a.work = static_cast<uint8_t*>(workspace);
-    if (!a.rows) return;
     cuda(launch_cache_attn(a, static_cast<cudaStream_t>(stream)), "sync_cache_attn");
   });
 }

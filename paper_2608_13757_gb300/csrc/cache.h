@@ -62,6 +62,7 @@ struct CacheArgs {
   int most_rows = 1;                           // query rows of a key head that a pass takes: 8, 16, 32
   int blocks = 0;
   uint8_t* work = nullptr;
+  bool whole = false;                          // no pass is cut between warps
 };
 
 cudaError_t launch_rope(const RopeArgs& a, cudaStream_t st);

@@ -4,7 +4,8 @@
 // The work is a list: sequence > key head > pass (of `rows` query rows) > tile
 // of `tile` keys, every pass counting kUnitCost tiles more for its start and end.
 // A warp has an equal run of it.  A pass that a warp begins but does not end is
-// continued by the warps that follow.
+// continued by the warps that follow.  Or (whole) passes are not cut and count one
+// each, where none can have more than a few tiles.
 #pragma once
 
 #include <cuda_runtime.h>
@@ -27,11 +28,11 @@ SYNCGB_BOTH int64_t more(int64_t a, int64_t b) { return a > b ? a : b; }
 // A sequence: its rows [begin, end) as the caller's arrays have them, brought
 // into the tensors' rows, and its tokens, of which pages hold `room` at most.
 struct Shape {
-  int row0, n, len, bad, tiles, passes;
+  int row0, n, len, bad, tiles, passes, unit;   // unit: what a pass costs
   int64_t cost;
 };
 SYNCGB_BOTH Shape shape(int64_t begin, int64_t end, int64_t all_rows, int len, int room, int group, int kv_heads, int rows,
-                        int tile) {
+                        int tile, bool whole) {
   Shape x;
   begin = less(more(begin, 0), all_rows);
   end = less(more(end, begin), all_rows);
@@ -41,12 +42,13 @@ SYNCGB_BOTH Shape shape(int64_t begin, int64_t end, int64_t all_rows, int len, i
   x.len = (int)less(more(len, 0), room);
   x.tiles = (x.len + tile - 1) / tile;
   x.passes = (int)(((int64_t)x.n * group + rows - 1) / rows);
-  x.cost = (int64_t)x.passes * kv_heads * (x.tiles + kUnitCost);
+  x.unit = whole ? 1 : x.tiles + kUnitCost;
+  x.cost = (int64_t)x.passes * kv_heads * x.unit;
   return x;
 }
 
 // Warps that take work, and where the run of one begins (and the last one's ends).
-SYNCGB_BOTH int takers(int64_t total, int warps) { return (int)more(1, less(warps, total / kLeast)); }
+SYNCGB_BOTH int takers(int64_t total, int warps, bool whole) { return (int)more(1, less(warps, whole ? total : total / kLeast)); }
 SYNCGB_BOTH int64_t bound(int64_t total, int takers, int warp) {
   warp = (int)less(warp, takers);
   if (total < (int64_t)1 << 32 && (uint64_t)total * (uint32_t)takers < (uint64_t)1 << 32) return (uint32_t)total * (uint32_t)warp / (uint32_t)takers;
@@ -80,14 +82,14 @@ struct Lister {
   SYNCGB_BOTH void start(const Shape& x, int seq, int64_t begin, int64_t into_seq, int64_t run) {
     now = x;
     s = seq;
-    const int cost = x.tiles + kUnitCost;
+    const int cost = x.unit;
     unit = into_seq < (int64_t)1 << 31 ? (int)((uint32_t)into_seq / (uint32_t)cost) : (int)(into_seq / cost);
     into = into_seq - (int64_t)unit * cost;
     left = run;
     at = begin - into;
   }
   template <class F>
-  SYNCGB_BOTH bool next(F&& shape_of, int n_seqs, int kv_heads, int rows, Piece& x) {
+  SYNCGB_BOTH bool next(F&& shape_of, int n_seqs, int kv_heads, int rows, bool whole, Piece& x) {
     while (left > 0) {
       if (unit >= now.passes * kv_heads) {
         if (++s >= n_seqs) return false;
@@ -96,13 +98,13 @@ struct Lister {
         into = 0;
         continue;
       }
-      const int64_t to = less(now.tiles + kUnitCost, into + left);
-      const int a = (int)more(0, into - kUnitCost), b = (int)more(0, to - kUnitCost);
+      const int64_t to = less(now.unit, into + left);
+      const int a = whole ? 0 : (int)more(0, into - kUnitCost), b = whole ? now.tiles : (int)more(0, to - kUnitCost);
       const bool some = b > a || (now.tiles == 0 && into == 0);
       if (some) x = Piece{s, unit / now.passes, unit % now.passes * rows, now.n, now.row0, now.len, now.bad, a, b, now.tiles, at};
       left -= to - into;
       into = 0;
-      at += now.tiles + kUnitCost;
+      at += now.unit;
       ++unit;
       if (some) return true;
     }

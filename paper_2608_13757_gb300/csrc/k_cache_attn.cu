@@ -572,7 +572,7 @@ struct Narrow {                            // 4 bits, G groups of 32 entries
 // ---- division of the work ----
 __device__ __forceinline__ Shape shape_of(const CacheArgs& a, int s, int rows, int tile) {
   const int64_t begin = a.starts ? __ldg(a.starts + s) : s, end = a.starts ? __ldg(a.starts + s + 1) : s + 1;
-  return division::shape(begin, end, a.rows, __ldg(a.lens + s), a.max_pages << a.page_shift, a.heads / a.kv_heads, a.kv_heads, rows, tile);
+  return division::shape(begin, end, a.rows, __ldg(a.lens + s), a.max_pages << a.page_shift, a.heads / a.kv_heads, a.kv_heads, rows, tile, a.whole);
 }
 
 // The runs of a block's warps: their bounds in the list, and the sequences where
@@ -607,7 +607,7 @@ __device__ __forceinline__ void find_runs(const CacheArgs& a, Runs& runs) {
   __syncthreads();
   if (threadIdx.x <= kWarps) {
     const int64_t total = runs.sum[0] + runs.sum[1] + runs.sum[2] + runs.sum[3];
-    const int takers = division::takers(total, gridDim.x * kWarps);
+    const int takers = division::takers(total, gridDim.x * kWarps, a.whole);
     runs.bound[threadIdx.x] = division::bound(total, takers, blockIdx.x * kWarps + threadIdx.x);
     if (threadIdx.x == 0) {
       runs.total = total;
@@ -745,7 +745,7 @@ __global__ void __launch_bounds__(kThreads, per_sm(K::kBits, NT)) k_cache_attn(c
     for (;;) {
       if (done) return false;
       int ok = 0;
-      if (lane == 0) ok = lister.next([&](int s) { return shape_of(a, s, ROWS, kTile); }, a.n_seqs, a.kv_heads, ROWS, list[made % kPieces]);
+      if (lane == 0) ok = lister.next([&](int s) { return shape_of(a, s, ROWS, kTile); }, a.n_seqs, a.kv_heads, ROWS, a.whole, list[made % kPieces]);
       __syncwarp();
       done = !__shfl_sync(~0u, ok, 0);
       if (done) return false;
@@ -975,6 +975,7 @@ __global__ void __launch_bounds__(kThreads, per_sm(K::kBits, NT)) k_cache_attn(c
     __syncwarp();
   }
   wait_groups<0>();
+  if (a.whole) return;
   __syncthreads();
 
   // Passes of which several warps have pieces, in the order of the warps: a chain
@@ -1136,6 +1137,7 @@ cudaError_t launch(const CacheArgs& a, cudaStream_t st) {
   k_cache_attn<K, NT, BF16><<<a.blocks, kThreads, kBytes, st>>>(a);
   if ((e = cudaGetLastError()) != cudaSuccess) return e;
   count_launch();
+  if (a.whole) return cudaSuccess;
   e = launch_early(k_cache_merge<K::DP, 8 * NT, BF16>, dim3((unsigned)a.blocks, 8 * NT), 16 * kMergers, 0, st, a, a.blocks);
   if (e == cudaSuccess) count_launch();
   return e;

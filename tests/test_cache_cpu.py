@@ -95,6 +95,9 @@ def test_tensors_refused(sg):
     for change in (dict(q=R(A + 8, 3, 256, 64)), dict(q=R(A, 3, 260, 64)), dict(q=R(A, 3, 256, 68)), dict(scale=0.0), dict(scale=float("nan")),
                    dict(scale=-1.0), dict(max_new=0)):
         assert calls(sg, c, s, **change)[1] == sg.ERR_ARG
+    long = seqs(sg, max_pages=9)                  # more than 128 tokens: a workspace is needed
+    for change in (dict(work=None), dict(work=A + 8)):
+        assert calls(sg, c, long, **change)[1] == sg.ERR_ARG
     q, k = R(A, 3, 256, 64), R(A, 3, 128, 64)
     assert lib.sync_cache_append(c, s, None, k, 0, None, None, None, 0, None) == sg.ERR_ARG
     assert lib.sync_cache_append(c, s, k, R(A, 2, 128, 64), 0, None, None, None, 0, None) == sg.ERR_ARG
@@ -112,13 +115,13 @@ def test_tensors_refused(sg):
     assert lib.sync_cache_attn_workspace(None, 4, 1, ctypes.c_int64()) == sg.ERR_ARG
 
 
-def work(sg, lens, starts, rows_all, room, kv, group, rows, tile, warps):
+def work(sg, lens, starts, rows_all, room, kv, group, rows, tile, warps, whole=0):
     f = sg.lib().syncgb_cache_attn_work
     f.restype = ctypes.c_int64
-    f.argtypes = [ctypes.c_int, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int64] + [ctypes.c_int] * 6 + [ctypes.c_void_p, ctypes.c_int64]
+    f.argtypes = [ctypes.c_int, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int64] + [ctypes.c_int] * 7 + [ctypes.c_void_p, ctypes.c_int64]
     a = np.array(lens, dtype=np.int32)
     b = None if starts is None else np.array(starts, dtype=np.int32)
-    args = (len(lens), a.ctypes.data, None if b is None else b.ctypes.data, rows_all, room, kv, group, rows, tile, warps)
+    args = (len(lens), a.ctypes.data, None if b is None else b.ctypes.data, rows_all, room, kv, group, rows, tile, whole, warps)
     n = f(*args, None, 0)
     out = np.zeros((n, 12), dtype=np.int64)
     assert f(*args, out.ctypes.data, n) == n
@@ -160,6 +163,20 @@ def test_pieces_cover_every_tile_once(sg):
         for b in set(got[:, 0]):
             mine = got[got[:, 0] == b]
             assert all(x[8] == 0 for x in mine[1:]) and all(x[9] == x[10] for x in mine[:-1])
+
+
+def test_whole_passes(sg):
+    """Where no sequence is long, passes are not cut, and warps have equally many."""
+    r = random.Random(5)
+    for rep in range(60):
+        n = r.choice([0, 1, 9, 200])
+        lens, tokens = [r.choice([0, r.randint(0, 128)]) for _ in range(n)], [r.choice([0, 1, 1, 5]) for _ in range(n)]
+        starts, kv, group, rows, tile = [sum(tokens[:i]) for i in range(n + 1)], r.choice([1, 8]), r.choice([1, 4, 16]), r.choice([8, 32]), r.choice([16, 32])
+        got = work(sg, lens, starts, sum(tokens), 128, kv, group, rows, tile, 1216, whole=1)
+        want = sorted((s, h, first) for s in range(n) for h in range(kv) for first in range(0, tokens[s] * group, rows))
+        assert sorted((x[1], x[2], x[3]) for x in got) == want and all(x[8] == 0 and x[9] == x[10] == -(-lens[x[1]] // tile) for x in got)
+        per = np.bincount(got[:, 0], minlength=1)
+        assert len(want) == 0 or per.max() <= -(-len(want) // 1216)
 
 
 def test_runs_are_equal(sg):

@@ -237,6 +237,22 @@ def test_nothing_to_do(sg):
 
 
 @BITS
+def test_short_tables_and_small_workspaces(sg, bits):
+    """Sequences of up to 128 tokens by way of short tables take no workspace; others
+    are refused one that is too small."""
+    lens = [128, 0, 1, 77, 64] * 30
+    run_and_check(sg, lens, 8, 2, 128, torch.bfloat16, bits, page=128)
+    run_and_check(sg, [16, 0, 3, 100], 10, 2, 64, torch.float16, bits, page=64, starts=[0, 3, 4, 4, 9], max_new=5)
+    cache, table = made(sg, 10, [200], 16, 2, 64, torch.bfloat16, bits)
+    q, n = queries(10, 1, 8, 64, torch.bfloat16), i32([200])
+    C, rows = sg.cache, sg.attention._rows(q, "q", q.dtype, 0, 8, 64)
+    work = torch.empty(cache.workspace(8, 1), dtype=torch.uint8, device="cuda")
+    for size, status in ((work.numel() - 1, sg.ERR_ARG), (work.numel(), sg.OK)):
+        assert sg.lib().sync_cache_attn(cache.desc, C._seqs(table, n, None, 0), 8, rows, 0.1, 1, rows, None, 0, work.data_ptr(), size, None) == status
+    torch.cuda.synchronize()
+
+
+@BITS
 def test_run_of_a_prompt_and_its_answer(sg, bits):
     """A prompt appended in pieces, read back for the packed attention of the
     next piece, then decoded token by token: as attention over all of it."""
