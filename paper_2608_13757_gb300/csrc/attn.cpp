@@ -191,6 +191,18 @@ bool packs(const AttnSeq& s, int group) {
   return (s.lq + per - 1) / per < (int64_t)group * ((s.lq + kTile - 1) / kTile);
 }
 
+// Plans of queries that see all keys go to the kernel of few queries (k_cache_attn.cu)
+// where a key head's queries fit in 16 of its columns: it reads what there is and
+// no more (48 sequences of one query and up to 1500 keys, 20 heads of 64: 56 us,
+// where tiles of 128 queries take 71).
+constexpr int64_t kFewRows = 16;
+bool few_queries(const sync_attn_desc* d, bool causal, const std::vector<AttnSeq>& seq) {
+  if (causal || d->train || seq.empty() || seq.size() > (1u << 20)) return false;
+  int64_t most = 0;
+  for (const AttnSeq& s : seq) most = std::max<int64_t>(most, s.lq);
+  return most > 0 && most * (d->heads / d->kv_heads) <= kFewRows;
+}
+
 struct ForwardWork {
   std::vector<AttnItem> item;
   std::vector<int32_t> block_first;
@@ -543,8 +555,32 @@ static sync_status make_plan(const sync_attn_desc* desc, bool causal, int device
     a.kv_heads = desc->kv_heads;
     a.dim = desc->head_dim;
     a.num_sms = P->num_sms;
-    const ForwardWork w = forward_work(desc, causal, seq, P->num_sms);
-    a.n_blocks = (int)w.block_first.size() - 1;
+    P->few = few_queries(desc, causal, seq);
+    std::vector<int32_t> q_row, q_len, k_len;
+    std::vector<int64_t> k_row;
+    CacheArgs& f = P->rows;
+    if (P->few) {
+      int32_t most_q = 0, most_k = 0;
+      for (const AttnSeq& s : seq) {
+        q_row.push_back((int32_t)s.q0);
+        q_len.push_back(s.lq);
+        k_len.push_back(s.lk);
+        k_row.push_back(s.k0);
+        most_q = std::max(most_q, s.lq);
+        most_k = std::max(most_k, s.lk);
+      }
+      f.bf16 = a.bf16;
+      f.heads = a.heads;
+      f.kv_heads = a.kv_heads;
+      f.dim = a.dim;
+      f.n_seqs = desc->n_seqs;
+      f.num_sms = P->num_sms;
+      f.most_rows = cache_attn_rows(16, a.heads / a.kv_heads, most_q);
+      f.blocks = cache_attn_blocks(16, f.most_rows, P->num_sms);
+      f.whole = most_k <= SYNC_CACHE_SHORT;
+    }
+    const ForwardWork w = P->few ? ForwardWork{} : forward_work(desc, causal, seq, P->num_sms);
+    a.n_blocks = std::max<int>(0, (int)w.block_first.size() - 1);
     std::vector<AttnTile> qt, kt;
     std::vector<int32_t> q_first, k_first;
     if (P->train) {
@@ -558,11 +594,13 @@ static sync_status make_plan(const sync_attn_desc* desc, bool causal, int device
     a.delta_rows = sz.q_rows;
     Arena m;
     const size_t at_item = m.add(w.item), at_first = m.add(w.block_first), at_split = m.add(w.split),
-                 at_qt = m.add(qt), at_kt = m.add(kt), at_qf = m.add(q_first), at_kf = m.add(k_first);
+                 at_qt = m.add(qt), at_kt = m.add(kt), at_qf = m.add(q_first), at_kf = m.add(k_first),
+                 at_row = m.add(q_row), at_len = m.add(q_len), at_keys = m.add(k_len), at_key = m.add(k_row);
     const size_t padded = a.dim <= 64 ? 64 : 128;
     const size_t at_part = m.reserve((size_t)w.slots * 2 * kTile * padded * sizeof(float)),
                  at_part_lse = m.reserve((size_t)w.slots * 2 * kTile * sizeof(float)),
                  at_delta = m.reserve(P->train ? (size_t)sz.q_rows * (size_t)a.heads * sizeof(float) : 0);
+    const size_t at_work = m.reserve(P->few && !f.whole ? (size_t)cache_attn_workspace(a.dim, f.most_rows, f.blocks) : 0);
     cuda(cudaMallocHost(reinterpret_cast<void**>(&P->error), sizeof(int)), "sync_attn_plan");
     *P->error = 0;
     a.error = P->error;
@@ -581,8 +619,13 @@ static sync_status make_plan(const sync_attn_desc* desc, bool causal, int device
     a.part_o = reinterpret_cast<float*>(base + at_part);
     a.part_lse = reinterpret_cast<float*>(base + at_part_lse);
     a.delta = reinterpret_cast<float*>(base + at_delta);
+    f.starts = reinterpret_cast<const int32_t*>(base + at_row);
+    f.counts = reinterpret_cast<const int32_t*>(base + at_len);
+    f.lens = reinterpret_cast<const int32_t*>(base + at_keys);
+    f.firsts = reinterpret_cast<const int64_t*>(base + at_key);
+    f.work = base + at_work;
     sz.device_bytes = (int64_t)m.size();
-    sz.n_items = (int32_t)w.item.size();
+    sz.n_items = P->few ? desc->n_seqs * a.kv_heads : (int32_t)w.item.size();
     sz.n_splits = w.slots;
     P->sz = sz;
     *out = P.release();
@@ -624,9 +667,29 @@ sync_status sync_attn_forward(const sync_attn* plan, const sync_rows* q, const s
     a.v = attn_tensor(v, plan->sz.k_rows, "v must not be NULL");
     a.o = attn_tensor(o, plan->sz.q_rows, "o must not be NULL");
     a.lse = lse;
-    if (!a.n_blocks) return;
+    if (!a.n_blocks && !plan->few) return;
     check_gave_up(plan);
     DeviceScope scope(plan->device);
+    if (plan->few) {
+      auto rows = [](const AttnTensor& t) {
+        HeadTensor r;
+        r.data = t.data;
+        r.rows = t.rows;
+        r.row = t.row;
+        r.head = t.head;
+        return r;
+      };
+      CacheArgs f = plan->rows;
+      f.rows = a.q.rows;
+      f.scale = scale;
+      f.q = rows(a.q);
+      f.q_out = rows(a.o);
+      f.k_rows = rows(a.k);
+      f.v_rows = rows(a.v);
+      f.lse = lse;
+      cuda(launch_few_queries(f, static_cast<cudaStream_t>(stream)), "sync_attn_forward");
+      return;
+    }
     const int group = a.heads / a.kv_heads;
     AttnMaps m{};
     m.q = tile_map(a.q, a.bf16, a.heads, a.dim, 1, kTile);

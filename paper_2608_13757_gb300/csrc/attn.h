@@ -8,6 +8,7 @@
 
 #include <vector>
 
+#include "cache.h"
 #include "sync.h"
 
 namespace syncgb {
@@ -91,6 +92,8 @@ struct sync_attn {
   bool train = false;
   sync_attn_sizes sz{};
   syncgb::AttnArgs args;           // sizes and device tables
+  bool few = false;                // few queries per sequence: k_cache_attn.cu, and what it takes
+  syncgb::CacheArgs rows;
   void* block = nullptr;           // device memory
   int* error = nullptr;            // pinned
 };

@@ -63,12 +63,18 @@ struct CacheArgs {
   int blocks = 0;
   uint8_t* work = nullptr;
   bool whole = false;                          // no pass is cut between warps
+  // attention of few queries over plain rows: sequence s has rows starts[s] and on,
+  // counts[s] of them, and lens[s] keys from row firsts[s] of k_rows and v_rows on,
+  // all of which they see
+  const int32_t* counts = nullptr;
+  const int64_t* firsts = nullptr;
 };
 
 cudaError_t launch_rope(const RopeArgs& a, cudaStream_t st);
 cudaError_t launch_cache_append(const CacheArgs& a, cudaStream_t st);
 cudaError_t launch_cache_read(const CacheArgs& a, cudaStream_t st);
 cudaError_t launch_cache_attn(const CacheArgs& a, cudaStream_t st);
+cudaError_t launch_few_queries(const CacheArgs& a, cudaStream_t st);
 
 // Blocks and workspace of an attention call.
 int cache_attn_rows(int bits, int group, int max_new);                // query rows of a pass: 8, 16, 32

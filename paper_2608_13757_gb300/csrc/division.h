@@ -40,7 +40,7 @@ SYNCGB_BOTH Shape shape(int64_t begin, int64_t end, int64_t all_rows, int len, i
   x.n = (int)(end - begin);
   x.bad = len > room;
   x.len = (int)less(more(len, 0), room);
-  x.tiles = (x.len + tile - 1) / tile;
+  x.tiles = (int)(((int64_t)x.len + tile - 1) / tile);
   x.passes = (int)(((int64_t)x.n * group + rows - 1) / rows);
   x.unit = whole ? 1 : x.tiles + kUnitCost;
   x.cost = (int64_t)x.passes * kv_heads * x.unit;

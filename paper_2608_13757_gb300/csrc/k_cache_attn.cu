@@ -28,6 +28,7 @@
 // two that a warp raises when a larger scale comes.
 #include <algorithm>
 #include <atomic>
+#include <type_traits>
 
 #include "cache.h"
 #include "division.h"
@@ -145,20 +146,25 @@ __device__ __forceinline__ uint32_t as_word(__half2 x) { return *reinterpret_cas
 // Each holds a warp's queries and outputs, copies a tile of 16 keys to shared
 // memory, and has the scores of a tile and the products with its values.
 
-template <int DP_, int NT, bool BF16>
-struct Wide {                              // 16 bits
+template <int DP_, int NT, bool BF16, bool PAGED>
+struct Wide {                              // 16 bits; plain rows where not PAGED
   static constexpr int kBits = 16;
+  static constexpr bool kPaged = PAGED;
   static constexpr int DP = DP_, MT = 1, kStages = 3, kSide = kKeys * DP * 2, kStage = 2 * kSide;
   uint32_t q[DP / 16][NT][2];
   float o[DP / 16][NT][4], f;
 
-  // What the copies of a tile of 16 keys, the row16-th of the cache, start from.
-  const uint8_t *k, *v;
+  // What the copies of a tile of 16 keys start from: the keys' and values' first
+  // row (in the cache: its row16-th 16 of them), and this lane's part of it.
+  using Step = std::conditional_t<PAGED, int, int64_t>;
+  Step k, v, k_step, v_step;               // bytes; from one row to the next
   uint32_t to;
   __device__ __forceinline__ void begin(const CacheArgs& a, uint32_t ring) {
     const int lane = threadIdx.x % 32, key = lane / (DP / 8), j = lane % (DP / 8);
-    k = a.k + key * a.dim * 2 + 16 * j;
-    v = a.v + key * a.dim * 2 + 16 * j;
+    k_step = (Step)(PAGED ? 2 * a.dim : 2 * a.k_rows.row);
+    v_step = (Step)(PAGED ? 2 * a.dim : 2 * a.v_rows.row);
+    k = key * k_step + 16 * j;
+    v = key * v_step + 16 * j;
     to = key * DP * 2 + ((j ^ key) * 16);
     if (a.dim < DP)                        // entries that the heads do not have: zero, and never written again
       for (int i = lane; i < kStages * kStage / 16; i += 32) asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(ring + 16 * i), "r"(0) : "memory");
@@ -166,20 +172,25 @@ struct Wide {                              // 16 bits
   }
   template <int T>
   __device__ __forceinline__ void fetch(const CacheArgs& a, uint32_t stage, uint32_t row16, int keys) const {
+    const uint64_t at = (uint64_t)row16 * (uint32_t)(32 * a.dim);
+    copy(a, stage, a.k + at, a.v + at, keys);
+  }
+  __device__ __forceinline__ void copy(const CacheArgs& a, uint32_t stage, const uint8_t* rows_k, const uint8_t* rows_v, int keys) const {
     constexpr int kStep = 256 / DP;        // keys that the lanes copy at a time
     const int lane = threadIdx.x % 32, key = lane / (DP / 8), j = lane % (DP / 8);
     if (j >= a.dim / 8) return;
-    const uint8_t *from_k = k + (uint64_t)row16 * (uint32_t)(32 * a.dim), *from_v = v + (uint64_t)row16 * (uint32_t)(32 * a.dim);
+    const uint8_t *from_k = rows_k + k, *from_v = rows_v + v;
 #pragma unroll
     for (int e = 0; e < kKeys / kStep; ++e) {
       const uint32_t at = stage + e * kStep * DP * 2 + (to ^ (e * kStep % 8 * 16));
-      const int step = e * kStep * a.dim * 2;
+      const uint8_t *at_k = from_k + e * kStep * k_step, *at_v = from_v + e * kStep * v_step;
       if (keys >= kKeys) {
-        copy16<0, 0>(at, from_k + step);
-        copy16<kSide, 0>(at, from_v + step);
+        copy16<0, 0>(at, at_k);
+        copy16<kSide, 0>(at, at_v);
       } else {                             // past the sequence's end anything may lie, and a zero weight does not hide a NaN
-        copy16(at, from_k + step, key + e * kStep < keys);
-        copy16(at + kSide, from_v + step, key + e * kStep < keys);
+        const bool on = key + e * kStep < keys;
+        copy16(at, on ? at_k : rows_k, on);
+        copy16(at + kSide, on ? at_v : rows_v, on);
       }
     }
   }
@@ -272,6 +283,7 @@ struct Wide {                              // 16 bits
 template <int G, int NT, bool BF16>
 struct Narrow {                            // 4 bits, G groups of 32 entries
   static constexpr int kBits = 4;
+  static constexpr bool kPaged = true;
   // Two times 16 keys at once where there are registers for them: what is done
   // once per tile counts half, and one's instructions cover the other's.
   static constexpr int DP = 32 * G, MT = NT == 1 ? 2 : 1, kStages = MT == 2 ? 3 : 4, kSide = kKeys * 16 * G, kScales = kKeys * 2 * G;
@@ -570,9 +582,11 @@ struct Narrow {                            // 4 bits, G groups of 32 entries
 };
 
 // ---- division of the work ----
+template <bool PAGED>
 __device__ __forceinline__ Shape shape_of(const CacheArgs& a, int s, int rows, int tile) {
-  const int64_t begin = a.starts ? __ldg(a.starts + s) : s, end = a.starts ? __ldg(a.starts + s + 1) : s + 1;
-  return division::shape(begin, end, a.rows, __ldg(a.lens + s), a.max_pages << a.page_shift, a.heads / a.kv_heads, a.kv_heads, rows, tile, a.whole);
+  const int64_t begin = a.starts ? __ldg(a.starts + s) : s;
+  const int64_t end = !PAGED ? begin + __ldg(a.counts + s) : a.starts ? __ldg(a.starts + s + 1) : s + 1;
+  return division::shape(begin, end, a.rows, __ldg(a.lens + s), PAGED ? a.max_pages << a.page_shift : INT32_MAX, a.heads / a.kv_heads, a.kv_heads, rows, tile, a.whole);
 }
 
 // The runs of a block's warps: their bounds in the list, and the sequences where
@@ -592,14 +606,14 @@ __device__ __forceinline__ int64_t summed_up(int64_t x) {     // over the lanes 
   return x;
 }
 
-template <int ROWS, int TILE>
+template <int ROWS, int TILE, bool PAGED>
 __device__ __forceinline__ void find_runs(const CacheArgs& a, Runs& runs) {
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
   const bool few = a.n_seqs <= kThreads;
   int64_t cost = 0;
   Shape x{};
   for (int s = threadIdx.x; s < a.n_seqs; s += kThreads) {
-    x = shape_of(a, s, ROWS, TILE);
+    x = shape_of<PAGED>(a, s, ROWS, TILE);
     cost += x.cost;
   }
   int64_t sum = summed_up(cost);
@@ -620,7 +634,7 @@ __device__ __forceinline__ void find_runs(const CacheArgs& a, Runs& runs) {
   for (int s0 = 0; s0 < a.n_seqs; s0 += kThreads) {
     const int s = s0 + threadIdx.x;
     if (!few) {
-      if (s < a.n_seqs) x = shape_of(a, s, ROWS, TILE);
+      if (s < a.n_seqs) x = shape_of<PAGED>(a, s, ROWS, TILE);
       cost = s < a.n_seqs ? x.cost : 0;
       sum = summed_up(cost);
       __syncthreads();
@@ -725,7 +739,7 @@ __global__ void __launch_bounds__(kThreads, per_sm(K::kBits, NT)) k_cache_attn(c
       }
   }
 
-  find_runs<ROWS, kTile>(a, runs);
+  find_runs<ROWS, kTile, K::kPaged>(a, runs);
   Lister& lister = listers[warp];
   Piece* const list = lists[warp];
   Left& left = lefts[warp];
@@ -745,7 +759,7 @@ __global__ void __launch_bounds__(kThreads, per_sm(K::kBits, NT)) k_cache_attn(c
     for (;;) {
       if (done) return false;
       int ok = 0;
-      if (lane == 0) ok = lister.next([&](int s) { return shape_of(a, s, ROWS, kTile); }, a.n_seqs, a.kv_heads, ROWS, a.whole, list[made % kPieces]);
+      if (lane == 0) ok = lister.next([&](int s) { return shape_of<K::kPaged>(a, s, ROWS, kTile); }, a.n_seqs, a.kv_heads, ROWS, a.whole, list[made % kPieces]);
       __syncwarp();
       done = !__shfl_sync(~0u, ok, 0);
       if (done) return false;
@@ -768,6 +782,7 @@ __global__ void __launch_bounds__(kThreads, per_sm(K::kBits, NT)) k_cache_attn(c
   // Tiles ahead: the next one to copy, whose page was looked up one tile before.
   int ap = 0, at_tile = 0, at_to = 0, at_len = 0, at_head = 0, page[MT];
   const int32_t* at_table = nullptr;
+  const uint8_t *at_k = nullptr, *at_v = nullptr;   // plain rows: the sequence's first key and value
   auto piece = [&] {                       // at_len 0 behind the last
     at_len = 0;
     if (ap == made && !make()) return;
@@ -776,9 +791,16 @@ __global__ void __launch_bounds__(kThreads, per_sm(K::kBits, NT)) k_cache_attn(c
     at_to = x.to;
     at_len = x.len;
     at_head = x.head;
-    at_table = a.table + x.s * a.table_stride;
+    if constexpr (K::kPaged) {
+      at_table = a.table + x.s * a.table_stride;
+    } else {
+      const int64_t row = __ldg(a.firsts + x.s);
+      at_k = static_cast<const uint8_t*>(a.k_rows.data) + 2 * (row * a.k_rows.row + at_head * a.k_rows.head);
+      at_v = static_cast<const uint8_t*>(a.v_rows.data) + 2 * (row * a.v_rows.row + at_head * a.v_rows.head);
+    }
   };
   auto look = [&] {
+    if (!K::kPaged) return;
     const int pos = at_tile * kTile;
     if (at_len) page[0] = __ldg(at_table + (pos >> a.page_shift));
     if (MT == 2 && a.page_shift == 4 && pos + kKeys < at_len) page[MT - 1] = __ldg(at_table + (pos >> a.page_shift) + 1);
@@ -787,20 +809,24 @@ __global__ void __launch_bounds__(kThreads, per_sm(K::kBits, NT)) k_cache_attn(c
   auto ahead = [&] {
     if (at_len) {
       const int pos = at_tile * kTile;
-      auto row16 = [&](int t) {
-        return (((uint32_t)page[t] * a.kv_heads + at_head) << (a.page_shift - 4)) + (pos / kKeys & ((1 << (a.page_shift - 4)) - 1));
-      };
-      const bool two = MT == 2 && pos + kKeys < at_len, apart = a.page_shift == 4;
-      bool has = (unsigned)page[0] < (unsigned)a.n_pages;
-      const uint32_t first = row16(0);
-      if (has) k.template fetch<0>(a, put, first, at_len - pos);
-      if (two && apart) {
-        has = has && (unsigned)page[MT - 1] < (unsigned)a.n_pages;
-        if (has) k.template fetch<MT - 1>(a, put, row16(MT - 1), at_len - pos - kKeys);
-      } else if (two && has) {
-        k.template fetch<MT - 1>(a, put, first + 1, at_len - pos - kKeys);
+      if constexpr (K::kPaged) {
+        auto row16 = [&](int t) {
+          return (((uint32_t)page[t] * a.kv_heads + at_head) << (a.page_shift - 4)) + (pos / kKeys & ((1 << (a.page_shift - 4)) - 1));
+        };
+        const bool two = MT == 2 && pos + kKeys < at_len, apart = a.page_shift == 4;
+        bool has = (unsigned)page[0] < (unsigned)a.n_pages;
+        const uint32_t first = row16(0);
+        if (has) k.template fetch<0>(a, put, first, at_len - pos);
+        if (two && apart) {
+          has = has && (unsigned)page[MT - 1] < (unsigned)a.n_pages;
+          if (has) k.template fetch<MT - 1>(a, put, row16(MT - 1), at_len - pos - kKeys);
+        } else if (two && has) {
+          k.template fetch<MT - 1>(a, put, first + 1, at_len - pos - kKeys);
+        }
+        if (!has) lost |= 1u << (put - mine) / K::kStage;
+      } else {
+        k.copy(a, put, at_k + pos * k.k_step, at_v + pos * k.v_step, at_len - pos);
       }
-      if (!has) lost |= 1u << (put - mine) / K::kStage;
       if (++at_tile >= at_to) piece();
       look();
     }
@@ -845,7 +871,7 @@ __global__ void __launch_bounds__(kThreads, per_sm(K::kBits, NT)) k_cache_attn(c
         split(x, x.first + 8 * nt + 2 * c + j, token, head);
         m[nt][j] = -INFINITY;
         l[nt][j] = shift[nt][j] = 0.f;
-        limit[nt][j] = len - x.n + min(token, x.n - 1) + 1;
+        limit[nt][j] = K::kPaged ? len - x.n + min(token, x.n - 1) + 1 : len;
         least = min(least, limit[nt][j]);
       }
     }
@@ -1145,7 +1171,7 @@ cudaError_t launch(const CacheArgs& a, cudaStream_t st) {
 
 template <int NT, bool BF16>
 cudaError_t launch_rows(const CacheArgs& a, cudaStream_t st) {
-  if (a.bits == 16) return a.dim <= 64 ? launch<Wide<64, NT, BF16>, NT, BF16>(a, st) : launch<Wide<128, NT, BF16>, NT, BF16>(a, st);
+  if (a.bits == 16) return a.dim <= 64 ? launch<Wide<64, NT, BF16, true>, NT, BF16>(a, st) : launch<Wide<128, NT, BF16, true>, NT, BF16>(a, st);
   if constexpr (NT <= 2) {
     switch (a.dim / kGroup) {
       case 1: return launch<Narrow<1, NT, BF16>, NT, BF16>(a, st);
@@ -1165,6 +1191,15 @@ cudaError_t launch_type(const CacheArgs& a, cudaStream_t st) {
 }
 
 }  // namespace
+
+cudaError_t launch_few_queries(const CacheArgs& a, cudaStream_t st) {
+  auto go = [&](auto bf16) {
+    constexpr bool B = decltype(bf16)::value;
+    if (a.most_rows == 8) return a.dim <= 64 ? launch<Wide<64, 1, B, false>, 1, B>(a, st) : launch<Wide<128, 1, B, false>, 1, B>(a, st);
+    return a.dim <= 64 ? launch<Wide<64, 2, B, false>, 2, B>(a, st) : launch<Wide<128, 2, B, false>, 2, B>(a, st);
+  };
+  return a.bf16 ? go(std::true_type()) : go(std::false_type());
+}
 
 int cache_attn_rows(int bits, int group, int max_new) {
   const int64_t rows = (int64_t)group * max_new;

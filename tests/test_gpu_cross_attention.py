@@ -152,3 +152,43 @@ def test_graph_and_stream(sg):
     other = sg.sync_attn_forward(plan, q, k, v, stream=side)
     side.synchronize()
     assert torch.equal(out, want) and torch.equal(other, want)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16], ids=["bf16", "fp16"])
+@pytest.mark.parametrize("dim", [8, 40, 64, 80, 128])
+@pytest.mark.parametrize("heads,kv", [(4, 4), (16, 1), (6, 2), (20, 10)], ids=str)
+def test_few_queries(sg, heads, kv, dim, dtype):
+    """Up to 16 rows of a key head go to a kernel of their own."""
+    run_and_check(sg, [1, 1, 0, 1, 1], [100, 0, 30, 1, 700], heads, kv, dim, dtype, train=False)
+    if heads // kv <= 4:
+        run_and_check(sg, [4, 1, 3], [129, 0, 2000], heads, kv, dim, dtype, train=False)
+
+
+def test_few_queries_in_strided_rows(sg):
+    """Values where a projection left them, head-major keys, gaps between and
+    NaN behind the sequences: rows of no sequence keep what they held."""
+    heads, kv, dim, dtype = 8, 4, 64, torch.bfloat16
+    q_lens, k_lens, q_starts, k_starts = [2, 1, 8], [300, 5, 131], [9, 0, 20], [400, 20, 40]
+    q, k, v, _ = inputs(21, 30, 701, heads, kv, dim, dtype)
+    wide = torch.full((701, 3 * kv, dim), math.nan, dtype=dtype, device="cuda")
+    k = k.transpose(0, 1).contiguous().transpose(0, 1)
+    for a, n in zip(k_starts, k_lens):
+        wide[a:a + n, kv:2 * kv] = v[a:a + n]
+    want = ref.packed(q, k, v, q_lens, k_lens, q_starts, k_starts, dim ** -0.5)
+    for other in (0.0, math.nan):
+        mine = torch.zeros(701, dtype=torch.bool, device="cuda")
+        for a, n in zip(k_starts, k_lens):
+            mine[a:a + n] = True
+        k[~mine] = other
+        plan = sg.sync_attn_plan(q_lens, k_lens, heads, kv, dim, dtype, q_starts=q_starts, k_starts=k_starts, causal=False)
+        out, lse = torch.full((30, heads + 1, dim), 7.0, dtype=dtype, device="cuda")[:, 1:], torch.full((heads, 30), 7.0, device="cuda")
+        sg.sync_attn_forward(plan, q, k, wide[:, kv:2 * kv], out=out, lse=lse)
+        ref.check(out, want["o"], want["o_tol"], "o")
+        ref.check(lse, want["lse"], want["lse_tol"], "lse")
+        none = torch.isnan(want["o"])
+        assert bool((out[none] == 7).all()) and bool((lse[torch.isnan(want["lse"])] == 7).all())
+
+
+def test_few_queries_many_and_long(sg):
+    run_and_check(sg, [1] * 300, [(i * 53) % 400 for i in range(300)], 4, 4, 64, torch.float16, train=False)
+    run_and_check(sg, [1, 2], [40000, 9], 8, 2, 128, torch.bfloat16, train=False)
