@@ -58,13 +58,18 @@ __device__ __forceinline__ void turned8(const T* head, const uint32_t* w, const 
     for (int i = 0; i < 8; i += 2)
       if (d + i < 2 * half) turn(x[i], x[i + 1], c[(d + i) / 2], s[(d + i) / 2]);
   } else if (half % 8 == 0) {
-    float y[8];
-    unpack8<T>(other, y);
     const int j = d < half ? d : d - half;
     const uint32_t sign = d < half ? 0x80000000u : 0u;      // a c - b s, or b c + a s
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-      x[i] = __fadd_rn(__fmul_rn(x[i], c[j + i]), __fmul_rn(__uint_as_float(__float_as_uint(y[i]) ^ sign), s[j + i]));
+    for (int i = 0; i < 8; i += 4) {
+      const Pack<float, 4> u = *reinterpret_cast<const Pack<float, 4>*>(c + j + i), v = *reinterpret_cast<const Pack<float, 4>*>(s + j + i);
+#pragma unroll
+      for (int e = 0; e < 4; e += 2) {
+        const float2 y = unpack<T>(other[(i + e) / 2]);
+        x[i + e] = __fadd_rn(__fmul_rn(x[i + e], u.x[e]), __fmul_rn(__uint_as_float(__float_as_uint(y.x) ^ sign), v.x[e]));
+        x[i + e + 1] = __fadd_rn(__fmul_rn(x[i + e + 1], u.x[e + 1]), __fmul_rn(__uint_as_float(__float_as_uint(y.y) ^ sign), v.x[e + 1]));
+      }
+    }
   } else {                                                  // 8 entries that are not all on one side
 #pragma unroll 1
     for (int i = 0; i < 8; ++i) {
@@ -151,7 +156,7 @@ struct QueryItem {
   __device__ __forceinline__ void read(int e, int64_t row) { x[e].read(from + row * in_row, p, half, pairs); }
   __device__ __forceinline__ void write(int e, int64_t row, const Where& w, const float* cs) {
     if (w.mine) {
-      if (p < half) x[e].by(cs + p, cs + half + p);
+      if (p < half) x[e].template by<true>(cs + p, cs + half + p);
     } else {
       if (!fill) return;
 #pragma unroll
@@ -224,15 +229,12 @@ template <class Item>
 __device__ __forceinline__ void through(const CacheArgs& a, const Columns& c, float* angles, Where* where, bool on, Item& item) {
   constexpr int kAhead = Item::kAhead;
   const int half = a.turn.half, tokens = c.tokens(), sub = threadIdx.x / c.each;
-  auto here = [&](int64_t group) {                          // tokens of this thread in a group
-    const int64_t left = a.rows - group * tokens - sub;
-    return on && left > 0 ? (int)min((int64_t)c.ahead, (left + c.par - 1) / c.par) : 0;
-  };
+  auto here = [&](int64_t row, int e) { return on && e < c.ahead && row < a.rows; };
   auto read = [&](int64_t group) {
-    const int n = here(group);
+    int64_t row = group * tokens + sub;
 #pragma unroll
-    for (int e = 0; e < kAhead; ++e)
-      if (e < n) item.read(e, group * tokens + sub + e * c.par);
+    for (int e = 0; e < kAhead; ++e, row += c.par)
+      if (here(row, e)) item.read(e, row);
   };
   auto search = [&](int64_t group, int groups) {            // into where, for that many groups
     for (int i = threadIdx.x; i < groups * tokens; i += blockDim.x) {
@@ -286,11 +288,11 @@ __device__ __forceinline__ void through(const CacheArgs& a, const Columns& c, fl
     for (int n = 0; n < known; ++n, group += gridDim.x) {
       const bool more = n + 1 < known;
       if (more) find(group + gridDim.x, (n + 1) * tokens);
-      const int mine = here(group);
 #pragma unroll
       for (int e = 0; e < kAhead; ++e) {
         const int token = sub + e * c.par;
-        if (e < mine) item.write(e, group * tokens + token, where[n * tokens + token], angles + ((n % 2 * tokens + token) * 2) * half);
+        const int64_t row = group * tokens + token;
+        if (here(row, e)) item.write(e, row, where[n * tokens + token], angles + ((n % 2 * tokens + token) * 2) * half);
       }
       if (group + gridDim.x < c.groups) read(group + gridDim.x);
       if (more) put((n + 1) % 2);
@@ -303,7 +305,7 @@ __device__ __forceinline__ void through(const CacheArgs& a, const Columns& c, fl
 // values, the others its queries.  T: their type; QVEC: pairs of a query head that
 // a thread takes at a time.
 template <class T, int QVEC, int BITS, bool INTER>
-__global__ void __launch_bounds__(kAppendResident, 1) k_append(const __grid_constant__ CacheArgs a, const __grid_constant__ Columns c, int kv_blocks, bool kv_wide) {
+__global__ void __launch_bounds__(kAppendThreads, kAppendResident / kAppendThreads) k_append(const __grid_constant__ CacheArgs a, const __grid_constant__ Columns c, int kv_blocks, bool kv_wide) {
   extern __shared__ __align__(16) float angles[];           // [2][tokens][cos, sin][half]
   __shared__ Where where[kFound];
   const bool on = (int)threadIdx.x / c.each < c.par;
@@ -359,7 +361,7 @@ __global__ void __launch_bounds__(kReadResident, 1) k_read(const __grid_constant
 #pragma unroll 1
     for (int n = 0; n < known; ++n, group += gridDim.x) {
       const int64_t row = group * tokens + sub, left = a.rows - row;
-      const int mine = on && left > 0 ? (int)min((int64_t)c.ahead, (left + c.par - 1) / c.par) : 0;
+      const int mine = !on ? 0 : left >= tokens ? c.ahead : left > 0 ? ((int)left + c.par - 1) / c.par : 0;
       const int64_t* const place = places + n * tokens + sub;
       Pack<uint32_t, 4> x[kReadAhead];                      // 16 bits: the entries; 4: a word of codes and its scale
 #pragma unroll

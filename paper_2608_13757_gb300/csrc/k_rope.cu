@@ -82,7 +82,7 @@ __global__ void __launch_bounds__(kResident, 1) k_rope(const __grid_constant__ R
       const int64_t row = group * tokens + token;
       if (on && e < c.ahead && row < a.rows) {
         const float* cs = angles + ((which * tokens + token) * 2) * half + p;
-        if (p < half) x[e].by(cs, cs + half);
+        if (p < half) x[e].template by<false>(cs, cs + half);
         x[e].write(to + row * out_row, p, half, pairs);
       }
     }
