@@ -596,7 +596,10 @@ sync_status sync_attn_plan(const sync_attn_desc *desc, int device, sync_attn **o
  * is 0).  Sequences that share their keys (several decoders of one encoder's
  * states) give the same k_start, unless train is set.  The plan serves the same
  * calls; it depends on the lengths alone, so one serves every step of decoding
- * against the same states. */
+ * against the same states.  Without train, where no sequence has more than 16
+ * queries for a key head (heads / kv_heads times its q_len), a forward call takes
+ * the kernel of sync_cache_attn instead of tiles of 128 queries, and n_items is
+ * the number of sequences times kv_heads. */
 sync_status sync_cross_attn_plan(const sync_attn_desc *desc, int device, sync_attn **out);
 
 sync_status sync_attn_query(const sync_attn *plan, sync_attn_sizes *out);
@@ -769,9 +772,10 @@ sync_status sync_cache_attn_workspace(const sync_cache *cache, int32_t heads, in
  * are rounded to dtype for the second product.  4 bits: codes enter the products
  * exactly; queries are scaled by a power of two to float16 (entries below 2^-21
  * of their head's largest lose bits), weights are rounded to float16 before and
- * after their value's scale.  Scores stay below 2^27 in size.  In 16 bits a NaN or an
- * infinity in the value of a token that some of a sequence's rows see may reach
- * its other rows; nothing past lens[s] or of other sequences ever does. */
+ * after their value's scale.  Scores stay below 2^27 in size.  A NaN or an infinity
+ * in the value (or in 4 bits its scale) of a token that some of a sequence's rows
+ * see may reach its other rows; nothing past lens[s] or of other sequences ever
+ * does.  Calls that may run at the same time have a workspace each. */
 sync_status sync_cache_attn(const sync_cache *cache, const sync_cache_seqs *seqs, int32_t heads, const sync_rows *q,
                             float scale, int32_t max_new, const sync_rows *o, float *lse, int32_t zero_rest,
                             void *workspace, int64_t workspace_bytes, void *stream);

@@ -2,7 +2,9 @@
 // the device and, for tests, on the host.
 //
 // The work is a list: sequence > key head > pass (of `rows` query rows) > tile
-// of `tile` keys, every pass counting kUnitCost tiles more for its start and end.
+// of `tile` keys, every pass counting kUnitCost tiles more for its start and end
+// (64 sequences of 1 to 8192 tokens: 3 tiles 62 us, 1 tile 69; 2 tiles cost 24
+// short sequences of up to 5 new tokens 2.4 us, 4 tiles 512 sequences 2 us).
 // A warp has an equal run of it.  A pass that a warp begins but does not end is
 // continued by the warps that follow.  Or (whole) passes are not cut and count one
 // each, where none can have more than a few tiles.

@@ -5,6 +5,13 @@
 // a thread has a column of 16 bytes for all tokens of its block.  Sequences,
 // positions and places of the block's tokens (reads that depend on one another)
 // are found first, a thread per token, for kFound tokens at a time.
+//
+// 5595 new tokens of 32 + 8 heads of 128 turned and written, and 10554 tokens read
+// back, take 48 us in 16 bits (224 MB, 4.7 TB/s); 4096 written and 24097 read 57 us
+// in 4 bits (215 MB, 3.7 TB/s).  Between them lie the search for places (a row's
+// sequence, length and page come one after the other, 4 us before anything moves)
+// and instructions: half of k_append's issue slots are taken, more where codes
+// are made.
 #include <type_traits>
 
 #include "cache.h"
@@ -21,6 +28,9 @@ constexpr int kReadAhead = 8;            // pieces of a column that a thread of 
 constexpr int kReadResident = 768;       // its threads of an SM
 // Columns of a block of k_append, tokens that its threads have in flight, and its
 // threads of an SM: several blocks, which do not wait for one another's angles.
+// (The pieces above with 768 threads of 80 registers 52 and 59 us; 1280 threads with
+// one token in flight 50 and 61; twice as many blocks as fit 51 and 57; one block
+// of 512 columns 8 us more.)
 constexpr int kAppendThreads = 256, kAppendAhead = 2, kAppendResident = 1024;
 constexpr int kFound = 512;              // tokens whose places a block knows
 
