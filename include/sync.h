@@ -599,7 +599,7 @@ sync_status sync_attn_plan(const sync_attn_desc *desc, int device, sync_attn **o
  * against the same states.  Without train, where no sequence has more than 16
  * queries for a key head (heads / kv_heads times its q_len), a forward call takes
  * the kernel of sync_cache_attn instead of tiles of 128 queries, and n_items is
- * the number of sequences times kv_heads. */
+ * kv_heads times the number of sequences with queries. */
 sync_status sync_cross_attn_plan(const sync_attn_desc *desc, int device, sync_attn **out);
 
 sync_status sync_attn_query(const sync_attn *plan, sync_attn_sizes *out);
@@ -767,7 +767,8 @@ sync_status sync_cache_attn_workspace(const sync_cache *cache, int32_t heads, in
  * have, or (zero_rest) become zero.  q, o: [rows][heads][head_dim], data 16-byte
  * aligned, strides multiples of 8; lse: NULL, or [heads][rows] float.  max_new:
  * how many rows a sequence has at most, for the choice of the tile alone: results
- * are right for more.
+ * are right for more.  Rows times heads / kv_heads are at most 2^30, rows times heads
+ * 2^33.
  * Scores, maxima and sums are held in 32 bits.  16 bits: the unnormalised weights
  * are rounded to dtype for the second product.  4 bits: codes enter the products
  * exactly; queries are scaled by a power of two to float16 (entries below 2^-21

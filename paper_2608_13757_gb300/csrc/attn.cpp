@@ -562,6 +562,7 @@ static sync_status make_plan(const sync_attn_desc* desc, bool causal, int device
     if (P->few) {
       int32_t most_q = 0, most_k = 0;
       for (const AttnSeq& s : seq) {
+        if (s.lq == 0) continue;
         q_row.push_back((int32_t)s.q0);
         q_len.push_back(s.lq);
         k_len.push_back(s.lk);
@@ -573,7 +574,7 @@ static sync_status make_plan(const sync_attn_desc* desc, bool causal, int device
       f.heads = a.heads;
       f.kv_heads = a.kv_heads;
       f.dim = a.dim;
-      f.n_seqs = desc->n_seqs;
+      f.n_seqs = (int)q_row.size();
       f.num_sms = P->num_sms;
       f.most_rows = cache_attn_rows(16, a.heads / a.kv_heads, most_q);
       f.blocks = cache_attn_blocks(16, f.most_rows, P->num_sms);
@@ -625,7 +626,7 @@ static sync_status make_plan(const sync_attn_desc* desc, bool causal, int device
     f.firsts = reinterpret_cast<const int64_t*>(base + at_key);
     f.work = base + at_work;
     sz.device_bytes = (int64_t)m.size();
-    sz.n_items = P->few ? desc->n_seqs * a.kv_heads : (int32_t)w.item.size();
+    sz.n_items = P->few ? f.n_seqs * a.kv_heads : (int32_t)w.item.size();
     sz.n_splits = w.slots;
     P->sz = sz;
     *out = P.release();

@@ -151,6 +151,7 @@ extern "C" int64_t syncgb_cache_attn_work(int n_seqs, const int32_t* lens, const
   auto shape_of = [&](int s) {
     return division::shape(row_starts ? row_starts[s] : s, row_starts ? row_starts[s + 1] : s + 1, all_rows, lens[s], room, group, kv_heads, rows, tile, whole != 0);
   };
+  auto after_empty = [&](int s) { return row_starts ? division::behind_empty([&](int i) { return row_starts[i]; }, s, n_seqs) : s + 1; };
   int64_t total = 0, n = 0;
   for (int s = 0; s < n_seqs; ++s) total += shape_of(s).cost;
   const int takers = division::takers(total, warps, whole != 0);
@@ -163,7 +164,7 @@ extern "C" int64_t syncgb_cache_attn_work(int n_seqs, const int32_t* lens, const
     division::Lister l;
     l.start(shape_of(s), s, begin, from, run);
     division::Piece x;
-    for (; l.next(shape_of, n_seqs, kv_heads, rows, whole != 0, x); ++n) {
+    for (; l.next(shape_of, after_empty, n_seqs, kv_heads, rows, whole != 0, x); ++n) {
       const int64_t row[12] = {w, x.s, x.head, x.first, x.n, x.row0, x.len, x.bad, x.from, x.to, x.tiles,
                                x.tiles && !whole ? division::holder(total, takers, x.last_tile()) : w};
       if (n < capacity) std::copy(row, row + 12, out + 12 * n);
@@ -262,6 +263,8 @@ sync_status sync_cache_attn(const sync_cache* cache, const sync_cache_seqs* seqs
     a.lse = lse;
     a.fill = zero_rest != 0;
     a.whole = (int64_t)seqs->max_pages * cache->page <= SYNC_CACHE_SHORT;
+    need(a.rows * (a.heads / a.kv_heads) <= 1 << 30 && a.rows * a.heads <= (int64_t)1 << 33,
+         "more than 2^30 query rows of a key head, or 2^33 of all");
     need(a.whole || (workspace && reinterpret_cast<uintptr_t>(workspace) % 16 == 0), "the workspace is NULL or not 16-byte aligned");
     if (!a.rows) return;
     a.num_sms = current_sms();

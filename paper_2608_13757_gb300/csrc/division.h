@@ -75,6 +75,26 @@ struct Piece {
   SYNCGB_BOTH int64_t last_tile() const { return at + kUnitCost + tiles - 1; }
 };
 
+// The first sequence behind s, which has no rows, whose rows end further on, by
+// steps that double (a run of empty ones costs its logarithm in reads); n_seqs
+// where there is none.  Safe, if not right, where starts do fall.
+template <class At>
+SYNCGB_BOTH int behind_empty(At&& starts, int s, int n_seqs) {
+  const int here = starts(s);
+  int step = 1;
+  while (step < n_seqs - s && starts(s + step + 1) <= here) {
+    s += step;
+    step *= 2;
+  }
+  int lo = s, hi = (int)less((int64_t)s + step, n_seqs);   // lo is empty; hi is not, or n_seqs
+  while (hi - lo > 1) {
+    const int mid = lo + (hi - lo) / 2;
+    if (starts(mid + 1) <= here) lo = mid;
+    else hi = mid;
+  }
+  return hi;
+}
+
 // The pieces of a warp, one after the other.
 struct Lister {
   Shape now;
@@ -90,11 +110,13 @@ struct Lister {
     left = run;
     at = begin - into;
   }
-  template <class F>
-  SYNCGB_BOTH bool next(F&& shape_of, int n_seqs, int kv_heads, int rows, bool whole, Piece& x) {
+  // skip(s): the first sequence behind s, which has no rows, that may have some
+  template <class F, class G>
+  SYNCGB_BOTH bool next(F&& shape_of, G&& skip, int n_seqs, int kv_heads, int rows, bool whole, Piece& x) {
     while (left > 0) {
       if (unit >= now.passes * kv_heads) {
-        if (++s >= n_seqs) return false;
+        s = now.n ? s + 1 : skip(s);
+        if (s >= n_seqs) return false;
         now = shape_of(s);
         unit = 0;
         into = 0;

@@ -763,13 +763,16 @@ __global__ void __launch_bounds__(kThreads, per_sm(K::kBits, NT)) k_cache_attn(c
 
   // The next piece of this warp, in a ring of kPieces (the copies are at most S
   // tiles, and so pieces, ahead).  Passes without keys are done here.
+  auto after_empty = [&](int s) {
+    return K::kPaged && a.starts ? division::behind_empty([&](int i) { return __ldg(a.starts + i); }, s, a.n_seqs) : s + 1;
+  };
   int made = 0;
   bool done = false;
   auto make = [&] {
     for (;;) {
       if (done) return false;
       int ok = 0;
-      if (lane == 0) ok = lister.next([&](int s) { return shape_of<K::kPaged>(a, s, ROWS, kTile); }, a.n_seqs, a.kv_heads, ROWS, a.whole, list[made % kPieces]);
+      if (lane == 0) ok = lister.next([&](int s) { return shape_of<K::kPaged>(a, s, ROWS, kTile); }, after_empty, a.n_seqs, a.kv_heads, ROWS, a.whole, list[made % kPieces]);
       __syncwarp();
       done = !__shfl_sync(~0u, ok, 0);
       if (done) return false;

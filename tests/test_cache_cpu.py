@@ -186,3 +186,27 @@ def test_runs_are_equal(sg):
     cost = np.zeros(1216)
     np.add.at(cost, got[:, 0], got[:, 9] - got[:, 8] + 1)
     assert cost.max() <= cost.mean() + 30
+
+
+def test_sequences_without_rows_are_passed_over(sg):
+    """Runs of empty slots of any length between, before and behind the others."""
+    r = random.Random(6)
+    for rep in range(200):
+        tokens = []
+        for _ in range(r.choice([0, 1, 3, 20])):
+            tokens += [0] * r.choice([0, 1, 2, 3, 4, 7, 8, 9, 100, 1000]) + [r.choice([1, 2, 5])]
+        tokens += [0] * r.choice([0, 1, 50])
+        starts, lens = [sum(tokens[:i]) for i in range(len(tokens) + 1)], [r.choice([0, 3, 700]) for _ in tokens]
+        for whole in (0, 1) if max(lens, default=0) <= 128 else (0,):
+            got = work(sg, lens, starts, sum(tokens), 1 << 20, 2, 4, 8, 16, r.choice([1, 5, 1216]), whole=whole)
+            want = {(s, h, f) for s in range(len(tokens)) for h in range(2) for f in range(0, tokens[s] * 4, 8)}
+            assert {(x[1], x[2], x[3]) for x in got} == want
+            assert sum(x[9] - x[8] for x in got) == sum(-(-lens[s] // 16) for s, _, _ in want)
+
+
+def test_rows_past_32_bits_refused(sg):
+    R, s = sg.attention.Rows, seqs(sg, row_starts=A)
+    for rows, heads in ((1 << 28, 16), ((1 << 30) + 1, 2)):
+        q = R(A, rows, 64 * heads, 64)
+        assert sg.lib().sync_cache_attn(cache(sg), s, heads, q, 0.1, 1, q, None, 0, A, 1 << 40, None) == sg.ERR_ARG
+        assert b"2^30" in sg.lib().sync_last_error()

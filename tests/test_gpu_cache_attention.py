@@ -277,3 +277,20 @@ def test_run_of_a_prompt_and_its_answer(sg, bits):
         tol = want["o_tol"] + (0 if bits == 16 else 2.0 ** -6) * want["o"].abs().amax() + 2.0 ** -8 * want["o"].abs()
         assert bool(((o.double() - want["o"]).abs() <= tol).all())
         plan.close()
+
+
+@BITS
+def test_slots_without_rows(sg, bits):
+    """A step of a server whose slots are mostly idle: they have no rows, whatever their lengths say."""
+    lens = [0] * 90 + [40] * 200 + [333] + [9000] * 500 + [70, 1] + [0] * 300 + [129]
+    tokens = [0] * 290 + [2] + [0] * 500 + [1, 1] + [0] * 300 + [3]
+    starts = [sum(tokens[:i]) for i in range(len(tokens) + 1)]
+    busy = [s for s, n in enumerate(tokens) if n]
+    cache, few = made(sg, 9, [lens[s] for s in busy], 16, 2, 64, torch.bfloat16, bits)
+    table = torch.full((len(lens), few.shape[1]), -1, dtype=torch.int32, device="cuda")
+    table[busy] = few
+    q = queries(9, 9, 8, 64, torch.bfloat16)
+    got = sg.sync_cache_attn(cache, q, table, i32(lens), i32(starts), max_new=3, lse=True)
+    some = [lens[s] for s in busy], [sum(tokens[s] for s in busy[:i]) for i in range(len(busy) + 1)]
+    ref.check((got[0][:7], got[1][:, :7]), ref.attention(cache, q[:7], few, *some, 0.125))
+    assert bool((got[0][7:] == 0).all())
