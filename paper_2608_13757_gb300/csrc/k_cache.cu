@@ -7,8 +7,8 @@
 // are found first, a thread per token, for kFound tokens at a time.
 //
 // 5595 new tokens of 32 + 8 heads of 128 turned and written, and 10554 tokens read
-// back, take 48 us in 16 bits (224 MB, 4.7 TB/s); 4096 written and 24097 read 57 us
-// in 4 bits (215 MB, 3.7 TB/s).  Between them lie the search for places (a row's
+// back, take 48 us in 16 bits (224 MB, 4.7 TB/s); 4096 written and 24097 read 53 us
+// in 4 bits (215 MB, 4.0 TB/s).  Between them lie the search for places (a row's
 // sequence, length and page come one after the other, 4 us before anything moves)
 // and instructions: half of k_append's issue slots are taken, more where codes
 // are made.
@@ -24,7 +24,7 @@ namespace {
 
 using namespace rotate;
 
-constexpr int kReadAhead = 8;            // pieces of a column that a thread of k_read has in flight
+constexpr int kReadAhead = 8;            // tokens that a thread of k_read has in flight in 16 bits; half as many in 4
 constexpr int kReadResident = 768;       // its threads of an SM
 // Columns of a block of k_append, tokens that its threads have in flight, and its
 // threads of an SM: several blocks, which do not wait for one another's angles.
@@ -331,12 +331,60 @@ __global__ void __launch_bounds__(kAppendThreads, kAppendResident / kAppendThrea
   }
 }
 
+// What a thread of k_read has of a cached token: 8 entries in 16 bits (G 0), or in
+// 4 bits a quarter of a row of G groups, 8 entries of every group (one group's 8
+// entries a thread, with twice as many tokens: 4 us more for 24097 tokens).
+template <class T, int G>
+struct Cached {
+  static constexpr int kAhead = kReadAhead / (G ? 2 : 1), kPieces = G ? G : 1;
+  alignas(16) uint32_t w[G ? G : 4];
+  alignas(8) uint32_t scale[G ? (G + 1) / 2 : 1];
+  __device__ __forceinline__ void read(const uint8_t* row, const uint8_t* scales) {
+    if constexpr (G == 3) {                                 // 12 bytes are aligned to 4, and 6 to 2
+#pragma unroll
+      for (int i = 0; i < 3; ++i) w[i] = __ldg(reinterpret_cast<const uint32_t*>(row) + i);
+      const uint16_t* h = reinterpret_cast<const uint16_t*>(scales);
+      scale[0] = __ldg(h) | (uint32_t)__ldg(h + 1) << 16;
+      scale[1] = __ldg(h + 2);
+    } else {
+      constexpr int N = G ? G : 4;
+      *reinterpret_cast<Pack<uint32_t, N>*>(w) = *reinterpret_cast<const Pack<uint32_t, N>*>(row);
+      if constexpr (G == 1) scale[0] = __ldg(reinterpret_cast<const uint16_t*>(scales));
+      else if constexpr (G != 0) *reinterpret_cast<Pack<uint32_t, G / 2>*>(scale) = *reinterpret_cast<const Pack<uint32_t, G / 2>*>(scales);
+    }
+  }
+  // piece i of the row at `to`
+  __device__ __forceinline__ void write(T* to, int i) const {
+    Pack<uint32_t, 4> z;
+    if constexpr (G == 0) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) z.x[e] = w[e];
+    } else {
+      const float by = __half2float(__ushort_as_half((uint16_t)(scale[i / 2] >> (16 * (i % 2)))));
+      float y[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {                         // 2^23 + code, as bits, less 2^23 + 8
+        y[e] = (__uint_as_float((w[i] >> (4 * e) & 15) | 0x4b000000u) - 8388616.f) * by;
+        // 7 scales may be past float16's end where the row's largest entry was not: the scale was rounded
+        if (std::is_same<T, __half>::value) y[e] = y[e] > 65504.f ? 65504.f : y[e] < -65504.f ? -65504.f : y[e];
+      }
+#pragma unroll
+      for (int e = 0; e < 4; ++e) z.x[e] = pack<T>(y[2 * e], y[2 * e + 1]);
+    }
+    *reinterpret_cast<Pack<uint32_t, 4>*>(to + kGroup * i) = z;
+  }
+  static __device__ __forceinline__ void fill(T* to, uint32_t with) {
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i) *reinterpret_cast<uint4*>(to + kGroup * i) = make_uint4(with, with, with, with);
+  }
+};
+
 // Cached tokens back to rows of 16 bits: the tokens of sequence s from its first
 // one on go to rows starts[s] .. starts[s + 1]; zeros past its length.
-template <class T, int BITS>
+template <class T, int G>
 __global__ void __launch_bounds__(kReadResident, 1) k_read(const __grid_constant__ CacheArgs a, const __grid_constant__ Columns c) {
   __shared__ int64_t places[kFound];                        // as in Where; -1: no such token, -2: no sequence's row, -3: no such page
-  const int tokens = c.tokens(), runs = a.dim / 8, g = a.dim / kGroup;
+  const int tokens = c.tokens(), runs = G ? 4 : a.dim / 8;
   const int sub = threadIdx.x / c.each, column = blockIdx.y * c.each + threadIdx.x % c.each;
   const bool on = sub < c.par && column < 2 * a.kv_heads * runs;
   const int at = column / runs, run = column - at * runs;
@@ -346,9 +394,9 @@ __global__ void __launch_bounds__(kReadResident, 1) k_read(const __grid_constant
   T* const to = static_cast<T*>(out.data) + head * out.head + 8 * run;
   const int64_t out_row = out.row, out_step = out_row * c.par, head_rows = (int64_t)head << a.page_shift;
   // this column's piece of the cache's rows
-  const int row_bytes = BITS == 16 ? 2 * a.dim : a.dim / 2;
-  const uint8_t* const data = (is_v ? a.v : a.k) + head_rows * row_bytes + (BITS == 16 ? 16 * run : 4 * paged::word_of(run, g));
-  const uint8_t* const scales = BITS == 16 ? nullptr : (is_v ? a.v_scale : a.k_scale) + (head_rows * g + run / 4) * 2;
+  const int row_bytes = G ? G * 16 : 2 * a.dim;
+  const uint8_t* const data = (is_v ? a.v : a.k) + head_rows * row_bytes + (G ? 4 * G : 16) * run;
+  const uint8_t* const scales = G ? (is_v ? a.v_scale : a.k_scale) + head_rows * G * 2 : nullptr;
 
   int64_t group = blockIdx.x;
   while (group < c.groups) {
@@ -373,42 +421,25 @@ __global__ void __launch_bounds__(kReadResident, 1) k_read(const __grid_constant
       const int64_t row = group * tokens + sub, left = a.rows - row;
       const int mine = !on ? 0 : left >= tokens ? c.ahead : left > 0 ? ((int)left + c.par - 1) / c.par : 0;
       const int64_t* const place = places + n * tokens + sub;
-      Pack<uint32_t, 4> x[kReadAhead];                      // 16 bits: the entries; 4: a word of codes and its scale
+      using Token = Cached<T, G>;
+      Token x[Token::kAhead];
 #pragma unroll
-      for (int e = 0; e < kReadAhead; ++e) {
+      for (int e = 0; e < Token::kAhead; ++e) {
         if (e >= mine) break;
         const int64_t p = place[e * c.par];
-        if (p < 0) continue;
-        if (BITS == 16) {
-          x[e] = *reinterpret_cast<const Pack<uint32_t, 4>*>(data + p * row_bytes);
-        } else {
-          x[e].x[0] = __ldg(reinterpret_cast<const uint32_t*>(data + p * row_bytes));
-          x[e].x[1] = __ldg(reinterpret_cast<const uint16_t*>(scales + p * (2 * g)));
-        }
+        if (p >= 0) x[e].read(data + p * row_bytes, scales + p * (2 * G));
       }
       T* o = to + row * out_row;
 #pragma unroll
-      for (int e = 0; e < kReadAhead; ++e, o += out_step) {
+      for (int e = 0; e < Token::kAhead; ++e, o += out_step) {
         if (e >= mine) break;
         const int64_t p = place[e * c.par];
-        if (p < 0) {
-          if (p == -2 && !a.fill) continue;
+        if (p >= 0) {
 #pragma unroll
-          for (int i = 0; i < 4; ++i) x[e].x[i] = p == -3 ? 0x7fff7fffu : 0u;   // NaN in both types
-        } else if (BITS == 4) {
-          const uint32_t word = x[e].x[0];
-          const float scale = __half2float(__ushort_as_half((uint16_t)x[e].x[1]));
-          float y[8];
-#pragma unroll
-          for (int i = 0; i < 8; ++i) {                     // 2^23 + code, as bits, less 2^23 + 8
-            y[i] = (__uint_as_float((word >> (4 * i) & 15) | 0x4b000000u) - 8388616.f) * scale;
-            // 7 scales may be past float16's end where the row's largest entry was not: the scale was rounded
-            if (std::is_same<T, __half>::value) y[i] = y[i] > 65504.f ? 65504.f : y[i] < -65504.f ? -65504.f : y[i];
-          }
-#pragma unroll
-          for (int i = 0; i < 4; ++i) x[e].x[i] = pack<T>(y[2 * i], y[2 * i + 1]);
+          for (int i = 0; i < Token::kPieces; ++i) x[e].write(o, i);
+        } else if (p != -2 || a.fill) {
+          Token::fill(o, p == -3 ? 0x7fff7fffu : 0u);        // NaN in both types
         }
-        *reinterpret_cast<Pack<uint32_t, 4>*>(o) = x[e];
       }
     }
     __syncthreads();
@@ -454,11 +485,23 @@ cudaError_t launch_cache_append(const CacheArgs& a, cudaStream_t st) {
 
 cudaError_t launch_cache_read(const CacheArgs& a, cudaStream_t st) {
   if (!a.rows) return cudaSuccess;
-  const Columns c = columns_of(a.rows, 2 * a.kv_heads * (a.dim / 8), kReadAhead, 0, a.num_sms, kMostThreads, kReadResident);
-  const dim3 grid((unsigned)c.blocks_x, (unsigned)c.blocks_y);
-  if (a.bits == 16) k_read<__nv_bfloat16, 16><<<grid, c.threads, 0, st>>>(a, c);   // (whichever type: the bits are copied)
-  else if (a.bf16) k_read<__nv_bfloat16, 4><<<grid, c.threads, 0, st>>>(a, c);
-  else k_read<__half, 4><<<grid, c.threads, 0, st>>>(a, c);
+  auto go = [&](auto type, auto groups) {
+    using Token = Cached<decltype(type), decltype(groups)::value>;
+    const int columns = 2 * a.kv_heads * (a.bits == 4 ? 4 : a.dim / 8);
+    const Columns c = columns_of(a.rows, columns, Token::kAhead, 0, a.num_sms, kMostThreads, kReadResident);
+    k_read<decltype(type), decltype(groups)::value><<<dim3((unsigned)c.blocks_x, (unsigned)c.blocks_y), c.threads, 0, st>>>(a, c);
+  };
+  auto narrow = [&](auto type) {
+    switch (a.dim / kGroup) {
+      case 1: return go(type, std::integral_constant<int, 1>());
+      case 2: return go(type, std::integral_constant<int, 2>());
+      case 3: return go(type, std::integral_constant<int, 3>());
+      default: return go(type, std::integral_constant<int, 4>());
+    }
+  };
+  if (a.bits == 16) go(__nv_bfloat16(), std::integral_constant<int, 0>());   // (whichever type: the bits are copied)
+  else if (a.bf16) narrow(__nv_bfloat16());
+  else narrow(__half());
   const cudaError_t e = cudaGetLastError();
   if (e == cudaSuccess) count_launch();
   return e;
