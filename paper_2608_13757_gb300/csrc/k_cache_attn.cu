@@ -599,6 +599,12 @@ __device__ __forceinline__ Shape shape_of(const CacheArgs& a, int s, int rows, i
   return division::shape(begin, end, a.rows, __ldg(a.lens + s), PAGED ? a.max_pages << a.page_shift : INT32_MAX, a.heads / a.kv_heads, a.kv_heads, rows, tile, a.whole);
 }
 
+// (A call of its own: in line it takes the calls that never need it half a
+// microsecond of ten.)
+__device__ __noinline__ int behind_empty(const int32_t* starts, int s, int n_seqs) {
+  return division::behind_empty([&](int i) { return __ldg(starts + i); }, s, n_seqs);
+}
+
 // The runs of a block's warps: their bounds in the list, and the sequences where
 // they begin with how far into them.
 struct Runs {
@@ -764,7 +770,7 @@ __global__ void __launch_bounds__(kThreads, per_sm(K::kBits, NT)) k_cache_attn(c
   // The next piece of this warp, in a ring of kPieces (the copies are at most S
   // tiles, and so pieces, ahead).  Passes without keys are done here.
   auto after_empty = [&](int s) {
-    return K::kPaged && a.starts ? division::behind_empty([&](int i) { return __ldg(a.starts + i); }, s, a.n_seqs) : s + 1;
+    return K::kPaged && a.starts ? behind_empty(a.starts, s, a.n_seqs) : s + 1;
   };
   int made = 0;
   bool done = false;
