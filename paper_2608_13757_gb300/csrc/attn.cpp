@@ -193,7 +193,7 @@ bool packs(const AttnSeq& s, int group) {
 
 // Plans of queries that see all keys go to the kernel of few queries (k_cache_attn.cu)
 // where a key head's queries fit in 16 of its columns: it reads what there is and
-// no more (48 sequences of one query and up to 1500 keys, 20 heads of 64: 56 us,
+// no more (48 sequences of one query and up to 1500 keys, 20 heads of 64: 52 us,
 // where tiles of 128 queries take 71).
 constexpr int64_t kFewRows = 16;
 bool few_queries(const sync_attn_desc* d, bool causal, const std::vector<AttnSeq>& seq) {

@@ -7,8 +7,8 @@
 // are found first, a thread per token, for kFound tokens at a time.
 //
 // 5595 new tokens of 32 + 8 heads of 128 turned and written, and 10554 tokens read
-// back, take 48 us in 16 bits (224 MB, 4.7 TB/s); 4096 written and 24097 read 53 us
-// in 4 bits (215 MB, 4.0 TB/s).  Between them lie the search for places (a row's
+// back, take 46 us in 16 bits (224 MB, 4.8 TB/s); 4096 written and 24097 read 50 us
+// in 4 bits (215 MB, 4.3 TB/s).  Between them lie the search for places (a row's
 // sequence, length and page come one after the other, 4 us before anything moves)
 // and instructions: half of k_append's issue slots are taken, more where codes
 // are made.
@@ -28,11 +28,14 @@ constexpr int kReadAhead = 8;            // tokens that a thread of k_read has i
 constexpr int kReadResident = 768;       // its threads of an SM
 // Columns of a block of k_append, tokens that its threads have in flight, and its
 // threads of an SM: several blocks, which do not wait for one another's angles.
-// (The pieces above with 768 threads of 80 registers 52 and 59 us; 1280 threads with
-// one token in flight 50 and 61; twice as many blocks as fit 51 and 57; one block
-// of 512 columns 8 us more.)
+// (The pieces above with 768 threads and four tokens in flight 52 and 56 us; 1280
+// threads of 48 registers 47 and 53; one block of 512 columns 8 us more.)
 constexpr int kAppendThreads = 256, kAppendAhead = 2, kAppendResident = 1024;
 constexpr int kFound = 512;              // tokens whose places a block knows
+// Angles that a block of k_append stages at a time, of at least one group: of many
+// groups, as a barrier for each and angles held in registers from one to the next
+// cost more (48 and 53 us) than waiting for them now and then.
+constexpr int kAngles = 2048;
 
 // 8 entries of a row, by one access or entry by entry
 template <class T>
@@ -260,30 +263,19 @@ __device__ __forceinline__ void through(const CacheArgs& a, const Columns& c, fl
       where[i] = w;
     }
   };
-  int t[kStaged], j[kStaged];                                 // staged entries of this thread: pair j of token t
-  float2 turned[kStaged];
-#pragma unroll
-  for (int e = 0; e < kStaged; ++e) {
-    const int i = threadIdx.x + e * blockDim.x;
-    t[e] = i < tokens * half ? i / half : -1;
-    j[e] = i - t[e] * half;
-  }
-  auto find = [&](int64_t group, int at) {                  // angles of a group, whose tokens are at `at` of where
-#pragma unroll
-    for (int e = 0; e < kStaged; ++e) {
-      if (t[e] < 0) continue;
-      const Where& w = where[at + t[e]];
-      if (w.mine) turned[e] = angle(a.turn, position(a.turn, group * tokens + t[e], w.pos, j[e]), j[e]);
+  // angles of the groups from `group` on whose tokens are [at, end) of where
+  auto stage = [&](int64_t group, int at, int end) {
+    const int some = (end - at) * half;
+#pragma unroll 2
+    for (int i = threadIdx.x; i < some; i += blockDim.x) {
+      const int t = i / half, j = i - t * half;
+      const Where& w = where[at + t];
+      if (!w.mine) continue;
+      const int64_t row = (group + (int64_t)(t / tokens) * gridDim.x) * tokens + t % tokens;
+      const float2 x = angle(a.turn, position(a.turn, row, w.pos, j), j);
+      angles[2 * t * half + j] = x.x;
+      angles[(2 * t + 1) * half + j] = x.y;
     }
-  };
-  auto put = [&](int which) {
-#pragma unroll
-    for (int e = 0; e < kStaged; ++e)
-      if (t[e] >= 0) {
-        float* to = angles + ((which * tokens + t[e]) * 2) * half + j[e];
-        to[0] = turned[e].x;
-        to[half] = turned[e].y;
-      }
   };
   int64_t group = blockIdx.x;
   read(group);
@@ -291,21 +283,23 @@ __device__ __forceinline__ void through(const CacheArgs& a, const Columns& c, fl
     const int known = known_groups(c, group);
     search(group, known);
     __syncthreads();
-    find(group, 0);
-    put(0);
-    __syncthreads();
 #pragma unroll 1
-    for (int n = 0; n < known; ++n, group += gridDim.x) {
-      const bool more = n + 1 < known;
-      if (more) find(group + gridDim.x, (n + 1) * tokens);
+    for (int first = 0; first < known; first += c.batch) {
+      const int last = min(first + c.batch, known);
+      stage(group, first * tokens, last * tokens);
+      __syncthreads();
+      const float* cs = angles + sub * 2 * half;
+#pragma unroll 1
+      for (int n = first; n < last; ++n, cs += tokens * 2 * half) {
 #pragma unroll
-      for (int e = 0; e < kAhead; ++e) {
-        const int token = sub + e * c.par;
-        const int64_t row = group * tokens + token;
-        if (here(row, e)) item.write(e, row, where[n * tokens + token], angles + ((n % 2 * tokens + token) * 2) * half);
+        for (int e = 0; e < kAhead; ++e) {
+          const int token = sub + e * c.par;
+          const int64_t row = group * tokens + token;
+          if (here(row, e)) item.write(e, row, where[n * tokens + token], cs + e * c.par * 2 * half);
+        }
+        group += gridDim.x;
+        if (group < c.groups) read(group);
       }
-      if (group + gridDim.x < c.groups) read(group + gridDim.x);
-      if (more) put((n + 1) % 2);
       __syncthreads();
     }
   }
@@ -316,7 +310,7 @@ __device__ __forceinline__ void through(const CacheArgs& a, const Columns& c, fl
 // a thread takes at a time.
 template <class T, int QVEC, int BITS, bool INTER>
 __global__ void __launch_bounds__(kAppendThreads, kAppendResident / kAppendThreads) k_append(const __grid_constant__ CacheArgs a, const __grid_constant__ Columns c, int kv_blocks, bool kv_wide) {
-  extern __shared__ __align__(16) float angles[];           // [2][tokens][cos, sin][half]
+  extern __shared__ __align__(16) float angles[];           // [batch][tokens][cos, sin][half]
   __shared__ Where where[kFound];
   const bool on = (int)threadIdx.x / c.each < c.par;
   const int column = threadIdx.x % c.each;
@@ -454,7 +448,8 @@ cudaError_t append(const CacheArgs& a, bool kv_wide, cudaStream_t st) {
   c.blocks_y = kv_blocks + (q + c.each - 1) / c.each;
   c.blocks_x = std::max(1, std::min(c.blocks_x, a.num_sms * std::max(1, kAppendResident / c.threads) / c.blocks_y));
   const dim3 grid((unsigned)c.blocks_x, (unsigned)c.blocks_y);
-  const size_t smem = (size_t)4 * c.tokens() * a.turn.half * sizeof(float);
+  c.batch = std::max(1, std::min(kFound, a.turn.half ? kAngles / a.turn.half : kFound) / c.tokens());
+  const size_t smem = (size_t)2 * c.batch * c.tokens() * a.turn.half * sizeof(float);
   if (a.turn.interleaved) k_append<T, QVEC, BITS, true><<<grid, c.threads, smem, st>>>(a, c, kv_blocks, kv_wide);
   else k_append<T, QVEC, BITS, false><<<grid, c.threads, smem, st>>>(a, c, kv_blocks, kv_wide);
   const cudaError_t e = cudaGetLastError();

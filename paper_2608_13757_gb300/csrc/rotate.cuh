@@ -5,8 +5,8 @@
 // its block takes: `par` tokens side by side where a token has few columns, and
 // `ahead` of them one after the other, whose reads are in flight together.  The
 // angles of a group of tokens are staged in shared memory, pair by pair from the
-// table rows of the pair's axis; blocks stay, and a group's angles and positions
-// are read while the one before it is turned.
+// table rows of the pair's axis; blocks stay, and in k_rope a group's angles and
+// positions are read while the one before it is turned.
 //
 // The products and their sum are rounded one by one (no fused multiply-add), so
 // that a rotation has the same 32-bit value wherever it is computed; every use
@@ -31,6 +31,7 @@ constexpr int kMostThreads = 512, kResident = 640, kAhead = 4, kStaged = 2;
 struct Columns {
   int each = 0;          // columns of a block: threads that one token takes
   int par = 1, ahead = 1, threads = 0;
+  int batch = 1;         // groups whose angles are staged at a time (k_append)
   int blocks_x = 0, blocks_y = 0;
   int64_t groups = 0;
   __host__ __device__ int tokens() const { return par * ahead; }
@@ -137,8 +138,8 @@ struct Pairs {
     }
   }
   // by the angles of its pairs, which lie at multiples of VEC (widest() below).  WIDE:
-  // read four at a time, which saves k_append instructions (4 us of 36 for 5595
-  // tokens); k_rope, which waits for memory, takes them one by one (gradient of
+  // read four at a time, which saves k_append instructions (with divisions of 64 bits left out, 4 us of 36 for
+  // 5595 tokens); k_rope, which waits for memory, takes them one by one (gradient of
   // 8192 tokens of 32 heads of 80: 17.3 us, 19.5 by fours).
   template <bool WIDE>
   __device__ __forceinline__ void by(const float* cosines, const float* sines) {
