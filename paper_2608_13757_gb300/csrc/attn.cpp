@@ -192,15 +192,21 @@ bool packs(const AttnSeq& s, int group) {
 }
 
 // Plans of queries that see all keys go to the kernel of few queries (k_cache_attn.cu)
-// where a key head's queries fit in 16 of its columns: it reads what there is and
-// no more (48 sequences of one query and up to 1500 keys, 20 heads of 64: 52 us,
-// where tiles of 128 queries take 71).
-constexpr int64_t kFewRows = 16;
+// where a key head's queries fit in 16 of its columns, or 8 in heads of more than
+// 64 entries: it reads what there is and no more.  us here and in tiles of 128
+// queries, bf16:
+//                                  48 x 1500 keys   300 x 300    1 x 100000    4 x 100
+//   20 heads of 64, 1 query            37.5 49.3    50.5 121.4    82.1 102.4   6.5 6.3
+//                  16 queries          50.7 54.9    65.9 120.3    86.3 103.4   6.7 6.4
+//   32/8 heads of 128, 1 query         31.1 29.7    41.9  63.1    67.1  71.3   7.7 6.5
+//                  2 queries           33.9 31.1    47.5  64.6    68.3  73.7   7.3 6.5
+//                  4 (not taken)       38.4 28.2    55.8  64.1    71.5  73.8   8.5 6.7
+int64_t few_rows(int dim) { return dim <= 64 ? 16 : 8; }
 bool few_queries(const sync_attn_desc* d, bool causal, const std::vector<AttnSeq>& seq) {
   if (causal || d->train || seq.empty() || seq.size() > (1u << 20)) return false;
   int64_t most = 0;
   for (const AttnSeq& s : seq) most = std::max<int64_t>(most, s.lq);
-  return most > 0 && most * (d->heads / d->kv_heads) <= kFewRows;
+  return most > 0 && most * (d->heads / d->kv_heads) <= few_rows(d->head_dim);
 }
 
 struct ForwardWork {

@@ -294,3 +294,35 @@ def test_slots_without_rows(sg, bits):
     some = [lens[s] for s in busy], [sum(tokens[s] for s in busy[:i]) for i in range(len(busy) + 1)]
     ref.check((got[0][:7], got[1][:, :7]), ref.attention(cache, q[:7], few, *some, 0.125))
     assert bool((got[0][7:] == 0).all())
+
+
+@BITS
+def test_pages_past_32_bits(sg, bits):
+    """The same tokens on the last pages of a cache of more than 4 GiB a tensor, and in a small one."""
+    page, kv, dim, lens = 1024, 8, 128, [1500, 3, 1025]
+    n = 2100 if bits == 16 else 8300
+    small, table = made(sg, 11, lens, page, kv, dim, torch.bfloat16, bits)
+    large = sg.sync_kv_cache(n, page, kv, dim, torch.bfloat16, bits=bits)
+    assert large.k.numel() * large.k.element_size() > 1 << 32
+    for name in ("k", "v", "k_scale", "v_scale"):
+        t = getattr(small, name)
+        if t is not None:
+            getattr(large, name)[n - small.n_pages:] = t
+    q = queries(11, 3, 32, dim, torch.bfloat16)
+    want = sg.sync_cache_attn(small, q, table, i32(lens), lse=True)
+    got = sg.sync_cache_attn(large, q, torch.where(table < 0, table, table + n - small.n_pages), i32(lens), lse=True)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+@BITS
+def test_two_calls_at_once(sg, bits):
+    """Calls on two streams, each with the workspace that it allocates."""
+    cache, table = made(sg, 12, [5000, 20, 3000], 64, 4, 128, torch.bfloat16, bits)
+    lens, some = i32([5000, 20, 3000]), i32([4000, 0, 2999])
+    q = queries(12, 3, 16, 128, torch.bfloat16)
+    want = sg.sync_cache_attn(cache, q, table, lens), sg.sync_cache_attn(cache, q, table, some)
+    streams = torch.cuda.Stream(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    got = [[sg.sync_cache_attn(cache, q, table, n, stream=s) for s, n in zip(streams, (lens, some))] for _ in range(20)]
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, want[0]) and torch.equal(b, want[1]) for a, b in got)

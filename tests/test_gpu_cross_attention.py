@@ -192,3 +192,34 @@ def test_few_queries_in_strided_rows(sg):
 def test_few_queries_many_and_long(sg):
     run_and_check(sg, [1] * 300, [(i * 53) % 400 for i in range(300)], 4, 4, 64, torch.float16, train=False)
     run_and_check(sg, [1, 2], [40000, 9], 8, 2, 128, torch.bfloat16, train=False)
+
+
+def test_few_queries_past_32_bits(sg):
+    """Keys and values behind the first 2^31 entries of their tensors."""
+    heads, kv, dim, rows, n = 8, 8, 128, (1 << 21) + 500, 400
+    q, k, v, _ = inputs(31, 2, n, heads, kv, dim, torch.bfloat16)
+    plan = sg.sync_attn_plan([2], [n], heads, kv, dim, torch.bfloat16, causal=False)
+    want = sg.sync_attn_forward(plan, q, k, v)
+    far = sg.sync_attn_plan([2], [n], heads, kv, dim, torch.bfloat16, k_starts=[rows - n], causal=False)
+    large = torch.empty((2, rows, kv, dim), dtype=torch.bfloat16, device="cuda")
+    large[0, rows - n:], large[1, rows - n:] = k, v
+    assert torch.equal(sg.sync_attn_forward(far, q, large[0], large[1]), want)
+
+
+def test_few_queries_while_an_encoder_changes(sg):
+    """A captured step reads what the states hold when it is replayed."""
+    q_lens, k_lens, heads, kv, dim = [1, 2, 0, 1], [700, 20, 9, 0], 8, 4, 64
+    q, k, v, _ = inputs(32, 4, 729, heads, kv, dim, torch.float16)
+    plan = sg.sync_attn_plan(q_lens, k_lens, heads, kv, dim, torch.float16, causal=False)
+    out, lse = torch.empty_like(q), torch.empty((heads, 4), device="cuda")
+    sg.sync_attn_forward(plan, q, k, v, out=out, lse=lse)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        sg.sync_attn_forward(plan, q, k, v, out=out, lse=lse)
+    for seed in (33, 34):
+        for t, new in zip((q, k, v), inputs(seed, 4, 729, heads, kv, dim, torch.float16)):
+            t.copy_(new)
+        graph.replay()
+        want = ref.packed(q, k, v, q_lens, k_lens, starts(q_lens), starts(k_lens), dim ** -0.5)
+        ref.check(out, want["o"], want["o_tol"], "o")
+        ref.check(lse, want["lse"], want["lse_tol"], "lse")
