@@ -597,9 +597,9 @@ sync_status sync_attn_plan(const sync_attn_desc *desc, int device, sync_attn **o
  * states) give the same k_start, unless train is set.  The plan serves the same
  * calls; it depends on the lengths alone, so one serves every step of decoding
  * against the same states.  Without train, where no sequence has more than 16
- * queries for a key head (heads / kv_heads times its q_len), a forward call takes
- * the kernel of sync_cache_attn instead of tiles of 128 queries, and n_items is
- * kv_heads times the number of sequences with queries. */
+ * queries for a key head (heads / kv_heads times its q_len; 8 in heads of more than
+ * 64 entries), a forward call takes the kernel of sync_cache_attn instead of tiles of
+ * 128 queries, and n_items is kv_heads times the number of sequences with queries. */
 sync_status sync_cross_attn_plan(const sync_attn_desc *desc, int device, sync_attn **out);
 
 sync_status sync_attn_query(const sync_attn *plan, sync_attn_sizes *out);

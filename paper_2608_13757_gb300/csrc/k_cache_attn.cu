@@ -1214,8 +1214,8 @@ cudaError_t launch_type(const CacheArgs& a, cudaStream_t st) {
 cudaError_t launch_few_queries(const CacheArgs& a, cudaStream_t st) {
   auto go = [&](auto bf16) {
     constexpr bool B = decltype(bf16)::value;
-    if (a.most_rows == 8) return a.dim <= 64 ? launch<Wide<64, 1, B, false>, 1, B>(a, st) : launch<Wide<128, 1, B, false>, 1, B>(a, st);
-    return a.dim <= 64 ? launch<Wide<64, 2, B, false>, 2, B>(a, st) : launch<Wide<128, 2, B, false>, 2, B>(a, st);
+    if (a.most_rows == 16) return launch<Wide<64, 2, B, false>, 2, B>(a, st);   // (heads of up to 64 alone)
+    return a.dim <= 64 ? launch<Wide<64, 1, B, false>, 1, B>(a, st) : launch<Wide<128, 1, B, false>, 1, B>(a, st);
   };
   return a.bf16 ? go(std::true_type()) : go(std::false_type());
 }
