@@ -326,3 +326,17 @@ def test_two_calls_at_once(sg, bits):
     got = [[sg.sync_cache_attn(cache, q, table, n, stream=s) for s, n in zip(streams, (lens, some))] for _ in range(20)]
     torch.cuda.synchronize()
     assert all(torch.equal(a, want[0]) and torch.equal(b, want[1]) for a, b in got)
+
+
+@BITS
+def test_on_a_thread_of_its_own(sg, bits):
+    """A thread that has made no call of the runtime yet."""
+    import threading
+    cache, table = made(sg, 13, [700, 40], 32, 2, 64, torch.float16, bits)
+    q, lens, got = queries(13, 2, 4, 64, torch.float16), i32([700, 40]), []
+    want = sg.sync_cache_attn(cache, q, table, lens, lse=True)
+    t = threading.Thread(target=lambda: got.extend(sg.sync_cache_attn(cache, q, table, lens, lse=True)))
+    t.start()
+    t.join()
+    torch.cuda.synchronize()
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])

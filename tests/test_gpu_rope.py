@@ -197,3 +197,26 @@ def test_refusals(sg):
     x = q.float().requires_grad_()
     with pytest.warns(UserWarning, match="sync_rope records nothing"):
         sg.sync_rope(x, k.float(), cos, sin)
+
+
+def test_in_an_autograd_function(sg):
+    """On the backward pass's thread, with two uses of the same leaf."""
+    class Turn(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, q, k, cos, sin, pos):
+            ctx.save_for_backward(cos, sin, pos)
+            return sg.sync_rope(q, k, cos, sin, pos)
+
+        @staticmethod
+        def backward(ctx, dq, dk):
+            return (*sg.sync_rope_backward(dq.contiguous(), dk.contiguous(), *ctx.saved_tensors), None, None, None)
+
+    g = torch.Generator(device="cuda").manual_seed(4)
+    q, k = (torch.randn(50, h, 64, generator=g, device="cuda").requires_grad_() for h in (4, 2))
+    angle = torch.randn(70, 32, generator=g, device="cuda")
+    pos = torch.randint(0, 70, (50,), generator=g, device="cuda", dtype=torch.int32)
+    weights = [torch.randn(t.shape, generator=g, device="cuda") for t in (q, k)]
+    a, b = Turn.apply(q, k, angle.cos(), angle.sin(), pos)
+    ((a * weights[0]).sum() + (b * weights[1]).sum() + (q * 2).sum()).backward()
+    dq, dk = sg.sync_rope_backward(*weights, angle.cos(), angle.sin(), pos)
+    assert torch.equal(q.grad, dq + 2) and torch.equal(k.grad, dk)
