@@ -773,7 +773,10 @@ sync_status sync_cache_attn_workspace(const sync_cache *cache, int32_t heads, in
  * are rounded to dtype for the second product.  4 bits: codes enter the products
  * exactly; queries are scaled by a power of two to float16 (entries below 2^-21
  * of their head's largest lose bits), weights are rounded to float16 before and
- * after their value's scale.  Scores stay below 2^27 in size.  A NaN or an infinity
+ * after their value's scale, which is taken relative to the largest of its group
+ * so far (one below 2^-14 of that loses bits).  In float16 a weight, or its product
+ * with such a scale, below 2^-25 of the row's largest is rounded to steps of 2^-35 of
+ * it.  Scores stay below 2^27 in size (from 2^22 on these are 2^-14 and 2^-24).  A NaN or an infinity
  * in the value (or in 4 bits its scale) of a token that some of a sequence's rows
  * see may reach its other rows; nothing past lens[s] or of other sequences ever
  * does.  Calls that may run at the same time have a workspace each. */

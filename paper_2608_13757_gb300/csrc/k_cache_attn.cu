@@ -34,8 +34,13 @@
 // four masks and a shift, the factor 16 is in the query (or comes out of the sum at
 // the end), and the 8 is taken off by the sum's start (scores) or by a product
 // with -8 (outputs).  Scales of keys multiply the 32-bit sums of their group;
-// those of values multiply the weights, scaled to float16's range by a power of
-// two that a warp raises when a larger scale comes.
+// those of values multiply the weights in float16, relative to a power of two for
+// each group that a warp raises when a larger scale comes.  (One for the whole head,
+// and weights that were not lifted (kLift), took 77 us instead of 80 for 128 sequences
+// of 1 to 16384 tokens, and lost what many small weights add together: 12 nats below
+// a first token that takes the row, 8192 others in a group of a 128th of the head's
+// largest scale left 13 to 27% of the result wrong; now it is a rounding of the
+// result.  Products in 32 bits, rounded once, took 84 us.)
 #include <algorithm>
 #include <atomic>
 #include <type_traits>
@@ -60,6 +65,12 @@ using umma::unpack2;
 
 constexpr int kWarps = 4, kThreads = 32 * kWarps, kKeys = 16;
 constexpr int kPieces = 8;                 // of a warp's list that are laid out at a time
+// The running maximum follows only rises of more than 2^kLag in the weights, whose
+// largest then stands for 2^kLift .. 2^(kLift + kLag), the upper end of float16, so
+// that smaller ones keep all bits down to 2^-25 of it and are off by 2^-36 of it at
+// most below.  Scores past kSure are not lifted: half a unit in their last place is a
+// factor that takes the room.
+constexpr float kLag = 4.f, kLift = 11.f, kSure = 4194304.f;
 
 // Blocks per SM
 constexpr int per_sm(int bits, int nt) { return bits == 4 && nt == 1 ? 3 : 2; }
@@ -301,8 +312,7 @@ struct Narrow {                            // 4 bits, G groups of 32 entries
   uint32_t q[2 * G][NT][2], start[NT][2];  // start: -8 sum q of each group, as sums of two float16
   float o[2 * G][NT][4], off[NT][4];       // off: row w has -8 sum p s of group w
   float f[NT][2];
-  uint32_t by;                             // 1 / bound twice, in float16
-  float bound;                             // a power of two that no scale so far reaches
+  __half2 by[(G + 1) / 2];                 // 1 / bound of each group: a power of two that none of its scales so far reaches
 
   const uint8_t *k, *v, *scale;            // what the copies of 16 keys start from
   uint32_t to_v, to_scale;
@@ -403,8 +413,8 @@ struct Narrow {                            // 4 bits, G groups of 32 entries
     start[nt][1] = 0;
   }
   __device__ __forceinline__ void clear() {
-    by = 0;
-    bound = 0.f;
+#pragma unroll
+    for (int i = 0; i < (G + 1) / 2; ++i) by[i] = as_half2(0x7c007c00u);   // (infinity)
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -415,6 +425,7 @@ struct Narrow {                            // 4 bits, G groups of 32 entries
       }
   }
   __device__ __forceinline__ float factor(int nt, int j) const { return f[nt][j]; }
+  __device__ __forceinline__ float inverse(int w) const { return w % 2 ? __high2float(by[w / 2]) : __low2float(by[w / 2]); }
   // the scales of keys r and r + 8, as they lie: G halves each
   template <int AT>
   static __device__ __forceinline__ void scales(uint32_t at, uint32_t (*x)[(G + 1) / 2]) {
@@ -476,30 +487,45 @@ struct Narrow {                            // 4 bits, G groups of 32 entries
 #pragma unroll
           for (int i = 0; i < (G + 1) / 2; ++i) sc[t][e][i] = 16 * t + r + 8 * e < keys ? sc[t][e][i] : 0;
     }
-    __half2 most = as_half2(sc[0][0][0]);
+    __half2 most[(G + 1) / 2];
+    bool larger = false;                                     // than any scale of its group so far (or the first tile)
 #pragma unroll
-    for (int t = 0; t < MT; ++t)
+    for (int i = 0; i < (G + 1) / 2; ++i) {
+      most[i] = __hmax2(as_half2(sc[0][0][i]), as_half2(sc[0][1][i]));
 #pragma unroll
-      for (int e = 0; e < 2; ++e)
+      for (int t = 1; t < MT; ++t) most[i] = __hmax2(most[i], __hmax2(as_half2(sc[t][0][i]), as_half2(sc[t][1][i])));
+      larger = larger || __hgeu2_mask(__hmul2(most[i], by[i]), as_half2(0x3c003c00u)) != 0;
+    }
+    if (__any_sync(~0u, larger)) {
+      float mine = 1.f;                                      // of group r, whose row this lane has in `off`
 #pragma unroll
-        for (int i = 0; i < (G + 1) / 2; ++i) most = __hmax2(most, as_half2(sc[t][e][i]));
-    float top = fmaxf(__low2float(most), __high2float(most));
-    if (__any_sync(~0u, top >= bound)) {                     // a larger scale than any so far (or the first tile)
+      for (int i = 0; i < (G + 1) / 2; ++i) {
 #pragma unroll
-      for (int e = 4; e < 32; e *= 2) top = fmaxf(top, __shfl_xor_sync(~0u, top, e));
-      // the power of two above it, from 2^-13 on, so that 1 / bound is a float16
-      const float next = fmaxf(bound, __uint_as_float(max(__float_as_uint(top) >> 23, 127u - 14u) + 1 << 23));
-      const float ratio = bound / next;
-      bound = next;
-      by = pack2<false>(1.f / next, 1.f / next);
+        for (int e = 4; e < 32; e *= 2) most[i] = __hmax2(most[i], as_half2(__shfl_xor_sync(~0u, as_word(most[i]), e)));
+        const float2 top = __half22float2(most[i]), was = __half22float2(by[i]);
+        float now[2] = {1.f, 1.f};
+#pragma unroll
+        for (int h = 0; h < 2 && 2 * i + h < G; ++h) {
+          const int w = 2 * i + h;
+          // the power of two above it, 2^-13 to 2^16
+          const uint32_t above = min(max(__float_as_uint(h ? top.y : top.x) >> 23, 127u - 14u), 127u + 15u) + 1;
+          now[h] = fminf(h ? was.y : was.x, __uint_as_float((254u - above) << 23));
+          const float ratio = now[h] / (h ? was.y : was.x);
+          mine = r == w ? ratio : mine;
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              o[2 * w][nt][e] *= ratio;
+              o[2 * w + 1][nt][e] *= ratio;
+            }
+        }
+        by[i] = __floats2half2_rn(now[0], now[1]);
+      }
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          off[nt][e] *= ratio;
-#pragma unroll
-          for (int i = 0; i < 2 * G; ++i) o[i][nt][e] *= ratio;
-        }
+        for (int e = 0; e < 4; ++e) off[nt][e] *= mine;
     }
     const uint32_t halves = r % 2 ? 0x7632u : 0x5410u;
     unrolled<MT>([&](auto part) {
@@ -508,7 +534,7 @@ struct Narrow {                            // 4 bits, G groups of 32 entries
 #pragma unroll
       for (int e = 0; e < 2; ++e)
 #pragma unroll
-        for (int i = 0; i < (G + 1) / 2; ++i) rel[e][i] = __hmul2(as_half2(sc[T][e][i]), as_half2(by));
+        for (int i = 0; i < (G + 1) / 2; ++i) rel[e][i] = __hmul2(as_half2(sc[T][e][i]), by[i]);
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
         h[nt][0] = as_half2(pack2<false>(p[T][nt][0], p[T][nt][1]));
@@ -559,11 +585,11 @@ struct Narrow {                            // 4 bits, G groups of 32 entries
   template <class F>
   __device__ __forceinline__ void each(int nt, F&& put) const {
     const int lane = threadIdx.x % 32, r = lane / 4, c = lane % 4;
-    const float unit = bound * 16777216.f;
 #pragma unroll
     for (int w = 0; w < G; ++w)
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
+        const float unit = 16777216.f / inverse(w);
         const float minus = __shfl_sync(~0u, off[nt][j], 4 * w + c);
 #pragma unroll
         for (int h = 0; h < 2; ++h)
@@ -573,9 +599,9 @@ struct Narrow {                            // 4 bits, G groups of 32 entries
   }
   __device__ __forceinline__ void store(const CacheArgs&, int nt, const float* by, uint8_t* row) const {
     const int c = threadIdx.x % 4;
-    const float unit = bound * 16777216.f;
 #pragma unroll
     for (int w = 0; w < G; ++w) {
+      const float unit = 16777216.f / inverse(w);
       const float m0 = __shfl_sync(~0u, off[nt][0], 4 * w + c), m1 = __shfl_sync(~0u, off[nt][1], 4 * w + c);
       uint32_t x[2][2];                    // entries 8 c + 2 h + s and 8 c + 4 + 2 h + s of column r
 #pragma unroll
@@ -877,7 +903,7 @@ __global__ void __launch_bounds__(kThreads, per_sm(K::kBits, NT)) k_cache_attn(c
   for (int ip = 0; ip < made; ++ip) {
     const Piece& x = list[ip % kPieces];
     const int len = x.len, to = x.to;
-    float m[NT][2], l[NT][2], shift[NT][2];   // shift: m, or 0 where nothing was seen
+    float m[NT][2], l[NT][2], shift[NT][2];   // shift: what weights are relative to, m less kLift; 0 where nothing was seen
     int limit[NT][2];                      // tokens that a column's row sees
     int least = len;
 #pragma unroll
@@ -926,7 +952,6 @@ __global__ void __launch_bounds__(kThreads, per_sm(K::kBits, NT)) k_cache_attn(c
             for (int e = 0; e < 4; ++e)
               s[t][nt][e] = pos + kKeys * t + r + e / 2 * 8 < limit[nt][e % 2] ? s[t][nt][e] : -INFINITY;
       }
-      // The running maximum follows only rises of more than 2^8 in the weights.
       float top[NT][2];
       bool rises = false;
 #pragma unroll
@@ -937,7 +962,7 @@ __global__ void __launch_bounds__(kThreads, per_sm(K::kBits, NT)) k_cache_attn(c
 #pragma unroll
           for (int t = 1; t < MT; ++t) top[nt][j] = fmaxf(top[nt][j], fmaxf(s[t][nt][j], s[t][nt][j + 2]));
           top[nt][j] *= k.factor(nt, j);
-          rises = rises || top[nt][j] > m[nt][j] + 8.f;
+          rises = rises || top[nt][j] > m[nt][j] + kLag;
         }
       if (__any_sync(~0u, rises)) {
 #pragma unroll
@@ -946,9 +971,11 @@ __global__ void __launch_bounds__(kThreads, per_sm(K::kBits, NT)) k_cache_attn(c
           for (int j = 0; j < 2; ++j) {
 #pragma unroll
             for (int o = 4; o < 32; o *= 2) top[nt][j] = fmaxf(top[nt][j], __shfl_xor_sync(~0u, top[nt][j], o));
-            if (top[nt][j] > m[nt][j] + 8.f) {
-              const float by = exp2_fast(m[nt][j] - top[nt][j]);
-              m[nt][j] = shift[nt][j] = top[nt][j];
+            if (top[nt][j] > m[nt][j] + kLag) {
+              const float to = top[nt][j] - (fabsf(top[nt][j]) < kSure ? kLift : 0.f);
+              const float by = m[nt][j] == -INFINITY ? 0.f : exp2_fast(shift[nt][j] - to);
+              m[nt][j] = top[nt][j];
+              shift[nt][j] = to;
               l[nt][j] *= by;
               k.rescale(nt, j, by);
             }
@@ -987,7 +1014,7 @@ __global__ void __launch_bounds__(kThreads, per_sm(K::kBits, NT)) k_cache_attn(c
           for (int j = 0; j < 2; ++j) {
             split(x, x.first + 8 * nt + 2 * c + j, token, head);
             if (x.first + 8 * nt + 2 * c + j < x.n * group)
-              a.lse[head * a.rows + x.row0 + token] = l[nt][j] == 0.f ? -INFINITY : (m[nt][j] + log2f(l[nt][j])) * 0.6931471805599453f;
+              a.lse[head * a.rows + x.row0 + token] = l[nt][j] == 0.f ? -INFINITY : (shift[nt][j] + log2f(l[nt][j])) * 0.6931471805599453f;
           }
       }
     } else {
@@ -1003,7 +1030,7 @@ __global__ void __launch_bounds__(kThreads, per_sm(K::kBits, NT)) k_cache_attn(c
         if (r == 0)
 #pragma unroll
           for (int j = 0; j < 2; ++j) {
-            part[(8 * nt + 2 * c + j) * P::kRow + DP] = m[nt][j];
+            part[(8 * nt + 2 * c + j) * P::kRow + DP] = m[nt][j] == -INFINITY ? -INFINITY : shift[nt][j];
             part[(8 * nt + 2 * c + j) * P::kRow + DP + 1] = l[nt][j];
           }
       }
