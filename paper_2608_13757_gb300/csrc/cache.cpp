@@ -265,7 +265,7 @@ sync_status sync_cache_attn(const sync_cache* cache, const sync_cache_seqs* seqs
     a.whole = (int64_t)seqs->max_pages * cache->page <= SYNC_CACHE_SHORT;
     need(a.rows * (a.heads / a.kv_heads) <= 1 << 30 && a.rows * a.heads <= (int64_t)1 << 33,
          "more than 2^30 query rows of a key head, or 2^33 of all");
-    need(a.whole || (workspace && reinterpret_cast<uintptr_t>(workspace) % 16 == 0), "the workspace is NULL or not 16-byte aligned");
+    need(a.whole || (workspace && reinterpret_cast<uintptr_t>(workspace) % kWorkAlign == 0), "the workspace is NULL or not 16-byte aligned");
     if (!a.rows) return;
     a.num_sms = current_sms();
     a.most_rows = cache_attn_rows(a.bits, a.heads / a.kv_heads, max_new);

@@ -76,7 +76,8 @@ cudaError_t launch_cache_read(const CacheArgs& a, cudaStream_t st);
 cudaError_t launch_cache_attn(const CacheArgs& a, cudaStream_t st);
 cudaError_t launch_few_queries(const CacheArgs& a, cudaStream_t st);
 
-// Blocks and workspace of an attention call.
+// Blocks and workspace of an attention call, at a multiple of kWorkAlign bytes.
+constexpr int kWorkAlign = 16;
 int cache_attn_rows(int bits, int group, int max_new);                // query rows of a pass: 8, 16, 32
 int cache_attn_blocks(int bits, int most_rows, int num_sms);
 int64_t cache_attn_workspace(int dim, int most_rows, int blocks);

@@ -77,15 +77,17 @@ constexpr int per_sm(int bits, int nt) { return bits == 4 && nt == 1 ? 3 : 2; }
 
 // What a block leaves for the kernel that joins the pieces: the pass that it has
 // begun and does not end, and the block that does.
-struct alignas(32) Header {
+struct alignas(kWorkAlign) Header {
   int open;                                // 0: none
   int last, row0, n, head, first;          // as in Piece
 };
+static_assert(alignof(Header) == kWorkAlign && sizeof(Header) % kWorkAlign == 0, "headers lie one after the other from the workspace's start");
 
 template <int DP, int ROWS>
 struct Parts {                             // the workspace
   static constexpr int kRow = DP + 4;      // a row's entries, then its maximum and sum
   static constexpr int kFloats = ROWS * kRow;
+  static_assert(kRow * sizeof(float) % kWorkAlign == 0, "rows are read and written 16 bytes at a time");
   static __host__ __device__ size_t header(int blocks) { return ((size_t)blocks * sizeof(Header) + 255) / 256 * 256; }
   // two slots per block, then one per warp
   static __device__ int64_t slot(int i) { return (int64_t)i * kFloats; }
