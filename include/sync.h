@@ -587,7 +587,7 @@ typedef struct sync_attn sync_attn;   /* opaque; owns device memory */
  * serves any number of calls on tensors of its sizes; calls on one plan share
  * its workspace and must not overlap on the GPU.  SYNC_ERR_ARG for a field
  * outside its range, SYNC_ERR_MALFORMED for ranges that overlap,
- * SYNC_ERR_OVERFLOW for rows past INT32_MAX. */
+ * SYNC_ERR_OVERFLOW for rows past INT32_MAX, or for more work items. */
 sync_status sync_attn_plan(const sync_attn_desc *desc, int device, sync_attn **out);
 
 /* The same for attention to the states of another sequence, as a decoder's to

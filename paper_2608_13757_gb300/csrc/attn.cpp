@@ -209,6 +209,23 @@ bool few_queries(const sync_attn_desc* d, bool causal, const std::vector<AttnSeq
   return most > 0 && most * (d->heads / d->kv_heads) <= few_rows(d->head_dim);
 }
 
+// The longest of a plan's lists, before pieces are cut: what it would take to lay
+// them out is known before anything is allocated for them.
+int64_t longest_list(const sync_attn_desc* d, bool few, const std::vector<AttnSeq>& seq) {
+  const int group = d->heads / d->kv_heads;
+  int64_t items = 0, q = 0, k = 0;
+  for (const AttnSeq& s : seq) {
+    const bool packed = packs(s, group);
+    const int64_t per = packed ? kTile / group : kTile;
+    if (few) items += s.lq ? d->kv_heads : 0;
+    else items += (s.lq + 2 * per - 1) / (2 * per) * (packed ? d->kv_heads : d->heads);
+    if (!d->train) continue;
+    q += (s.lq + kTile - 1ll) / kTile * d->heads;
+    k += (s.lk + kTile - 1ll) / kTile * d->kv_heads;
+  }
+  return std::max(items, std::max(q, k));
+}
+
 struct ForwardWork {
   std::vector<AttnItem> item;
   std::vector<int32_t> block_first;
@@ -550,6 +567,8 @@ static sync_status make_plan(const sync_attn_desc* desc, bool causal, int device
     check_attn(desc);
     sync_attn_sizes sz{};
     const std::vector<AttnSeq> seq = sequences(desc, causal, sz);
+    const bool few = few_queries(desc, causal, seq);
+    if (longest_list(desc, few, seq) > INT32_MAX) fail(SYNC_ERR_OVERFLOW, "more than INT32_MAX work items");
     DeviceScope scope(device);
     std::unique_ptr<sync_attn, void (*)(sync_attn*)> P(new sync_attn, sync_attn_free);
     P->device = device;
@@ -561,7 +580,7 @@ static sync_status make_plan(const sync_attn_desc* desc, bool causal, int device
     a.kv_heads = desc->kv_heads;
     a.dim = desc->head_dim;
     a.num_sms = P->num_sms;
-    P->few = few_queries(desc, causal, seq);
+    P->few = few;
     std::vector<int32_t> q_row, q_len, k_len;
     std::vector<int64_t> k_row;
     CacheArgs& f = P->rows;
