@@ -84,12 +84,14 @@ def _need(ok, what):
         raise _sg.SyncError(_sg.ERR_ARG, what)
 
 
-def _not_recorded(name):
-    """Says that a call drops the gradient that an input of it requires."""
+def _not_recorded(name, backward=True):
+    """Says that a call drops the gradient that an input of it requires; backward:
+    whether there is a call that computes it."""
     import torch
     if torch.is_grad_enabled():
+        use = f"use {name.replace('_forward', '')}_backward, and torch.no_grad()" if backward else "it has none; use torch.no_grad()"
         warnings.warn(f"{name} records nothing for autograd: its outputs carry no gradient to the inputs that require one "
-                      f"(use {name.replace('_forward', '')}_backward, and torch.no_grad() around this call)", stacklevel=3)
+                      f"({use} around this call)", stacklevel=3)
 
 
 def _current_stream(device: int) -> int:

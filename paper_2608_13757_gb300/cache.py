@@ -211,7 +211,7 @@ def sync_cache_append(cache: KVCache, k, v, page_table, lens, row_starts=None, q
             return sync_cache_append(cache, k, v, page_table, lens, row_starts, q, cos, sin, positions, axes, interleaved, out)
     a, b = _rows(k, "k", dtype, device, kv, dim), _rows(v, "v", dtype, device, kv, dim)
     if k.requires_grad or v.requires_grad or q is not None and q.requires_grad:
-        _not_recorded("sync_cache_append")
+        _not_recorded("sync_cache_append", backward=False)
     _need((cos is None) == (sin is None), "cos and sin must both be given or both be None")
     turn = None if cos is None else _rotation(cos, sin, positions, axes, interleaved, a.rows, device)
     heads, given, to, fill = 0, None, None, False
@@ -268,7 +268,7 @@ def sync_cache_attn(cache: KVCache, q, page_table, lens, row_starts=None, max_ne
     heads = q.shape[1] if q.dim() == 3 else 0
     a = _rows(q, "q", dtype, device, heads, dim)
     if q.requires_grad:
-        _not_recorded("sync_cache_attn")
+        _not_recorded("sync_cache_attn", backward=False)
     n = a.rows
     fill = out is None
     if fill:
