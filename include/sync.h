@@ -718,8 +718,8 @@ typedef struct {
  * sequence s is in page page_table[s * table_stride + p / page], at p % page.
  * lens[s] counts its tokens, the step's new ones included.  Sequence s has rows
  * row_starts[s] .. row_starts[s + 1] - 1 of the step's tensors, its last tokens in
- * order (row_starts does not fall, from 0 on); NULL: one row each.  Rows from
- * row_starts[n_seqs] on belong to no sequence: padding.
+ * order (row_starts does not fall); NULL: one row each.  Rows before row_starts[0]
+ * and from row_starts[n_seqs] on belong to no sequence: padding.
  * Pages of tokens that are written belong to one sequence; others may be shared.
  * (A slot that one call writes twice holds either row, or parts of both.) */
 typedef struct {

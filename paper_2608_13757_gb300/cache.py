@@ -197,8 +197,8 @@ def sync_cache_append(cache: KVCache, k, v, page_table, lens, row_starts=None, q
 
     page_table: int32 [sequences, pages], the pages of every sequence in order;
     lens: int32 [sequences], their tokens with the new ones; row_starts: int32
-    [sequences + 1], the first row of each in k, v and q, rows past the last being
-    padding (None: one row each).  cos, sin, positions, axes and interleaved are
+    [sequences + 1], the first row of each in k, v and q, rows before the first and
+    past the last being padding (None: one row each).  cos, sin, positions, axes and interleaved are
     sync_rope's, positions None meaning a token's place in its sequence; without
     cos and sin nothing is turned."""
     import torch

@@ -773,14 +773,17 @@ __global__ void __launch_bounds__(kThreads, per_sm(K::kBits, NT)) k_cache_attn(c
   float* const parts = reinterpret_cast<float*>(a.work + P::header(gridDim.x));
   auto out_row = [&](const int64_t row, int head) { return static_cast<uint8_t*>(a.q_out.data) + 2 * (row * a.q_out.row + head * a.q_out.head); };
 
-  if (a.fill) {                            // padding behind the last sequence
-    const int64_t end = a.starts ? min(max((int64_t)__ldg(a.starts + a.n_seqs), (int64_t)0), a.rows) : a.rows;
-    for (int64_t row = end + blockIdx.x; row < a.rows; row += gridDim.x)
+  if (a.fill) {                            // padding in front of the first sequence and behind the last
+    auto start = [&](int s) { return min(max((int64_t)__ldg(a.starts + s), (int64_t)0), a.rows); };
+    const int64_t first = a.starts ? start(0) : 0, end = a.starts ? max(first, start(a.n_seqs)) : a.rows;
+    for (int64_t pad = blockIdx.x; pad < first + a.rows - end; pad += gridDim.x) {
+      const int64_t row = pad < first ? pad : end + pad - first;
       for (int i = threadIdx.x; i < a.heads * (a.dim / 8); i += kThreads) {
         const int h = i / (a.dim / 8), d = i % (a.dim / 8) * 8;
         *reinterpret_cast<uint4*>(out_row(row, h) + 2 * d) = make_uint4(0, 0, 0, 0);
         if (a.lse && d == 0) a.lse[h * a.rows + row] = -INFINITY;
       }
+    }
   }
 
   find_runs<ROWS, kTile, K::kPaged>(a, runs);
