@@ -389,8 +389,8 @@ struct Narrow {                            // 4 bits, G groups of 32 entries
         q[2 * w + h][nt][1] = pack2<false>(x[w][2 * h + 1] * up * 0.0625f, x[w][2 * h + 5] * up * 0.0625f);
       }
 #pragma unroll
-    for (int j = 0; j < 2; ++j)            // (not 0, which would make a NaN of a hidden score)
-      f[nt][j] = fmaxf(a.scale * 1.4426950408889634f * 16777216.f * __shfl_sync(~0u, down, (2 * c + j) * 4), 1.17549435e-38f);
+    for (int j = 0; j < 2; ++j)            // (not 0, which would make a NaN of a hidden score, nor infinity: of a score of 0)
+      f[nt][j] = fminf(fmaxf(a.scale * 1.4426950408889634f * 16777216.f * __shfl_sync(~0u, down, (2 * c + j) * 4), 1.17549435e-38f), 3.40282347e38f);
     // -8 sum q of the groups, to lanes c = 0 (groups 0, 1) and 1 (2, 3), and what
     // their rounding leaves to lanes c = 2 and 3
     float sum[4] = {0.f, 0.f, 0.f, 0.f};
