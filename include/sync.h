@@ -621,7 +621,8 @@ sync_status sync_attn_status(const sync_attn *plan);
  * each row's sum of exponentials (-inf for a query that sees no key).
  * Products are summed in 32 bits, the softmax's maximum and sum are held in
  * 32 bits, and its unnormalised weights are rounded to dtype for the second
- * product.  Scores, scale * q k^T, stay below 2^27 in size (above it, half a
+ * product (in SYNC_FP16 those below 2^-21 of the row's largest to steps of 2^-31 of
+ * it).  Scores, scale * q k^T, stay below 2^27 in size (above it, half a
  * unit in the last place of a score is a factor that the weights may not hold).
  * Keys and values of other sequences never reach a row, whatever they hold;
  * within a sequence, a NaN or an infinity in the value of a key may reach
