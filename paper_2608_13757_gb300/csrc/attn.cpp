@@ -193,14 +193,22 @@ bool packs(const AttnSeq& s, int group) {
 
 // Plans of queries that see all keys go to the kernel of few queries (k_cache_attn.cu)
 // where a key head's queries fit in 16 of its columns, or 8 in heads of more than
-// 64 entries: it reads what there is and no more.  us here and in tiles of 128
-// queries, bf16:
-//                                  48 x 1500 keys   300 x 300    1 x 100000    4 x 100
-//   20 heads of 64, 1 query            37.5 49.3    50.5 121.4    82.1 102.4   6.5 6.3
-//                  16 queries          50.7 54.9    65.9 120.3    86.3 103.4   6.7 6.4
-//   32/8 heads of 128, 1 query         31.1 29.7    41.9  63.1    67.1  71.3   7.7 6.5
-//                  2 queries           33.9 31.1    47.5  64.6    68.3  73.7   7.3 6.5
-//                  4 (not taken)       38.4 28.2    55.8  64.1    71.5  73.8   8.5 6.7
+// 64 entries: it reads what there is and no more.  us there and in tiles of 128
+// queries, bf16; n x m: n sequences of 1 to m keys, evenly drawn (one: m).  Up to 12
+// sets of keys and values, 500 MB where 12 are enough for it, are taken in turn, so that
+// they come from memory but for 4 x 100 and 16/2 heads at 300 x 100 and 16 x 1500:
+//                              4 x 100  300 x 100  16 x 1500  48 x 1500   300 x 300  16 x 10000  1 x 100000
+//   20 heads of 64, 1 query    6.8 6.2  25.2 93.6  17.1 20.5  39.0 49.1   52.4 120.8  78.7 92.5   89.3 102.8
+//                 16 queries   7.9 6.0  32.7 93.6  23.4 20.3  48.1 49.3   70.0 120.6  87.2 92.9   92.8 104.0
+//   16/2 heads of 64, 2        7.9 6.0   9.6 13.2  12.4 10.3  14.9 15.9   19.6  17.5  18.2 19.6   21.7  30.1
+//   32/8 heads of 128, 1       7.8 6.6  18.3 49.6  15.5 18.3  32.4 30.3   45.0  64.5  61.3 59.5   69.1  73.4
+//                      2       8.1 6.6  18.9 49.8  16.6 18.3  33.9 30.4   47.5  65.1  62.5 60.8   70.4  75.6
+// The rule looks at rows and entries alone, and so takes the slower one in places: by
+// 1 to 2.5 us of 6 where all tiles are one wave of blocks on up to 128 keys, by up to
+// 27% with 9 to 16 rows in a few hundred passes or less, and by up to 20% in heads of
+// more than 64 entries with hundreds of passes.  Tiles are up to three
+// times as slow where sequences are many and short.  (16 rows of 128 entries, in a
+// form that is gone: 48 x 1500 keys 38.4 against 28.2, 300 x 300 55.8 against 64.1.)
 int64_t few_rows(int dim) { return dim <= 64 ? 16 : 8; }
 bool few_queries(const sync_attn_desc* d, bool causal, const std::vector<AttnSeq>& seq) {
   if (causal || d->train || seq.empty() || seq.size() > (1u << 20)) return false;

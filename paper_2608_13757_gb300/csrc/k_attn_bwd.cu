@@ -601,7 +601,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dq(const __grid_constant__
 // is of the rounded output, the one that the forward pass leaves: an unrounded
 // copy would be twice its bytes, and rowsum(P dP), which equals it, a third walk.
 // Its error is shared by a row's dS: in bf16 dq is off by 3.2e-3 at 8 keys and
-// 2.5e-3 at 1024 where rounding dq alone takes 1.7e-3.
+// 2.5e-3 at 1024 where rounding dq alone takes 1.7e-3; where every query of a batch
+// sees 2, 3, 4, 8 or 32 keys of another sequence, by 3.9e-3, 3.3e-3, 3.0e-3, 2.7e-3
+// and 2.5e-3 (fp16 4.8e-4 at 2, 3.0e-4 from 256 on, rounding 2.1e-4).
 // Bound by memory: 8192 rows of 32 heads of 128 take 24 us (5.6 TB/s).
 template <int LANES, bool BF16>
 __global__ void __launch_bounds__(256) k_attn_delta(const __grid_constant__ AttnArgs a) {

@@ -22,9 +22,14 @@
 // of 1802 tokens 14.2 us against 10.3, 131072 tokens in 4 bits 52 against 45.)
 //
 // Measured, 8 key heads of 128 and 4 queries for each: 16 bits 524287 tokens
-// 305 us, 7.0 TB/s; 64 sequences of 1 to 8192 tokens 62.4 us, 5.6 TB/s.  4 bits
-// 524287 tokens 125 us, 4.8 TB/s: there the schedulers are the bound (taking codes
-// apart and scales in), at 5.6 TB/s for what longer sequences add.  One token
+// 306 us, 7.0 TB/s; 64 sequences of 1 to 8192 tokens 62.5 us, 5.6 TB/s.  4 bits
+// 524287 tokens 126 us, 4.8 TB/s, and 5.6 TB/s for what longer sequences add.  Nothing
+// is saturated there (128 sequences of 1 to 16384 tokens: issue slots 53%, DRAM 52%):
+// from one instruction of a warp to the next pass 5.4 cycles, 1.6 of them for the
+// result before it, 1.5 for the scheduler, a pipe or dispatch, 0.7 for shared or
+// global memory, and 2.8 warps a scheduler do not cover that.  Passes of 16 columns are further off, with 8 warps an SM and all
+// codes taken apart for every 16 rows: 64 sequences of 1 to 8192 tokens with up to 4
+// new ones 52 us, where memory would take 9.  One token
 // over one key takes 6 us, over 1024 10 (16 bits) and 13 (4 bits): finding the
 // runs 2 us, the first tiles 6, the second kernel 5 after the last block.
 //
