@@ -775,7 +775,8 @@ sync_status sync_cache_attn_workspace(const sync_cache *cache, int32_t heads, in
  * exactly; queries are scaled by a power of two to float16 (entries below 2^-21
  * of their head's largest lose bits), weights are rounded to float16 before and
  * after their value's scale, which is taken relative to the largest of its group
- * so far (one below 2^-14 of that loses bits).  In float16 a weight, or its product
+ * so far (one below 2^-14 of that loses bits); a weight times its scale and code is
+ * cut at about 2^-15 of the largest weight times scale among 16 tokens.  In float16 a weight, or its product
  * with such a scale, below 2^-25 of the row's largest is rounded to steps of 2^-35 of
  * it.  Scores stay below 2^27 in size (from 2^22 on these are 2^-14 and 2^-24).  A NaN or an infinity
  * in the value (or in 4 bits its scale) of a token that some of a sequence's rows

@@ -22,7 +22,7 @@
 // of 1802 tokens 14.2 us against 10.3, 131072 tokens in 4 bits 52 against 45.)
 //
 // Measured, 8 key heads of 128 and 4 queries for each: 16 bits 524287 tokens
-// 306 us, 7.0 TB/s; 64 sequences of 1 to 8192 tokens 62.5 us, 5.6 TB/s.  4 bits
+// 307 us, 7.0 TB/s; 64 sequences of 1 to 8192 tokens 62.5 us, 5.6 TB/s.  4 bits
 // 524287 tokens 126 us, 4.8 TB/s, and 5.6 TB/s for what longer sequences add.  Nothing
 // is saturated there (128 sequences of 1 to 16384 tokens: issue slots 53%, DRAM 52%):
 // from one instruction of a warp to the next pass 5.4 cycles, 1.6 of them for the
@@ -38,10 +38,15 @@
 // products take exactly.  So a word of 8 codes becomes four operand registers by
 // four masks and a shift, the factor 16 is in the query (or comes out of the sum at
 // the end), and the 8 is taken off by the sum's start (scores) or by a product
-// with -8 (outputs).  Scales of keys multiply the 32-bit sums of their group;
+// with -8 behind each with codes (outputs: so that nothing larger than the result is
+// carried along; -8 summed for itself and added at the end left rows of 16384 equal
+// weights wrong by 1.4%, 65536 by 2.4%).  A product of subnormal numbers is lined up
+// with the others of its 16 tokens as if it were at 2^-14, and cut there: in terms of
+// the largest weight times scale among them at about 2^-15 of a code's step, the same
+// for the codes and the -8, so that a code that stands for 0 leaves nothing.  Scales of keys multiply the 32-bit sums of their group;
 // those of values multiply the weights in float16, relative to a power of two for
 // each group that a warp raises when a larger scale comes.  (One for the whole head,
-// and weights that were not lifted (kLift), took 77 us instead of 80 for 128 sequences
+// and weights that were not lifted (kLift), took 3 us of 80 less for 128 sequences
 // of 1 to 16384 tokens, and lost what many small weights add together: 12 nats below
 // a first token that takes the row, 8192 others in a group of a 128th of the head's
 // largest scale left 13 to 27% of the result wrong; now it is a rounding of the
@@ -317,7 +322,7 @@ struct Narrow {                            // 4 bits, G groups of 32 entries
   static constexpr int DP = 32 * G, MT = NT == 1 ? 2 : 1, kStages = MT == 2 ? 3 : 4, kSide = kKeys * 16 * G, kScales = kKeys * 2 * G;
   static constexpr int kPart = 2 * (kSide + kScales), kStage = MT * kPart;
   uint32_t q[2 * G][NT][2], start[NT][2];  // start: -8 sum q of each group, as sums of two float16
-  float o[2 * G][NT][4], off[NT][4];       // off: row w has -8 sum p s of group w
+  float o[2 * G][NT][4];
   float f[NT][2];
   __half2 by[(G + 1) / 2];                 // 1 / bound of each group: a power of two that none of its scales so far reaches
 
@@ -425,11 +430,9 @@ struct Narrow {                            // 4 bits, G groups of 32 entries
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        off[nt][e] = 0.f;
+      for (int e = 0; e < 4; ++e)
 #pragma unroll
         for (int i = 0; i < 2 * G; ++i) o[i][nt][e] = 0.f;
-      }
   }
   __device__ __forceinline__ float factor(int nt, int j) const { return f[nt][j]; }
   __device__ __forceinline__ float inverse(int w) const { return w % 2 ? __high2float(by[w / 2]) : __low2float(by[w / 2]); }
@@ -504,7 +507,6 @@ struct Narrow {                            // 4 bits, G groups of 32 entries
       larger = larger || __hgeu2_mask(__hmul2(most[i], by[i]), as_half2(0x3c003c00u)) != 0;
     }
     if (__any_sync(~0u, larger)) {
-      float mine = 1.f;                                      // of group r, whose row this lane has in `off`
 #pragma unroll
       for (int i = 0; i < (G + 1) / 2; ++i) {
 #pragma unroll
@@ -518,7 +520,6 @@ struct Narrow {                            // 4 bits, G groups of 32 entries
           const uint32_t above = min(max(__float_as_uint(h ? top.y : top.x) >> 23, 127u - 14u), 127u + 15u) + 1;
           now[h] = fminf(h ? was.y : was.x, __uint_as_float((254u - above) << 23));
           const float ratio = now[h] / (h ? was.y : was.x);
-          mine = r == w ? ratio : mine;
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -529,12 +530,9 @@ struct Narrow {                            // 4 bits, G groups of 32 entries
         }
         by[i] = __floats2half2_rn(now[0], now[1]);
       }
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) off[nt][e] *= mine;
     }
     const uint32_t halves = r % 2 ? 0x7632u : 0x5410u;
+    const uint32_t eight[4] = {0x80088008u, 0x80808080u, 0x80088008u, 0x80808080u};   // -8, and 16 times that
     unrolled<MT>([&](auto part) {
       constexpr int T = decltype(part)::value;
       __half2 rel[2][(G + 1) / 2], h[NT][2];
@@ -557,13 +555,10 @@ struct Narrow {                            // 4 bits, G groups of 32 entries
         uint32_t b[NT][2];
         const __half2 r0 = w % 2 ? __high2half2(rel[0][w / 2]) : __low2half2(rel[0][w / 2]);
         const __half2 r1 = w % 2 ? __high2half2(rel[1][w / 2]) : __low2half2(rel[1][w / 2]);
-        const uint32_t mark = r == w ? 0x80088008u : 0u;     // -8 in row w
-        const uint32_t eight[4] = {mark, 0u, mark, 0u};
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
           b[nt][0] = transposed(as_word(__hmul2(h[nt][0], r0)));
           b[nt][1] = transposed(as_word(__hmul2(h[nt][1], r1)));
-          mma<false>(off[nt], eight, b[nt][0], b[nt][1], off[nt]);
         }
         const uint32_t y0 = __byte_perm(x[0][w], x[1][w], halves), y1 = __byte_perm(x[2][w], x[3][w], halves);
         const uint32_t lo[4] = {y0 & 0x000f000fu, y0 & 0x00f000f0u, y1 & 0x000f000fu, y1 & 0x00f000f0u};
@@ -573,12 +568,13 @@ struct Narrow {                            // 4 bits, G groups of 32 entries
         for (int nt = 0; nt < NT; ++nt) {
           mma<false>(o[2 * w][nt], lo, b[nt][0], b[nt][1], o[2 * w][nt]);
           mma<false>(o[2 * w + 1][nt], hi, b[nt][0], b[nt][1], o[2 * w + 1][nt]);
+          mma<false>(o[2 * w][nt], eight, b[nt][0], b[nt][1], o[2 * w][nt]);
+          mma<false>(o[2 * w + 1][nt], eight, b[nt][0], b[nt][1], o[2 * w + 1][nt]);
         }
       }
     });
   }
   __device__ __forceinline__ void rescale(int nt, int j, float by_) {
-    off[nt][j] *= by_;
 #pragma unroll
     for (int i = 0; i < 2 * G; ++i) {
       o[i][nt][j] *= by_;
@@ -586,36 +582,31 @@ struct Narrow {                            // 4 bits, G groups of 32 entries
     }
   }
   // output entries 32 w + 4 r + 2 h (s = 0) and the one after it (s = 1) of column 2 c + j
-  __device__ __forceinline__ float output(int w, int h, int s, int nt, int j, float minus, float unit) const {
-    return s ? fmaf(o[2 * w + h][nt][j + 2], 0.0625f, minus) * unit : (o[2 * w + h][nt][j] + minus) * unit;
+  __device__ __forceinline__ float output(int w, int h, int s, int nt, int j) const {
+    return o[2 * w + h][nt][j + 2 * s] * ((s ? 1048576.f : 16777216.f) * __frcp_rn(inverse(w)));
   }
   template <class F>
   __device__ __forceinline__ void each(int nt, F&& put) const {
-    const int lane = threadIdx.x % 32, r = lane / 4, c = lane % 4;
+    const int r = threadIdx.x % 32 / 4;
 #pragma unroll
     for (int w = 0; w < G; ++w)
 #pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        const float unit = 16777216.f / inverse(w);
-        const float minus = __shfl_sync(~0u, off[nt][j], 4 * w + c);
+      for (int j = 0; j < 2; ++j)
 #pragma unroll
         for (int h = 0; h < 2; ++h)
 #pragma unroll
-          for (int s = 0; s < 2; ++s) put(32 * w + 4 * r + 2 * h + s, j, output(w, h, s, nt, j, minus, unit));
-      }
+          for (int s = 0; s < 2; ++s) put(32 * w + 4 * r + 2 * h + s, j, output(w, h, s, nt, j));
   }
   __device__ __forceinline__ void store(const CacheArgs&, int nt, const float* by, uint8_t* row) const {
     const int c = threadIdx.x % 4;
 #pragma unroll
     for (int w = 0; w < G; ++w) {
-      const float unit = 16777216.f / inverse(w);
-      const float m0 = __shfl_sync(~0u, off[nt][0], 4 * w + c), m1 = __shfl_sync(~0u, off[nt][1], 4 * w + c);
       uint32_t x[2][2];                    // entries 8 c + 2 h + s and 8 c + 4 + 2 h + s of column r
 #pragma unroll
       for (int h = 0; h < 2; ++h)
 #pragma unroll
         for (int s = 0; s < 2; ++s)
-          x[h][s] = transposed(pack2<BF16>(output(w, h, s, nt, 0, m0, unit) * by[0], output(w, h, s, nt, 1, m1, unit) * by[1]));
+          x[h][s] = transposed(pack2<BF16>(output(w, h, s, nt, 0) * by[0], output(w, h, s, nt, 1) * by[1]));
       if (row)
         *reinterpret_cast<uint4*>(row + 2 * (32 * w + 8 * c)) =
             make_uint4(__byte_perm(x[0][0], x[0][1], 0x5410), __byte_perm(x[1][0], x[1][1], 0x5410),
