@@ -27,30 +27,32 @@
 // is saturated there (128 sequences of 1 to 16384 tokens: issue slots 53%, DRAM 52%):
 // from one instruction of a warp to the next pass 5.4 cycles, 1.6 of them for the
 // result before it, 1.5 for the scheduler, a pipe or dispatch, 0.7 for shared or
-// global memory, and 2.8 warps a scheduler do not cover that.  Passes of 16 columns are further off, with 8 warps an SM and all
-// codes taken apart for every 16 rows: 64 sequences of 1 to 8192 tokens with up to 4
-// new ones 52 us, where memory would take 9.  One token
-// over one key takes 6 us, over 1024 10 (16 bits) and 13 (4 bits): finding the
-// runs 2 us, the first tiles 6, the second kernel 5 after the last block.
+// global memory, and 2.8 warps a scheduler do not cover that.  Passes of 16 columns
+// are further off, with 8 warps an SM and all codes taken apart for every 16 rows: 64
+// sequences of 1 to 8192 tokens with up to 4 new ones 51 us, where memory would take
+// 9.  One token over one key takes 6 us, over 1024 10 (16 bits) and 13 (4 bits):
+// finding the runs 2 us, the first tiles 6, the second kernel 5 after the last block.
 //
 // 4 bits.  A stored code n = value / scale + 8 is a float16 as it is: bits 0-3 of
 // a half word are n 2^-24 and bits 4-7 are 16 n 2^-24, subnormal numbers that the
-// products take exactly.  So a word of 8 codes becomes four operand registers by
-// four masks and a shift, the factor 16 is in the query (or comes out of the sum at
-// the end), and the 8 is taken off by the sum's start (scores) or by a product
-// with -8 behind each with codes (outputs: so that nothing larger than the result is
-// carried along; -8 summed for itself and added at the end left rows of 16384 equal
-// weights wrong by 1.4%, 65536 by 2.4%).  A product of subnormal numbers is lined up
-// with the others of its 16 tokens as if it were at 2^-14, and cut there: in terms of
-// the largest weight times scale among them at about 2^-15 of a code's step, the same
-// for the codes and the -8, so that a code that stands for 0 leaves nothing.  Scales of keys multiply the 32-bit sums of their group;
-// those of values multiply the weights in float16, relative to a power of two for
-// each group that a warp raises when a larger scale comes.  (One for the whole head,
-// and weights that were not lifted (kLift), took 3 us of 80 less for 128 sequences
-// of 1 to 16384 tokens, and lost what many small weights add together: 12 nats below
-// a first token that takes the row, 8192 others in a group of a 128th of the head's
-// largest scale left 13 to 27% of the result wrong; now it is a rounding of the
-// result.  Products in 32 bits, rounded once, took 84 us.)
+// products take.  So a word of 8 codes becomes four operand registers by four masks
+// and a shift, and the factor 16 is in the query or comes out of the sum at the end.
+// The 8 is taken off by the sum's start (scores) or by a product with -8 behind each
+// with codes (outputs), so that nothing larger than the result is carried along: -8
+// summed for itself and added at the end left rows of 16384 equal weights wrong by
+// 1.4%, of 65536 by 2.4%.  Subnormal products are lined up with the others of their 16
+// tokens as if they were at 2^-14, and cut there: at about 2^-15 of a code's step of
+// the largest weight times scale among them, alike for codes and -8, so that a code
+// that stands for 0 leaves nothing.
+//
+// Scales of keys multiply the 32-bit sums of their group; those of values multiply
+// the weights in float16, relative to a power of two for each group that a warp
+// raises when a larger scale comes.  (One for the whole head, and weights that were
+// not lifted (kLift), took 3 us of 80 less for 128 sequences of 1 to 16384 tokens,
+// and lost what many small weights add together: 12 nats below a first token that
+// takes the row, 8192 others in a group of a 128th of the head's largest scale left
+// 13 to 27% of the result wrong; now it is a rounding of the result.  Products in 32
+// bits, rounded once, took 84 us.)
 #include <algorithm>
 #include <atomic>
 #include <type_traits>
